@@ -237,7 +237,8 @@ def prepare(case, seed):
             st["cache"] = veda.Cache(st["k_pool"].shape[0], case["page"], case["kv_heads"], d, dt, k=st["k_pool"], v=st["v_pool"])
             st["batch"] = veda.CacheBatch(st["table"], st["kv_len"], st["q_start"], max_new=max(st["new"]))
             if case["kind"] == "attend":
-                st["workspace"] = torch.empty(veda.veda_cache_attn_workspace_bytes(st["cache"], st["batch"], case["q_heads"]), dtype=torch.uint8, device=dev)
+                st["workspace"] = torch.empty(veda.veda_cache_attn_workspace_bytes(st["cache"], st["batch"], case["q_heads"], rows),
+                                              dtype=torch.uint8, device=dev)
     return st
 
 
