@@ -6,7 +6,8 @@
  * Conventions (all entry points):
  *  - "device" pointers are HIP device memory owned by the caller; "host" pointers are
  *    ordinary host memory read during the call.  The library allocates device memory only
- *    inside veda_plan_create (a few KB of per-head tables, freed by veda_plan_destroy).
+ *    inside veda_plan_create (a few KB of per-head tables, freed by veda_plan_destroy) and
+ *    veda_rope_create (the frequencies, freed by veda_rope_destroy).
  *  - Every stage call only enqueues kernels on `stream` (a hipStream_t passed as void*; NULL
  *    is the default stream) and returns without synchronising.
  *  - Arguments are checked on the host before anything is launched; a failed check returns
@@ -369,6 +370,127 @@ veda_status veda_tile_recall(const veda_plan*, const int32_t* k_per_head, const 
  * Sec. 4.2 is this call around stages 1, heat map, 3 and 4 for every candidate tile shape. */
 veda_status veda_output_sqerr(const veda_plan*, const void* a, veda_strides sa, const void* b, veda_strides sb,
                               double* err, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- streaming generation: rotary positions, and a paged cache of earlier chunks' keys and values ------------------
+ * A generator that makes a clip chunk by chunk rotates the newest chunk's Q and K, appends K and V to a cache and attends to
+ * that cache.  These calls take the conventions above (device buffers and workspaces are the caller's, only kernels are
+ * enqueued, equal inputs give equal bytes); head_dim in {64, 128} for the cache, f32 and bf16. */
+
+/* Rotary positions: pair p of a row's channels, of axis a, is turned by the angle position[a] * freq[p]:
+ *   y0 = A (x0 cos - x1 sin),  y1 = A (x0 sin + x1 cos).
+ * The pairs are dealt to the axes one after the other (axis a takes axis_dim[a] / 2 of them); with i the pair's index inside its
+ * axis and w = axis_dim[a],  f = base^(-2i/w),  freq = f (PLAIN), f / factor (LINEAR), (base * factor^(w/(w-2)))^(-2i/w) (NTK; w > 2),
+ * or f * (g + (1 - g) / factor) (BY_PARTS) with g = clamp((trained_len * f / 2 pi - beta_slow) / (beta_fast - beta_slow), 0, 1).
+ * A = amplitude; 0 means the default: 1, BY_PARTS 0.1 ln(factor) + 1.
+ * Pairs are channels (2p, 2p+1) (INTERLEAVED) or (p, p + rot/2) (HALVES), rot = sum of axis_dim <= head_dim; channels from rot on
+ * are copied.  Angles are reduced to a turn in 64 bits, so far positions lose nothing; the rotation is in fp32, rounded once. */
+typedef enum { VEDA_ROPE_INTERLEAVED = 0, VEDA_ROPE_HALVES = 1 } veda_rope_pairs;
+typedef enum { VEDA_ROPE_PLAIN = 0, VEDA_ROPE_LINEAR = 1, VEDA_ROPE_NTK = 2, VEDA_ROPE_BY_PARTS = 3 } veda_rope_scaling;
+typedef struct {
+    int32_t head_dim;             /* channels of a row: a multiple of 8, up to 512                                  */
+    int32_t axes;                 /* positions of a token: 1..3                                                     */
+    int32_t axis_dim[3];          /* channels of every axis: even, >= 2; unused entries are ignored                 */
+    veda_rope_pairs pairs;
+    veda_rope_scaling scaling;
+    double base;                  /* > 1                                                                            */
+    double factor;                /* >= 1; ignored by PLAIN                                                         */
+    double trained_len, beta_fast, beta_slow;   /* BY_PARTS: > 0, beta_fast > beta_slow >= 0                        */
+    double amplitude;             /* >= 0                                                                           */
+} veda_rope_config;
+typedef struct veda_rope veda_rope;   /* opaque; holds the frequencies on the device that was current when it was made */
+/* Synchronous (one allocation and one copy); not to be called under stream capture.  *out is written only on VEDA_OK. */
+veda_status veda_rope_create(const veda_rope_config*, veda_rope** out);
+void veda_rope_destroy(veda_rope*);   /* NULL is allowed */
+/* freq: host, rot / 2 radians per position; amplitude: host, one value.  Either may be NULL. */
+veda_status veda_rope_frequencies(const veda_rope*, double* freq, double* amplitude);
+/* x, y       device, [batch][heads][tokens][head_dim] with strides sx, sy; y == x (with equal strides) rotates in place, other
+ *            overlaps are not allowed.
+ * positions  device i32 [batch][tokens][axes], any sign; position_stride elements from a sample to the next (0: all alike).
+ * transpose  0: rotate; 1: apply the transposed matrix, which turns the gradient of y into that of x (the rotation back, times
+ *            A once more, not divided by it). */
+veda_status veda_rope_apply(const veda_rope*, veda_dtype dtype, int32_t batch, int32_t heads, int32_t tokens, const void* x,
+                            veda_strides sx, const int32_t* positions, int64_t position_stride, int32_t transpose, void* y,
+                            veda_strides sy, void* stream);
+
+/* The cache of one layer: a pool of K pages and one of V pages, [pages][kv_heads][page_tokens][head_dim], in the caller's memory. */
+typedef struct {
+    int32_t pages;                /* pages of each pool                                                             */
+    int32_t page_tokens;          /* 16, 32, 64, 128 or 256                                                         */
+    int32_t kv_heads, head_dim;   /* kv_heads 1..1024                                                               */
+    veda_dtype dtype;
+    int64_t page_stride;          /* elements from a page to the next, a multiple of 16 bytes; 0: pages lie close   */
+    void *k, *v;                  /* device, 16-byte aligned                                                        */
+} veda_cache;
+/* The sequences of one call.  The rows (new tokens) of all sequences lie one behind the other; rows behind the last sequence's
+ * are left as they were by every call.  Row i of a sequence with n rows has the position kv_len - n + i.
+ * All three arrays are read on the device, so a captured call sees what they hold when it is replayed.  Nothing in them can lead a
+ * call outside its buffers: a page number outside [0, pages) is a hole (its keys do not exist: evicted pages are marked -1), q_start
+ * is cut to [0, rows], kv_len to [0, max_pages * page_tokens], and rows from max_new on of a sequence are left as they were.
+ * Two sequences may share pages; a page that a call writes must not be shared. */
+typedef struct {
+    int32_t seqs;                 /* sequences, >= 0                                                                */
+    int32_t rows;                 /* rows of the row buffers, >= 0                                                  */
+    int32_t max_new;              /* no sequence has more rows than this, >= 0: it sizes the launches               */
+    int32_t max_pages;            /* entries of a sequence in the page table, >= 1                                  */
+    int64_t table_stride;         /* entries from a sequence to the next, >= max_pages                              */
+    const int32_t* page_table;    /* device [seqs][table_stride]: page of tokens [i * page_tokens, (i+1) * page_tokens) */
+    const int32_t* kv_len;        /* device [seqs]: tokens of a sequence, the new ones among them                   */
+    const int32_t* q_start;       /* device [seqs + 1]: first row of every sequence, ascending                      */
+} veda_cache_batch;
+/* Writes the new rows' K and V into the cache, in one launch; rope (may be NULL) turns K, and Q on the way to q_out.
+ * k, v       device, [rows][kv_heads][head_dim]: element strides s.n from row to row, s.h from head to head (s.b is ignored)
+ * q, q_out   optional (both NULL with q_heads == 0): [rows][q_heads][head_dim]; copied where rope is NULL; q_out == q (with equal
+ *            strides) works in place
+ * positions  device i32 [rows][axes of rope]; NULL: the row's position in its sequence (ropes of one axis only)
+ * A row whose position is negative or whose page is a hole writes no K and V. */
+veda_status veda_cache_append(const veda_cache*, const veda_cache_batch*, const void* k, veda_strides sk, const void* v,
+                              veda_strides sv, int32_t q_heads, const void* q, veda_strides sq, void* q_out,
+                              veda_strides sq_out, const veda_rope* rope, const int32_t* positions, void* stream);
+/* Which keys a row at position p >= 0 sees, with e = kv_len if block == 0, else (p / block + 1) * block (the end of its block):
+ * the existing keys j < min(e, kv_len) with window == 0, or j >= e - window, or j < sinks.  block == 1 is causal token by token;
+ * block = tokens of a chunk of frames lets a chunk's tokens see each other; 0 shows the whole cache.  window counts keys back from e,
+ * sinks first keys that stay visible.  Each 0 .. 2^30. */
+typedef struct { int32_t block, window, sinks; } veda_visible;
+/* Attention of the new rows over the cache (their own keys included, so append first).
+ * q          device, [rows][q_heads][head_dim], strides sq (s.n from row to row, s.h from head to head); q_heads a multiple of
+ *            kv_heads, up to 32 * kv_heads: query head h reads key head h / (q_heads / kv_heads)
+ * out        device, the same shape, strides so; not to overlap q.  A row that sees no key gets zeros.
+ * lse        optional device fp32 [q_heads][rows]: natural-log sum of exp of the visible logits, -inf where there are none
+ * workspace  device, 16-byte aligned, veda_cache_attn_workspace_bytes() (0 for most calls with many rows: NULL is allowed then);
+ *            contents undefined after.  Calls that may overlap need one each.
+ * bf16: products on bf16 MFMA with fp32 accumulation, softmax in fp32 (logits scaled there, Q is not rounded again), P rounded to
+ * bf16 before P V.  f32: products on fp32 MFMA.  Values behind a sequence's end, in holes and at keys that a row does not see
+ * do not reach that row, whatever they are (infinities and NaN too). */
+size_t veda_cache_attn_workspace_bytes(const veda_cache*, const veda_cache_batch*, int32_t q_heads);
+veda_status veda_cache_attn_fwd(const veda_cache*, const veda_cache_batch*, int32_t q_heads, const void* q, veda_strides sq,
+                                float softmax_scale, veda_visible visible, void* out, veda_strides so, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream);
+/* Copies pages inside both pools.  pairs: host i32 [n][2] = (from, to), as if copied one after the other in this order (a page
+ * may appear any number of times); numbers outside [0, pages) are refused.  Pairs that do not touch each other's pages share a
+ * launch, up to 448 of them. */
+veda_status veda_cache_copy_pages(const veda_cache*, const int32_t* pairs, int64_t n, void* stream);
+
+/* Which page belongs to which sequence: a host object, no device memory, not thread-safe.  Pages are counted: a forked sequence
+ * shares its parent's pages, and the calls that come to write a shared page or move one tell which pages to copy.
+ * Free pages are given out lowest number first.
+ * copies     host i32 [capacity][2]: pairs for veda_cache_copy_pages, which has to run (in stream order) before the pages are
+ *            used; *n_copies of them.  Where capacity is too small the call fails with VEDA_ERR_WORKSPACE and changes nothing; a call
+ *            that fails never changes anything. */
+typedef struct veda_pages veda_pages;
+veda_status veda_pages_create(int32_t pages, int32_t page_tokens, int32_t max_seqs, int32_t max_pages, veda_pages** out);
+void veda_pages_destroy(veda_pages*);
+const int32_t* veda_pages_table(const veda_pages*);              /* host [max_seqs][max_pages], -1 where there is no page; NULL on bad args */
+int32_t veda_pages_length(const veda_pages*, int32_t seq);       /* tokens; -1 on bad args                             */
+int32_t veda_pages_free_count(const veda_pages*);                /* pages that nobody holds; -1 on bad args            */
+/* Makes the sequence `tokens` (>= its length) long: pages for the new tokens, and pages of its own in place of shared ones that
+ * the new tokens fall into (at most one, so one copy).  Too few free pages: VEDA_ERR_WORKSPACE. */
+veda_status veda_pages_extend(veda_pages*, int32_t seq, int32_t tokens, int32_t* copies, int32_t capacity, int32_t* n_copies);
+veda_status veda_pages_fork(veda_pages*, int32_t from, int32_t to);         /* `to` must be empty (length 0)               */
+veda_status veda_pages_truncate(veda_pages*, int32_t seq, int32_t tokens);  /* keeps the first tokens; 0 frees the sequence */
+/* Gives back the pages that lie wholly in [first, last) of the sequence and marks them -1 in its table. */
+veda_status veda_pages_evict(veda_pages*, int32_t seq, int32_t first, int32_t last);
+/* Moves pages down so that those in use are the lowest numbers: one copy for each page moved, no page copied to twice. */
+veda_status veda_pages_compact(veda_pages*, int32_t* copies, int32_t capacity, int32_t* n_copies);
 
 const char* veda_status_string(veda_status);
 /* Text of the last HIP error seen by this thread inside the library ("" if none). */

@@ -27,6 +27,8 @@ VEDA_OPT_FP32_CHAIN_UNIT = 2
 VEDA_OPT_FP32_PRODUCTS = 3
 VEDA_PRODUCTS_FP32, VEDA_PRODUCTS_SPLIT = 1, 2
 VEDA_CHAINS_MATRIX, VEDA_CHAINS_VECTOR = 1, 2
+VEDA_ROPE_INTERLEAVED, VEDA_ROPE_HALVES = 0, 1
+VEDA_ROPE_PLAIN, VEDA_ROPE_LINEAR, VEDA_ROPE_NTK, VEDA_ROPE_BY_PARTS = range(4)
 
 EXPORTS = (
     "veda_plan_create", "veda_plan_destroy", "veda_plan_set_option", "veda_plan_chain_unit", "veda_plan_tiles", "veda_plan_tile_offset",
@@ -38,7 +40,12 @@ EXPORTS = (
     "veda_sparse_attn_fwd", "veda_sparse_attn_fwd_q_tokens",
     "veda_sparse_attn_fwd_qk_tokens", "veda_tile_heatmap", "veda_tile_heatmap_rows",
     "veda_tile_heatmap_ws", "veda_plan_heatmap_workspace_bytes",
-    "veda_tile_recall", "veda_output_sqerr", "veda_status_string", "veda_last_error",
+    "veda_tile_recall", "veda_output_sqerr",
+    "veda_rope_create", "veda_rope_destroy", "veda_rope_frequencies", "veda_rope_apply",
+    "veda_cache_append", "veda_cache_attn_workspace_bytes", "veda_cache_attn_fwd", "veda_cache_copy_pages",
+    "veda_pages_create", "veda_pages_destroy", "veda_pages_table", "veda_pages_length", "veda_pages_free_count", "veda_pages_extend",
+    "veda_pages_fork", "veda_pages_truncate", "veda_pages_evict", "veda_pages_compact",
+    "veda_status_string", "veda_last_error",
 )
 
 
@@ -65,6 +72,26 @@ class veda_mlp(C.Structure):
 
 class veda_workspace_layout(C.Structure):
     _fields_ = [("stats_q", C.c_int64), ("stats_k", C.c_int64), ("latent_q", C.c_int64), ("latent_k", C.c_int64)]
+
+
+class veda_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("axes", C.c_int32), ("axis_dim", C.c_int32 * 3), ("pairs", C.c_int), ("scaling", C.c_int),
+                ("base", C.c_double), ("factor", C.c_double), ("trained_len", C.c_double), ("beta_fast", C.c_double),
+                ("beta_slow", C.c_double), ("amplitude", C.c_double)]
+
+
+class veda_cache(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("page_tokens", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int),
+                ("page_stride", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class veda_cache_batch(C.Structure):
+    _fields_ = [("seqs", C.c_int32), ("rows", C.c_int32), ("max_new", C.c_int32), ("max_pages", C.c_int32), ("table_stride", C.c_int64),
+                ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("q_start", C.c_void_p)]
+
+
+class veda_visible(C.Structure):
+    _fields_ = [("block", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32)]
 
 
 _lib = None
@@ -146,6 +173,40 @@ def load():
     L.veda_tile_recall.restype = C.c_int
     L.veda_output_sqerr.argtypes = [vp, vp, veda_strides, vp, veda_strides, vp, vp, C.c_size_t, vp]
     L.veda_output_sqerr.restype = C.c_int
+    L.veda_rope_create.argtypes = [C.POINTER(veda_rope_config), C.POINTER(vp)]
+    L.veda_rope_create.restype = C.c_int
+    L.veda_rope_destroy.argtypes = [vp]
+    L.veda_rope_destroy.restype = None
+    L.veda_rope_frequencies.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    L.veda_rope_frequencies.restype = C.c_int
+    L.veda_rope_apply.argtypes = [vp, C.c_int, i32, i32, i32, vp, veda_strides, vp, i64, i32, vp, veda_strides, vp]
+    L.veda_rope_apply.restype = C.c_int
+    cache, batch = C.POINTER(veda_cache), C.POINTER(veda_cache_batch)
+    L.veda_cache_append.argtypes = [cache, batch, vp, veda_strides, vp, veda_strides, i32, vp, veda_strides, vp, veda_strides, vp, vp, vp]
+    L.veda_cache_append.restype = C.c_int
+    L.veda_cache_attn_workspace_bytes.argtypes = [cache, batch, i32]
+    L.veda_cache_attn_workspace_bytes.restype = C.c_size_t
+    L.veda_cache_attn_fwd.argtypes = [cache, batch, i32, vp, veda_strides, C.c_float, veda_visible, vp, veda_strides, vp, vp, C.c_size_t, vp]
+    L.veda_cache_attn_fwd.restype = C.c_int
+    L.veda_cache_copy_pages.argtypes = [cache, vp, i64, vp]
+    L.veda_cache_copy_pages.restype = C.c_int
+    L.veda_pages_create.argtypes = [i32, i32, i32, i32, C.POINTER(vp)]
+    L.veda_pages_create.restype = C.c_int
+    L.veda_pages_destroy.argtypes = [vp]
+    L.veda_pages_destroy.restype = None
+    L.veda_pages_table.argtypes = [vp]
+    L.veda_pages_table.restype = C.POINTER(i32)
+    L.veda_pages_length.argtypes = [vp, i32]
+    L.veda_pages_free_count.argtypes = [vp]
+    for name in ("veda_pages_length", "veda_pages_free_count"):
+        getattr(L, name).restype = i32
+    L.veda_pages_extend.argtypes = [vp, i32, i32, vp, i32, C.POINTER(i32)]
+    L.veda_pages_fork.argtypes = [vp, i32, i32]
+    L.veda_pages_truncate.argtypes = [vp, i32, i32]
+    L.veda_pages_evict.argtypes = [vp, i32, i32, i32]
+    L.veda_pages_compact.argtypes = [vp, vp, i32, C.POINTER(i32)]
+    for name in ("extend", "fork", "truncate", "evict", "compact"):
+        getattr(L, "veda_pages_" + name).restype = C.c_int
     L.veda_status_string.argtypes = [C.c_int]
     L.veda_status_string.restype = C.c_char_p
     L.veda_last_error.argtypes = []
@@ -600,3 +661,262 @@ def veda_attention(plan: Plan, q, k, v, phi_q: Mlp, phi_k: Mlp, k_per_head, scor
                                   q_tokens=q if from_tokens else None, k_tokens=k if from_tokens else None)
     bufs.update(qt=qt, kt=kt, vt=vt, vm=vm, vc=vc, s=s, ws=ws, rp=rp, ci=ci, out=out)
     return out, bufs
+
+
+# ---- streaming generation: rotary positions, a paged cache and the attention over it -------------------------------------
+
+class Rope:
+    """veda_rope handle: the frequencies of one rotary scheme, on the current device.
+    axis_dim: channels of every axis (one number or up to three), the first sum(axis_dim) channels of a row rotate."""
+
+    def __init__(self, head_dim: int, axis_dim, base: float = 10000.0, pairs: int = VEDA_ROPE_INTERLEAVED, scaling: int = VEDA_ROPE_PLAIN,
+                 factor: float = 1.0, trained_len: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0, amplitude: float = 0.0):
+        dims = [int(axis_dim)] if isinstance(axis_dim, int) else [int(x) for x in axis_dim]
+        self.handle = None
+        if not 1 <= len(dims) <= 3:
+            raise VedaError(VEDA_ERR_INVALID_ARG, "Rope", "axis_dim must name 1 to 3 axes")
+        cfg = veda_rope_config(head_dim, len(dims), (C.c_int32 * 3)(*dims), pairs, scaling, base, factor, trained_len, beta_fast, beta_slow,
+                               amplitude)
+        h = C.c_void_p()
+        _check(load().veda_rope_create(C.byref(cfg), C.byref(h)), "veda_rope_create")
+        self.handle = h
+        self.head_dim, self.axes, self.rot_dim = int(head_dim), len(dims), sum(dims)
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def frequencies(self):
+        """(radians per position of every pair, float64 [rot_dim / 2]; the amplitude)"""
+        f, a = np.empty(self.rot_dim // 2, np.float64), C.c_double()
+        _check(load().veda_rope_frequencies(self.handle, f.ctypes.data_as(C.POINTER(C.c_double)), C.byref(a)), "veda_rope_frequencies")
+        return f, a.value
+
+    def close(self):
+        if self.handle is not None:
+            load().veda_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _need(ok: bool, where: str, what: str):
+    if not ok:
+        raise VedaError(VEDA_ERR_INVALID_ARG, where, what)
+
+
+def _on(dev: torch.device, where: str):
+    """The kernels run on the current device, so that is where the tensors have to be."""
+    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device(), where, f"tensors on {dev}, which is not the current device")
+
+
+def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Optional[torch.Tensor] = None, transpose: bool = False):
+    """Rotates x [batch, heads, N, d] by positions i32 [batch or 1, N, axes] (or [N], one axis) into y (x itself: in place).
+    transpose=True turns the gradient of the result into the gradient of x."""
+    w = "veda_rope_apply"
+    _need(x.dim() == 4 and x.shape[3] == rope.head_dim and (x.stride(3) == 1 or x.numel() == 0), w,
+          "x must be [batch, heads, N, head_dim] with unit channel stride")
+    _on(x.device, w)
+    if rope.axes == 1 and positions.dim() == 1:
+        positions = positions.reshape(1, -1, 1)
+    _need(positions.dim() == 3 and positions.shape[0] in (1, x.shape[0]) and tuple(positions.shape[1:]) == (x.shape[2], rope.axes) and
+          positions.dtype == torch.int32 and positions.is_contiguous() and positions.device == x.device, w,
+          f"positions must be contiguous i32 [{x.shape[0]} or 1, {x.shape[2]}, {rope.axes}] on {x.device}")
+    if y is None:
+        y = torch.empty_like(x)
+        if y.stride(3) != 1:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _need(y.shape == x.shape and y.dtype == x.dtype and y.device == x.device and (y.stride(3) == 1 or y.numel() == 0), w,
+          "y must be as x, with unit channel stride")
+    pos_b = 0 if positions.shape[0] == 1 else positions.stride(0)
+    _check(load().veda_rope_apply(rope.handle, _dtype_code(x.dtype), x.shape[0], x.shape[1], x.shape[2], _ptr(x), veda_strides(*x.stride()[:3]),
+                                  _ptr(positions), pos_b, int(transpose), _ptr(y), veda_strides(*y.stride()[:3]), _stream()), w)
+    return y
+
+
+class Cache:
+    """One layer's paged cache: pools k, v [pages, kv_heads, page_tokens, d], made here unless given (views with a larger page
+    stride are fine)."""
+
+    def __init__(self, pages: int, page_tokens: int, kv_heads: int, head_dim: int, dtype: torch.dtype, device="cuda",
+                 k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+        shape = (pages, kv_heads, page_tokens, head_dim)
+        if k is None and v is None:
+            k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        inner = (page_tokens * head_dim, head_dim, 1)
+        for t in (k, v):
+            _need(t is not None and tuple(t.shape) == shape and t.dtype == dtype and t.stride()[1:] == inner and t.device == k.device and
+                  t.stride(0) == k.stride(0), "Cache", f"k and v must be {dtype} {list(shape)} with close rows, heads and tokens")
+        self.k, self.v = k, v
+        self.pages, self.page_tokens, self.kv_heads, self.head_dim, self.dtype = int(pages), int(page_tokens), int(kv_heads), int(head_dim), dtype
+        stride = k.stride(0) if pages > 1 else 0
+        self._struct = veda_cache(self.pages, self.page_tokens, self.kv_heads, self.head_dim, _dtype_code(dtype), stride, _ptr(k), _ptr(v))
+
+
+class CacheBatch:
+    """The sequences of a call: page_table i32 [seqs, max_pages], kv_len i32 [seqs], q_start i32 [seqs + 1] on the GPU (read when the
+    kernels run), max_new: the most new tokens of any sequence."""
+
+    def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor, max_new: int):
+        seqs = page_table.shape[0]
+        _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and (page_table.stride(1) == 1 or page_table.shape[1] == 1), "CacheBatch",
+              "page_table must be i32 [seqs, max_pages]")
+        for t, n in ((kv_len, seqs), (q_start, seqs + 1)):
+            _need(tuple(t.shape) == (n,) and t.dtype == torch.int32 and t.is_contiguous() and t.device == page_table.device, "CacheBatch",
+                  "kv_len and q_start must be contiguous i32 [seqs] and [seqs + 1] where the page table is")
+        self.page_table, self.kv_len, self.q_start, self.max_new, self.seqs = page_table, kv_len, q_start, int(max_new), int(seqs)
+
+    def struct(self, rows: int) -> veda_cache_batch:
+        t = self.page_table
+        return veda_cache_batch(self.seqs, rows, self.max_new, t.shape[1], max(t.stride(0), t.shape[1]), _ptr(t), _ptr(self.kv_len), _ptr(self.q_start))
+
+
+def _rows(cache: Cache, t: torch.Tensor, rows: int, where: str, name: str) -> veda_strides:
+    _need(t.dim() == 3 and t.shape[0] == rows and t.shape[2] == cache.head_dim and t.dtype == cache.dtype and t.device == cache.k.device and
+          (t.stride(2) == 1 or t.numel() == 0), where, f"{name} must be {cache.dtype} [{rows}, heads, {cache.head_dim}] beside the cache")
+    return veda_strides(0, t.stride(1), t.stride(0))
+
+
+def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                      positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
+    """Writes the new rows' k (rotated) and v [rows, kv_heads, d] into the cache; with q [rows, q_heads, d], returns q rotated (q_out).
+    positions i32 [rows, axes]; without them the position in the sequence (ropes of one axis)."""
+    w, rows = "veda_cache_append", k.shape[0]
+    _on(cache.k.device, w)
+    sk, sv = _rows(cache, k, rows, w, "k"), _rows(cache, v, rows, w, "v")
+    _need(k.shape[1] == cache.kv_heads and v.shape[1] == cache.kv_heads, w, "k and v must have the cache's heads")
+    _need(batch.page_table.device == cache.k.device, w, "the batch must be where the cache is")
+    sq = so = veda_strides(0, 0, 0)
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty((rows, q.shape[1], cache.head_dim), dtype=cache.dtype, device=q.device)
+        sq, so = _rows(cache, q, rows, w, "q"), _rows(cache, q_out, rows, w, "q_out")
+        _need(q.shape[1] == q_out.shape[1], w, "q and q_out must have the same heads")
+    else:
+        _need(q_out is None, w, "q_out without q")
+    if positions is not None:
+        _need(rope is not None and tuple(positions.shape) == (rows, rope.axes) and positions.dtype == torch.int32 and positions.is_contiguous() and
+              positions.device == k.device, w, "positions must be contiguous i32 [rows, axes of rope]")
+    bs = batch.struct(rows)
+    _check(load().veda_cache_append(C.byref(cache._struct), C.byref(bs), _ptr(k), sk, _ptr(v), sv, 0 if q is None else q.shape[1], _ptr(q), sq,
+                                    _ptr(q_out), so, None if rope is None else rope.handle, _ptr(positions), _stream()), w)
+    return q_out
+
+
+def veda_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, q_heads: int, rows: int) -> int:
+    """Bytes of scratch for veda_cache_attn_fwd on buffers of `rows` rows."""
+    bs = batch.struct(rows)
+    return int(load().veda_cache_attn_workspace_bytes(C.byref(cache._struct), C.byref(bs), q_heads))
+
+
+def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                        workspace: Optional[torch.Tensor] = None):
+    """Attention of the new rows q [rows, q_heads, d] over the cache.  block, window, sinks: which keys a row sees (veda_visible: block 1
+    causal, 0 everything).  Returns (out [rows, q_heads, d], lse fp32 [q_heads, rows] or None); rows of no sequence are left as they are
+    in buffers given, and undefined in buffers made here."""
+    w, rows = "veda_cache_attn_fwd", q.shape[0]
+    _on(cache.k.device, w)
+    sq = _rows(cache, q, rows, w, "q")
+    _need(batch.page_table.device == cache.k.device, w, "the batch must be where the cache is")
+    if out is None:
+        out = torch.empty((rows, q.shape[1], cache.head_dim), dtype=cache.dtype, device=q.device)
+    so = _rows(cache, out, rows, w, "out")
+    _need(out.shape[1] == q.shape[1], w, "out must have q's heads")
+    if want_lse and lse is None:
+        lse = torch.empty((q.shape[1], rows), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _need(tuple(lse.shape) == (q.shape[1], rows) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == q.device, w,
+              "lse must be contiguous fp32 [q_heads, rows]")
+    bs = batch.struct(rows)
+    if workspace is None:
+        need = int(load().veda_cache_attn_workspace_bytes(C.byref(cache._struct), C.byref(bs), q.shape[1]))
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().veda_cache_attn_fwd(C.byref(cache._struct), C.byref(bs), q.shape[1], _ptr(q), sq, C.c_float(softmax_scale),
+                                      veda_visible(block, window, sinks), _ptr(out), so, _ptr(lse), _ptr(workspace) or None, nbytes, _stream()), w)
+    return out, lse
+
+
+def veda_cache_copy_pages(cache: Cache, pairs):
+    """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
+    _on(cache.k.device, "veda_cache_copy_pages")
+    p = np.ascontiguousarray(pairs, np.int32).reshape(-1, 2)
+    _check(load().veda_cache_copy_pages(C.byref(cache._struct), p.ctypes.data_as(C.c_void_p), p.shape[0], _stream()), "veda_cache_copy_pages")
+
+
+class Pages:
+    """veda_pages: which page belongs to which sequence (host).  extend and compact return the pairs [n, 2] for
+    veda_cache_copy_pages, which has to run before the pages are used."""
+
+    def __init__(self, pages: int, page_tokens: int, max_seqs: int, max_pages: int):
+        h = C.c_void_p()
+        self.handle = None
+        _check(load().veda_pages_create(pages, page_tokens, max_seqs, max_pages, C.byref(h)), "veda_pages_create")
+        self.handle, self.pages, self.page_tokens, self.max_seqs, self.max_pages = h, pages, page_tokens, max_seqs, max_pages
+
+    def _copies(self, name: str, capacity: int, *args):
+        buf, n = np.empty((capacity, 2), np.int32), C.c_int32()
+        _book(getattr(load(), name)(self.handle, *args, buf.ctypes.data_as(C.c_void_p), capacity, C.byref(n)), name)
+        return buf[:n.value]
+
+    def table(self) -> np.ndarray:
+        """A copy of the table, i32 [max_seqs, max_pages], -1 where there is no page."""
+        t = load().veda_pages_table(self.handle)
+        return np.ctypeslib.as_array(t, (self.max_seqs, self.max_pages)).copy()
+
+    def length(self, seq: int) -> int:
+        return int(load().veda_pages_length(self.handle, seq))
+
+    def free_count(self) -> int:
+        return int(load().veda_pages_free_count(self.handle))
+
+    def extend(self, seq: int, tokens: int) -> np.ndarray:
+        return self._copies("veda_pages_extend", 1, seq, tokens)
+
+    def fork(self, source: int, target: int):
+        _book(load().veda_pages_fork(self.handle, source, target), "veda_pages_fork")
+
+    def truncate(self, seq: int, tokens: int = 0):
+        _book(load().veda_pages_truncate(self.handle, seq, tokens), "veda_pages_truncate")
+
+    def evict(self, seq: int, first: int, last: int):
+        _book(load().veda_pages_evict(self.handle, seq, first, last), "veda_pages_evict")
+
+    def compact(self) -> np.ndarray:
+        return self._copies("veda_pages_compact", self.pages)
+
+    def close(self):
+        if self.handle is not None:
+            load().veda_pages_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _book(status: int, where: str):
+    if status == VEDA_ERR_WORKSPACE:
+        raise VedaError(status, where, load().veda_last_error().decode())
+    _check(status, where)
+
+
+def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale: float, rope: Optional[Rope] = None,
+                         positions: Optional[torch.Tensor] = None, block: int = 1, window: int = 0, sinks: int = 0,
+                         buffers: Optional[dict] = None):
+    """One attention call of a streaming step: q and k rotated, k and v appended, attention of the new rows over the cache.
+    Returns (out [rows, q_heads, d], buffers); `buffers` (optional dict) is filled on the first call and reused afterwards."""
+    b = {} if buffers is None else buffers
+    if rope is not None:
+        b["q"] = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))
+    else:
+        veda_cache_append(cache, batch, k, v)
+    need = veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])
+    if "ws" not in b or b["ws"].numel() < need:
+        b["ws"] = torch.empty(need, dtype=torch.uint8, device=q.device)
+    b["out"], _ = veda_cache_attn_fwd(cache, batch, q if rope is None else b["q"], softmax_scale, block, window, sinks, b.get("out"), workspace=b["ws"])
+    return b["out"], b

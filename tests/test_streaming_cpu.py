@@ -1,0 +1,307 @@
+"""Streaming operators, the parts that need no GPU: refusals at the C entry points and in the binding, and the page book against
+a plain model of it."""
+import ctypes as C
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_30325_amd import veda
+
+INVALID, UNSUPPORTED, WORKSPACE, OK = veda.VEDA_ERR_INVALID_ARG, veda.VEDA_ERR_UNSUPPORTED, veda.VEDA_ERR_WORKSPACE, veda.VEDA_OK
+AT = 1 << 20     # a 16-byte aligned address that no check reads from
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not veda.LIB_PATH.exists():
+        from paper_2605_30325_amd import build
+        build.build()
+    return veda.load()
+
+
+def _cache(**more):
+    f = dict(pages=8, page_tokens=64, kv_heads=2, head_dim=128, dtype=veda.VEDA_BF16, page_stride=0, k=AT, v=AT)
+    f.update(more)
+    return veda.veda_cache(*f.values())
+
+
+def _batch(**more):
+    f = dict(seqs=2, rows=10, max_new=5, max_pages=4, table_stride=4, page_table=AT, kv_len=AT, q_start=AT)
+    f.update(more)
+    return veda.veda_cache_batch(*f.values())
+
+
+BAD_CACHES = [
+    (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(pages=0), INVALID), (dict(kv_heads=0), INVALID), (dict(dtype=2), INVALID),
+    (dict(page_stride=-1), INVALID), (dict(page_stride=2 * 64 * 128 - 8), INVALID), (dict(page_stride=2 * 64 * 128 + 4), UNSUPPORTED),
+    (dict(head_dim=96), UNSUPPORTED), (dict(kv_heads=1025), UNSUPPORTED), (dict(page_tokens=8), UNSUPPORTED), (dict(page_tokens=48), UNSUPPORTED),
+    (dict(page_tokens=512), UNSUPPORTED), (dict(k=AT + 8), UNSUPPORTED),
+]
+BAD_BATCHES = [
+    (dict(seqs=-1), INVALID), (dict(rows=-1), INVALID), (dict(max_new=-1), INVALID), (dict(max_pages=0), INVALID), (dict(table_stride=3), INVALID),
+    (dict(page_table=None), INVALID), (dict(kv_len=None), INVALID), (dict(q_start=None), INVALID),
+    (dict(max_pages=1 << 25, table_stride=1 << 25), UNSUPPORTED), (dict(rows=(1 << 30) + 1), UNSUPPORTED),
+]
+
+
+def _append(lib, cache, batch, **more):
+    s = veda.veda_strides(0, 128, 256)
+    f = dict(k=AT, sk=s, v=AT, sv=s, q_heads=4, q=AT, sq=veda.veda_strides(0, 128, 512), q_out=AT, so=veda.veda_strides(0, 128, 512), rope=None, positions=None)
+    f.update(more)
+    return lib.veda_cache_append(None if cache is None else C.byref(cache), None if batch is None else C.byref(batch), *f.values(), None)
+
+
+def _attend(lib, cache, batch, **more):
+    s = veda.veda_strides(0, 128, 512)
+    f = dict(q_heads=4, q=AT, sq=s, scale=0.1, visible=veda.veda_visible(1, 0, 0), out=AT, so=s, lse=None, workspace=AT, workspace_bytes=1 << 30)
+    f.update(more)
+    return lib.veda_cache_attn_fwd(None if cache is None else C.byref(cache), None if batch is None else C.byref(batch), *f.values(), None)
+
+
+@pytest.mark.parametrize("field,status", BAD_CACHES)
+def test_bad_caches_are_refused(lib, field, status):
+    c = _cache(**field)
+    assert _append(lib, c, _batch()) == status
+    assert _attend(lib, c, _batch()) == status
+    assert lib.veda_cache_copy_pages(C.byref(c), None, 0, None) == status
+    assert lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(_batch()), 4) == 0
+
+
+@pytest.mark.parametrize("field,status", BAD_BATCHES)
+def test_bad_batches_are_refused(lib, field, status):
+    assert _append(lib, _cache(), _batch(**field)) == status
+    assert _attend(lib, _cache(), _batch(**field)) == status
+    assert lib.veda_cache_attn_workspace_bytes(C.byref(_cache()), C.byref(_batch(**field)), 4) == 0
+
+
+def test_null_cache_or_batch_is_refused(lib):
+    assert _append(lib, None, _batch()) == INVALID and _append(lib, _cache(), None) == INVALID
+    assert _attend(lib, None, _batch()) == INVALID and _attend(lib, _cache(), None) == INVALID
+    assert lib.veda_cache_copy_pages(None, None, 0, None) == INVALID
+
+
+@pytest.mark.parametrize("more,status", [
+    (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(q=None), INVALID), (dict(q_out=None), INVALID), (dict(q_heads=0), INVALID),
+    (dict(q_heads=-1), INVALID), (dict(q_heads=40000), UNSUPPORTED), (dict(sk=veda.veda_strides(0, -8, 256)), INVALID),
+    (dict(so=veda.veda_strides(0, 128, 64)), INVALID), (dict(so=veda.veda_strides(0, 64, 512)), INVALID), (dict(so=veda.veda_strides(0, 128, 1024)), INVALID),
+    (dict(sv=veda.veda_strides(0, 128, 260)), UNSUPPORTED), (dict(k=AT + 2), UNSUPPORTED),
+])
+def test_append_refusals(lib, more, status):
+    assert _append(lib, _cache(), _batch(), **more) == status
+
+
+@pytest.mark.parametrize("more,status", [
+    (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(q_heads=0), INVALID), (dict(q_heads=3), INVALID), (dict(q_heads=66), UNSUPPORTED),
+    (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(visible=veda.veda_visible(-1, 0, 0)), INVALID), (dict(visible=veda.veda_visible(1, -1, 0)), INVALID),
+    (dict(visible=veda.veda_visible(1, 0, -1)), INVALID), (dict(visible=veda.veda_visible((1 << 30) + 1, 0, 0)), INVALID),
+    (dict(so=veda.veda_strides(0, 128, 120)), INVALID), (dict(sq=veda.veda_strides(0, 128, 516)), UNSUPPORTED), (dict(out=AT + 8), UNSUPPORTED),
+])
+def test_attention_refusals(lib, more, status):
+    assert _attend(lib, _cache(), _batch(), **more) == status
+
+
+def test_attention_workspace_refusals(lib):
+    c, b = _cache(), _batch(seqs=1, rows=1, max_new=1, max_pages=4096, table_stride=4096)
+    need = lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(b), 4)
+    assert need > 0
+    assert _attend(lib, c, b, workspace_bytes=need - 1) == WORKSPACE
+    assert _attend(lib, c, b, workspace=None) == INVALID
+    assert _attend(lib, c, b, workspace=AT + 4, workspace_bytes=need) == UNSUPPORTED
+    # the rows of the buffers count
+    assert lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(_batch(seqs=1, rows=2, max_new=1, max_pages=4096, table_stride=4096)), 4) == 2 * need
+
+
+def test_empty_calls_do_nothing(lib):
+    for more in (dict(seqs=0, page_table=None, kv_len=None, q_start=None), dict(rows=0), dict(max_new=0)):
+        assert _append(lib, _cache(), _batch(**more), k=None, v=None) == OK
+        assert _attend(lib, _cache(), _batch(**more), q=None, out=None) == OK
+    assert lib.veda_cache_copy_pages(C.byref(_cache()), None, 0, None) == OK
+    same = np.asarray([[3, 3], [5, 5]], np.int32)      # a page onto itself: nothing to launch
+    assert lib.veda_cache_copy_pages(C.byref(_cache()), same.ctypes.data_as(C.c_void_p), 2, None) == OK
+
+
+@pytest.mark.parametrize("pair", [(0, 8), (8, 0), (-1, 3), (3, -1)])
+def test_copies_outside_the_pool_are_refused(lib, pair):
+    p = np.asarray([[0, 1], pair], np.int32)
+    assert lib.veda_cache_copy_pages(C.byref(_cache()), p.ctypes.data_as(C.c_void_p), 2, None) == INVALID
+    assert lib.veda_cache_copy_pages(C.byref(_cache()), None, 1, None) == INVALID
+    assert lib.veda_cache_copy_pages(C.byref(_cache()), p.ctypes.data_as(C.c_void_p), -1, None) == INVALID
+
+
+def _config(**more):
+    f = dict(head_dim=128, axes=3, axis_dim=(44, 42, 42), pairs=0, scaling=0, base=1e4, factor=1.0, trained_len=0.0, beta_fast=32.0, beta_slow=1.0, amplitude=0.0)
+    f.update(more)
+    f["axis_dim"] = (C.c_int32 * 3)(*f["axis_dim"])
+    return veda.veda_rope_config(*f.values())
+
+
+@pytest.mark.parametrize("more,status", [
+    (dict(axes=0), INVALID), (dict(axes=4), INVALID), (dict(axis_dim=(44, 42, 44)), INVALID), (dict(axis_dim=(43, 42, 42)), INVALID),
+    (dict(axis_dim=(0, 42, 42)), INVALID), (dict(pairs=2), INVALID), (dict(scaling=4), INVALID), (dict(base=1.0), INVALID),
+    (dict(base=float("nan")), INVALID), (dict(scaling=1, factor=0.5), INVALID), (dict(scaling=2, factor=float("inf")), INVALID),
+    (dict(scaling=2, factor=2.0, axis_dim=(2, 42, 42)), INVALID), (dict(scaling=3, factor=2.0), INVALID),
+    (dict(scaling=3, factor=2.0, trained_len=4096.0, beta_fast=1.0), INVALID), (dict(amplitude=-1.0), INVALID), (dict(amplitude=float("nan")), INVALID),
+    (dict(head_dim=0), INVALID), (dict(head_dim=132), UNSUPPORTED), (dict(head_dim=520), UNSUPPORTED),
+])
+def test_rope_config_refusals(lib, more, status):
+    out = C.c_void_p()
+    assert lib.veda_rope_create(C.byref(_config(**more)), C.byref(out)) == status
+    assert out.value is None
+
+
+def test_rope_null_arguments(lib):
+    out, s = C.c_void_p(), veda.veda_strides(0, 0, 128)
+    assert lib.veda_rope_create(None, C.byref(out)) == INVALID and lib.veda_rope_create(C.byref(_config()), None) == INVALID
+    assert lib.veda_rope_frequencies(None, None, None) == INVALID
+    assert lib.veda_rope_apply(None, 1, 1, 1, 1, AT, s, AT, 0, 0, AT, s, None) == INVALID
+    lib.veda_rope_destroy(None)
+
+
+# ---- the page book ------------------------------------------------------------------------------------------------------
+
+class Model:
+    """Sequences as lists of (page or None), straight from the description."""
+
+    def __init__(self, pages, page, seqs, width):
+        self.pages, self.page, self.width = pages, page, width
+        self.rows, self.length = [[] for _ in range(seqs)], [0] * seqs
+
+    def held(self, p):
+        return sum(r.count(p) for r in self.rows)
+
+    def free(self):
+        used = {p for r in self.rows for p in r if p is not None}
+        return [p for p in range(self.pages) if p not in used]
+
+    def table(self):
+        return np.asarray([[-1 if p is None else p for p in r] + [-1] * (self.width - len(r)) for r in self.rows], np.int32)
+
+    def extend(self, s, tokens):
+        row, copies = list(self.rows[s]), []
+        free = self.free()
+        need = -(-tokens // self.page) - len(row)
+        open_page = tokens > self.length[s] and self.length[s] % self.page
+        fresh = open_page and (row[-1] is None or self.held(row[-1]) > 1)
+        if need + bool(fresh) > len(free):
+            return None
+        if fresh:
+            if row[-1] is not None:
+                copies.append((row[-1], free[0]))
+            row[-1] = free.pop(0)
+        row += free[:need]
+        self.rows[s], self.length[s] = row, tokens
+        return copies
+
+
+@pytest.mark.parametrize("seed,page", [(0, 16), (1, 64), (2, 1), (3, 16), (4, 256)])
+def test_page_book_against_a_model(lib, seed, page):
+    rng = random.Random(seed)
+    pages, seqs, width = 24, 5, 12
+    book, model = veda.Pages(pages, page, seqs, width), Model(pages, page, seqs, width)
+    refused = {"extend": 0, "fork": 0}
+    for _ in range(600):
+        s, t = rng.randrange(seqs), rng.randrange(seqs)
+        n = model.length[s]
+        op = rng.choice(["extend"] * 4 + ["fork", "truncate", "evict", "compact"])
+        before = book.table()
+        if op == "extend":
+            tokens = min(width * page, n + rng.choice([0, 1, page - 1, page, 2 * page + 3]))
+            want = model.extend(s, tokens)
+            if want is None:
+                refused["extend"] += 1
+                with pytest.raises(veda.VedaError) as e:
+                    book.extend(s, tokens)
+                assert e.value.status == WORKSPACE and np.array_equal(book.table(), before) and book.length(s) == n
+            else:
+                assert [tuple(x) for x in book.extend(s, tokens).tolist()] == want
+        elif op == "fork":
+            if s == t or model.length[t]:
+                refused["fork"] += 1
+                with pytest.raises(veda.VedaError):
+                    book.fork(s, t)
+                assert np.array_equal(book.table(), before)
+            else:
+                book.fork(s, t)
+                model.rows[t], model.length[t] = list(model.rows[s]), n
+        elif op == "truncate":
+            tokens = rng.randint(0, n)
+            book.truncate(s, tokens)
+            model.rows[s], model.length[s] = model.rows[s][:-(-tokens // page)], tokens
+        elif op == "evict":
+            a = rng.randint(0, n)
+            b = rng.randint(a, n)
+            book.evict(s, a, b)
+            for i in range(-(-a // page), b // page):
+                model.rows[s][i] = None
+        else:
+            copies = [tuple(x) for x in book.compact().tolist()]
+            used = pages - len(model.free())
+            sources, targets = [c[0] for c in copies], [c[1] for c in copies]
+            assert len(set(targets)) == len(targets) and not set(sources) & set(targets)
+            assert all(a >= used > b and model.held(a) and not model.held(b) for a, b in copies)
+            move = dict(copies)
+            model.rows = [[move.get(p, p) for p in r] for r in model.rows]
+            assert sorted({p for r in model.rows for p in r if p is not None}) == list(range(used))
+        assert np.array_equal(book.table(), model.table())
+        assert [book.length(i) for i in range(seqs)] == model.length and book.free_count() == len(model.free())
+    assert refused["extend"] and refused["fork"]
+    for s in range(seqs):
+        book.truncate(s)
+    assert book.free_count() == pages
+
+
+def test_page_book_refusals(lib):
+    out, n = C.c_void_p(), C.c_int32(7)
+    for bad in ((0, 16, 1, 1), (1, 0, 1, 1), (1, 16, 0, 1), (1, 16, 1, 0)):
+        assert lib.veda_pages_create(*bad, C.byref(out)) == INVALID
+    assert lib.veda_pages_create(1, 16, 1, 1 << 27, C.byref(out)) == UNSUPPORTED
+    assert lib.veda_pages_create(1, 16, 1, 1, None) == INVALID and out.value is None
+    for call in (lib.veda_pages_fork, lib.veda_pages_truncate):
+        assert call(None, 0, 0) == INVALID
+    assert lib.veda_pages_evict(None, 0, 0, 0) == INVALID and lib.veda_pages_compact(None, None, 0, C.byref(n)) == INVALID
+    assert lib.veda_pages_extend(None, 0, 1, None, 0, C.byref(n)) == INVALID
+    assert lib.veda_pages_length(None, 0) == -1 and lib.veda_pages_free_count(None) == -1 and not lib.veda_pages_table(None)
+    lib.veda_pages_destroy(None)
+    book = veda.Pages(4, 16, 2, 3)
+    h = book.handle
+    assert lib.veda_pages_extend(h, 0, 20, None, 0, C.byref(n)) == OK and n.value == 0     # no copy, no list needed
+    assert lib.veda_pages_extend(h, 0, 19, None, 0, C.byref(n)) == INVALID                 # shorter
+    assert lib.veda_pages_extend(h, 0, 49, None, 0, C.byref(n)) == INVALID                 # beyond the table
+    assert lib.veda_pages_extend(h, 2, 1, None, 0, C.byref(n)) == INVALID and lib.veda_pages_extend(h, -1, 1, None, 0, C.byref(n)) == INVALID
+    assert lib.veda_pages_extend(h, 0, 20, None, 0, None) == INVALID
+    book.fork(0, 1)
+    assert lib.veda_pages_extend(h, 1, 21, None, 0, C.byref(n)) == WORKSPACE and book.length(1) == 20   # a copy, and no room to tell
+    assert lib.veda_pages_truncate(h, 0, 21) == INVALID and lib.veda_pages_truncate(h, 0, -1) == INVALID
+    assert lib.veda_pages_evict(h, 0, 5, 4) == INVALID and lib.veda_pages_evict(h, 0, 0, 21) == INVALID
+    assert lib.veda_pages_length(h, 2) == -1 and lib.veda_pages_length(h, -1) == -1
+    assert [tuple(x) for x in book.extend(1, 21).tolist()] == [(1, 2)]
+    book.truncate(0)
+    assert lib.veda_pages_compact(h, None, 0, C.byref(n)) == WORKSPACE and book.table()[1].tolist() == [0, 2, -1]
+    assert [tuple(x) for x in book.compact().tolist()] == [(2, 1)]
+
+
+# ---- the binding --------------------------------------------------------------------------------------------------------
+
+def test_binding_refuses_before_the_library(monkeypatch, lib):
+    monkeypatch.setattr(veda, "load", lambda: pytest.fail("the library was called"))
+    with pytest.raises(veda.VedaError, match="axis_dim"):
+        veda.Rope(128, (2, 2, 2, 2))
+    with pytest.raises(veda.VedaError, match="close rows"):
+        veda.Cache(4, 16, 2, 64, torch.float32, k=torch.zeros(4, 2, 16, 64), v=torch.zeros(4, 16, 2, 64).transpose(1, 2))
+    with pytest.raises(veda.VedaError, match="close rows"):
+        veda.Cache(4, 16, 2, 64, torch.float32, k=torch.zeros(4, 2, 16, 64))
+    table, length, start = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for bad in ((table.long(), length, start), (table, length[:1], start), (table, length, start[:2]), (table.T.contiguous().T, length, start)):
+        with pytest.raises(veda.VedaError):
+            veda.CacheBatch(*bad, 1)
+    cache, batch = veda.Cache(4, 16, 2, 64, torch.float32, device="cpu"), veda.CacheBatch(table, length, start, 1)
+    x = torch.zeros(3, 2, 64)
+    with pytest.raises(veda.VedaError, match="current device"):
+        veda.veda_cache_append(cache, batch, x, x)
+    with pytest.raises(veda.VedaError, match="current device"):
+        veda.veda_cache_attn_fwd(cache, batch, x, 0.1)
+    with pytest.raises(veda.VedaError, match="current device"):
+        veda.veda_cache_copy_pages(cache, [(0, 1)])

@@ -1,0 +1,679 @@
+"""Streaming operators on the GPU against plain 64-bit formulas: rotary positions, appends, attention over the paged cache, page
+copies, and all of them together as a generator uses them.
+
+Tolerances.  A rounding is off by at most half a step: bf16 2^-8, fp32 2^-24 of the value.
+  rope       an angle is 2 pi times a fraction of a turn rounded to fp32 (|fraction| <= 1/2: pi 2^-24 < 2^-22), sine and cosine and the
+             amplitude's product add a few 2^-24, two products and a sum three more: 2^-21 (|x0| + |x1|) A holds all; then the output's rounding.
+  attention  a logit is a sum of d products in fp32, however ordered: at most (d + 2) 2^-24 S off, S the largest sum of |q_c k_c| scale of
+             the row; the exponential's argument (logit minus reference, both up to S log2 e) and the exponential add 4 S 2^-24 and 2^-22.
+             The sum over n keys, the rescalings and the division add (n + 64) 2^-24.  All act on probabilities that average |v|, so
+             |error| <= A (2 ((d + 8) 2^-24 S + 2^-22) + 2 (n + 64) 2^-24) with A = sum p |v|.  bf16 rounds every probability
+             once, 2^-8 A, and the output, 2^-8 |o|; both a little enlarged (1.01) by each other."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_30325_amd import veda
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def dev():
+    return torch.device("cuda:0")
+
+
+def normal(shape, dtype, seed, gain=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (gain * torch.randn(shape, generator=g)).to(dtype).to(dev())
+
+
+# ---- rotary positions ---------------------------------------------------------------------------------------------------
+
+def frequencies(dims, base=10000.0, scaling="plain", factor=1.0, trained=0.0, fast=32.0, slow=1.0):
+    f, axis = [], []
+    for a, w in enumerate(dims):
+        for i in range(w // 2):
+            x = (base * factor ** (w / (w - 2)) if scaling == "ntk" else base) ** (-2.0 * i / w)
+            if scaling == "linear":
+                x /= factor
+            if scaling == "parts":
+                g = min(1.0, max(0.0, (trained * x / (2 * math.pi) - slow) / (fast - slow)))
+                x = x * g + x / factor * (1 - g)
+            f.append(x)
+            axis.append(a)
+    return np.asarray(f), axis
+
+
+def rotated(x, positions, dims, halves, transpose=False, amplitude=1.0, **scheme):
+    """x [..., tokens, d] and positions [..., tokens, axes] in 64 bits on the CPU; and the bound of the fp32 rotation."""
+    f, axis = frequencies(dims, **scheme)
+    x, rot = x.double().cpu(), sum(dims)
+    angle = positions.double().cpu()[..., axis] * torch.from_numpy(f)
+    c, s = amplitude * torch.cos(angle), amplitude * torch.sin(angle) * (-1.0 if transpose else 1.0)
+    i0 = torch.arange(rot // 2) if halves else 2 * torch.arange(rot // 2)
+    i1 = i0 + rot // 2 if halves else i0 + 1
+    y, bound = x.clone(), torch.zeros_like(x)
+    x0, x1 = x[..., i0], x[..., i1]
+    y[..., i0], y[..., i1] = x0 * c - x1 * s, x0 * s + x1 * c
+    bound[..., i0] = bound[..., i1] = 2.0 ** -21 * amplitude * (x0.abs() + x1.abs())
+    return y, bound
+
+
+def close(got, want, bound, dtype, what=""):
+    step = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    over = (got.double().cpu() - want).abs() - (bound + 1.01 * step * want.abs())
+    assert not torch.isnan(over).any() and over.max().item() <= 0.0, f"{what}: {over.max().item():.3e} over the bound"
+
+
+SCHEMES = [dict(), dict(scaling="linear", factor=4.0), dict(scaling="ntk", factor=8.0), dict(scaling="parts", factor=16.0, trained=4096.0)]
+KIND = {"plain": veda.VEDA_ROPE_PLAIN, "linear": veda.VEDA_ROPE_LINEAR, "ntk": veda.VEDA_ROPE_NTK, "parts": veda.VEDA_ROPE_BY_PARTS}
+
+
+def make_rope(d, dims, halves, base=10000.0, scaling="plain", factor=1.0, trained=0.0, **more):
+    return veda.Rope(d, dims, base=base, pairs=veda.VEDA_ROPE_HALVES if halves else veda.VEDA_ROPE_INTERLEAVED, scaling=KIND[scaling], factor=factor,
+                     trained_len=trained, **more)
+
+
+@pytest.mark.parametrize("scheme", SCHEMES, ids=lambda s: s.get("scaling", "plain"))
+def test_rope_frequencies(scheme):
+    rope = make_rope(128, (64, 20, 4), False, **scheme)
+    f, amp = rope.frequencies()
+    want, _ = frequencies((64, 20, 4), **scheme)
+    np.testing.assert_allclose(f, want, rtol=1e-14)
+    assert amp == pytest.approx(0.1 * math.log(16.0) + 1.0 if scheme.get("scaling") == "parts" else 1.0, rel=1e-15)
+    assert make_rope(64, 8, True, amplitude=1.5).frequencies()[1] == 1.5
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("halves", [False, True], ids=["interleaved", "halves"])
+@pytest.mark.parametrize("d,dims", [(128, (128,)), (64, (64,)), (128, (44, 42, 42)), (128, (64,)), (128, (34,)), (64, (2,)), (64, (6, 4)), (8, (8,)),
+                                    (40, (20, 10)), (512, (512,)), (504, (250,))])
+def test_rope_against_the_formula(dtype, halves, d, dims):
+    scheme = SCHEMES[(d + len(dims) + halves) % 4 if 2 not in dims else 0]
+    rope = make_rope(d, dims, halves, **scheme)
+    amp = rope.frequencies()[1]
+    for b, h, n, first in ((1, 1, 1, 0), (2, 3, 17, 1 << 20), (1, 5, 40, -9), (3, 40, 2, 1 << 30)):
+        x = normal((b, h, n, d), dtype, n)
+        pos = (first + torch.arange(b * n * len(dims)) * 37 % 1013).reshape(b, n, len(dims)).to(torch.int32).to(dev())
+        for transpose in (False, True):
+            y = veda.veda_rope_apply(rope, x, pos, transpose=transpose)
+            want, bound = rotated(x, pos[:, None], dims, halves, transpose, amp, **scheme)
+            close(y, want, bound, dtype, f"{b}x{h}x{n} from {first}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_rope_strides_sharing_and_in_place(dtype):
+    rope = make_rope(64, (32,), True)
+    buf = normal((2, 19, 5, 3 * 64), dtype, 5)                       # [b, n, h, (q k v)]
+    x = buf[..., 64:128].transpose(1, 2)
+    pos = torch.arange(19, dtype=torch.int32, device=dev()) * 1000
+    want, bound = rotated(x, pos[:, None], (32,), True)
+    out = torch.full((2, 5, 19, 128), 7.0, dtype=dtype, device=dev())
+    y = out[..., :64]
+    assert veda.veda_rope_apply(rope, x, pos, y) is y
+    close(y, want, bound, dtype)
+    assert bool((out[..., 64:] == 7.0).all())
+    before = buf.clone()
+    veda.veda_rope_apply(rope, x, pos.view(1, -1, 1), x)             # in place, positions of all samples
+    assert torch.equal(x, y)
+    keep = torch.ones_like(buf, dtype=torch.bool)
+    keep[..., 64:128] = False
+    assert torch.equal(buf[keep], before[keep])
+    for empty in (x[:0], x[:, :0], x[:, :, :0]):
+        assert veda.veda_rope_apply(rope, empty, pos[:empty.shape[2]].view(1, -1, 1)).shape == empty.shape
+
+
+def test_rope_gradient():
+    # the map is linear: <R x, g> = <x, R^T g>, and differences along single channels give R^T g exactly up to rounding
+    rope = make_rope(128, (64,), False, scaling="parts", factor=8.0, trained=2048.0)
+    x, g = normal((2, 3, 33, 128), F32, 1), normal((2, 3, 33, 128), F32, 2)
+    pos = (torch.arange(66, dtype=torch.int32, device=dev()) * 911).view(2, 33, 1)
+    dx = veda.veda_rope_apply(rope, g, pos, transpose=True)
+    y = veda.veda_rope_apply(rope, x, pos)
+    # each product of the two sums carries 2^-21 of its size, the sums of 25,344 terms in 64 bits none
+    size = (y.abs() * g.abs()).double().sum().item()
+    assert abs((y.double() * g.double()).sum().item() - (x.double() * dx.double()).sum().item()) <= 2.0 ** -20 * 2 * size
+    amp = rope.frequencies()[1]
+    for c in (0, 1, 62, 63, 64, 127):
+        step = torch.zeros_like(x)
+        step[..., c] = 0.5
+        hi, lo = (veda.veda_rope_apply(rope, x + s * step, pos).double() for s in (1, -1))
+        slope = ((hi - lo) * g.double()).sum(-1)            # (R(x + h e) - R(x - h e)) . g / (2 h), 2 h = 1
+        # the two results round up to 2^-21 A (|x| + 1) a channel, two channels are met, and x + h itself rounds
+        bound = 2 * 2.0 ** -20 * amp * (x.abs().amax(-1) + 2.0).double() * g.abs().amax(-1).double() * 2
+        assert bool(((slope - dx[..., c].double()).abs() <= bound).all())
+
+
+def test_rope_refuses_what_does_not_fit():
+    rope = make_rope(64, (24, 20, 20), False)
+    x, pos = normal((2, 3, 10, 64), F32, 0), torch.zeros((2, 10, 3), dtype=torch.int32, device=dev())
+    wrong = [(x[0], pos), (x[..., :32], pos), (x.transpose(2, 3), pos), (x.cpu(), pos), (x, pos[:, :9]), (x, pos.long()), (x, pos[..., :1]), (x, pos.cpu()),
+             (x, pos.transpose(0, 1).contiguous().transpose(0, 1)), (x, pos, x[:, :2]), (x, pos, x.bfloat16())]
+    for args in wrong:
+        with pytest.raises(veda.VedaError):
+            veda.veda_rope_apply(rope, *args)
+    with pytest.raises(veda.VedaError):      # rows of y on top of each other
+        veda.veda_rope_apply(rope, x, pos, x[:, :1].expand(2, 3, 10, 64))
+    with pytest.raises(TypeError):
+        veda.veda_rope_apply(rope, x.double(), pos)
+
+
+# ---- the cache ----------------------------------------------------------------------------------------------------------
+
+class Setup:
+    """Sequences of `new` rows behind `past` cached tokens, pages in no order, rows of no sequence before (lead) and behind."""
+
+    def __init__(self, new, past, hq, hk, d, dtype, page=16, holes=(), tail=3, seed=0, extra_width=0, spare=2, gain=1.0, pools=None):
+        self.new, self.past, self.hq, self.hk, self.d, self.dtype, self.page = list(new), list(past), hq, hk, d, dtype, page
+        self.len = [n + p for n, p in zip(new, past)]
+        width = max(1, max(-(-x // page) for x in self.len)) + extra_width
+        need = sum(-(-x // page) for x in self.len)
+        total = need + spare
+        ids = list(range(total))
+        random.Random(seed).shuffle(ids)
+        table = np.full((len(new), width), -1, np.int32)
+        for s, n in enumerate(self.len):
+            for i in range(-(-n // page)):
+                table[s, i] = ids.pop()
+        for s, i, mark in holes:
+            table[s, i] = mark
+        self.table = table
+        if pools is None:
+            pools = [normal((total, hk, page, d), dtype, 10 * seed + j + 1) for j in range(2)]
+        self.k, self.v = pools
+        self.cache = veda.Cache(self.k.shape[0], page, hk, d, dtype, k=self.k, v=self.v)
+        self.start = np.cumsum([0] + self.new)
+        self.batch = veda.CacheBatch(torch.from_numpy(table).to(dev()), torch.tensor(self.len, dtype=torch.int32, device=dev()),
+                                     torch.tensor(self.start, dtype=torch.int32, device=dev()), max_new=max(self.new + [0]))
+        self.rows = int(self.start[-1]) + tail
+        self.qkv = normal((self.rows, hq + 2 * hk, d), dtype, 10 * seed + 7, gain)
+        self.q = self.qkv[:, :hq]
+
+    def keys(self, s):
+        """(token numbers, K, V in 64 bits) of the keys that exist, on the CPU."""
+        at = [(t, self.table[s, t // self.page], t % self.page) for t in range(self.len[s])]
+        at = [x for x in at if 0 <= x[1] < self.k.shape[0]]
+        p, o = torch.tensor([x[1] for x in at], dtype=torch.int64), torch.tensor([x[2] for x in at], dtype=torch.int64)
+        k, v = (pool.cpu()[p, :, o].double() for pool in (self.k, self.v))
+        return torch.tensor([x[0] for x in at], dtype=torch.int64), k, v
+
+
+def attention(t, q, scale, block, window, sinks):
+    """out, lse and the bounds of both, [rows, q_heads, d] and [q_heads, rows], in 64 bits on the CPU."""
+    rows, hq, d = q.shape
+    out, lse = torch.zeros(rows, hq, d, dtype=torch.float64), torch.zeros(hq, rows, dtype=torch.float64)
+    ob, lb = torch.zeros_like(out), torch.zeros_like(lse)
+    g = t.hq // t.hk
+    for s, n in enumerate(t.new):
+        if not n:
+            continue
+        tok, k, v = t.keys(s)
+        r = slice(int(t.start[s]), int(t.start[s + 1]))
+        p = t.len[s] - n + torch.arange(n)
+        e = (torch.div(p, block, rounding_mode="floor") + 1) * block if block else torch.full_like(p, t.len[s])
+        seen = (tok < e[:, None]) & (p >= 0)[:, None]
+        if window:
+            seen &= (tok >= e[:, None] - window) | (tok < sinks)
+        for h in range(hq):
+            qh, kh, vh = q[r, h].double().cpu(), k[:, h // g], v[:, h // g]
+            x = (qh @ kh.T * scale).masked_fill(~seen, -math.inf)
+            big = (qh.abs() @ kh.abs().T * scale).masked_fill(~seen, 0.0).amax(1) if len(tok) else torch.zeros(n, dtype=torch.float64)
+            pr = torch.nan_to_num(torch.softmax(x, 1), nan=0.0) if len(tok) else torch.zeros(n, 0, dtype=torch.float64)
+            vis = torch.where(seen.any(0)[:, None], vh, 0.0)          # what no row sees may be anything
+            out[r, h] = pr @ vis
+            lse[h, r] = torch.logsumexp(x, 1) if len(tok) else -math.inf
+            count = seen.sum(1).double()
+            delta = (d + 8) * 2.0 ** -24 * big + 2.0 ** -22
+            mean = pr @ vis.abs()
+            ob[r, h] = mean * (2 * delta + 2 * (count + 64) * 2.0 ** -24)[:, None] * 1.01
+            if t.dtype == BF16:
+                ob[r, h] += 1.01 * 2.0 ** -8 * mean
+            lb[h, r] = delta + (count + 64) * 2.0 ** -24 + 2.0 ** -21 * lse[h, r].nan_to_num(neginf=0.0).abs()
+    return out, lse, ob, lb
+
+
+def check_attention(t, scale=None, block=1, window=0, sinks=0, q=None):
+    q = t.q if q is None else q
+    scale = 1.0 / math.sqrt(t.d) if scale is None else scale
+    out = torch.full((t.rows, t.hq, t.d), 3.0, dtype=t.dtype, device=dev())
+    lse = torch.full((t.hq, t.rows), 5.0, device=dev())
+    veda.veda_cache_attn_fwd(t.cache, t.batch, q, scale, block, window, sinks, out, lse)
+    want, want_lse, ob, lb = attention(t, q, scale, block, window, sinks)
+    used = int(t.start[-1])
+    assert bool((out[used:] == 3.0).all()) and bool((lse[:, used:] == 5.0).all())       # rows of no sequence
+    close(out[:used], want[:used], ob[:used], t.dtype, "out")
+    g, w = lse[:, :used].double().cpu(), want_lse[:, :used]
+    assert torch.equal(g == -math.inf, w == -math.inf)
+    assert bool(((g - w).nan_to_num(nan=0.0).abs() <= lb[:, :used]).all()), "lse"
+    again, again_lse = veda.veda_cache_attn_fwd(t.cache, t.batch, q, scale, block, window, sinks, out.clone(), lse.clone())
+    assert torch.equal(again, out) and torch.equal(again_lse, lse)                       # equal inputs, equal bytes
+    return out, lse
+
+
+TYPES = [(F32, 64), (F32, 128), (BF16, 64), (BF16, 128)]
+IDS = ["f32-64", "f32-128", "bf16-64", "bf16-128"]
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("hq,hk", [(2, 2), (8, 2), (5, 1), (32, 1)])
+def test_single_tokens(dtype, d, hq, hk):
+    # every tile edge: lengths from the token alone on
+    t = Setup([1] * 12, [0, 1, 14, 15, 16, 30, 31, 32, 63, 64, 127, 500], hq, hk, d, dtype, page=16, seed=hq)
+    check_attention(t)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_ragged_chunks_and_pages(dtype, d, page):
+    t = Setup([37, 0, 1, 130, 64, 0], [0, 5, 300, 71, 64, 0], 4, 2, d, dtype, page=page, seed=page, extra_width=2)
+    check_attention(t)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("block,window,sinks", [(0, 0, 0), (1, 1, 0), (1, 7, 2), (1, 64, 4), (1, 100, 70), (16, 48, 0), (50, 0, 0), (50, 75, 33),
+                                                (0, 90, 16), (1000, 0, 0), (1, 0, 9), (3, 1 << 30, 1 << 30), (1 << 30, 5, 1)])
+def test_masks(dtype, d, block, window, sinks):
+    t = Setup([150, 9, 1], [60, 200, 333], 3, 1, d, dtype, page=32, seed=3)
+    check_attention(t, block=block, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+def test_rows_that_see_nothing(dtype, d):
+    # blocks whose end lies far behind the sequence's: the window ends before its first key; and holes instead of pages
+    t = Setup([20, 3], [0, 40], 2, 1, d, dtype, holes=[(1, 0, -1), (1, 1, -1), (1, 2, 99999)], seed=4)
+    out, lse = check_attention(t, block=1000, window=100)
+    assert bool((out[:23] == 0).all()) and bool((lse[:, :23] == -math.inf).all())
+    # more rows than tokens: rows at negative positions
+    t = Setup([20, 3], [0, 40], 2, 1, d, dtype, seed=5)
+    t.len, t.batch.kv_len = [12, 43], torch.tensor([12, 43], dtype=torch.int32, device=dev())
+    out, lse = check_attention(t)
+    assert bool((out[:8] == 0).all()) and bool((lse[:, :8] == -math.inf).all()) and bool((lse[:, 8:23] > -math.inf).all())
+    check_attention(t, block=0)
+    check_attention(t, block=7, window=9, sinks=1)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n", [1, 70])
+def test_holes_anywhere(dtype, d, n):
+    holes = [(0, 0, -1), (0, 3, -7), (0, 9, 1 << 30), (1, 1, -1), (1, 2, 2 ** 31 - 1)]
+    check_attention(Setup([n, n], [300, 90], 4, 1, d, dtype, holes=holes, seed=6))
+    check_attention(Setup([n, n], [300, 90], 4, 1, d, dtype, holes=holes, seed=6), window=40, sinks=50)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("n", [1, 90])
+def test_unseen_values_do_not_matter(dtype, d, bad, n):
+    # infinities and NaN behind the ends, in holes' pages, outside the window and in later tokens of the chunk
+    t = Setup([n, n], [200, 33], 4, 2, d, dtype, page=32, seed=8)
+    clean = check_attention(t, window=50, sinks=3)[0].clone()
+    seen = torch.zeros(t.k.shape[0], t.page, dtype=torch.bool)
+    for s in range(2):
+        for x in range(t.len[s]):
+            if x >= t.past[s] + 1 - 50 or x < 3:
+                seen[t.table[s, x // t.page], x % t.page] = True
+    hide = (~seen).to(dev())[:, None, :, None]
+    for pool in (t.k, t.v):
+        pool.copy_(torch.where(hide, torch.full_like(pool, bad), pool))
+    assert torch.equal(check_attention(t, window=50, sinks=3)[0], clean)
+    # a bad value of the chunk's last token reaches the last row alone, and only its channel
+    if n > 1:
+        page, at = t.table[0, (t.len[0] - 1) // t.page], (t.len[0] - 1) % t.page
+        t.v[page, :, at, 5] = bad
+        out, _ = veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 1.0 / math.sqrt(d), window=50, sinks=3, out=clean.clone())
+        assert torch.equal(out[:n - 1], clean[:n - 1]) and torch.equal(out[n:], clean[n:])
+        row = out[n - 1].float()
+        assert bool(torch.isnan(row[:, 5]).all()) if math.isnan(bad) else bool((row[:, 5] == bad).all())
+        keep = [c for c in range(d) if c != 5]
+        assert torch.equal(out[n - 1][:, keep], clean[n - 1][:, keep])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 40])
+def test_bad_queries_and_keys_that_are_seen(dtype, n):
+    t = Setup([n, 2], [100, 9], 2, 1, 64, dtype, seed=9)
+    clean = check_attention(t)[0].clone()
+    t.q[0, 1, 3] = math.nan
+    out, lse = veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.125, out=clean.clone(), want_lse=True)
+    assert bool(torch.isnan(out[0, 1]).all()) and bool(torch.isnan(lse[1, 0]))
+    out[0, 1], out[-3:] = clean[0, 1], clean[-3:]
+    assert torch.equal(out, clean)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+def test_large_logits(dtype, d):
+    # queries forty times as large: one key takes almost all; the reference moves often
+    t = Setup([5, 140], [400, 100], 4, 2, d, dtype, page=64, seed=11, gain=40.0)
+    check_attention(t)
+    check_attention(t, scale=1e-6)
+    check_attention(t, scale=3.0)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,hq,hk", [(1, 3, 1), (3, 8, 2), (40, 4, 1)])
+def test_long_caches_are_split(dtype, d, n, hq, hk):
+    # one long sequence beside short and empty ones: splits with and without work, joined
+    t = Setup([n, 1, 0, n], [9000, 0, 70, 130], hq, hk, d, dtype, page=128, seed=12)
+    assert veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, hq, t.rows) > 0
+    check_attention(t)
+    check_attention(t, window=5000, sinks=100)
+    check_attention(t, block=0)
+
+
+def test_pools_beyond_4_gib():
+    # 16 KB a page and head: 150,000 pages of each pool are 4.9 GB, and the sequence lies at both ends
+    pages, page, hk, d = 150000, 64, 2, 128
+    pools = [torch.empty((pages, hk, page, d), dtype=BF16, device=dev()) for _ in range(2)]
+    t = Setup([3, 70], [200, 500], 4, hk, d, BF16, page=page, seed=13)
+    for pool, small in zip(pools, (t.k, t.v)):
+        pool[-small.shape[0]:] = small
+    moved = t.table + np.int32(pages - t.k.shape[0]) * (t.table >= 0)
+    cache = veda.Cache(pages, page, hk, d, BF16, k=pools[0], v=pools[1])
+    batch = veda.CacheBatch(torch.from_numpy(moved.astype(np.int32)).to(dev()), t.batch.kv_len, t.batch.q_start, 70)
+    out, _ = veda.veda_cache_attn_fwd(cache, batch, t.q, 0.1)
+    want, _ = veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.1)
+    assert torch.equal(out[:73], want[:73])
+    veda.veda_cache_append(cache, batch, t.qkv[:, 4:6], t.qkv[:, 6:])
+    veda.veda_cache_append(t.cache, t.batch, t.qkv[:, 4:6], t.qkv[:, 6:])
+    veda.veda_cache_copy_pages(cache, [(pages - 1, 0), (pages - 2, pages // 2)])
+    assert torch.equal(pools[0][-t.k.shape[0]:], t.k) and torch.equal(pools[1][-t.k.shape[0]:], t.v)
+    assert torch.equal(pools[0][0], t.k[-1]) and torch.equal(pools[1][pages // 2], t.v[-2])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_strided_tensors_and_pools(dtype):
+    # K and V pages of one allocation, queries and outputs as slices of wider rows and as [heads, rows, d]
+    t = Setup([33, 5], [50, 100], 4, 2, 64, dtype, seed=14)
+    want, lse = check_attention(t)
+    both = torch.zeros((t.k.shape[0], 2, 2, t.page, 64), dtype=dtype, device=dev())
+    both[:, 0], both[:, 1] = t.k, t.v
+    cache = veda.Cache(t.k.shape[0], t.page, 2, 64, dtype, k=both[:, 0], v=both[:, 1])
+    q = t.q.transpose(0, 1).contiguous().transpose(0, 1)
+    wide = torch.full((t.rows, 4, 192), 3.0, dtype=dtype, device=dev())
+    out, lse2 = veda.veda_cache_attn_fwd(cache, t.batch, q, 0.125, out=wide[..., 64:128], want_lse=True)
+    assert torch.equal(out[:38], want[:38]) and torch.equal(lse2[:, :38], lse[:, :38]) and bool((wide[..., :64] == 3.0).all())
+    spread = torch.full((2, 3), -1, dtype=torch.int32, device=dev())
+    table = torch.cat([t.batch.page_table, spread], 1)[:, :t.batch.page_table.shape[1]]      # rows of a wider table
+    out, _ = veda.veda_cache_attn_fwd(cache, veda.CacheBatch(table, t.batch.kv_len, t.batch.q_start, 33), q, 0.125)
+    assert torch.equal(out[:38], want[:38])
+
+
+def test_lists_out_of_range_stay_inside():
+    t = Setup([4, 4], [30, 30], 2, 1, 64, F32, seed=15)
+    out = torch.full((t.rows, 2, 64), 3.0, device=dev())
+    # rows from 6 on are cut off by max_new, lengths are cut to the table's width, starts to the buffer
+    odd = veda.CacheBatch(t.batch.page_table, torch.tensor([10 ** 9, -5], dtype=torch.int32, device=dev()),
+                          torch.tensor([-3, 9, 2 ** 31 - 1], dtype=torch.int32, device=dev()), max_new=6)
+    veda.veda_cache_attn_fwd(t.cache, odd, t.q, 0.1, out=out)
+    veda.veda_cache_append(t.cache, odd, t.qkv[:, 2:3], t.qkv[:, 3:4])
+    torch.cuda.synchronize()
+    assert bool((out[6:9] == 3.0).all()) and bool((out[9:] == 0.0).all()) and not bool((out[:6] == 3.0).any())
+
+
+# ---- appends ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("rope_dims,halves", [(None, False), ("all", True), ("all", False), ("axes", False), ("some", True), ("odd", True), ("odd", False)])
+def test_append(dtype, d, rope_dims, halves):
+    dims = {None: None, "all": (d,), "axes": (d // 2, d // 4, d // 4), "some": (d // 2,), "odd": (d // 4 + 2,)}[rope_dims]
+    rope = None if dims is None else make_rope(d, dims, halves)
+    t = Setup([19, 0, 1, 70, 40], [5, 9, 63, 128, 0], 6, 2, d, dtype, page=32, seed=21, holes=[(3, 5, -1)])
+    t.batch.kv_len = torch.tensor([24, 9, 64, 198, 25], dtype=torch.int32, device=dev())     # the last: 15 rows at negative positions
+    lens, used = [24, 9, 64, 198, 25], int(t.start[-1])
+    k, v = t.qkv[:, 6:8], t.qkv[:, 8:]
+    axes = 1 if dims is None else len(dims)
+    where = torch.cat([lens[s] - n + torch.arange(n) for s, n in enumerate(t.new)] + [torch.zeros(3, dtype=torch.int64)])
+    pos = torch.stack([where * (a + 1) + a for a in range(axes)], 1).to(torch.int32).to(dev()) if axes > 1 else None
+    k0, v0 = t.k.clone(), t.v.clone()
+    q_out = torch.full((t.rows, 6, d), 3.0, dtype=dtype, device=dev())
+    veda.veda_cache_append(t.cache, t.batch, k, v, rope, pos, t.q, q_out)
+    kw, vw, bound = k0.double().cpu(), v0.double().cpu(), torch.zeros(k0.shape, dtype=torch.float64)
+    p = pos.cpu() if pos is not None else where[:, None]
+    if rope is None:
+        kr, kb = k.double().cpu(), torch.zeros(k.shape, dtype=torch.float64)
+        qr, qb = t.q.double().cpu(), torch.zeros(t.q.shape, dtype=torch.float64)
+    else:
+        (kr, kb), (qr, qb) = (tuple(y.transpose(0, 1) for y in rotated(x.transpose(0, 1), p, dims, halves)) for x in (k, t.q))
+    written = torch.zeros(k0.shape[0], t.page, dtype=torch.bool)
+    for s, n in enumerate(t.new):
+        for i in range(n):
+            x, row = lens[s] - n + i, int(t.start[s]) + i
+            page = t.table[s, x // t.page] if x >= 0 else -1
+            if page < 0:
+                continue
+            kw[page, :, x % t.page], bound[page, :, x % t.page], vw[page, :, x % t.page] = kr[row], kb[row], v[row].double().cpu()
+            written[page, x % t.page] = True
+    assert torch.equal(t.v.double().cpu(), vw)
+    close(t.k, kw, bound, dtype, "k")
+    keep = (~written).to(dev())[:, None, :, None].expand_as(t.k)
+    assert torch.equal(t.k[keep], k0[keep])
+    close(q_out[:used], qr[:used], qb[:used], dtype, "q")
+    assert bool((q_out[used:] == 3.0).all())
+    if rope is None:
+        assert torch.equal(q_out[:used], t.q[:used])
+    # without q, and with q in place: the same bytes
+    t.k.copy_(k0)
+    veda.veda_cache_append(t.cache, t.batch, k, v, rope, pos)
+    close(t.k, kw, bound, dtype, "k alone")
+    veda.veda_cache_append(t.cache, t.batch, k, v, rope, pos, t.q, t.q)
+    assert torch.equal(t.q[:used], q_out[:used])
+
+
+def test_append_refuses_what_does_not_fit():
+    t = Setup([4], [8], 4, 2, 64, F32, seed=22)
+    k, v, rope = t.qkv[:, 4:6], t.qkv[:, 6:], make_rope(64, (24, 20, 20), False)
+    pos = torch.zeros((t.rows, 3), dtype=torch.int32, device=dev())
+    wrong = [dict(k=k[:, :1]), dict(v=v[:-1]), dict(k=k.bfloat16()), dict(q_out=t.q), dict(rope=rope), dict(positions=pos), dict(rope=rope, positions=pos[:-1]),
+             dict(rope=rope, positions=pos.long()), dict(rope=make_rope(128, (128,), True)), dict(q=t.q, q_out=t.q[:, :2]), dict(k=k.cpu())]
+    for more in wrong:
+        args = dict(k=k, v=v)
+        args.update(more)
+        with pytest.raises(veda.VedaError):
+            veda.veda_cache_append(t.cache, t.batch, **args)
+    with pytest.raises(veda.VedaError):
+        veda.veda_cache_attn_fwd(t.cache, t.batch, t.q[:, :3], 0.1)
+    with pytest.raises(veda.VedaError):
+        veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.1, lse=torch.zeros((t.rows, 4), device=dev()))
+
+
+# ---- copies of pages ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d,hk,page", [(BF16, 64, 1, 16), (F32, 128, 3, 64), (BF16, 128, 12, 256)])
+def test_copies_in_order(dtype, d, hk, page):
+    n = 40
+    both = normal((n, 2, hk, page, d), dtype, 31)
+    cache = veda.Cache(n, page, hk, d, dtype, k=both[:, 0], v=both[:, 1])
+    for pairs in ([(3, 4)], [(1, 2), (2, 3), (3, 1), (1, 1)], [(0, 5), (0, 6), (7, 5), (5, 8)], [(i, (i + 1) % n) for i in range(n)],
+                  [(9, 10)] * 3, [], [(random.Random(i).randrange(n), random.Random(i + 99).randrange(n)) for i in range(120)]):
+        want = both.clone()
+        for a, b in pairs:
+            want[b] = want[a]
+        veda.veda_cache_copy_pages(cache, np.asarray(pairs, np.int32).reshape(-1, 2))
+        assert torch.equal(both, want)
+
+
+def test_more_copies_than_a_launch_holds():
+    k, v = normal((2000, 1, 16, 64), BF16, 32), normal((2000, 1, 16, 64), BF16, 33)
+    cache, k0, v0 = veda.Cache(2000, 16, 1, 64, BF16, k=k, v=v), k.clone(), v.clone()
+    order = np.random.default_rng(0).permutation(2000).astype(np.int32).reshape(-1, 2)
+    veda.veda_cache_copy_pages(cache, order)
+    src, dst = torch.from_numpy(order[:, 0].astype(np.int64)).to(dev()), torch.from_numpy(order[:, 1].astype(np.int64)).to(dev())
+    k0[dst], v0[dst] = k0[src], v0[src]
+    assert torch.equal(k, k0) and torch.equal(v, v0)
+
+
+# ---- together -----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d,page", [(F32, 64, 16), (BF16, 128, 64)], ids=["f32", "bf16"])
+def test_a_streaming_run(dtype, d, page):
+    """Two clips made chunk by chunk, one branched on the way, old frames dropped, pages moved together: every attention against
+    the whole history of its clip in 64 bits."""
+    hq, hk, frame, sinks, window = 4, 2, 30, 20, 150
+    grid_h, grid_w, dims = 5, 6, (d // 2, d // 4, d // 4)
+    rope, book = make_rope(d, dims, False), veda.Pages(60, page, 4, 40)
+    cache = veda.Cache(60, page, hk, d, dtype)
+    for pool in (cache.k, cache.v):
+        pool.fill_(math.nan)
+    history = {s: [torch.zeros(0, hk, d, dtype=torch.float64) for _ in range(2)] for s in range(4)}
+    bufs, steps = {}, 0
+
+    def positions(a, n):
+        x = torch.arange(a, a + n)
+        return torch.stack([x // frame, x // grid_w % grid_h, x % grid_w], 1).to(torch.int32)
+
+    def step(seqs, news, seed):
+        nonlocal steps
+        starts = np.cumsum([0] + news)
+        for s, n in zip(seqs, news):
+            copies = book.extend(s, book.length(s) + n)
+            veda.veda_cache_copy_pages(cache, copies)
+        table = torch.from_numpy(book.table()[seqs]).to(dev())
+        lens = [book.length(s) for s in seqs]
+        batch = veda.CacheBatch(table, torch.tensor(lens, dtype=torch.int32, device=dev()), torch.tensor(starts, dtype=torch.int32, device=dev()), max(news))
+        rows = int(starts[-1])
+        qkv = normal((rows, hq + 2 * hk, d), dtype, seed)
+        pos = torch.cat([positions(a - n, n) for a, n in zip(lens, news)]).to(dev())
+        out, _ = veda.veda_cache_attention(cache, batch, qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:], 1.0 / math.sqrt(d), rope, pos,
+                                           block=frame, window=window, sinks=sinks, buffers=bufs if rows == 2 * frame else None)
+        for i, (s, n) in enumerate(zip(seqs, news)):
+            r = slice(int(starts[i]), int(starts[i + 1]))
+            step_cast = (lambda x: x.to(dtype).double())       # what the cache holds is rounded once
+            kr, qr = (step_cast(rotated(x[r].transpose(0, 1), pos[r].cpu(), dims, False)[0].transpose(0, 1)) for x in (qkv[:, hq:hq + hk], qkv[:, :hq]))
+            history[s] = [torch.cat([history[s][0], kr]), torch.cat([history[s][1], qkv[r, hq + hk:].double().cpu()])]
+            k, v = history[s]
+            tok, p = torch.arange(len(k)), lens[i] - n + torch.arange(n)
+            e = (p // frame + 1) * frame
+            seen = (tok < e[:, None]) & ((tok >= e[:, None] - window) | (tok < sinks))
+            for h in range(hq):
+                x = (qr[:, h] @ k[:, h // 2].T / math.sqrt(d)).masked_fill(~seen, -math.inf)
+                pr = torch.softmax(x, 1)
+                mean = pr @ v[:, h // 2].abs()
+                big = (qr[:, h].abs() @ k[:, h // 2].abs().T / math.sqrt(d)).amax(1, keepdim=True)
+                # q and k of the call and of the formula may round to different neighbours (their rotations differ by 2^-21): one step
+                # of the largest logit's sum each, and the attention's own bound
+                unit = 2.0 ** -7 if dtype == BF16 else 2.0 ** -20
+                tol = mean * (2 * 2 * unit * big + 2.0 ** -16) + (1.01 * 2.0 ** -8 * (mean + (pr @ v[:, h // 2]).abs()) if dtype == BF16 else 0.0)
+                err = (out[r, h].double().cpu() - pr @ v[:, h // 2]).abs()
+                assert bool((err <= tol).all()), (steps, s, h, (err - tol).max().item())
+        steps += 1
+
+    seed = 100
+    for _ in range(3):
+        step([0, 1], [frame, frame], seed)
+        seed += 1
+    step([0], [7], seed)                       # a part of a frame
+    book.fork(0, 2)                            # a branch that shares the open page
+    history[2] = list(history[0])
+    free = book.free_count()
+    step([2, 0], [23, 23], seed + 1)           # both write the same tokens' places: one of them on a copy
+    assert book.free_count() < free
+    for s in (0, 1, 2):                        # frames that nobody will see again
+        book.evict(s, sinks, max(sinks, book.length(s) + frame - window))
+    step([1, 2], [frame, frame], seed + 2)
+    book.truncate(0)                           # one clip ends; its pages are free
+    history[0] = [x[:0] for x in history[0]]
+    copies = book.compact()
+    assert len(copies) > 0
+    veda.veda_cache_copy_pages(cache, copies)
+    used = book.pages - book.free_count()
+    for pool in (cache.k, cache.v):
+        pool[used:].fill_(math.nan)
+    step([2, 1, 0], [frame, 1, 5], seed + 3)
+    step([1], [1], seed + 4)
+    step([1, 2], [frame, frame], seed + 5)
+    for s in (0, 1, 2):
+        book.truncate(s)
+    assert book.free_count() == 60
+
+
+def test_beside_the_tile_sparse_attention():
+    """One clip whose chunk is the whole clip: rotated rows through the tile-sparse path with every tile kept, and through the cache."""
+    from paper_2605_30325_amd import workloads as wlm
+    grid, heads, d = (4, 9, 10), 3, 128
+    n = 4 * 9 * 10
+    shapes = np.asarray([(4, 4, 4), (1, 8, 8), (16, 2, 2)], np.int32)
+    plan = veda.Plan(1, heads, d, grid, shapes, BF16)
+    plan.set_option(veda.VEDA_OPT_EXACT_LOGIT_SCALE, 1)
+    wl = wlm.custom_workload("streaming", heads, d, "bf16", grid, True, (1, 1), seed=5)
+    q, k, v = wlm.make_qkv(wl, dev())
+    rope = make_rope(d, (44, 42, 42), False)
+    x = torch.arange(n, device=dev())
+    pos = torch.stack([x // 90, x // 10 % 9, x % 10], 1).to(torch.int32)
+    qr, kr = (veda.veda_rope_apply(rope, y, pos[None]) for y in (q, k))
+    qt, vm, _ = veda.veda_tile_layout(plan, qr)
+    kt, _, _ = veda.veda_tile_layout(plan, kr, want_mask=False)
+    vt, _, _ = veda.veda_tile_layout(plan, v, veda.VEDA_CHANNEL_MAJOR, want_mask=False)
+    rp = torch.tensor(np.cumsum([0] + [t for t in plan.tiles for _ in range(t)]), dtype=torch.int32, device=dev())
+    ci = torch.cat([torch.arange(t, dtype=torch.int32) for t in plan.tiles for _ in range(t)]).to(dev())
+    tiled, _ = veda.veda_sparse_attn_fwd(plan, qt, kt, vt, vm, rp, ci, 1.0 / math.sqrt(d))
+    book, cache = veda.Pages(6, 64, 1, 6), veda.Cache(6, 64, heads, d, BF16)
+    assert len(book.extend(0, n)) == 0
+    batch = veda.CacheBatch(torch.from_numpy(book.table()).to(dev()), torch.tensor([n], dtype=torch.int32, device=dev()),
+                            torch.tensor([0, n], dtype=torch.int32, device=dev()), n)
+    rows = [y[0].transpose(0, 1) for y in (q, k, v)]
+    out, _ = veda.veda_cache_attention(cache, batch, *rows, 1.0 / math.sqrt(d), rope, pos, block=0)
+    # both round every probability and the output once: 2^-8 of at most the largest |v| each, on either side
+    assert (out.transpose(0, 1).float() - tiled[0].float()).abs().max().item() <= 4 * 2.0 ** -8 * v.abs().max().item()
+    assert (out.transpose(0, 1).float() - tiled[0].float()).abs().mean().item() <= 2.0 ** -8 * v.float().abs().mean().item()
+
+
+def test_captured_and_replayed():
+    """Two graphs with their own workspaces over one cache, lengths and pages changed between the replays."""
+    hq, hk, d, page, width = 8, 2, 128, 32, 200
+    rope = make_rope(d, (d,), True)
+    cache = veda.Cache(2 * width, page, hk, d, BF16, k=normal((2 * width, hk, page, d), BF16, 41), v=normal((2 * width, hk, page, d), BF16, 42))
+    table = torch.arange(2 * width, dtype=torch.int32, device=dev()).view(2, width)
+    lens = torch.tensor([page * width - 40, 77], dtype=torch.int32, device=dev())
+    graphs = []
+    for new in (1, 20):
+        start = torch.tensor([0, new, 2 * new], dtype=torch.int32, device=dev())
+        batch = veda.CacheBatch(table, lens, start, new)
+        qkv = normal((2 * new, hq + 2 * hk, d), BF16, new)
+        ws = torch.empty(veda.veda_cache_attn_workspace_bytes(cache, batch, hq, 2 * new), dtype=torch.uint8, device=dev())
+        out, q_out = (torch.zeros((2 * new, hq, d), dtype=BF16, device=dev()) for _ in range(2))
+
+        def call(batch=batch, qkv=qkv, ws=ws, out=out, q_out=q_out):
+            veda.veda_cache_append(cache, batch, qkv[:, hq:hq + hk], qkv[:, hq + hk:], rope, None, qkv[:, :hq], q_out)
+            veda.veda_cache_attn_fwd(cache, batch, q_out, 0.09, window=3000, sinks=5, out=out, workspace=ws)
+
+        call()
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+            call()
+        graphs.append((g, call, qkv, out))
+    for i in range(4):
+        lens.copy_(torch.tensor([page * width - 39 + i, 77 + 40 * i], dtype=torch.int32))
+        table.copy_(torch.randperm(2 * width, generator=torch.Generator().manual_seed(i)).to(torch.int32).view(2, width))
+        for g, call, qkv, out in graphs:
+            qkv.copy_(normal(qkv.shape, BF16, 50 + i))
+            out.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            got, k, v = out.clone(), cache.k.clone(), cache.v.clone()
+            out.zero_()
+            call()
+            torch.cuda.synchronize()
+            assert torch.equal(got, out) and torch.equal(k, cache.k) and torch.equal(v, cache.v) and bool(got.float().abs().sum() > 0)
+
+
+def test_two_streams_at_once():
+    calls = []
+    for seed in (1, 2):
+        t = Setup([1, 2], [5000, 900], 8, 2, 128, BF16, page=64, seed=seed)
+        want, _ = veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.09)
+        calls.append((t, want[:3].clone(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for t, _, s in calls:
+            with torch.cuda.stream(s):
+                got.append(veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.09)[0])
+    torch.cuda.synchronize()
+    for i, o in enumerate(got):
+        assert torch.equal(o[:3], calls[i % 2][1])
