@@ -48,6 +48,9 @@ template <bool kBf16, int D> struct AttnTile {
     // 16-byte chunk c of row r lies at chunk c ^ swizzle: operand reads of a wave then fall into different banks.
     __device__ static int k_swizzle(int r) { return kBf16 ? (D == 128 ? r & 15 : (r >> 1) & 7) : r & 7; }
     __device__ static int v_swizzle(int r) { return kBf16 ? (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) : ((r >> 2) & 1) << 3; }
+    // What the swizzles of load j of a segment (1024 / kRowB rows each) have on top of load 0's, as address bits.
+    __device__ static constexpr uint32_t k_step(int j) { return (uint32_t)j << (kBf16 || D == 64 ? 6 : 5); }
+    __device__ static constexpr uint32_t v_step(int j) { return kBf16 ? 0u : (uint32_t)(D == 64 ? j : j >> 1) << 7; }
 };
 
 template <bool kBf16, int D> struct AttnRow {
@@ -78,6 +81,29 @@ template <bool kBf16, int D> __device__ __forceinline__ f32x16 attn_scores(const
     return s;
 }
 
+// Moves every row's reference up to its maximum mx (of this lane's half, log2 units) and rescales what was summed.
+template <bool kBf16, int D> __device__ __forceinline__ void attn_move_ref(AttnRow<kBf16, D>& st, float mx) {
+    const float ref = fmaxf(st.ref, max_with_other_half(mx));
+    const float alpha = ref == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.ref - ref);
+    st.ref = ref;
+    st.sub = ref == -INFINITY ? 0.0f : -ref;
+    st.l *= alpha;
+#pragma unroll
+    for (int nb = 0; nb < D / 32; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[nb][i] *= alpha;
+}
+
+// A value that is not finite reaches the rows that see it, and no others, as a count: 1 for +inf, 64 for -inf, 65 for NaN, of at most
+// 32 keys, so a sum of them says which there were.
+__device__ __forceinline__ float attn_code(float x) {
+    return (x < INFINITY ? 0.0f : 1.0f) + (x > -INFINITY ? 0.0f : 64.0f);
+}
+__device__ __forceinline__ float attn_decode(float code) {
+    const float down = floorf(code * (1.0f / 64.0f));
+    return (code > 64.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+}
+
 // 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.
 template <bool kBf16, int D>
 __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16, D>& st, uint32_t k, uint32_t v, int key0, uint32_t exists,
@@ -97,17 +123,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
     mx *= a.scale_log2;
-    if (__any(mx > st.ref + kAttnSlack)) {
-        const float ref = fmaxf(st.ref, max_with_other_half(mx));
-        const float alpha = ref == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.ref - ref);
-        st.ref = ref;
-        st.sub = ref == -INFINITY ? 0.0f : -ref;
-        st.l *= alpha;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) st.o[nb][i] *= alpha;
-    }
+    if (__any(mx > st.ref + kAttnSlack)) attn_move_ref<kBf16, D>(st, mx);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -139,7 +155,10 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kk, nb), zero, z, 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) {
+                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kk, nb), zero, z, 0, 0, 0);
+                    if (nb & 1) __builtin_amdgcn_sched_barrier(0);
+                }
             float t = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) t += z[i];
@@ -149,37 +168,42 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kk, nb), p[kk], st.o[nb], 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) {
+                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kk, nb), p[kk], st.o[nb], 0, 0, 0);
+                    if (nb & 1) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
+                }
         } else {
             bf16x8 on[2];
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) on[kk][e] = (__bf16)((float)p[kk][e] > 0.0f ? 1.0f : 0.0f);
+            f32x16 o[NB];   // indexed as the loop goes, so it lies in memory: this path must not cost the others registers
 #pragma unroll
+            for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
+#pragma unroll 1
             for (int nb = 0; nb < NB; ++nb) {
-                f32x16 up, down;   // visible values that are +inf or NaN, -inf or NaN
+                f32x16 sum = o[nb], code;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) up[i] = down[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) code[i] = 0.0f;
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
-                    const bf16x8 x = operand(kk, nb);
-                    bf16x8 f, u, d;
+                    bf16x8 x = operand(kk, nb), y;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float y = (float)x[e];
-                        const bool finite = fabsf(y) < INFINITY;
-                        f[e] = finite ? x[e] : (__bf16)0.0f;
-                        u[e] = (__bf16)(!finite && !(y < 0.0f) ? 1.0f : 0.0f);
-                        d[e] = (__bf16)(!finite && !(y > 0.0f) ? 1.0f : 0.0f);
+                        y[e] = (__bf16)attn_code((float)x[e]);
+                        x[e] = (float)y[e] == 0.0f ? x[e] : (__bf16)0.0f;
                     }
-                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[kk], st.o[nb], 0, 0, 0);
-                    up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u, on[kk], up, 0, 0, 0);
-                    down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d, on[kk], down, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[kk], sum, 0, 0, 0);
+                    code = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, on[kk], code, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) st.o[nb][i] += (up[i] > 0.0f ? INFINITY : 0.0f) + (down[i] > 0.0f ? -INFINITY : 0.0f);
+                for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
+                o[nb] = sum;
             }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) st.o[nb] = o[nb];
         }
     } else {
         // step i takes keys 8 (i / 4) + i % 4 of either lane half: register i is the operand
@@ -206,25 +230,142 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(operand(i, nb), s[i], st.o[nb], 0, 0, 0);
         } else {
+            f32x16 o[NB];   // in memory, as above
 #pragma unroll
+            for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
+#pragma unroll 1
             for (int nb = 0; nb < NB; ++nb) {
-                f32x16 up, down;
+                f32x16 sum = o[nb], code;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) up[i] = down[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) code[i] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float y = operand(i, nb), on = s[i] > 0.0f ? 1.0f : 0.0f;
-                    const bool finite = fabsf(y) < INFINITY;
-                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(finite ? y : 0.0f, s[i], st.o[nb], 0, 0, 0);
-                    up = __builtin_amdgcn_mfma_f32_32x32x2f32(!finite && !(y < 0.0f) ? 1.0f : 0.0f, on, up, 0, 0, 0);
-                    down = __builtin_amdgcn_mfma_f32_32x32x2f32(!finite && !(y > 0.0f) ? 1.0f : 0.0f, on, down, 0, 0, 0);
+                    const float x = operand(i, nb), y = attn_code(x);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(y == 0.0f ? x : 0.0f, s[i], sum, 0, 0, 0);
+                    code = __builtin_amdgcn_mfma_f32_32x32x2f32(y, s[i] > 0.0f ? 1.0f : 0.0f, code, 0, 0, 0);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) st.o[nb][i] += (up[i] > 0.0f ? INFINITY : 0.0f) + (down[i] > 0.0f ? -INFINITY : 0.0f);
+                for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
+                o[nb] = sum;
             }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) st.o[nb] = o[nb];
         }
     }
 }
+
+// A tile of 64 keys that every row of a wave sees, bf16, with the order of issue pinned: an MFMA holds the matrix pipe for 32 cycles, in
+// whose shadow vector instructions issue (4 cycles each, 8 an exponential), so each segment below is one MFMA and what belongs
+// under it.  Operand reads are issued kAhead MFMAs before their use.  The first scores' maximum and exponentials ride on the second
+// block's products; the exponentials assume that the reference stays, and are formed again in the rare other case.  The other
+// exponentials ride on the second product, 16 keys behind it.  (The same division of a step as the tile-sparse kernel's, attn_step.h; here
+// V lies token by token, so its operand takes two transposing reads.)
+template <int D> struct AttnStep {
+    static constexpr int G = D / 16, NB = D / 32, kAhead = 6, kRowB = D * 2, NF = 2 * G + 4 * NB;
+    static constexpr int kPieces = 4, kSeg = G / kPieces;   // block 0 comes in pieces, between which the caller asks for the next tile
+    bf16x8 fr[NF], p[4];
+    f32x16 s[2];
+    uint32_t k, v;
+
+    template <int F> __device__ __forceinline__ void read() {
+        if constexpr (F < 2 * G) {
+            fr[F] = *(lds_bf16x8_p)(uintptr_t)((k ^ (uint32_t)((F % G) << 5)) + (uint32_t)((F / G) * 32 * kRowB));
+        } else if constexpr (F < NF) {
+            constexpr int kk = (F - 2 * G) / NB, nb = (F - 2 * G) % NB;
+            const uint32_t at = (v ^ (uint32_t)(nb << 6)) + kk * 16 * kRowB;
+            const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
+            const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 8 * kRowB));
+            fr[F] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    template <int F, int E> __device__ __forceinline__ void read_to() {
+        if constexpr (F < E) { read<F>(); read_to<F + 1, E>(); }
+    }
+    __device__ __forceinline__ void begin(uint32_t k_at, uint32_t v_at) {
+        k = k_at;
+        v = v_at;
+        read_to<0, kAhead>();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <int F, int E> __device__ __forceinline__ void first(const AttnRow<true, D>& st) {
+        if constexpr (F < E) {
+            read<F + kAhead>();
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[F], st.qb[F], F == 0 ? z : s[0], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            first<F + 1, E>(st);
+        }
+    }
+    template <int P> __device__ __forceinline__ void piece(const AttnRow<true, D>& st) { first<P * kSeg, (P + 1) * kSeg>(st); }
+
+    // exponentials of registers e, e + 1 of key step kk
+    __device__ __forceinline__ void exp_pair(int kk, int e, float c, float sub, float& sum) {
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kk >> 1][8 * (kk & 1) + e], c, sub));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kk >> 1][8 * (kk & 1) + e + 1], c, sub));
+        const bf16x2 pr = {(__bf16)p0, (__bf16)p1};
+        sum += p0;
+        sum += p1;
+        p[kk][e] = pr[0];
+        p[kk][e + 1] = pr[1];
+    }
+    static constexpr int kMaxSeg = G >= 8 ? 2 : 1, kExpSeg = G - 2 - kMaxSeg;   // block 0's last product needs two more to retire
+    static_assert(kExpSeg >= 1 && 8 % kExpSeg == 0 && (8 / kExpSeg) % 2 == 0, "exponentials come in pairs");
+    template <int F> __device__ __forceinline__ void second(const AttnRow<true, D>& st, float c, float& mx, float& sum) {
+        if constexpr (F < 2 * G) {
+            read<F + kAhead>();
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+            s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[F], st.qb[F - G], F == G ? z : s[1], 0, 0, 0);
+            constexpr int i = F - G - 2;
+            if constexpr (i >= 0 && i < kMaxSeg) {
+#pragma unroll
+                for (int e = i * (16 / kMaxSeg); e < (i + 1) * (16 / kMaxSeg); ++e) mx = fmaxf(mx, s[0][e]);
+            }
+            if constexpr (i >= kMaxSeg) {
+#pragma unroll
+                for (int e = (i - kMaxSeg) * (8 / kExpSeg); e < (i - kMaxSeg + 1) * (8 / kExpSeg); e += 2) exp_pair(0, e, c, st.sub, sum);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            second<F + 1>(st, c, mx, sum);
+        }
+    }
+    template <int I> __device__ __forceinline__ void third(AttnRow<true, D>& st, float c, float& sum) {
+        if constexpr (I < 4 * NB) {
+            constexpr int kk = I / NB, nb = I % NB;
+            read<2 * G + I + kAhead>();
+            st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[2 * G + I], p[kk], st.o[nb], 0, 0, 0);
+            if constexpr (kk < 3) {
+#pragma unroll
+                for (int e = nb * (8 / NB); e < (nb + 1) * (8 / NB); e += 2) exp_pair(kk + 1, e, c, st.sub, sum);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            third<I + 1>(st, c, sum);
+        }
+    }
+    __device__ __forceinline__ void finish(AttnRow<true, D>& st, float c) {
+        float sum = 0.0f, mx = -INFINITY;
+        second<G>(st, c, mx, sum);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
+        mx *= c;
+        if (__builtin_expect(__any(mx > st.ref + kAttnSlack), 0)) {
+            asm volatile("" ::: "memory");   // a real branch
+            attn_move_ref<true, D>(st, mx);
+            sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) exp_pair(0, e, c, st.sub, sum);
+        }
+        __builtin_amdgcn_s_setprio(1);   // a wave in its second product goes first: the SIMD's other one would delay these MFMAs
+        __builtin_amdgcn_sched_barrier(0);
+        third<0>(st, c, sum);
+        __builtin_amdgcn_s_setprio(0);
+        st.l += sum;
+    }
+};
 
 template <bool kBf16, int D, bool kKeys> struct AttnShape {
     typedef AttnTile<kBf16, D> T;
@@ -242,7 +383,7 @@ template <bool kBf16, int D, bool kKeys> struct AttnShape {
 // kKeys = false: a workgroup takes 128 rows, 32 a wave; its four waves load a tile of keys together and each attends to all of it.
 // kKeys = true (few rows): 32 rows, and every wave walks tiles of its own; the waves' results are put together at the end.
 template <bool kBf16, int D, bool kKeys>
-__global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves)) void cache_attn_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves), kBf16 && !kKeys ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a) {
     typedef AttnShape<kBf16, D, kKeys> Sh;
     typedef AttnTile<kBf16, D> T;
     constexpr int kRowB = T::kRowB, kKeyTile = Sh::kKeyTile, NB = D / 32, kEs = kBf16 ? 2 : 4;
@@ -298,13 +439,10 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves)) void cac
     const int wave_lo_max = __builtin_amdgcn_readlane(st.lo, 31), wave_hi_min = __builtin_amdgcn_readlane(st.hi, 0);   // every row sees
 
     // Loads: lane i of a load lands at byte 16 i of its KB, so the swizzle is applied to what it fetches.
-    uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
-#pragma unroll
-    for (int j = 0; j < T::kSegLoads; ++j) {
-        const int row = (64 * j + lane) / T::kChunks, c = lane % T::kChunks;
-        k_off[j] = (uint32_t)(row * kRowB + ((c ^ T::k_swizzle(row)) << 4) - 1024 * j);
-        v_off[j] = (uint32_t)(row * kRowB + ((c ^ T::v_swizzle(row)) << 4) - 1024 * j);
-    }
+    // A segment's loads move on by 1 KB in either memory (the immediate offset), what is left of their swizzles is a constant each.
+    const int load_row = lane / T::kChunks, load_c = lane % T::kChunks;
+    const uint32_t k_off0 = (uint32_t)(load_row * kRowB + ((load_c ^ T::k_swizzle(load_row)) << 4));
+    const uint32_t v_off0 = (uint32_t)(load_row * kRowB + ((load_c ^ T::v_swizzle(load_row)) << 4));
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + (kKeys ? wave * 2 * Sh::kSlot : 0);
     const int64_t head_b = (int64_t)head * kRowB << a.c.log_page;
     const int page_mask = (1 << a.c.log_page) - 1;
@@ -312,7 +450,8 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves)) void cac
 
     // Pages of the wave's next 64 tiles, one tile a lane: looked up together, so that no step waits for the table.
     constexpr int kGroups = kKeyTile / 16;     // 16 keys never lie in two pages
-    int32_t ids[kGroups];
+    constexpr int kIds = kKeys ? kGroups : 1;  // those that this wave loads
+    int32_t ids[kIds];
     uint32_t there = 0;                        // which of the groups exist
     const int t_step = kKeys ? Sh::kWaves : 1, t0 = kKeys ? t_beg + wave : t_beg;
     auto look_up = [&](int t) {
@@ -324,7 +463,8 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves)) void cac
             const int id = mine < t_end && at < sr.len ? table[at >> a.c.log_page] : -1;
             const bool ok = id >= 0 && id < a.c.pages;
             there |= (ok ? 1u : 0u) << g;
-            ids[g] = ok ? id : 0;
+            if (kKeys) ids[kKeys ? g : 0] = ok ? id : 0;
+            else if (g == wave * T::kSegRows / 16) ids[0] = ok ? id : 0;
         }
     };
     // asks for tile t, number `at` of the pages looked up
@@ -333,16 +473,15 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves)) void cac
 #pragma unroll
         for (int sg = 0; sg < Sh::kSegs; ++sg) {
             const int row = (kKeys ? sg : wave) * T::kSegRows;
-            int id;
-            if constexpr (kKeys) id = __builtin_amdgcn_readlane(ids[row / 16], at);
-            else {
-                int mine = ids[0];
-#pragma unroll
-                for (int g = 1; g < kGroups; ++g) mine = row / 16 == g ? ids[g] : mine;
-                id = __builtin_amdgcn_readlane(mine, at);
-            }
+            const int id = __builtin_amdgcn_readlane(ids[kKeys ? row / 16 : 0], at);
             const int64_t from = id * a.c.page_b + head_b + ((tok + row) & page_mask) * kRowB;
             const uint32_t to = lds + slot * Sh::kSlot + row * kRowB;
+            uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
+#pragma unroll
+            for (int j = 0; j < T::kSegLoads; ++j) {
+                k_off[j] = k_off0 ^ T::k_step(j);
+                v_off[j] = v_off0 ^ T::v_step(j);
+            }
             dma16_group_to_lds<T::kSegLoads>(to, a.c.k + from, k_off);
             dma16_group_to_lds<T::kSegLoads>(to + kKeyTile * kRowB, a.c.v + from, v_off);
         }
@@ -386,13 +525,26 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves)) void cac
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (more) load_tile(t + t_step, at, slot ^ 1);
         }
         const bool none = !active || key0 >= wave_hi || (key0 + kKeyTile <= wave_lo && key0 >= a.sinks) || exists == 0;
+        const bool full = key0 + kKeyTile <= wave_hi_min && (key0 >= wave_lo_max || key0 + kKeyTile <= a.sinks) && exists == (1u << kGroups) - 1;
+        const uint32_t base = lds + slot * Sh::kSlot;
+        if constexpr (kBf16 && !kKeys) {
+            if (!none && full) {
+                AttnStep<D> step;
+                step.begin(base + k_at, base + v_at + kKeyTile * kRowB);
+                step.template piece<0>(st);
+                if (more) load_tile(t + t_step, at, slot ^ 1);
+                step.template piece<1>(st);
+                step.template piece<2>(st);
+                step.template piece<3>(st);
+                step.finish(st, a.scale_log2);
+                continue;
+            }
+        }
+        if (!kKeys && more) load_tile(t + t_step, at, slot ^ 1);
         if (!none) {
-            const bool full = key0 + kKeyTile <= wave_hi_min && (key0 >= wave_lo_max || key0 + kKeyTile <= a.sinks) && exists == (1u << kGroups) - 1;
-            const uint32_t base = lds + slot * Sh::kSlot;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < kKeyTile / 32; ++c)
                 attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key0 + 32 * c, exists >> (2 * c), full, hh);
         }
