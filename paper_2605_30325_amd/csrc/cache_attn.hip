@@ -94,14 +94,97 @@ template <bool kBf16, int D> __device__ __forceinline__ void attn_move_ref(AttnR
         for (int i = 0; i < 16; ++i) st.o[nb][i] *= alpha;
 }
 
-// A value that is not finite reaches the rows that see it, and no others, as a count: 1 for +inf, 64 for -inf, 65 for NaN, of at most
-// 32 keys, so a sum of them says which there were.
+// A value that is not finite reaches the rows that see it, and no others, as a count: 1 for +inf, 128 for -inf, 129 for NaN, of at
+// most 32 keys, so a sum of them says which there were.
 __device__ __forceinline__ float attn_code(float x) {
-    return (x < INFINITY ? 0.0f : 1.0f) + (x > -INFINITY ? 0.0f : 64.0f);
+    return (x < INFINITY ? 0.0f : 1.0f) + (x > -INFINITY ? 0.0f : 128.0f);
 }
 __device__ __forceinline__ float attn_decode(float code) {
-    const float down = floorf(code * (1.0f / 64.0f));
-    return (code > 64.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+    const float down = floorf(code * (1.0f / 128.0f));
+    return (code > 128.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+}
+
+// bf16: operand of V for channels 32 nb.. and key step kk (16 keys; the lane half's are 8 (e / 4) + 4 hh + e % 4), by transposing reads.
+template <int D> __device__ __forceinline__ bf16x8 attn_v(uint32_t v, int kk, int nb) {
+    const uint32_t at = (v ^ (uint32_t)(nb << 6)) + kk * 16 * (D * 2);
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 8 * (D * 2)));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Whether all values of 32 keys are finite: their product with zeros is zero exactly then.
+template <int D> __device__ __forceinline__ bool attn_finite(uint32_t v) {
+    bf16x8 zero;
+    f32x16 z;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) zero[e] = (__bf16)0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int nb = 0; nb < D / 32; ++nb) {
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D>(v, kk, nb), zero, z, 0, 0, 0);
+            if (nb & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += z[i];
+    return !__any(t != 0.0f);   // NaN != 0
+}
+
+// O^T += V^T P^T of 32 keys some of whose values are not finite: those reach the rows whose p there is not zero.
+template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& st, uint32_t v, const bf16x8 (&p)[2]) {
+    constexpr int NB = D / 32;
+    f32x16 o[NB];   // indexed as the loop goes, so it lies in memory: this path must not cost the others registers
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
+#pragma unroll 1
+    for (int nb = 0; nb < NB; ++nb) {
+        f32x16 sum = o[nb], code;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) code[i] = 0.0f;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            bf16x8 x = attn_v<D>(v, kk, nb), y, on;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[e] = (__bf16)attn_code((float)x[e]);
+                x[e] = (float)y[e] == 0.0f ? x[e] : (__bf16)0.0f;
+                on[e] = (__bf16)((float)p[kk][e] > 0.0f ? 1.0f : 0.0f);
+            }
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[kk], sum, 0, 0, 0);
+            code = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, on, code, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
+        o[nb] = sum;
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) st.o[nb] = o[nb];
+}
+
+// Scores of 32 keys from key0 on: -inf where the lane's row does not see the key.  Register i is key 8 (i / 4) + 4 hh + i % 4.
+template <bool kBf16, int D>
+__device__ __forceinline__ void attn_mask(const AttnRow<kBf16, D>& st, f32x16& s, int key0, uint32_t exists, int sinks, int hh) {
+    const int from = st.lo - key0 - 4 * hh, to = st.hi - key0 - 4 * hh;
+    if (key0 < sinks) {
+        const int first = min(sinks - key0 - 4 * hh, to);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int x = 8 * (i >> 2) + (i & 3);
+            s[i] = (x >= from && x < to) || x < first ? s[i] : -INFINITY;
+        }
+    } else {
+        const uint32_t span = (uint32_t)max(to - from, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(8 * (i >> 2) + (i & 3) - from) < span ? s[i] : -INFINITY;
+    }
+    if ((exists & 3u) != 3u) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (exists >> (i >> 3)) & 1u ? s[i] : -INFINITY;
+    }
 }
 
 // 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.
@@ -110,15 +193,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
                                            bool full, int hh) {
     constexpr int NB = D / 32, kRowB = AttnTile<kBf16, D>::kRowB;
     f32x16 s = attn_scores<kBf16, D>(st, k);
-    if (!full) {
-        // register i is key 8 (i / 4) + 4 hh + i % 4
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int key = key0 + 8 * (i >> 2) + 4 * hh + (i & 3);
-            const bool seen = key < st.hi && (key >= st.lo || key < a.sinks) && ((exists >> (i >> 3)) & 1u);
-            s[i] = seen ? s[i] : -INFINITY;
-        }
-    }
+    if (!full) attn_mask<kBf16, D>(st, s, key0, exists, a.sinks, hh);
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
@@ -137,73 +212,16 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[kk][e] = (__bf16)s[8 * kk + e];
-        auto operand = [&](int kk, int nb) __attribute__((always_inline)) {
-            const uint32_t at = (v ^ (uint32_t)(nb << 6)) + kk * 16 * kRowB;
-            const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
-            const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 8 * kRowB));
-            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        bool plain = true;
-        if (!full) {
-            // A product with zeros is not zero where a value is infinite or NaN.
-            bf16x8 zero;
-            f32x16 z;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) zero[e] = (__bf16)0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+        if (full || attn_finite<D>(v)) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kk, nb), zero, z, 0, 0, 0);
-                    if (nb & 1) __builtin_amdgcn_sched_barrier(0);
-                }
-            float t = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) t += z[i];
-            plain = !__any(t != 0.0f);   // NaN != 0
-        }
-        if (plain) {
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(kk, nb), p[kk], st.o[nb], 0, 0, 0);
+                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D>(v, kk, nb), p[kk], st.o[nb], 0, 0, 0);
                     if (nb & 1) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
                 }
         } else {
-            bf16x8 on[2];
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) on[kk][e] = (__bf16)((float)p[kk][e] > 0.0f ? 1.0f : 0.0f);
-            f32x16 o[NB];   // indexed as the loop goes, so it lies in memory: this path must not cost the others registers
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
-#pragma unroll 1
-            for (int nb = 0; nb < NB; ++nb) {
-                f32x16 sum = o[nb], code;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) code[i] = 0.0f;
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 x = operand(kk, nb), y;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        y[e] = (__bf16)attn_code((float)x[e]);
-                        x[e] = (float)y[e] == 0.0f ? x[e] : (__bf16)0.0f;
-                    }
-                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[kk], sum, 0, 0, 0);
-                    code = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, on[kk], code, 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
-                o[nb] = sum;
-            }
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) st.o[nb] = o[nb];
+            attn_careful<D>(st, v, p);
         }
     } else {
         // step i takes keys 8 (i / 4) + i % 4 of either lane half: register i is the operand
@@ -272,10 +290,7 @@ template <int D> struct AttnStep {
             fr[F] = *(lds_bf16x8_p)(uintptr_t)((k ^ (uint32_t)((F % G) << 5)) + (uint32_t)((F / G) * 32 * kRowB));
         } else if constexpr (F < NF) {
             constexpr int kk = (F - 2 * G) / NB, nb = (F - 2 * G) % NB;
-            const uint32_t at = (v ^ (uint32_t)(nb << 6)) + kk * 16 * kRowB;
-            const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
-            const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 8 * kRowB));
-            fr[F] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            fr[F] = attn_v<D>(v, kk, nb);
         }
     }
     template <int F, int E> __device__ __forceinline__ void read_to() {
@@ -526,11 +541,14 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves), kBf16 &&
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         }
-        const bool none = !active || key0 >= wave_hi || (key0 + kKeyTile <= wave_lo && key0 >= a.sinks) || exists == 0;
-        const bool full = key0 + kKeyTile <= wave_hi_min && (key0 >= wave_lo_max || key0 + kKeyTile <= a.sinks) && exists == (1u << kGroups) - 1;
+        // of 32 or 64 keys from `key` on: does some row see some, does every row see all of them
+        auto some = [&](int key, int n, uint32_t ex) { return active && key < wave_hi && (key + n > wave_lo || key < a.sinks) && ex != 0; };
+        auto all = [&](int key, int n, uint32_t ex) {
+            return key + n <= wave_hi_min && (key >= wave_lo_max || key + n <= a.sinks) && ex == (1u << n / 16) - 1;
+        };
         const uint32_t base = lds + slot * Sh::kSlot;
         if constexpr (kBf16 && !kKeys) {
-            if (!none && full) {
+            if (active && all(key0, 64, exists)) {
                 AttnStep<D> step;
                 step.begin(base + k_at, base + v_at + kKeyTile * kRowB);
                 step.template piece<0>(st);
@@ -543,10 +561,12 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves), kBf16 &&
             }
         }
         if (!kKeys && more) load_tile(t + t_step, at, slot ^ 1);
-        if (!none) {
 #pragma unroll 1
-            for (int c = 0; c < kKeyTile / 32; ++c)
-                attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key0 + 32 * c, exists >> (2 * c), full, hh);
+        for (int c = 0; c < kKeyTile / 32; ++c) {
+            const int key = key0 + 32 * c;
+            const uint32_t ex = (exists >> (2 * c)) & 3u;
+            if (some(key, 32, ex))
+                attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, all(key, 32, ex), hh);
         }
     }
 
