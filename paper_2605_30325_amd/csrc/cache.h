@@ -22,6 +22,52 @@ veda_status check_rows(const veda_cache* c, int32_t rows, int32_t heads, const v
 
 #if defined(__HIPCC__)
 
+// Sum over the lanes up to and with this one, by DPP; all 64 lanes take part.
+__device__ __forceinline__ int lanes_up_to(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+// Work items: every sequence's rows in blocks (of `size`, where a token counts as `group` rows), sequence by sequence.  Only the
+// device knows the sequences' lengths; a grid of the longest's blocks for each of them is mostly empty where they are ragged, and an empty
+// workgroup costs its launch: prompts of 4096 rows and less, 8192 workgroups of which 4176 empty, 530 us, with the items numbered as here
+// ...  Returns false for numbers beyond the last item.
+struct RowBlock { int seq, block, blocks; };   // block of blocks of its sequence
+__device__ __forceinline__ bool find_block(const CacheArgs& c, int group, int size, int item, RowBlock& out) {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int s0 = 0; s0 < c.seqs; s0 += 64) {
+        const int s = s0 + lane;
+        int n = 0;
+        if (s < c.seqs) {
+            const int first = min(max(c.q_start[s], 0), c.rows);
+            n = min(max(min(c.q_start[s + 1], c.rows) - first, 0), c.max_new);
+        }
+        const int blocks = (int)(((int64_t)n * group + size - 1) / size);
+        const int up_to = lanes_up_to(blocks);
+        const int total = __builtin_amdgcn_readlane(up_to, 63);
+        if (item < base + total) {
+            const int at = __popcll(__ballot(base + up_to <= item));
+            out.seq = s0 + at;
+            out.blocks = __builtin_amdgcn_readlane(blocks, at);
+            out.block = item - (base + __builtin_amdgcn_readlane(up_to, at) - out.blocks);
+            return true;
+        }
+        base += total;
+    }
+    return false;
+}
+// Items that a grid has to have, as far as the host knows.
+inline int64_t block_items(int64_t seqs, int64_t rows, int64_t max_new, int64_t group, int64_t size) {
+    const int64_t each = seqs * ((max_new * group + size - 1) / size), all = rows * group / size + seqs;
+    return each < all ? each : all;
+}
+
 // Rows and length of a sequence, whatever the arrays hold.
 struct SeqRows {
     int first;    // row of its first new token

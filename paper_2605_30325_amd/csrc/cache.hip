@@ -54,7 +54,7 @@ struct AppendArgs {
     char* q_out;
     int64_t sq_h, sq_n, so_h, so_n, sk_h, sk_n, sv_h, sv_n;   // bytes
     const int32_t* positions;   // null: the position in the sequence
-    int32_t q_heads, head_dim, units, log_tb, hb, blocks;      // blocks: of rows, for each sequence
+    int32_t q_heads, head_dim, units, log_tb, hb;
 };
 
 // A workgroup takes up to 16 new rows of one sequence and some of the heads of Q, K and V (numbered one behind the other): Q goes to
@@ -62,10 +62,11 @@ struct AppendArgs {
 template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) void append_kernel(AppendArgs a) {
     extern __shared__ float2 cs[];
     __shared__ int page_s[16];
-    const int s = blockIdx.x / a.blocks, i0 = (blockIdx.x % a.blocks) << a.log_tb;
+    RowBlock rb;
+    if (!find_block(a.c, 1, 1 << a.log_tb, blockIdx.x, rb)) return;
+    const int s = rb.seq, i0 = rb.block << a.log_tb;
     const SeqRows sr = seq_rows(a.c, s);
     const int n = min(min(sr.n, a.c.max_new) - i0, 1 << a.log_tb);
-    if (n <= 0) return;
     const int row0 = sr.first + i0, p0 = sr.len - sr.n + i0, page_mask = (1 << a.c.log_page) - 1;
     if ((int)threadIdx.x < n) {
         const int p = p0 + (int)threadIdx.x;
@@ -160,8 +161,7 @@ extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_b
     const bool chunks = veda::rope_in_chunks(a.rope, chunk);
     a.units = veda::rope_units(a.rope, c->head_dim, chunk, chunks);
     veda::rope_blocks(a.c.max_new, b->seqs, heads, &a.log_tb, &a.hb);
-    a.blocks = (a.c.max_new + (1 << a.log_tb) - 1) >> a.log_tb;
-    const int64_t gx = (int64_t)a.blocks * b->seqs;
+    const int64_t gx = veda::block_items(b->seqs, b->rows, a.c.max_new, 1, (int64_t)1 << a.log_tb);
     const int64_t gy = (heads + a.hb - 1) / a.hb;
     if (gx >= (int64_t)1 << 31 || gy > 65535) return VEDA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)gx, (unsigned)gy);

@@ -16,7 +16,7 @@ struct CacheAttnArgs {
     float* lse;
     int64_t sq_h, sq_n, so_h, so_n;   // bytes
     int32_t q_heads, group;           // group: query heads of a key head
-    int32_t row_blocks, splits;       // workgroups along the rows and along the keys
+    int32_t splits;                   // workgroups along the keys
     int32_t block, window, sinks;
     float scale_log2;                 // softmax_scale * log2(e)
     float* part;                      // splits > 1: [split][row][query head][D] sums, then [split][row][query head][2] reference and l
@@ -406,12 +406,14 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves), kBf16 &&
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l31 = lane & 31, hh = lane >> 5;
 
-    const int pairs = a.c.seqs * a.c.kv_heads;
-    const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, split = rest % a.splits, rb = a.row_blocks - 1 - rest / a.splits;
-    const int seq = pair / a.c.kv_heads, head = pair % a.c.kv_heads;
+    // Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of a head meet in few L2 caches.
+    const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, split = rest % a.splits;
+    RowBlock rb;
+    if (!find_block(a.c, a.group, Sh::kRows, rest / a.splits, rb)) return;
+    const int seq = rb.seq;
     const SeqRows sr = seq_rows(a.c, seq);
-    const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = rb * Sh::kRows;
-    if (r0 >= rows) return;
+    const int n = min(sr.n, a.c.max_new), rows = n * a.group;
+    const int r0 = (rb.blocks - 1 - rb.block) * Sh::kRows;   // the last rows of a causal sequence see the most
     const int r_end = min(rows, r0 + Sh::kRows);
 
     // tiles that some row of the workgroup sees: [0, first) and [rest0, rest1), split along the list
@@ -675,12 +677,15 @@ __global__ __launch_bounds__(64 * (AttnShape<kBf16, D, kKeys>::kWaves), kBf16 &&
 // Puts the splits of a row together; a wave for each (row, query head).
 template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnArgs a) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int per_seq = (a.c.max_new * a.q_heads + 3) / 4;
-    const int seq = blockIdx.x / per_seq, item = blockIdx.x % per_seq * 4 + wave;
-    const SeqRows sr = seq_rows(a.c, seq);
-    const int i = item / a.q_heads, qh = item % a.q_heads;
-    if (i >= min(sr.n, a.c.max_new)) return;
-    const int64_t token = sr.first + i, part_rows = (int64_t)a.c.rows * a.q_heads, row = token * a.q_heads + qh;
+    const int64_t row = (int64_t)blockIdx.x * 4 + wave, part_rows = (int64_t)a.c.rows * a.q_heads;
+    if (row >= part_rows) return;
+    const int token = (int)(row / a.q_heads), qh = (int)(row % a.q_heads);
+    bool mine = false;   // is the row one of a sequence
+    for (int s = lane; s < a.c.seqs; s += 64) {
+        const int first = max(a.c.q_start[s], 0), last = a.c.q_start[s + 1];
+        mine = mine || (token >= first && token < last && token - first < a.c.max_new);
+    }
+    if (!__any(mine)) return;
     const float* pm = a.part + a.splits * part_rows * D;
     float ref = -INFINITY;
     for (int s = lane; s < a.splits; s += 64) ref = fmaxf(ref, pm[((int64_t)s * part_rows + row) * 2]);
@@ -713,19 +718,20 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_j
 // rows alone do not fill the card's 256 compute units.
 struct AttnCut {
     bool keys;
-    int32_t row_blocks, splits;
+    int64_t items;      // blocks of rows, at most, of one key head
+    int32_t splits;
 };
 static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t q_heads, veda_visible vis) {
     AttnCut cut;
     const int64_t max_new = b->max_new < b->rows ? b->max_new : b->rows, rows = max_new * (q_heads / c->kv_heads);
     cut.keys = rows <= 32;
-    cut.row_blocks = (int32_t)((rows + (cut.keys ? 31 : 127)) / (cut.keys ? 32 : 128));
+    cut.items = block_items(b->seqs, b->rows, max_new, q_heads / c->kv_heads, cut.keys ? 32 : 128);
     int64_t keys = (int64_t)b->max_pages * c->page_tokens;
     if (vis.window) {   // what a workgroup's rows can see at most, sinks apart
         const int64_t span = (int64_t)vis.window + vis.sinks + (vis.block ? vis.block : 0) + 128;
         keys = keys < span ? keys : span;
     }
-    const int64_t items = (int64_t)b->seqs * c->kv_heads * cut.row_blocks, most = (keys + 511) / 512;
+    const int64_t items = cut.items * c->kv_heads, most = (keys + 511) / 512;
     int64_t splits = items > 0 ? 512 / items : 1;
     if (splits > most) splits = most;
     if (splits > 256) splits = 256;
@@ -751,7 +757,7 @@ template <bool kBf16, int D, bool kKeys> static veda_status launch_cache_attn(co
 template <bool kBf16, int D> static veda_status launch_cache_attn_d(const CacheAttnArgs& a, bool keys, unsigned grid, hipStream_t s) {
     const veda_status st = keys ? launch_cache_attn<kBf16, D, true>(a, grid, s) : launch_cache_attn<kBf16, D, false>(a, grid, s);
     if (st != VEDA_OK || a.splits == 1) return st;
-    const int64_t joins = (int64_t)a.c.seqs * (((int64_t)a.c.max_new * a.q_heads + 3) / 4);
+    const int64_t joins = ((int64_t)a.c.rows * a.q_heads + 3) / 4;
     hipLaunchKernelGGL((cache_attn_join_kernel<kBf16, D>), dim3((unsigned)joins), dim3(256), 0, s, a);
     return launch_status("veda_cache_attn_fwd");
 }
@@ -790,13 +796,12 @@ extern "C" veda_status veda_cache_attn_fwd(const veda_cache* c, const veda_cache
     a.q = (const char*)q; a.out = (char*)out; a.lse = lse;
     a.sq_h = sq.h * es; a.sq_n = sq.n * es; a.so_h = so.h * es; a.so_n = so.n * es;
     a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
-    a.row_blocks = cut.row_blocks; a.splits = cut.splits;
+    a.splits = cut.splits;
     a.block = vis.block; a.window = vis.window; a.sinks = vis.window ? vis.sinks : 0;
     a.scale_log2 = softmax_scale * veda::kLog2e;
     a.part = (float*)workspace;
-    const int64_t grid = (int64_t)b->seqs * c->kv_heads * cut.row_blocks * cut.splits;
-    if (grid >= (int64_t)1 << 31 || (int64_t)a.c.max_new * q_heads >= (int64_t)1 << 30 ||
-        (int64_t)b->seqs * (((int64_t)a.c.max_new * q_heads + 3) / 4) >= (int64_t)1 << 31)
+    const int64_t grid = cut.items * c->kv_heads * cut.splits;
+    if (grid >= (int64_t)1 << 31 || (int64_t)a.c.max_new * a.group >= (int64_t)1 << 30 || (int64_t)b->rows * q_heads >= (int64_t)1 << 32)
         return VEDA_ERR_UNSUPPORTED;
     const hipStream_t s = (hipStream_t)stream;
     if (c->dtype == VEDA_BF16)
