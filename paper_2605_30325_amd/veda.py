@@ -225,7 +225,7 @@ def _check(status: int, where: str):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # current_stream() makes an object first: 2 us of a call's 12
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -701,37 +701,44 @@ class Rope:
             pass
 
 
+def _refuse(where: str, what: str):
+    raise VedaError(VEDA_ERR_INVALID_ARG, where, what)
+
+
 def _need(ok: bool, where: str, what: str):
     if not ok:
-        raise VedaError(VEDA_ERR_INVALID_ARG, where, what)
+        _refuse(where, what)
 
 
 def _on(dev: torch.device, where: str):
     """The kernels run on the current device, so that is where the tensors have to be."""
-    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device(), where, f"tensors on {dev}, which is not the current device")
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        _refuse(where, f"tensors on {dev}, which is not the current device")
 
 
 def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Optional[torch.Tensor] = None, transpose: bool = False):
     """Rotates x [batch, heads, N, d] by positions i32 [batch or 1, N, axes] (or [N], one axis) into y (x itself: in place).
     transpose=True turns the gradient of the result into the gradient of x."""
-    w = "veda_rope_apply"
-    _need(x.dim() == 4 and x.shape[3] == rope.head_dim and (x.stride(3) == 1 or x.numel() == 0), w,
-          "x must be [batch, heads, N, head_dim] with unit channel stride")
-    _on(x.device, w)
+    w, dev = "veda_rope_apply", x.device
+    if x.dim() != 4 or x.shape[3] != rope.head_dim or (x.stride(3) != 1 and x.numel()):
+        _refuse(w, "x must be [batch, heads, N, head_dim] with unit channel stride")
+    _on(dev, w)
+    b, h, n, _ = x.shape
     if rope.axes == 1 and positions.dim() == 1:
         positions = positions.reshape(1, -1, 1)
-    _need(positions.dim() == 3 and positions.shape[0] in (1, x.shape[0]) and tuple(positions.shape[1:]) == (x.shape[2], rope.axes) and
-          positions.dtype == torch.int32 and positions.is_contiguous() and positions.device == x.device, w,
-          f"positions must be contiguous i32 [{x.shape[0]} or 1, {x.shape[2]}, {rope.axes}] on {x.device}")
+    if (positions.dim() != 3 or positions.shape[0] not in (1, b) or positions.shape[1] != n or positions.shape[2] != rope.axes or
+            positions.dtype != torch.int32 or positions.device != dev or not positions.is_contiguous()):
+        _refuse(w, f"positions must be contiguous i32 [{b} or 1, {n}, {rope.axes}] on {dev}")
     if y is None:
         y = torch.empty_like(x)
         if y.stride(3) != 1:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _need(y.shape == x.shape and y.dtype == x.dtype and y.device == x.device and (y.stride(3) == 1 or y.numel() == 0), w,
-          "y must be as x, with unit channel stride")
-    pos_b = 0 if positions.shape[0] == 1 else positions.stride(0)
-    _check(load().veda_rope_apply(rope.handle, _dtype_code(x.dtype), x.shape[0], x.shape[1], x.shape[2], _ptr(x), veda_strides(*x.stride()[:3]),
-                                  _ptr(positions), pos_b, int(transpose), _ptr(y), veda_strides(*y.stride()[:3]), _stream()), w)
+            y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    elif y.shape != x.shape or y.dtype != x.dtype or y.device != dev or (y.stride(3) != 1 and y.numel()):
+        _refuse(w, "y must be as x, with unit channel stride")
+    sx, sy = x.stride(), y.stride()
+    _check(load().veda_rope_apply(rope.handle, _dtype_code(x.dtype), b, h, n, x.data_ptr(), veda_strides(sx[0], sx[1], sx[2]),
+                                  positions.data_ptr(), 0 if positions.shape[0] == 1 else n * rope.axes, int(transpose), y.data_ptr(),
+                                  veda_strides(sy[0], sy[1], sy[2]), _stream()), w)
     return y
 
 
@@ -751,7 +758,9 @@ class Cache:
         self.k, self.v = k, v
         self.pages, self.page_tokens, self.kv_heads, self.head_dim, self.dtype = int(pages), int(page_tokens), int(kv_heads), int(head_dim), dtype
         stride = k.stride(0) if pages > 1 else 0
+        self.device = k.device
         self._struct = veda_cache(self.pages, self.page_tokens, self.kv_heads, self.head_dim, _dtype_code(dtype), stride, _ptr(k), _ptr(v))
+        self._ref = C.byref(self._struct)
 
 
 class CacheBatch:
@@ -769,13 +778,17 @@ class CacheBatch:
 
     def struct(self, rows: int) -> veda_cache_batch:
         t = self.page_table
-        return veda_cache_batch(self.seqs, rows, self.max_new, t.shape[1], max(t.stride(0), t.shape[1]), _ptr(t), _ptr(self.kv_len), _ptr(self.q_start))
+        width, stride = t.shape[1], t.stride(0)
+        return veda_cache_batch(self.seqs, rows, self.max_new, width, stride if stride > width else width, t.data_ptr(), self.kv_len.data_ptr(),
+                                self.q_start.data_ptr())
 
 
 def _rows(cache: Cache, t: torch.Tensor, rows: int, where: str, name: str) -> veda_strides:
-    _need(t.dim() == 3 and t.shape[0] == rows and t.shape[2] == cache.head_dim and t.dtype == cache.dtype and t.device == cache.k.device and
-          (t.stride(2) == 1 or t.numel() == 0), where, f"{name} must be {cache.dtype} [{rows}, heads, {cache.head_dim}] beside the cache")
-    return veda_strides(0, t.stride(1), t.stride(0))
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 3 or shape[0] != rows or shape[2] != cache.head_dim or t.dtype != cache.dtype or t.device != cache.device or
+            (stride[2] != 1 and t.numel())):
+        _refuse(where, f"{name} must be {cache.dtype} [{rows}, heads, {cache.head_dim}] beside the cache")
+    return veda_strides(0, stride[1], stride[0])
 
 
 def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
@@ -783,23 +796,26 @@ def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch
     """Writes the new rows' k (rotated) and v [rows, kv_heads, d] into the cache; with q [rows, q_heads, d], returns q rotated (q_out).
     positions i32 [rows, axes]; without them the position in the sequence (ropes of one axis)."""
     w, rows = "veda_cache_append", k.shape[0]
-    _on(cache.k.device, w)
+    _on(cache.device, w)
     sk, sv = _rows(cache, k, rows, w, "k"), _rows(cache, v, rows, w, "v")
-    _need(k.shape[1] == cache.kv_heads and v.shape[1] == cache.kv_heads, w, "k and v must have the cache's heads")
-    _need(batch.page_table.device == cache.k.device, w, "the batch must be where the cache is")
-    sq = so = veda_strides(0, 0, 0)
+    if k.shape[1] != cache.kv_heads or v.shape[1] != cache.kv_heads:
+        _refuse(w, "k and v must have the cache's heads")
+    if batch.page_table.device != cache.device:
+        _refuse(w, "the batch must be where the cache is")
     if q is not None:
         if q_out is None:
-            q_out = torch.empty((rows, q.shape[1], cache.head_dim), dtype=cache.dtype, device=q.device)
+            q_out = torch.empty((rows, q.shape[1], cache.head_dim), dtype=cache.dtype, device=cache.device)
         sq, so = _rows(cache, q, rows, w, "q"), _rows(cache, q_out, rows, w, "q_out")
-        _need(q.shape[1] == q_out.shape[1], w, "q and q_out must have the same heads")
+        if q.shape[1] != q_out.shape[1]:
+            _refuse(w, "q and q_out must have the same heads")
     else:
+        sq = so = veda_strides(0, 0, 0)
         _need(q_out is None, w, "q_out without q")
-    if positions is not None:
-        _need(rope is not None and tuple(positions.shape) == (rows, rope.axes) and positions.dtype == torch.int32 and positions.is_contiguous() and
-              positions.device == k.device, w, "positions must be contiguous i32 [rows, axes of rope]")
+    if positions is not None and (rope is None or tuple(positions.shape) != (rows, rope.axes) or positions.dtype != torch.int32 or
+                                  positions.device != cache.device or not positions.is_contiguous()):
+        _refuse(w, "positions must be contiguous i32 [rows, axes of rope]")
     bs = batch.struct(rows)
-    _check(load().veda_cache_append(C.byref(cache._struct), C.byref(bs), _ptr(k), sk, _ptr(v), sv, 0 if q is None else q.shape[1], _ptr(q), sq,
+    _check(load().veda_cache_append(cache._ref, C.byref(bs), k.data_ptr(), sk, v.data_ptr(), sv, 0 if q is None else q.shape[1], _ptr(q), sq,
                                     _ptr(q_out), so, None if rope is None else rope.handle, _ptr(positions), _stream()), w)
     return q_out
 
@@ -807,7 +823,7 @@ def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch
 def veda_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, q_heads: int, rows: int) -> int:
     """Bytes of scratch for veda_cache_attn_fwd on buffers of `rows` rows."""
     bs = batch.struct(rows)
-    return int(load().veda_cache_attn_workspace_bytes(C.byref(cache._struct), C.byref(bs), q_heads))
+    return int(load().veda_cache_attn_workspace_bytes(cache._ref, C.byref(bs), q_heads))
 
 
 def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
@@ -816,34 +832,36 @@ def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softma
     """Attention of the new rows q [rows, q_heads, d] over the cache.  block, window, sinks: which keys a row sees (veda_visible: block 1
     causal, 0 everything).  Returns (out [rows, q_heads, d], lse fp32 [q_heads, rows] or None); rows of no sequence are left as they are
     in buffers given, and undefined in buffers made here."""
-    w, rows = "veda_cache_attn_fwd", q.shape[0]
-    _on(cache.k.device, w)
+    w, rows, heads = "veda_cache_attn_fwd", q.shape[0], q.shape[1]
+    _on(cache.device, w)
     sq = _rows(cache, q, rows, w, "q")
-    _need(batch.page_table.device == cache.k.device, w, "the batch must be where the cache is")
+    if batch.page_table.device != cache.device:
+        _refuse(w, "the batch must be where the cache is")
     if out is None:
-        out = torch.empty((rows, q.shape[1], cache.head_dim), dtype=cache.dtype, device=q.device)
+        out = torch.empty((rows, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
     so = _rows(cache, out, rows, w, "out")
-    _need(out.shape[1] == q.shape[1], w, "out must have q's heads")
+    if out.shape[1] != heads:
+        _refuse(w, "out must have q's heads")
     if want_lse and lse is None:
-        lse = torch.empty((q.shape[1], rows), dtype=torch.float32, device=q.device)
-    if lse is not None:
-        _need(tuple(lse.shape) == (q.shape[1], rows) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == q.device, w,
-              "lse must be contiguous fp32 [q_heads, rows]")
+        lse = torch.empty((heads, rows), dtype=torch.float32, device=cache.device)
+    if lse is not None and (tuple(lse.shape) != (heads, rows) or lse.dtype != torch.float32 or lse.device != cache.device or not lse.is_contiguous()):
+        _refuse(w, "lse must be contiguous fp32 [q_heads, rows]")
     bs = batch.struct(rows)
+    lib, ref = load(), C.byref(bs)
     if workspace is None:
-        need = int(load().veda_cache_attn_workspace_bytes(C.byref(cache._struct), C.byref(bs), q.shape[1]))
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        need = int(lib.veda_cache_attn_workspace_bytes(cache._ref, ref, heads))
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().veda_cache_attn_fwd(C.byref(cache._struct), C.byref(bs), q.shape[1], _ptr(q), sq, C.c_float(softmax_scale),
-                                      veda_visible(block, window, sinks), _ptr(out), so, _ptr(lse), _ptr(workspace) or None, nbytes, _stream()), w)
+    _check(lib.veda_cache_attn_fwd(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, veda_visible(block, window, sinks), out.data_ptr(), so,
+                                   _ptr(lse), _ptr(workspace) or None, nbytes, _stream()), w)
     return out, lse
 
 
 def veda_cache_copy_pages(cache: Cache, pairs):
     """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
-    _on(cache.k.device, "veda_cache_copy_pages")
+    _on(cache.device, "veda_cache_copy_pages")
     p = np.ascontiguousarray(pairs, np.int32).reshape(-1, 2)
-    _check(load().veda_cache_copy_pages(C.byref(cache._struct), p.ctypes.data_as(C.c_void_p), p.shape[0], _stream()), "veda_cache_copy_pages")
+    _check(load().veda_cache_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream()), "veda_cache_copy_pages")
 
 
 class Pages:
