@@ -1,0 +1,87 @@
+// Declarations shared by the kernels of the attention over the paged cache.  Not part of the public ABI.
+#pragma once
+
+#include "attn_common.h"
+#include "cache.h"
+
+namespace veda {
+
+struct CacheAttnArgs {
+    CacheArgs c;
+    const char* q;
+    char* out;
+    float* lse;
+    int64_t sq_h, sq_n, so_h, so_n;   // bytes
+    int32_t q_heads, group;           // group: query heads of a key head
+    int32_t splits;                   // workgroups along the keys of a block of rows
+    int32_t per_seq;                  // blocks of rows of every sequence, or 0: numbered by find_block
+    int32_t workers;                  // few rows: workgroups that share all keys evenly, or 0: one for each block of rows
+    int32_t block, window, sinks;
+    float scale_log2;                 // softmax_scale * log2(e)
+    float* part;                      // unfinished sums, and their references and l (see the kernels)
+};
+
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef const __attribute__((address_space(3))) float* lds_f32_ptr;
+typedef __attribute__((ext_vector_type(4))) float f32x4v;
+typedef const __attribute__((address_space(3))) f32x4v* lds_f32x4_ptr;
+typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_p;
+typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4_p;
+
+constexpr float kAttnSlack = 8.0f;    // log2 units a row maximum may outgrow the reference of its exponentials
+
+// Keys that row r (clamped to the rows there are) of a sequence sees: [lo, hi) and [0, min(sinks, hi)).
+struct Seen { int lo, hi; };
+__device__ __forceinline__ Seen seen_by(const CacheAttnArgs& a, const SeqRows& sr, int n, int r) {
+    const int p = sr.len - sr.n + min(r / a.group, n - 1);
+    if (p < 0) return {0, 0};
+    const int e = a.block ? (p / a.block + 1) * a.block : sr.len;
+    return {a.window ? max(0, e - a.window) : 0, min(e, sr.len)};
+}
+
+// A value that is not finite reaches the rows that see it, and no others, as a count: 1 for +inf, 128 for -inf, 129 for NaN, of at
+// most 32 keys, so a sum of them says which there were.
+__device__ __forceinline__ float attn_code(float x) {
+    return (x < INFINITY ? 0.0f : 1.0f) + (x > -INFINITY ? 0.0f : 128.0f);
+}
+__device__ __forceinline__ float attn_decode(float code) {
+    const float down = floorf(code * (1.0f / 128.0f));
+    return (code > 128.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+}
+
+// Sums of the softmax over no key are 0: such a row gives zeros and -inf.
+__device__ __forceinline__ float attn_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float attn_lse(float ref, float l) { return (ref + __log2f(l)) * kLn2; }
+
+// Tiles of `size` keys that some row of a block sees: [0, first) (tokens that stay visible) and [rest, end), as one list.
+struct AttnTiles {
+    int first, rest, count;
+    __device__ __forceinline__ int at(int t) const { return t < first ? t : rest + t - first; }
+};
+__device__ __forceinline__ AttnTiles tiles_seen(const CacheAttnArgs& a, const SeqRows& sr, int n, int r_first, int r_last, int size) {
+    const int lo = seen_by(a, sr, n, r_first).lo, hi = seen_by(a, sr, n, r_last).hi;   // both grow from row to row
+    AttnTiles t;
+    t.first = a.window ? (min(a.sinks, hi) + size - 1) / size : 0;
+    t.rest = max(t.first, lo / size);
+    t.count = t.first + max(0, (hi + size - 1) / size - t.rest);
+    return t;
+}
+
+// Item -> block of rows: by division where the grid has as many for every sequence, else by what the sequences hold.
+__device__ __forceinline__ bool attn_block_of(const CacheAttnArgs& a, int size, int item, RowBlock& out) {
+    if (!a.per_seq) return find_block(a.c, a.group, size, item, out);
+    out.seq = item / a.per_seq;
+    out.block = item % a.per_seq;
+    const SeqRows sr = seq_rows(a.c, out.seq);
+    out.blocks = (min(sr.n, a.c.max_new) * a.group + size - 1) / size;
+    return out.block < out.blocks;
+}
+
+// Launches (cache_attn_rows.hip, cache_attn_keys.hip).  Rows of a workgroup, and of unfinished sums in the workspace:
+constexpr int kAttnRows = 128;
+veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, int64_t items, hipStream_t s);
+// 16 or 32 rows, workgroups that fit the card's 256 compute units at once
+int attn_keys_workers(bool bf16, int d);
+veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, int rows, int64_t items, hipStream_t s);
+
+}  // namespace veda

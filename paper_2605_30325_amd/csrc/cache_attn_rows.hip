@@ -1,0 +1,567 @@
+// Attention over the paged cache, blocks of many rows.
+//
+// The query heads that share a key head are put together: row r of a (sequence, key head) is query head r % G of token r / G,
+// so a key that is loaded once serves G heads.  Scores are formed transposed (S^T = K Q^T, O^T = V^T P^T): a lane owns one row,
+// its accumulators run over keys, the running maximum and sum of the softmax stay in registers, and P^T is the second product's operand
+// as it stands.  A workgroup takes 128 rows, 32 a wave; its four waves load a tile of keys together (straight into LDS, one tile ahead)
+// and each attends to all of it.
+#include "cache_attn.h"
+
+namespace veda {
+
+template <bool kBf16, int D> struct AttnTile {
+    static constexpr int kRowB = D * (kBf16 ? 2 : 4), kChunks = kRowB / 16;
+    static constexpr int kSegRows = kBf16 ? 16 : 8;               // rows of a group of loads: never across a page's end
+    static constexpr int kSegLoads = kSegRows * kRowB / 1024;     // 1 KB each
+    static constexpr int kQ = kBf16 ? D / 16 : D / 2;             // Q operands of a lane
+    // 16-byte chunk c of row r lies at chunk c ^ swizzle: operand reads of a wave then fall into different banks.
+    __device__ static int k_swizzle(int r) { return kBf16 ? (D == 128 ? r & 15 : (r >> 1) & 7) : r & 7; }
+    __device__ static int v_swizzle(int r) { return kBf16 ? (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) : ((r >> 2) & 1) << 3; }
+    // What the swizzles of load j of a segment (1024 / kRowB rows each) have on top of load 0's, as address bits.
+    __device__ static constexpr uint32_t k_step(int j) { return (uint32_t)j << (kBf16 || D == 64 ? 6 : 5); }
+    __device__ static constexpr uint32_t v_step(int j) { return kBf16 ? 0u : (uint32_t)(D == 64 ? j : j >> 1) << 7; }
+};
+
+template <bool kBf16, int D> struct AttnRow {
+    f32x16 o[D / 32];
+    bf16x8 qb[kBf16 ? D / 16 : 1];
+    float qf[kBf16 ? 1 : D / 2];
+    float ref, sub, l;   // reference of the exponentials (log2 units), 0 or -ref, this half's sum
+    int lo, hi;          // visible keys
+};
+
+// Scores of 32 keys whose K rows lie at LDS address `k` (+ the lane's part).
+template <bool kBf16, int D> __device__ __forceinline__ f32x16 attn_scores(const AttnRow<kBf16, D>& st, uint32_t k) {
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+    if constexpr (kBf16) {
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8_p)(uintptr_t)(k ^ (uint32_t)(t << 5)), st.qb[t], s, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int u = 0; u < D / 8; ++u) {
+            const f32x4v x = *(lds_f32x4_ptr)(uintptr_t)(k ^ (uint32_t)(u << 5));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], st.qf[4 * u + e], s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// Moves every row's reference up to its maximum mx (of this lane's half, log2 units) and rescales what was summed.
+template <bool kBf16, int D> __device__ __forceinline__ void attn_move_ref(AttnRow<kBf16, D>& st, float mx) {
+    const float ref = fmaxf(st.ref, max_with_other_half(mx));
+    const float alpha = ref == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.ref - ref);
+    st.ref = ref;
+    st.sub = ref == -INFINITY ? 0.0f : -ref;
+    st.l *= alpha;
+#pragma unroll
+    for (int nb = 0; nb < D / 32; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[nb][i] *= alpha;
+}
+
+// bf16: operand of V for channels 32 nb.. and key step kk (16 keys; the lane half's are 8 (e / 4) + 4 hh + e % 4), by transposing reads.
+template <int D> __device__ __forceinline__ bf16x8 attn_v(uint32_t v, int kk, int nb) {
+    const uint32_t at = (v ^ (uint32_t)(nb << 6)) + kk * 16 * (D * 2);
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 8 * (D * 2)));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Whether all values of 32 keys are finite: their product with zeros is zero exactly then.
+template <int D> __device__ __forceinline__ bool attn_finite(uint32_t v) {
+    bf16x8 zero;
+    f32x16 z;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) zero[e] = (__bf16)0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int nb = 0; nb < D / 32; ++nb) {
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D>(v, kk, nb), zero, z, 0, 0, 0);
+            if (nb & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += z[i];
+    return !__any(t != 0.0f);   // NaN != 0
+}
+
+// O^T += V^T P^T of 32 keys some of whose values are not finite: those reach the rows whose p there is not zero.
+template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& st, uint32_t v, const bf16x8 (&p)[2]) {
+    constexpr int NB = D / 32;
+    f32x16 o[NB];   // indexed as the loop goes, so it lies in memory: this path must not cost the others registers
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
+#pragma unroll 1
+    for (int nb = 0; nb < NB; ++nb) {
+        f32x16 sum = o[nb], code;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) code[i] = 0.0f;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            bf16x8 x = attn_v<D>(v, kk, nb), y, on;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[e] = (__bf16)attn_code((float)x[e]);
+                x[e] = (float)y[e] == 0.0f ? x[e] : (__bf16)0.0f;
+                on[e] = (__bf16)((float)p[kk][e] > 0.0f ? 1.0f : 0.0f);
+            }
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[kk], sum, 0, 0, 0);
+            code = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, on, code, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
+        o[nb] = sum;
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) st.o[nb] = o[nb];
+}
+
+// Scores of 32 keys from key0 on: -inf where the lane's row does not see the key.  Register i is key 8 (i / 4) + 4 hh + i % 4.
+template <bool kBf16, int D>
+__device__ __forceinline__ void attn_mask(const AttnRow<kBf16, D>& st, f32x16& s, int key0, uint32_t exists, int sinks, int hh) {
+    const int from = st.lo - key0 - 4 * hh, to = st.hi - key0 - 4 * hh;
+    if (key0 < sinks) {
+        const int first = min(sinks - key0 - 4 * hh, to);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int x = 8 * (i >> 2) + (i & 3);
+            s[i] = (x >= from && x < to) || x < first ? s[i] : -INFINITY;
+        }
+    } else {
+        const uint32_t span = (uint32_t)max(to - from, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(8 * (i >> 2) + (i & 3) - from) < span ? s[i] : -INFINITY;
+    }
+    if ((exists & 3u) != 3u) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (exists >> (i >> 3)) & 1u ? s[i] : -INFINITY;
+    }
+}
+
+// 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.
+template <bool kBf16, int D>
+__device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16, D>& st, uint32_t k, uint32_t v, int key0, uint32_t exists,
+                                           bool full, int hh) {
+    constexpr int NB = D / 32, kRowB = AttnTile<kBf16, D>::kRowB;
+    f32x16 s = attn_scores<kBf16, D>(st, k);
+    if (!full) attn_mask<kBf16, D>(st, s, key0, exists, a.sinks, hh);
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx *= a.scale_log2;
+    if (__any(mx > st.ref + kAttnSlack)) attn_move_ref<kBf16, D>(st, mx);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, st.sub));
+        sum += s[i];
+    }
+    st.l += sum;
+    if constexpr (kBf16) {
+        bf16x8 p[2];   // operand of keys 16 kk ...: the lane half's are 16 kk + 8 (e / 4) + 4 hh + e % 4
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[kk][e] = (__bf16)s[8 * kk + e];
+        if (full || attn_finite<D>(v)) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D>(v, kk, nb), p[kk], st.o[nb], 0, 0, 0);
+                    if (nb & 1) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
+                }
+        } else {
+            attn_careful<D>(st, v, p);
+        }
+    } else {
+        // step i takes keys 8 (i / 4) + i % 4 of either lane half: register i is the operand
+        auto operand = [&](int i, int nb) __attribute__((always_inline)) {
+            return *(lds_f32_ptr)(uintptr_t)((v ^ (uint32_t)(nb << 7)) + (8 * (i >> 2) + (i & 3)) * kRowB);
+        };
+        bool plain = true;
+        if (!full) {
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) z = __builtin_amdgcn_mfma_f32_32x32x2f32(operand(i, nb), 0.0f, z, 0, 0, 0);
+            float t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) t += z[i];
+            plain = !__any(t != 0.0f);
+        }
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(operand(i, nb), s[i], st.o[nb], 0, 0, 0);
+        } else {
+            f32x16 o[NB];   // in memory, as above
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
+#pragma unroll 1
+            for (int nb = 0; nb < NB; ++nb) {
+                f32x16 sum = o[nb], code;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) code[i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = operand(i, nb), y = attn_code(x);
+                    sum = __builtin_amdgcn_mfma_f32_32x32x2f32(y == 0.0f ? x : 0.0f, s[i], sum, 0, 0, 0);
+                    code = __builtin_amdgcn_mfma_f32_32x32x2f32(y, s[i] > 0.0f ? 1.0f : 0.0f, code, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
+                o[nb] = sum;
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) st.o[nb] = o[nb];
+        }
+    }
+}
+
+// A tile of 64 keys that every row of a wave sees, bf16, with the order of issue pinned: an MFMA holds the matrix pipe for 32 cycles, in
+// whose shadow vector instructions issue (4 cycles each, 8 an exponential), so each segment below is one MFMA and what belongs
+// under it.  Operand reads are issued kAhead MFMAs before their use.  The first scores' maximum and exponentials ride on the second
+// block's products; the exponentials assume that the reference stays, and are formed again in the rare other case.  The other
+// exponentials ride on the second product, 16 keys behind it.  (The same division of a step as the tile-sparse kernel's, attn_step.h; here
+// V lies token by token, so its operand takes two transposing reads.)
+template <int D> struct AttnStep {
+    static constexpr int G = D / 16, NB = D / 32, kAhead = 6, kRowB = D * 2, NF = 2 * G + 4 * NB;
+    static constexpr int kPieces = 4, kSeg = G / kPieces;   // block 0 comes in pieces, between which the caller asks for the next tile
+    bf16x8 fr[NF], p[4];
+    f32x16 s[2];
+    uint32_t k, v;
+
+    template <int F> __device__ __forceinline__ void read() {
+        if constexpr (F < 2 * G) {
+            fr[F] = *(lds_bf16x8_p)(uintptr_t)((k ^ (uint32_t)((F % G) << 5)) + (uint32_t)((F / G) * 32 * kRowB));
+        } else if constexpr (F < NF) {
+            constexpr int kk = (F - 2 * G) / NB, nb = (F - 2 * G) % NB;
+            fr[F] = attn_v<D>(v, kk, nb);
+        }
+    }
+    template <int F, int E> __device__ __forceinline__ void read_to() {
+        if constexpr (F < E) { read<F>(); read_to<F + 1, E>(); }
+    }
+    __device__ __forceinline__ void begin(uint32_t k_at, uint32_t v_at) {
+        k = k_at;
+        v = v_at;
+        read_to<0, kAhead>();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <int F, int E> __device__ __forceinline__ void first(const AttnRow<true, D>& st) {
+        if constexpr (F < E) {
+            read<F + kAhead>();
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[F], st.qb[F], F == 0 ? z : s[0], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            first<F + 1, E>(st);
+        }
+    }
+    template <int P> __device__ __forceinline__ void piece(const AttnRow<true, D>& st) { first<P * kSeg, (P + 1) * kSeg>(st); }
+
+    // exponentials of registers e, e + 1 of key step kk
+    __device__ __forceinline__ void exp_pair(int kk, int e, float c, float sub, float& sum) {
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kk >> 1][8 * (kk & 1) + e], c, sub));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kk >> 1][8 * (kk & 1) + e + 1], c, sub));
+        const bf16x2 pr = {(__bf16)p0, (__bf16)p1};
+        sum += p0;
+        sum += p1;
+        p[kk][e] = pr[0];
+        p[kk][e + 1] = pr[1];
+    }
+    static constexpr int kMaxSeg = G >= 8 ? 2 : 1, kExpSeg = G - 2 - kMaxSeg;   // block 0's last product needs two more to retire
+    static_assert(kExpSeg >= 1 && 8 % kExpSeg == 0 && (8 / kExpSeg) % 2 == 0, "exponentials come in pairs");
+    template <int F> __device__ __forceinline__ void second(const AttnRow<true, D>& st, float c, float& mx, float& sum) {
+        if constexpr (F < 2 * G) {
+            read<F + kAhead>();
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+            s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[F], st.qb[F - G], F == G ? z : s[1], 0, 0, 0);
+            constexpr int i = F - G - 2;
+            if constexpr (i >= 0 && i < kMaxSeg) {
+#pragma unroll
+                for (int e = i * (16 / kMaxSeg); e < (i + 1) * (16 / kMaxSeg); ++e) mx = fmaxf(mx, s[0][e]);
+            }
+            if constexpr (i >= kMaxSeg) {
+#pragma unroll
+                for (int e = (i - kMaxSeg) * (8 / kExpSeg); e < (i - kMaxSeg + 1) * (8 / kExpSeg); e += 2) exp_pair(0, e, c, st.sub, sum);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            second<F + 1>(st, c, mx, sum);
+        }
+    }
+    template <int I> __device__ __forceinline__ void third(AttnRow<true, D>& st, float c, float& sum) {
+        if constexpr (I < 4 * NB) {
+            constexpr int kk = I / NB, nb = I % NB;
+            read<2 * G + I + kAhead>();
+            st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[2 * G + I], p[kk], st.o[nb], 0, 0, 0);
+            if constexpr (kk < 3) {
+#pragma unroll
+                for (int e = nb * (8 / NB); e < (nb + 1) * (8 / NB); e += 2) exp_pair(kk + 1, e, c, st.sub, sum);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            third<I + 1>(st, c, sum);
+        }
+    }
+    __device__ __forceinline__ void finish(AttnRow<true, D>& st, float c) {
+        float sum = 0.0f, mx = -INFINITY;
+        second<G>(st, c, mx, sum);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
+        mx *= c;
+        if (__builtin_expect(__any(mx > st.ref + kAttnSlack), 0)) {
+            asm volatile("" ::: "memory");   // a real branch
+            attn_move_ref<true, D>(st, mx);
+            sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) exp_pair(0, e, c, st.sub, sum);
+        }
+        __builtin_amdgcn_s_setprio(1);   // a wave in its second product goes first: the SIMD's other one would delay these MFMAs
+        __builtin_amdgcn_sched_barrier(0);
+        third<0>(st, c, sum);
+        __builtin_amdgcn_s_setprio(0);
+        st.l += sum;
+    }
+};
+
+template <bool kBf16, int D> struct AttnShape {
+    typedef AttnTile<kBf16, D> T;
+    static constexpr int kKeyTile = kBf16 ? 64 : 32;          // keys of a tile: one segment of loads a wave
+    static constexpr int kSlot = 2 * kKeyTile * T::kRowB;     // K tile, V tile
+    static constexpr int kOutRowB = T::kRowB + 16;            // a row of the results in LDS
+    static constexpr int kOutB = kAttnRows * (kOutRowB + 4);
+    static constexpr int kLds = 2 * kSlot > kOutB ? 2 * kSlot : kOutB;
+};
+
+template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) void cache_attn_rows_kernel(CacheAttnArgs a) {
+    typedef AttnShape<kBf16, D> Sh;
+    typedef AttnTile<kBf16, D> T;
+    constexpr int kRowB = T::kRowB, kKeyTile = Sh::kKeyTile, NB = D / 32;
+    extern __shared__ __align__(1024) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l31 = lane & 31, hh = lane >> 5;
+
+    // Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of a head meet in few L2 caches.
+    const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, split = rest % a.splits;
+    RowBlock rb;
+    if (!attn_block_of(a, kAttnRows, rest / a.splits, rb)) return;
+    const int seq = rb.seq;
+    const SeqRows sr = seq_rows(a.c, seq);
+    const int n = min(sr.n, a.c.max_new), rows = n * a.group;
+    const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
+    const int r_end = min(rows, r0 + kAttnRows);
+    const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, kKeyTile);
+    const int t_beg = (int)((int64_t)tiles.count * split / a.splits), t_end = (int)((int64_t)tiles.count * (split + 1) / a.splits);
+
+    // the wave's rows
+    const int w0 = r0 + 32 * wave;
+    const bool active = w0 < rows;
+    const int r = min(w0 + l31, rows - 1);
+    AttnRow<kBf16, D> st;
+    {
+        const Seen v = seen_by(a, sr, n, r);
+        st.lo = v.lo;
+        st.hi = v.hi;
+        const char* q = a.q + (int64_t)(sr.first + r / a.group) * a.sq_n + (int64_t)(head * a.group + r % a.group) * a.sq_h;
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) st.qb[t] = *reinterpret_cast<const bf16x8*>(q + 32 * t + 16 * hh);
+        } else {
+#pragma unroll
+            for (int u = 0; u < D / 8; ++u) {
+                const f32x4v x = *reinterpret_cast<const f32x4v*>(q + 32 * u + 16 * hh);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.qf[4 * u + e] = x[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[nb][i] = 0.0f;
+    st.ref = -INFINITY;
+    st.sub = st.l = 0.0f;
+    const int wave_lo = __builtin_amdgcn_readlane(st.lo, 0), wave_hi = __builtin_amdgcn_readlane(st.hi, 31);       // some row sees
+    const int wave_lo_max = __builtin_amdgcn_readlane(st.lo, 31), wave_hi_min = __builtin_amdgcn_readlane(st.hi, 0);   // every row sees
+
+    // Loads: lane i of a load lands at byte 16 i of its KB, so the swizzle is applied to what it fetches.
+    // A segment's loads move on by 1 KB in either memory (the immediate offset), what is left of their swizzles is a constant each.
+    const int load_row = lane / T::kChunks, load_c = lane % T::kChunks;
+    const uint32_t k_off0 = (uint32_t)(load_row * kRowB + ((load_c ^ T::k_swizzle(load_row)) << 4));
+    const uint32_t v_off0 = (uint32_t)(load_row * kRowB + ((load_c ^ T::v_swizzle(load_row)) << 4));
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    const int64_t head_b = (int64_t)head * kRowB << a.c.log_page;
+    const int page_mask = (1 << a.c.log_page) - 1;
+    const int32_t* table = a.c.table + seq * a.c.table_stride;
+
+    // Pages of the next 64 tiles, one tile a lane: looked up together, so that no step waits for the table.
+    constexpr int kGroups = kKeyTile / 16;     // 16 keys never lie in two pages
+    int32_t page = 0;                          // of the wave's segment
+    uint32_t there = 0;                        // which of the groups exist
+    auto look_up = [&](int t) {
+        const int mine = t + lane, tok = tiles.at(mine) * kKeyTile;
+        there = 0;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int at = tok + 16 * g;
+            const int id = mine < t_end && at < sr.len ? table[at >> a.c.log_page] : -1;
+            const bool ok = id >= 0 && id < a.c.pages;
+            there |= (ok ? 1u : 0u) << g;
+            if (g == wave * T::kSegRows / 16) page = ok ? id : 0;
+        }
+    };
+    // asks for the wave's segment of tile t, number `at` of the pages looked up
+    auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
+        const int row = wave * T::kSegRows, id = __builtin_amdgcn_readlane(page, at);
+        const int64_t from = id * a.c.page_b + head_b + ((tiles.at(t) * kKeyTile + row) & page_mask) * kRowB;
+        const uint32_t to = lds + slot * Sh::kSlot + row * kRowB;
+        uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
+#pragma unroll
+        for (int j = 0; j < T::kSegLoads; ++j) {
+            k_off[j] = k_off0 ^ T::k_step(j);
+            v_off[j] = v_off0 ^ T::v_step(j);
+        }
+        dma16_group_to_lds<T::kSegLoads>(to, a.c.k + from, k_off);
+        dma16_group_to_lds<T::kSegLoads>(to + kKeyTile * kRowB, a.c.v + from, v_off);
+    };
+
+    // the lane's part of operand addresses
+    const uint32_t k_at = (uint32_t)(l31 * kRowB + ((hh ^ T::k_swizzle(l31)) << 4));
+    uint32_t v_at;
+    if constexpr (kBf16) {
+        // transposing read: lane i of 16 names channels 4 (i % 4) ..+3 of key i / 4 and gets channel i of the four keys
+        const int key = 4 * hh + ((lane >> 2) & 3), c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        v_at = (uint32_t)(key * kRowB + ((c ^ T::v_swizzle(key)) << 4) + 8 * (lane & 1));
+    } else {
+        v_at = (uint32_t)(4 * hh * kRowB + 4 * l31 + (hh << 7));
+    }
+
+    int slot = 0, at = 0;
+    if (t_beg < t_end) {
+        look_up(t_beg);
+        load_tile(t_beg, 0, 0);
+    }
+    for (int t = t_beg; t < t_end; ++t, slot ^= 1) {
+        const uint32_t exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
+        const int key0 = tiles.at(t) * kKeyTile;
+        const bool more = t + 1 < t_end;
+        if (++at == 64 && more) {
+            look_up(t + 1);
+            at = 0;
+        }
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the other slot has been read
+        wait_vmcnt<0>();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // of 32 or 64 keys from `key` on: does some row see some, does every row see all of them
+        auto some = [&](int key, int n, uint32_t ex) { return active && key < wave_hi && (key + n > wave_lo || key < a.sinks) && ex != 0; };
+        auto all = [&](int key, int n, uint32_t ex) {
+            return key + n <= wave_hi_min && (key >= wave_lo_max || key + n <= a.sinks) && ex == (1u << n / 16) - 1;
+        };
+        const uint32_t base = lds + slot * Sh::kSlot;
+        if constexpr (kBf16) {
+            if (active && all(key0, 64, exists)) {
+                AttnStep<D> step;
+                step.begin(base + k_at, base + v_at + kKeyTile * kRowB);
+                step.template piece<0>(st);
+                if (more) load_tile(t + 1, at, slot ^ 1);
+                step.template piece<1>(st);
+                step.template piece<2>(st);
+                step.template piece<3>(st);
+                step.finish(st, a.scale_log2);
+                continue;
+            }
+        }
+        if (more) load_tile(t + 1, at, slot ^ 1);
+#pragma unroll 1
+        for (int c = 0; c < kKeyTile / 32; ++c) {
+            const int key = key0 + 32 * c;
+            const uint32_t ex = (exists >> (2 * c)) & 3u;
+            if (some(key, 32, ex))
+                attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, all(key, 32, ex), hh);
+        }
+    }
+
+    // Results.  A lane holds channels 32 nb + 8 j + 4 hh + 0..3 of its row.
+    const float l = sum_with_other_half(st.l);
+    __syncthreads();
+    float* ml = reinterpret_cast<float*>(smem + kAttnRows * Sh::kOutRowB);   // [128]
+    char* orow = smem + (wave * 32 + l31) * Sh::kOutRowB;
+    const int64_t part_rows = (int64_t)a.c.rows * a.q_heads;
+    if (a.splits > 1) {   // unfinished: [split][row][query head][D] sums, then [split][row][query head] reference and l
+        if (w0 + l31 < rows) {
+            const int64_t row = (int64_t)(sr.first + r / a.group) * a.q_heads + head * a.group + r % a.group;
+            float* po = a.part + ((int64_t)split * part_rows + row) * D;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<f32x4v*>(po + 32 * nb + 8 * j + 4 * hh) = f32x4v{st.o[nb][4 * j], st.o[nb][4 * j + 1], st.o[nb][4 * j + 2], st.o[nb][4 * j + 3]};
+            if (hh == 0) {
+                float* pm = a.part + a.splits * part_rows * D + ((int64_t)split * part_rows + row) * 2;
+                pm[0] = st.ref;
+                pm[1] = l;
+            }
+        }
+        return;
+    }
+    const float inv = attn_inverse(l);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int ch = 32 * nb + 8 * j + 4 * hh;
+            if constexpr (kBf16) {
+                bf16x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (__bf16)(st.o[nb][4 * j + e] * inv);
+                *reinterpret_cast<bf16x4*>(orow + ch * 2) = x;
+            } else {
+                *reinterpret_cast<f32x4v*>(orow + ch * 4) = f32x4v{st.o[nb][4 * j] * inv, st.o[nb][4 * j + 1] * inv, st.o[nb][4 * j + 2] * inv, st.o[nb][4 * j + 3] * inv};
+            }
+        }
+    if (hh == 0) ml[wave * 32 + l31] = attn_lse(st.ref, l);
+    __syncthreads();
+    for (int i = tid; i < (r_end - r0) * T::kChunks; i += 256) {
+        const int rr = i / T::kChunks, c = i % T::kChunks, at_row = r0 + rr;
+        char* o = a.out + (int64_t)(sr.first + at_row / a.group) * a.so_n + (int64_t)(head * a.group + at_row % a.group) * a.so_h;
+        *reinterpret_cast<uint4*>(o + 16 * c) = *reinterpret_cast<const uint4*>(smem + rr * Sh::kOutRowB + 16 * c);
+    }
+    if (a.lse && tid < r_end - r0) {
+        const int at_row = r0 + tid;
+        a.lse[(int64_t)(head * a.group + at_row % a.group) * a.c.rows + sr.first + at_row / a.group] = ml[tid];
+    }
+}
+
+template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs& a, int64_t items, hipStream_t s) {
+    typedef AttnShape<kBf16, D> Sh;
+    auto kern = cache_attn_rows_kernel<kBf16, D>;
+    if (Sh::kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds));
+    hipLaunchKernelGGL(kern, dim3((unsigned)(items * a.c.kv_heads * a.splits)), dim3(256), Sh::kLds, s, a);
+    return launch_status("veda_cache_attn_fwd");
+}
+
+veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, int64_t items, hipStream_t s) {
+    if (bf16) return d == 128 ? launch_rows<true, 128>(a, items, s) : launch_rows<true, 64>(a, items, s);
+    return d == 128 ? launch_rows<false, 128>(a, items, s) : launch_rows<false, 64>(a, items, s);
+}
+
+}  // namespace veda
