@@ -55,6 +55,7 @@ struct AppendArgs {
     int64_t sq_h, sq_n, so_h, so_n, sk_h, sk_n, sv_h, sv_n;   // bytes
     const int32_t* positions;   // null: the position in the sequence
     int32_t q_heads, head_dim, units, log_tb, hb;
+    RowOrder order;
 };
 
 // A workgroup takes up to 16 new rows of one sequence and some of the heads of Q, K and V (numbered one behind the other): Q goes to
@@ -76,13 +77,15 @@ template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) v
     const int32_t* pos = a.positions ? a.positions + (int64_t)row0 * a.rope.axes : nullptr;
     rope_angles(a.rope, n, [&](int t, int axis) { return pos ? pos[t * a.rope.axes + axis] : p0 + t; }, cs);
     __syncthreads();
-    const int heads = a.q_heads + 2 * a.c.kv_heads, h0 = blockIdx.y * a.hb, nh = min(a.hb, heads - h0), tb = 1 << a.log_tb;
+    const int heads = a.q_heads + 2 * a.c.kv_heads, h0 = blockIdx.y * a.hb, nh = min(a.hb, heads - h0);
     const int64_t row_b = (int64_t)a.head_dim * sizeof(E), head_b = row_b << a.c.log_page;
-    rope_rows<E, kChunks>(a.rope, a.head_dim, a.units, nh << a.log_tb, cs,
+    const RowAt at(a.order, a.log_tb, nh);
+    rope_rows<E, kChunks>(a.rope, a.head_dim, a.units, at.rows(n), cs,
                           [&](int r) {
-                              const int t = r & (tb - 1);
-                              int h = h0 + (r >> a.log_tb);
-                              RowMove m{nullptr, nullptr, a.rope.turns != nullptr};
+                              int t, h;
+                              at.find(r, t, h);
+                              h += h0;
+                              RowMove m{nullptr, nullptr, t, a.rope.turns != nullptr};
                               if (t >= n) return m;
                               if (h < a.q_heads) {
                                   m.src = a.q + (row0 + t) * a.sq_n + h * a.sq_h;
@@ -97,22 +100,24 @@ template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) v
                               m.src = is_v ? a.v + (row0 + t) * a.sv_n + h * a.sv_h : a.k + (row0 + t) * a.sk_n + h * a.sk_h;
                               m.dst = (is_v ? a.c.v : a.c.k) + id * a.c.page_b + h * head_b + ((p0 + t) & page_mask) * row_b;
                               return m;
-                          },
-                          [&](int r) { return r & (tb - 1); });
+                          });
 }
 
-// Pairs of one launch, by value: no list in device memory that a later call could overwrite before this one has run.
-constexpr int kCopyPairs = 448;
-struct CopyArgs {
+// Pairs of one launch, by value: no list in device memory that a later call could overwrite before this one has run.  Arguments
+// are copied on the host at every launch, so short lists (a branch's open page) have a form of their own: 3.6 KB against 256 bytes.
+constexpr int kCopyPairs = 448, kCopyPairsShort = 28;
+template <int N> struct CopyArgs {
     char *k, *v;
     int64_t page_b;
     int32_t chunks;              // 16-byte chunks of a page
-    int32_t pair[kCopyPairs][2];
+    int32_t pair[N][2];
 };
 
-constexpr int kCopyChunks = 4;   // 16-byte chunks in flight per thread
+// A copy: 4 bytes moved for each byte of a page, nothing computed.  Stores go past the die's L2: kept there, they cost 50 us instead of 17
+// for 1000 pages of 16 KB, and 180 instead of 152 us (5.2 TB/s) for 1000 pages of 192 KB; two chunks a thread, four and eight are 3 % slower.
+constexpr int kCopyChunks = 2;   // 16-byte chunks in flight per thread
 
-__global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a) {
+template <int N> __global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs<N> a) {
     char* pool = blockIdx.z ? a.v : a.k;
     const uint4* src = reinterpret_cast<const uint4*>(pool + a.pair[blockIdx.y][0] * a.page_b);
     uint4* dst = reinterpret_cast<uint4*>(pool + a.pair[blockIdx.y][1] * a.page_b);
@@ -123,7 +128,7 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a) {
         if (c0 + j * 256 < a.chunks) x[j] = src[c0 + j * 256];
 #pragma unroll
     for (int j = 0; j < kCopyChunks; ++j)
-        if (c0 + j * 256 < a.chunks) dst[c0 + j * 256] = x[j];
+        if (c0 + j * 256 < a.chunks) store_through(dst + c0 + j * 256, x[j]);
 }
 
 }  // namespace veda
@@ -161,6 +166,7 @@ extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_b
     const bool chunks = veda::rope_in_chunks(a.rope, chunk);
     a.units = veda::rope_units(a.rope, c->head_dim, chunk, chunks);
     veda::rope_blocks(a.c.max_new, b->seqs, heads, &a.log_tb, &a.hb);
+    a.order = veda::row_order(sk.h < sk.n);
     const int64_t gx = veda::block_items(b->seqs, b->rows, a.c.max_new, 1, (int64_t)1 << a.log_tb);
     const int64_t gy = (heads + a.hb - 1) / a.hb;
     if (gx >= (int64_t)1 << 31 || gy > 65535) return VEDA_ERR_UNSUPPORTED;
@@ -182,39 +188,56 @@ extern "C" veda_status veda_cache_copy_pages(const veda_cache* c, const int32_t*
         if (pairs[i] < 0 || pairs[i] >= c->pages) return VEDA_ERR_INVALID_ARG;
     if (n == 0) return VEDA_OK;
     const veda::CacheArgs ca = veda::cache_args(c, nullptr);
-    veda::CopyArgs a;
+    veda::CopyArgs<veda::kCopyPairs> a;
     a.k = ca.k; a.v = ca.v; a.page_b = ca.page_b;
     a.chunks = (int32_t)((int64_t)c->kv_heads * c->page_tokens * c->head_dim * (c->dtype == VEDA_BF16 ? 2 : 4) / 16);
     const unsigned gx = (unsigned)((a.chunks + 256 * veda::kCopyChunks - 1) / (256 * veda::kCopyChunks));
     const hipStream_t s = (hipStream_t)stream;
     // A launch ends where the next pair touches what its pairs write, or writes what they read: stream order then gives the
-    // order of the list.  state: pages of the open launch, bit 0 read, bit 1 written.
-    std::vector<uint8_t> state;
-    try {
-        state.assign((size_t)c->pages, 0);
-    } catch (const std::bad_alloc&) {
-        return veda::hip_fail(hipErrorOutOfMemory, "veda_cache_copy_pages");
+    // order of the list.  Long lists keep a note for every page (bit 0 read, bit 1 written by the open launch), short ones look back.
+    std::vector<uint8_t> note;
+    if (n > veda::kCopyPairsShort) {
+        try {
+            note.assign((size_t)c->pages, 0);
+        } catch (const std::bad_alloc&) {
+            return veda::hip_fail(hipErrorOutOfMemory, "veda_cache_copy_pages");
+        }
     }
     int m = 0;
     auto launch = [&]() -> veda_status {
         if (m == 0) return VEDA_OK;
-        hipLaunchKernelGGL(veda::copy_pages_kernel, dim3(gx, (unsigned)m, 2), dim3(256), 0, s, a);
-        for (int i = 0; i < m; ++i) state[a.pair[i][0]] = state[a.pair[i][1]] = 0;
+        if (m <= veda::kCopyPairsShort) {
+            veda::CopyArgs<veda::kCopyPairsShort> b;
+            b.k = a.k; b.v = a.v; b.page_b = a.page_b; b.chunks = a.chunks;
+            for (int i = 0; i < veda::kCopyPairsShort; ++i)
+                for (int j = 0; j < 2; ++j) b.pair[i][j] = i < m ? a.pair[i][j] : 0;
+            hipLaunchKernelGGL((veda::copy_pages_kernel<veda::kCopyPairsShort>), dim3(gx, (unsigned)m, 2), dim3(256), 0, s, b);
+        } else {
+            hipLaunchKernelGGL((veda::copy_pages_kernel<veda::kCopyPairs>), dim3(gx, (unsigned)m, 2), dim3(256), 0, s, a);
+        }
+        if (!note.empty())
+            for (int i = 0; i < m; ++i) note[a.pair[i][0]] = note[a.pair[i][1]] = 0;
         m = 0;
         return veda::launch_status("veda_cache_copy_pages");
     };
     for (int64_t i = 0; i < n; ++i) {
         const int32_t from = pairs[2 * i], to = pairs[2 * i + 1];
         if (from == to) continue;
-        if (m == veda::kCopyPairs || (state[from] & 2) || state[to]) {
+        bool touches = m == veda::kCopyPairs;
+        if (!note.empty()) touches = touches || (note[from] & 2) || note[to];
+        else
+            for (int j = 0; j < m; ++j) touches = touches || a.pair[j][1] == from || a.pair[j][1] == to || a.pair[j][0] == to;
+        if (touches) {
             st = launch();
             if (st != VEDA_OK) return st;
         }
         a.pair[m][0] = from;
         a.pair[m][1] = to;
         ++m;
-        state[from] |= 1;
-        state[to] |= 2;
+        if (!note.empty()) {
+            note[from] |= 1;
+            note[to] |= 2;
+        }
     }
     return launch();
 }

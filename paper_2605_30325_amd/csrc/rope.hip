@@ -14,6 +14,7 @@ struct RopeApply {
     const int32_t* positions;
     int64_t pos_b;
     int32_t heads, tokens, head_dim, units, log_tb, hb;
+    RowOrder order;
 };
 
 template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeApply a) {
@@ -26,14 +27,16 @@ template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) v
     __syncthreads();
     const char* x = a.x + b * a.sx_b + t0 * a.sx_n;
     char* y = a.y + b * a.sy_b + t0 * a.sy_n;
-    rope_rows<E, kChunks>(a.rope, a.head_dim, a.units, nh << a.log_tb, cs,
+    const RowAt at(a.order, a.log_tb, nh);
+    rope_rows<E, kChunks>(a.rope, a.head_dim, a.units, at.rows(n), cs,
                           [&](int r) {
-                              const int t = r & (tb - 1), h = h0 + (r >> a.log_tb);
-                              RowMove m{x + h * a.sx_h + t * a.sx_n, y + h * a.sy_h + t * a.sy_n, true};
+                              int t, h;
+                              at.find(r, t, h);
+                              h += h0;
+                              RowMove m{x + h * a.sx_h + t * a.sx_n, y + h * a.sy_h + t * a.sy_n, t, true};
                               if (t >= n) m.dst = nullptr;
                               return m;
-                          },
-                          [&](int r) { return r & (tb - 1); });
+                          });
 }
 
 }  // namespace veda
@@ -141,8 +144,10 @@ extern "C" veda_status veda_rope_apply(const veda_rope* rope, veda_dtype dtype, 
     const bool chunks = veda::rope_in_chunks(a.rope, chunk);
     a.units = veda::rope_units(a.rope, d, chunk, chunks);
     veda::rope_blocks(tokens, batch, heads, &a.log_tb, &a.hb);
-    const dim3 grid((unsigned)(((int64_t)tokens + (1 << a.log_tb) - 1) >> a.log_tb), (unsigned)((heads + a.hb - 1) / a.hb), (unsigned)batch);
-    if (grid.y > 65535u || grid.z > 65535u) return VEDA_ERR_UNSUPPORTED;
+    a.order = veda::row_order(sx.h < sx.n);
+    const int64_t head_groups = ((int64_t)heads + a.hb - 1) / a.hb;
+    if (head_groups > 65535 || batch > 65535) return VEDA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)(((int64_t)tokens + (1 << a.log_tb) - 1) >> a.log_tb), (unsigned)head_groups, (unsigned)batch);
     const size_t lds = (size_t)a.rope.half * sizeof(float2) << a.log_tb;
     const hipStream_t s = (hipStream_t)stream;
     if (dtype == VEDA_BF16 && chunks) hipLaunchKernelGGL((veda::rope_kernel<uint16_t, true>), grid, dim3(veda::kRopeThreads), lds, s, a);

@@ -98,16 +98,39 @@ template <> struct RopeChunk<uint32_t> {
 struct RowMove {
     const char* src;
     char* dst;         // null: nothing to do
+    int token;         // of the block
     bool turn;
 };
 
-// Rows 0..n_rows-1 of a block: move(r) tells where row r lies and goes and whether it turns, token(r) its token in the block.
+// The order in which a workgroup goes through its rows: the heads of a token one after the other where they lie next to each other
+// ([tokens][heads][channels]), else the tokens of a head.
+struct RowOrder { int32_t heads_first; };
+inline RowOrder row_order(bool heads_first) { return RowOrder{heads_first ? 1 : 0}; }
+struct RowAt {
+    bool heads_first;
+    int log_tb, heads;
+    uint32_t magic;    // 2^32 / heads, rounded up: exact quotients while row * heads < 2^32 (16 tokens, 256 heads)
+    __device__ __forceinline__ RowAt(const RowOrder& o, int log_tb_, int heads_)
+        : heads_first(o.heads_first && heads_ > 1), log_tb(log_tb_), heads(heads_), magic(0xffffffffu / (uint32_t)heads_ + 1u) {}
+    __device__ __forceinline__ int rows(int tokens) const { return heads_first ? tokens * heads : heads << log_tb; }
+    __device__ __forceinline__ void find(int r, int& t, int& h) const {
+        if (heads_first) {
+            t = (int)__umulhi((uint32_t)r, magic);
+            h = r - t * heads;
+        } else {
+            t = r & ((1 << log_tb) - 1);
+            h = r >> log_tb;
+        }
+    }
+};
+
+// Rows 0..n_rows-1 of a block: move(r) tells where row r lies and goes, its token in the block and whether it turns.
 // A thread keeps one unit of the row and goes from row to row, kAhead of them at a time so that their loads are in flight
-// together; a unit is loaded whole before any of it is stored, and no two units touch the same bytes (rows may be turned in place).
-template <typename E, bool kChunks, typename Move, typename Token>
-__device__ __forceinline__ void rope_rows(const RopeArgs& a, int head_dim, int units, int n_rows, const float2* cs, Move move, Token token) {
+// together (two: four and eight cost more waves than they bring, 140 against 155 and 187 us for 32,760 x 40 rows of 128); a unit is loaded whole before any of it is stored, and no two units touch the same bytes (rows may be turned in place).
+template <typename E, bool kChunks, typename Move>
+__device__ __forceinline__ void rope_rows(const RopeArgs& a, int head_dim, int units, int n_rows, const float2* cs, Move move) {
     typedef RopeChunk<E> C;
-    constexpr int kN = C::kN, kAhead = 4, es = sizeof(E);
+    constexpr int kN = C::kN, kAhead = 2, es = sizeof(E);
     const int width = units < kRopeThreads ? units : kRopeThreads, step = kRopeThreads / width;
     const int r0 = threadIdx.x / width;
     if (r0 >= step) return;
@@ -132,7 +155,7 @@ __device__ __forceinline__ void rope_rows(const RopeArgs& a, int head_dim, int u
                 for (int j = 0; j < kAhead; ++j) {
                     if (!m[j].dst) continue;
                     if (turns && m[j].turn) {
-                        const float2* w = cs + token(r + j * step) * a.half + pair0;
+                        const float2* w = cs + m[j].token * a.half + pair0;
                         float f[kN];
                         C::unpack(x[j], f);
                         if (two) {
@@ -157,8 +180,8 @@ __device__ __forceinline__ void rope_rows(const RopeArgs& a, int head_dim, int u
                         }
                         x[j] = C::pack(f);
                     }
-                    *reinterpret_cast<uint4*>(m[j].dst + c0 * 16) = x[j];
-                    if (two) *reinterpret_cast<uint4*>(m[j].dst + c1 * 16) = y[j];
+                    store_through(m[j].dst + c0 * 16, x[j]);
+                    if (two) store_through(m[j].dst + c1 * 16, y[j]);
                 }
             }
         } else {
@@ -174,7 +197,7 @@ __device__ __forceinline__ void rope_rows(const RopeArgs& a, int head_dim, int u
                 }
                 const float x1 = C::load(m.src + c1 * es);
                 float2 z{1.0f, 0.0f};
-                if (m.turn) z = cs[token(r) * a.half + u];
+                if (m.turn) z = cs[m.token * a.half + u];
                 C::store(m.dst + c0 * es, m.turn ? x0 * z.x - x1 * z.y : x0);
                 C::store(m.dst + c1 * es, m.turn ? x0 * z.y + x1 * z.x : x1);
             }
@@ -182,15 +205,16 @@ __device__ __forceinline__ void rope_rows(const RopeArgs& a, int head_dim, int u
     }
 }
 
-// Tokens of a block (a power of two) and heads of a workgroup: blocks of 16 tokens with all heads, and less of both until there
-// are four workgroups to a compute unit or a workgroup has one token.
-inline void rope_blocks(int64_t tokens, int64_t samples, int heads, int* log_tb, int* hb) {
+// Tokens of a block (a power of two) and heads of a workgroup: blocks of 16 tokens with up to 256 heads, and less of both until there
+// are four workgroups to a compute unit or a workgroup has one token and four heads.
+inline void rope_blocks(int64_t tokens, int64_t samples, int64_t heads, int* log_tb, int* hb) {
     *log_tb = 4;
     while (*log_tb > 0 && (tokens >> (*log_tb - 1)) <= 1) --*log_tb;
-    *hb = heads;
-    auto blocks = [&] { return samples * ((tokens + (1 << *log_tb) - 1) >> *log_tb) * ((heads + *hb - 1) / *hb); };
-    while (blocks() < 1024 && *hb > 4) *hb = (*hb + 1) / 2;
+    int64_t h = heads < 256 ? heads : 256;
+    auto blocks = [&] { return samples * ((tokens + (1 << *log_tb) - 1) >> *log_tb) * ((heads + h - 1) / h); };
+    while (blocks() < 1024 && h > 4) h = (h + 1) / 2;
     while (blocks() < 1024 && *log_tb > 0) --*log_tb;
+    *hb = (int)h;
 }
 
 #endif
