@@ -242,6 +242,7 @@ template <int D> struct AttnStep {
     static constexpr int kPieces = 4, kSeg = G / kPieces;   // block 0 comes in pieces, between which the caller asks for the next tile
     bf16x8 fr[NF], p[4];
     f32x16 s[2];
+    float sum;
     uint32_t k, v;
 
     template <int F> __device__ __forceinline__ void read() {
@@ -320,19 +321,16 @@ template <int D> struct AttnStep {
             third<I + 1>(st, c, sum);
         }
     }
-    __device__ __forceinline__ void finish(AttnRow<true, D>& st, float c) {
-        float sum = 0.0f, mx = -INFINITY;
+    // Scores of block 1.  false: some row's maximum has outgrown its reference, and nothing has been added to st.
+    __device__ __forceinline__ bool scores(const AttnRow<true, D>& st, float c) {
+        float mx = -INFINITY;
+        sum = 0.0f;
         second<G>(st, c, mx, sum);
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
-        mx *= c;
-        if (__builtin_expect(__any(mx > st.ref + kAttnSlack), 0)) {
-            asm volatile("" ::: "memory");   // a real branch
-            attn_move_ref<true, D>(st, mx);
-            sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) exp_pair(0, e, c, st.sub, sum);
-        }
+        return !__any(mx * c > st.ref + kAttnSlack);
+    }
+    __device__ __forceinline__ void values(AttnRow<true, D>& st, float c) {
         __builtin_amdgcn_s_setprio(1);   // a wave in its second product goes first: the SIMD's other one would delay these MFMAs
         __builtin_amdgcn_sched_barrier(0);
         third<0>(st, c, sum);
@@ -458,10 +456,19 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) vo
         look_up(t_beg);
         load_tile(t_beg, 0, 0);
     }
-    for (int t = t_beg; t < t_end; ++t, slot ^= 1) {
-        const uint32_t exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
-        const int key0 = tiles.at(t) * kKeyTile;
-        const bool more = t + 1 < t_end;
+    // of 32 or 64 keys from `key` on: does some row see some, does every row see all of them
+    auto some = [&](int key, int n, uint32_t ex) { return active && key < wave_hi && (key + n > wave_lo || key < a.sinks) && ex != 0; };
+    auto all = [&](int key, int n, uint32_t ex) {
+        return active && key + n <= wave_hi_min && (key >= wave_lo_max || key + n <= a.sinks) && ex == (1u << n / 16) - 1;
+    };
+    int t = t_beg, key0 = 0;
+    uint32_t exists = 0;
+    bool more = false, asked = false, started = false;   // asked: for tile t + 1
+    // Tile t has landed in its slot and everyone has read the other one; look-up of the next.
+    auto arrive = [&]() __attribute__((always_inline)) {
+        exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
+        key0 = tiles.at(t) * kKeyTile;
+        more = t + 1 < t_end;
         if (++at == 64 && more) {
             look_up(t + 1);
             at = 0;
@@ -471,14 +478,17 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) vo
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        // of 32 or 64 keys from `key` on: does some row see some, does every row see all of them
-        auto some = [&](int key, int n, uint32_t ex) { return active && key < wave_hi && (key + n > wave_lo || key < a.sinks) && ex != 0; };
-        auto all = [&](int key, int n, uint32_t ex) {
-            return key + n <= wave_hi_min && (key >= wave_lo_max || key + n <= a.sinks) && ex == (1u << n / 16) - 1;
-        };
-        const uint32_t base = lds + slot * Sh::kSlot;
+    };
+    while (t < t_end) {
+        arrive();
         if constexpr (kBf16) {
-            if (active && all(key0, 64, exists)) {
+            // Tiles that every row sees, in a loop without any other path through the sums: with a branch that rescales them, or the
+            // other kind of tile, in it, the compiler copies them from registers to registers at every step (64 of 224 vector
+            // instructions).  So a tile for which a reference has to move leaves the loop and is done again below, and the first one
+            // is done there at once.
+            bool left = true;
+            while (started && all(key0, 64, exists)) {
+                const uint32_t base = lds + slot * Sh::kSlot;
                 AttnStep<D> step;
                 step.begin(base + k_at, base + v_at + kKeyTile * kRowB);
                 step.template piece<0>(st);
@@ -486,11 +496,21 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) vo
                 step.template piece<1>(st);
                 step.template piece<2>(st);
                 step.template piece<3>(st);
-                step.finish(st, a.scale_log2);
-                continue;
+                asked = true;
+                if (!step.scores(st, a.scale_log2)) break;
+                step.values(st, a.scale_log2);
+                asked = false;
+                slot ^= 1;
+                left = ++t < t_end;
+                if (!left) break;
+                arrive();
             }
+            if (!left) break;
         }
-        if (more) load_tile(t + 1, at, slot ^ 1);
+        const uint32_t base = lds + slot * Sh::kSlot;
+        if (more && !asked) load_tile(t + 1, at, slot ^ 1);
+        asked = false;
+        started = true;
 #pragma unroll 1
         for (int c = 0; c < kKeyTile / 32; ++c) {
             const int key = key0 + 32 * c;
@@ -498,6 +518,8 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) vo
             if (some(key, 32, ex))
                 attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, all(key, 32, ex), hh);
         }
+        ++t;
+        slot ^= 1;
     }
 
     // Results.  A lane holds channels 32 nb + 8 j + 4 hh + 0..3 of its row.
