@@ -13,9 +13,10 @@ struct CacheAttnArgs {
     float* lse;
     int64_t sq_h, sq_n, so_h, so_n;   // bytes
     int32_t q_heads, group;           // group: query heads of a key head
-    int32_t splits;                   // workgroups along the keys of a block of rows
+    int64_t items;                    // blocks of rows of one key head, at most
     int32_t per_seq;                  // blocks of rows of every sequence, or 0: numbered by find_block
-    int32_t workers;                  // few rows: workgroups that share all keys evenly, or 0: one for each block of rows
+    int32_t workers;                  // workgroups that share all keys evenly, or 0: one for each block of rows and key head
+    int32_t part_rows;                // rows of a block's unfinished sums in the workspace
     int32_t block, window, sinks;
     float scale_log2;                 // softmax_scale * log2(e)
     float* part;                      // unfinished sums, and their references and l (see the kernels)
@@ -77,11 +78,20 @@ __device__ __forceinline__ bool attn_block_of(const CacheAttnArgs& a, int size, 
     return out.block < out.blocks;
 }
 
-// Launches (cache_attn_rows.hip, cache_attn_keys.hip).  Rows of a workgroup, and of unfinished sums in the workspace:
+// `total` tiles in equal parts: part p is [begin(p), begin(p + 1)).
+struct TileShare {
+    int total, parts;
+    __device__ __forceinline__ TileShare(int total_, int most, int least) : total(total_), parts(max(1, min(most, (total_ + least - 1) / least))) {}
+    __device__ __forceinline__ int begin(int p) const { return (int)((int64_t)p * total / parts); }
+    __device__ __forceinline__ int owner(int tile) const { return (int)((((int64_t)tile + 1) * parts + total - 1) / total) - 1; }
+};
+
+// Launches: blocks of 128 rows (cache_attn_rows.hip), and blocks of 16 or 32 (cache_attn_keys.hip); and the workgroups of either that
+// run at once on the card's 256 compute units.
 constexpr int kAttnRows = 128;
-veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, int64_t items, hipStream_t s);
-// 16 or 32 rows, workgroups that fit the card's 256 compute units at once
+int attn_rows_workers();
+veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);
 int attn_keys_workers(bool bf16, int d);
-veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, int rows, int64_t items, hipStream_t s);
+veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);   // a.part_rows: rows of a block
 
 }  // namespace veda

@@ -238,14 +238,6 @@ __device__ __forceinline__ int keys_tiles_of(const CacheAttnArgs& a, int s) {
     return n == 0 ? 0 : max(1, tiles_seen(a, sr, n, 0, n * a.group - 1, 32).count);
 }
 constexpr int kShareTiles = 8;    // least part of a workgroup: shorter ones are over before their set-up is paid for
-struct KeysShare {
-    int total;        // tiles of all sequences
-    int parts;        // of them: part p is [p * total / parts, (p + 1) * total / parts)
-    __device__ __forceinline__ KeysShare(const CacheAttnArgs& a, int tiles)
-        : total(tiles), parts(max(1, min(a.workers / a.c.kv_heads, (tiles + kShareTiles - 1) / kShareTiles))) {}
-    __device__ __forceinline__ int begin(int p) const { return (int)((int64_t)p * total / parts); }
-    __device__ __forceinline__ int owner(int tile) const { return (int)((((int64_t)tile + 1) * parts + total - 1) / total) - 1; }
-};
 // The first 64 sequences' tiles by lane, and the sum over all.
 struct KeysCount {
     int mine, up_to, total;
@@ -474,7 +466,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
     const KeysLane<kBf16, D> ln(lane);
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const KeysCount count(a);
-    const KeysShare share(a, count.total);
+    const TileShare share(count.total, a.workers / a.c.kv_heads, kShareTiles);
     const int head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads;
     if (mine >= share.parts || share.total == 0) return;
     int now = share.begin(mine);
@@ -616,7 +608,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
         }
         total += __builtin_amdgcn_readlane(up_to, 63);
     }
-    const KeysShare share(a, total);
+    const TileShare share(total, a.workers / a.c.kv_heads, kShareTiles);
     const int w0 = each ? share.owner(first) : 0, n = each ? share.owner(first + each - 1) - w0 + 1 : 1;
     if (n == 1) return;   // one workgroup had it all (with W = 8 the same for all waves)
     const float2* ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * D);
@@ -682,12 +674,12 @@ int attn_keys_workers(bool bf16, int d) {
     return 256 * (fit < 4 ? fit : 4);
 }
 
-template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheAttnArgs& a, int64_t items, hipStream_t s) {
+template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheAttnArgs& a, hipStream_t s) {
     typedef KeysTile<kBf16, D> T;
     static_assert(T::kWaves * 16 * RB * (T::kOutRowB + 8) <= T::kLds, "the sums fit the slots");
     static_assert(T::kLds <= 64 * 1024, "no more dynamic LDS than a launch may have without asking");
     if (!a.workers) {
-        hipLaunchKernelGGL((cache_attn_keys_kernel<kBf16, D, RB>), dim3((unsigned)(items * a.c.kv_heads)), dim3(64 * T::kWaves), T::kLds, s, a);
+        hipLaunchKernelGGL((cache_attn_keys_kernel<kBf16, D, RB>), dim3((unsigned)(a.items * a.c.kv_heads)), dim3(64 * T::kWaves), T::kLds, s, a);
         return launch_status("veda_cache_attn_fwd");
     }
     hipLaunchKernelGGL((cache_attn_share_kernel<kBf16, D, RB>), dim3((unsigned)a.workers), dim3(64), (keys_slots<kBf16, D>()), s, a);
@@ -699,13 +691,13 @@ template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheA
     return launch_status("veda_cache_attn_fwd");
 }
 
-template <bool kBf16, int D> static veda_status launch_keys_d(const CacheAttnArgs& a, int rows, int64_t items, hipStream_t s) {
-    return rows == 16 ? launch_keys<kBf16, D, 1>(a, items, s) : launch_keys<kBf16, D, 2>(a, items, s);
+template <bool kBf16, int D> static veda_status launch_keys_d(const CacheAttnArgs& a, hipStream_t s) {
+    return a.part_rows == 16 ? launch_keys<kBf16, D, 1>(a, s) : launch_keys<kBf16, D, 2>(a, s);
 }
 
-veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, int rows, int64_t items, hipStream_t s) {
-    if (bf16) return d == 128 ? launch_keys_d<true, 128>(a, rows, items, s) : launch_keys_d<true, 64>(a, rows, items, s);
-    return d == 128 ? launch_keys_d<false, 128>(a, rows, items, s) : launch_keys_d<false, 64>(a, rows, items, s);
+veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) {
+    if (bf16) return d == 128 ? launch_keys_d<true, 128>(a, s) : launch_keys_d<true, 64>(a, s);
+    return d == 128 ? launch_keys_d<false, 128>(a, s) : launch_keys_d<false, 64>(a, s);
 }
 
 }  // namespace veda

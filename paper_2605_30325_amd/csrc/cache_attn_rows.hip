@@ -40,11 +40,16 @@ template <bool kBf16, int D> __device__ __forceinline__ f32x16 attn_scores(const
         for (int t = 0; t < D / 16; ++t)
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8_p)(uintptr_t)(k ^ (uint32_t)(t << 5)), st.qb[t], s, 0, 0, 0);
     } else {
+        // reads one group of products ahead, and no further: there are no registers for more
+        f32x4v x = *(lds_f32x4_ptr)(uintptr_t)k;
 #pragma unroll
         for (int u = 0; u < D / 8; ++u) {
-            const f32x4v x = *(lds_f32x4_ptr)(uintptr_t)(k ^ (uint32_t)(u << 5));
+            f32x4v next = x;
+            if (u + 1 < D / 8) next = *(lds_f32x4_ptr)(uintptr_t)(k ^ (uint32_t)((u + 1) << 5));
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], st.qf[4 * u + e], s, 0, 0, 0);
+            x = next;
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     return s;
@@ -195,17 +200,31 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
 #pragma unroll
             for (int i = 0; i < 16; ++i)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) z = __builtin_amdgcn_mfma_f32_32x32x2f32(operand(i, nb), 0.0f, z, 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) {
+                    z = __builtin_amdgcn_mfma_f32_32x32x2f32(operand(i, nb), 0.0f, z, 0, 0, 0);
+                    if (nb == NB - 1 && i % 2) __builtin_amdgcn_sched_barrier(0);
+                }
             float t = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) t += z[i];
             plain = !__any(t != 0.0f);
         }
         if (plain) {
+            float x[NB];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int nb = 0; nb < NB; ++nb) x[nb] = operand(0, nb);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(operand(i, nb), s[i], st.o[nb], 0, 0, 0);
+            for (int i = 0; i < 16; ++i) {
+                float next[NB];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) next[nb] = i + 1 < 16 ? operand(i + 1 < 16 ? i + 1 : i, nb) : x[nb];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[nb], s[i], st.o[nb], 0, 0, 0);
+                    x[nb] = next[nb];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         } else {
             f32x16 o[NB];   // in memory, as above
 #pragma unroll
@@ -283,6 +302,9 @@ template <int D> struct AttnStep {
         const bf16x2 pr = {(__bf16)p0, (__bf16)p1};
         sum += p0;
         sum += p1;
+        // d = 64: here, under an MFMA; left to itself the compiler adds everything behind the last one.  d = 128: left to itself, its
+        // shadows are full already (4680 rows x 12 heads, 34,320 keys, here / behind: 575 / 598 us at d = 64, 960 / 941 at 128).
+        if constexpr (D == 64) asm volatile("" : "+v"(sum));
         p[kk][e] = pr[0];
         p[kk][e + 1] = pr[1];
     }
@@ -348,25 +370,20 @@ template <bool kBf16, int D> struct AttnShape {
     static constexpr int kLds = 2 * kSlot > kOutB ? 2 * kSlot : kOutB;
 };
 
-template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) void cache_attn_rows_kernel(CacheAttnArgs a) {
+// Pieces that unfinished sums can come in, at most (see the sharing kernel).
+__device__ __forceinline__ int64_t rows_pieces(const CacheAttnArgs& a) { return 2 * (int64_t)a.workers + a.items * a.c.kv_heads; }
+
+// Tiles t_beg .. t_end - 1 of those that rows r0 .. r_end - 1 of a sequence see, for one key head.  part: where the unfinished sums go,
+// or -1 if these are all the tiles.
+template <bool kBf16, int D>
+__device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, int seq, const SeqRows& sr, int r0, int r_end, int head,
+                                           const AttnTiles& tiles, int t_beg, int t_end, int64_t part) {
     typedef AttnShape<kBf16, D> Sh;
     typedef AttnTile<kBf16, D> T;
     constexpr int kRowB = T::kRowB, kKeyTile = Sh::kKeyTile, NB = D / 32;
-    extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l31 = lane & 31, hh = lane >> 5;
-
-    // Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of a head meet in few L2 caches.
-    const int head = blockIdx.x % a.c.kv_heads, rest = blockIdx.x / a.c.kv_heads, split = rest % a.splits;
-    RowBlock rb;
-    if (!attn_block_of(a, kAttnRows, rest / a.splits, rb)) return;
-    const int seq = rb.seq;
-    const SeqRows sr = seq_rows(a.c, seq);
     const int n = min(sr.n, a.c.max_new), rows = n * a.group;
-    const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
-    const int r_end = min(rows, r0 + kAttnRows);
-    const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, kKeyTile);
-    const int t_beg = (int)((int64_t)tiles.count * split / a.splits), t_end = (int)((int64_t)tiles.count * (split + 1) / a.splits);
 
     // the wave's rows
     const int w0 = r0 + 32 * wave;
@@ -527,21 +544,16 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) vo
     __syncthreads();
     float* ml = reinterpret_cast<float*>(smem + kAttnRows * Sh::kOutRowB);   // [128]
     char* orow = smem + (wave * 32 + l31) * Sh::kOutRowB;
-    const int64_t part_rows = (int64_t)a.c.rows * a.q_heads;
-    if (a.splits > 1) {   // unfinished: [split][row][query head][D] sums, then [split][row][query head] reference and l
-        if (w0 + l31 < rows) {
-            const int64_t row = (int64_t)(sr.first + r / a.group) * a.q_heads + head * a.group + r % a.group;
-            float* po = a.part + ((int64_t)split * part_rows + row) * D;
+    if (part >= 0) {   // [part][row][D] sums, then [part][row] reference and l
+        if (w0 + l31 < r_end) {
+            const int64_t row = part * a.part_rows + 32 * wave + l31;
+            float* po = a.part + row * D;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     *reinterpret_cast<f32x4v*>(po + 32 * nb + 8 * j + 4 * hh) = f32x4v{st.o[nb][4 * j], st.o[nb][4 * j + 1], st.o[nb][4 * j + 2], st.o[nb][4 * j + 3]};
-            if (hh == 0) {
-                float* pm = a.part + a.splits * part_rows * D + ((int64_t)split * part_rows + row) * 2;
-                pm[0] = st.ref;
-                pm[1] = l;
-            }
+            if (hh == 0) *reinterpret_cast<float2*>(a.part + rows_pieces(a) * a.part_rows * D + row * 2) = float2{st.ref, l};
         }
         return;
     }
@@ -573,17 +585,193 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, kBf16 ? 2 : 1) vo
     }
 }
 
-template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs& a, int64_t items, hipStream_t s) {
+// A workgroup for each (block of rows, key head).  Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of
+// a head meet in few L2 caches.
+template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnArgs a) {
+    extern __shared__ __align__(1024) char smem[];
+    RowBlock rb;
+    if (!attn_block_of(a, kAttnRows, blockIdx.x / a.c.kv_heads, rb)) return;
+    const SeqRows sr = seq_rows(a.c, rb.seq);
+    const int rows = min(sr.n, a.c.max_new) * a.group;
+    const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
+    const int r_end = min(rows, r0 + kAttnRows);
+    const AttnTiles tiles = tiles_seen(a, sr, min(sr.n, a.c.max_new), r0, r_end - 1, AttnShape<kBf16, D>::kKeyTile);
+    rows_piece<kBf16, D>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
+}
+
+// Where there are few blocks, a workgroup for each leaves compute units idle, so their tiles are dealt out to as many workgroups as fit the
+// card at once, all with the same number of tiles, `level`.  Of every block's list the first whole multiples of `level` go to workgroups of
+// their own: piece k of every block walks the same tiles of its head at the same time, out of the dies' L2.  (Pieces that
+// merely lie one behind the other, each beginning where the last one ended, do not: 12 heads of 37 blocks, 444 on 512 places, 1.04 ms instead of
+// 0.90 with a workgroup for each.)  What is left of the lists is laid end to end and shared by the other workgroups.  Every workgroup counts
+// the blocks' tiles itself, 64 at a time.
+template <int kTile> __device__ __forceinline__ int rows_tiles_of(const CacheAttnArgs& a, int item) {
+    if (item >= a.items) return 0;
+    const SeqRows sr = seq_rows(a.c, item / a.per_seq);
+    const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = item % a.per_seq * kAttnRows;
+    return r0 >= rows ? 0 : max(1, tiles_seen(a, sr, n, r0, min(rows, r0 + kAttnRows) - 1, kTile).count);
+}
+constexpr int kRowsShareTiles = 4;   // least level
+// Number of a piece of unfinished sums: whole multiples by workgroup, the others (block and workgroup both only grow from one to the next)
+// by their sum.
+__device__ __forceinline__ int64_t rows_piece_id(const CacheAttnArgs& a, int parts, int item, int q, int head) {
+    return (int64_t)(q < 0 ? item : parts + item + q) * a.c.kv_heads + head;
+}
+template <int D> __device__ __forceinline__ int4* rows_cuts(const CacheAttnArgs& a) {
+    return reinterpret_cast<int4*>(a.part + rows_pieces(a) * a.part_rows * (D + 2));
+}
+
+template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
+    constexpr int kTile = AttnShape<kBf16, D>::kKeyTile;
+    extern __shared__ __align__(1024) char smem[];
+    const int lane = threadIdx.x & 63, head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads, parts = a.workers / a.c.kv_heads;
+    auto sum = [&](int x) { return __builtin_amdgcn_readlane(lanes_up_to(x), 63); };
+    int total = 0, fulls = 0;
+    for (int i0 = 0; i0 < a.items; i0 += 64) total += sum(rows_tiles_of<kTile>(a, i0 + lane));
+    const int level = max(kRowsShareTiles, (total + parts - 1) / parts);
+    for (int i0 = 0; i0 < a.items; i0 += 64) fulls += sum(rows_tiles_of<kTile>(a, i0 + lane) / level);
+    const TileShare rests(total - fulls * level, parts - fulls, 1);
+    const bool full = mine < fulls;
+    const int q = full ? -1 : mine - fulls;
+    if (!full && (rests.total == 0 || q >= rests.parts)) return;
+    // the block: of the whole multiples, number `mine`; of what is left, the one that tile `now` of it falls into
+    int now = full ? 0 : rests.begin(q), end = full ? 1 : rests.begin(q + 1), item = 0, first_full = 0, first_rest = 0;
+    for (int i0 = 0; i0 < a.items; i0 += 64) {
+        const int count = rows_tiles_of<kTile>(a, i0 + lane), f = count / level, r = count - f * level, up_f = lanes_up_to(f), up_r = lanes_up_to(r);
+        const int all_f = __builtin_amdgcn_readlane(up_f, 63), all_r = __builtin_amdgcn_readlane(up_r, 63);
+        if (full ? mine < first_full + all_f : now < first_rest + all_r) {
+            const int at = __popcll(__ballot(full ? first_full + up_f <= mine : first_rest + up_r <= now));
+            item = i0 + at;
+            first_full += __builtin_amdgcn_readlane(up_f, at) - __builtin_amdgcn_readlane(f, at);
+            first_rest += __builtin_amdgcn_readlane(up_r, at) - __builtin_amdgcn_readlane(r, at);
+            break;
+        }
+        first_full += all_f;
+        first_rest += all_r;
+    }
+    for (bool again = false; now < end && item < a.items; ++item) {
+        const int seq = item / a.per_seq;
+        const SeqRows sr = seq_rows(a.c, seq);
+        const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = item % a.per_seq * kAttnRows;
+        if (r0 >= rows) continue;
+        const int r_end = min(rows, r0 + kAttnRows);
+        const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, kTile);
+        const int count = max(1, tiles.count), f = count / level, rest = count - f * level;
+        // tiles of this piece, and whether it is the block's first
+        const int t_beg = full ? (mine - first_full) * level : f * level + now - first_rest, t_end = full ? t_beg + level : min(count, t_beg + end - now);
+        if (t_end > t_beg) {
+            const bool whole = t_beg == 0 && t_end == count;
+            if (t_beg == 0 && threadIdx.x == 0) {   // whole multiples: how many, from which workgroup on; then the others
+                const int q0 = rest ? rests.owner(first_rest) : 0, q1 = rest ? rests.owner(first_rest + rest - 1) : -1;
+                rows_cuts<D>(a)[item * a.c.kv_heads + head] = int4{whole ? 0 : f, first_full, whole ? 0 : q1 - q0 + 1, q0};
+            }
+            if (again) __syncthreads();   // the last piece's results have left the slots
+            rows_piece<kBf16, D>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
+            again = true;
+        }
+        now += t_end - t_beg;
+        first_rest += rest;
+        first_full += f;
+    }
+}
+
+// Puts a cut block's unfinished sums together, four rows a workgroup: its waves take every fourth piece.
+template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_rows_join_kernel(CacheAttnArgs a) {
+    constexpr int V = D / 64;
+    __shared__ float sums[4][4][D + 2];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.x % a.c.kv_heads, item = blockIdx.x / a.c.kv_heads;
+    const SeqRows sr = seq_rows(a.c, item / a.per_seq);
+    const int block_rows = min(min(sr.n, a.c.max_new) * a.group - item % a.per_seq * kAttnRows, kAttnRows), r0 = 4 * blockIdx.y, rows = min(4, block_rows - r0);
+    if (rows <= 0) return;
+    const int4 cut = rows_cuts<D>(a)[blockIdx.x];
+    const int n = cut.x + cut.z, parts = a.workers / a.c.kv_heads;
+    if (n == 0) return;   // one workgroup had it whole
+    const float2* ml = reinterpret_cast<const float2*>(a.part + rows_pieces(a) * a.part_rows * D);
+    auto part_row = [&](int j, int r) {
+        const int64_t id = j < cut.x ? rows_piece_id(a, parts, cut.y + j, -1, head) : rows_piece_id(a, parts, item, cut.w + j - cut.x, head);
+        return id * a.part_rows + r0 + min(r, rows - 1);
+    };
+    float ref[4], l[4], o[4][V];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        ref[r] = -INFINITY;
+        l[r] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < V; ++c) o[r][c] = 0.0f;
+    }
+    for (int j = lane; j < n; j += 64)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ref[r] = fmaxf(ref[r], ml[part_row(j, r)].x);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int x = 32; x >= 1; x >>= 1) ref[r] = fmaxf(ref[r], __shfl_xor(ref[r], x));
+    for (int j = wave; j < n; j += 4) {
+        float2 m[4];
+        float x[4][V];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t at = part_row(j, r);
+            m[r] = ml[at];
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[r][c] = a.part[at * D + V * lane + c];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (m[r].y == 0.0f) continue;
+            const float f = m[r].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[r].x - ref[r]);   // -inf: the sum is NaN
+            l[r] += f * m[r].y;
+#pragma unroll
+            for (int c = 0; c < V; ++c) o[r][c] += f * x[r][c];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int c = 0; c < V; ++c) sums[wave][r][V * lane + c] = o[r][c];
+        if (lane == 0) sums[wave][r][D] = l[r];
+    }
+    __syncthreads();
+    if (wave >= rows) return;   // one wave for each row from here on
+    float lsum = 0.0f, y[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) y[c] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        lsum += sums[w][wave][D];
+#pragma unroll
+        for (int c = 0; c < V; ++c) y[c] += sums[w][wave][V * lane + c];
+    }
+    const float inv = attn_inverse(lsum);
+    const int row = item % a.per_seq * kAttnRows + r0 + wave, qh = head * a.group + row % a.group;
+    const int64_t token = sr.first + row / a.group;
+    char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h;
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+        if constexpr (kBf16) reinterpret_cast<__bf16*>(dst)[V * lane + c] = (__bf16)(y[c] * inv);
+        else reinterpret_cast<float*>(dst)[V * lane + c] = y[c] * inv;
+    }
+    const float top = wave == 0 ? ref[0] : wave == 1 ? ref[1] : wave == 2 ? ref[2] : ref[3];
+    if (a.lse && lane == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(top, lsum);
+}
+
+template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs& a, hipStream_t s) {
     typedef AttnShape<kBf16, D> Sh;
-    auto kern = cache_attn_rows_kernel<kBf16, D>;
+    auto kern = a.workers ? cache_attn_rows_share_kernel<kBf16, D> : cache_attn_rows_kernel<kBf16, D>;
     if (Sh::kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds));
-    hipLaunchKernelGGL(kern, dim3((unsigned)(items * a.c.kv_heads * a.splits)), dim3(256), Sh::kLds, s, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.workers ? a.workers : a.items * a.c.kv_heads)), dim3(256), Sh::kLds, s, a);
+    const veda_status st = launch_status("veda_cache_attn_fwd");
+    if (st != VEDA_OK || !a.workers) return st;
+    hipLaunchKernelGGL((cache_attn_rows_join_kernel<kBf16, D>), dim3((unsigned)(a.items * a.c.kv_heads), (unsigned)((a.part_rows + 3) / 4)), dim3(256), 0, s, a);
     return launch_status("veda_cache_attn_fwd");
 }
 
-veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, int64_t items, hipStream_t s) {
-    if (bf16) return d == 128 ? launch_rows<true, 128>(a, items, s) : launch_rows<true, 64>(a, items, s);
-    return d == 128 ? launch_rows<false, 128>(a, items, s) : launch_rows<false, 64>(a, items, s);
+// One wave of the fp32 kernel at d = 128 needs more than half of a SIMD's registers.
+int attn_rows_workers(bool bf16, int d) { return 512; }
+
+veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) {
+    if (bf16) return d == 128 ? launch_rows<true, 128>(a, s) : launch_rows<true, 64>(a, s);
+    return d == 128 ? launch_rows<false, 128>(a, s) : launch_rows<false, 64>(a, s);
 }
 
 }  // namespace veda

@@ -110,10 +110,12 @@ def test_attention_workspace_refusals(lib):
     assert _attend(lib, c, b, workspace_bytes=need - 1) == WORKSPACE
     assert _attend(lib, c, b, workspace=None) == INVALID
     assert _attend(lib, c, b, workspace=AT + 4, workspace_bytes=need) == UNSUPPORTED
-    # many rows: those of the buffers count
-    many = [lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(_batch(seqs=1, rows=r, max_new=40, max_pages=4096, table_stride=4096)), 4)
-            for r in (40, 80)]
-    assert 0 < many[0] < many[1]
+    # few or many rows over long caches ask for some, short caches for none
+    for rows in (1, 8, 9, 16, 17, 64, 65, 1000):
+        many = _batch(seqs=1, rows=rows, max_new=rows, max_pages=4096, table_stride=4096)
+        need = lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(many), 4)
+        assert need > 0 and _attend(lib, c, many, workspace_bytes=need - 1) == WORKSPACE
+    assert lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(_batch(max_pages=8, table_stride=8)), 4) == 0
 
 
 def test_empty_calls_do_nothing(lib):
