@@ -766,8 +766,8 @@ template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs&
     return launch_status("veda_cache_attn_fwd");
 }
 
-// One wave of the fp32 kernel at d = 128 needs more than half of a SIMD's registers.
-int attn_rows_workers(bool bf16, int d) { return 512; }
+// Two to a compute unit, by LDS and registers alike.
+int attn_rows_workers() { return 512; }
 
 veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) {
     if (bf16) return d == 128 ? launch_rows<true, 128>(a, s) : launch_rows<true, 64>(a, s);
