@@ -33,41 +33,6 @@ __device__ __forceinline__ int lanes_up_to(int x) {
     return x;
 }
 
-// Work items: every sequence's rows in blocks (of `size`, where a token counts as `group` rows), sequence by sequence.  Only the
-// device knows the sequences' lengths; a grid of the longest's blocks for each of them is mostly empty where they are ragged, and an empty
-// workgroup costs its launch: prompts of 4096 rows and less, 8192 workgroups of which 4176 empty, 530 us, with the items numbered as here
-// ...  Returns false for numbers beyond the last item.
-struct RowBlock { int seq, block, blocks; };   // block of blocks of its sequence
-__device__ __forceinline__ bool find_block(const CacheArgs& c, int group, int size, int item, RowBlock& out) {
-    const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int s0 = 0; s0 < c.seqs; s0 += 64) {
-        const int s = s0 + lane;
-        int n = 0;
-        if (s < c.seqs) {
-            const int first = min(max(c.q_start[s], 0), c.rows);
-            n = min(max(min(c.q_start[s + 1], c.rows) - first, 0), c.max_new);
-        }
-        const int blocks = (int)(((int64_t)n * group + size - 1) / size);
-        const int up_to = lanes_up_to(blocks);
-        const int total = __builtin_amdgcn_readlane(up_to, 63);
-        if (item < base + total) {
-            const int at = __popcll(__ballot(base + up_to <= item));
-            out.seq = s0 + at;
-            out.blocks = __builtin_amdgcn_readlane(blocks, at);
-            out.block = item - (base + __builtin_amdgcn_readlane(up_to, at) - out.blocks);
-            return true;
-        }
-        base += total;
-    }
-    return false;
-}
-// Items that a grid has to have, as far as the host knows.
-inline int64_t block_items(int64_t seqs, int64_t rows, int64_t max_new, int64_t group, int64_t size) {
-    const int64_t each = seqs * ((max_new * group + size - 1) / size), all = rows * group / size + seqs;
-    return each < all ? each : all;
-}
-
 // Rows and length of a sequence, whatever the arrays hold.
 struct SeqRows {
     int first;    // row of its first new token
@@ -80,6 +45,38 @@ __device__ __forceinline__ SeqRows seq_rows(const CacheArgs& c, int s) {
     r.n = max(min(c.q_start[s + 1], c.rows) - r.first, 0);
     r.len = min(max(c.kv_len[s], 0), c.max_pages << c.log_page);
     return r;
+}
+
+// Work items: every sequence's rows in blocks (of `size`, where a token counts as `group` rows), sequence by sequence.  Only the
+// device knows the sequences' lengths; a grid of the longest's blocks for each of them is mostly empty where they are ragged, and an empty
+// workgroup costs its launch: prompts of 4096 rows and less, 8192 workgroups of which 4176 empty, 527 us instead
+// of 352 with the items numbered as here.  Returns false for numbers beyond the last item.
+struct RowBlock { int seq, block, blocks; SeqRows rows; };   // block of blocks of its sequence
+__device__ __forceinline__ bool find_block(const CacheArgs& c, int group, int size, int item, RowBlock& out) {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int s0 = 0; s0 < c.seqs; s0 += 64) {
+        SeqRows r{0, 0, 0};
+        if (s0 + lane < c.seqs) r = seq_rows(c, s0 + lane);
+        const int blocks = (int)(((int64_t)min(r.n, c.max_new) * group + size - 1) / size);
+        const int up_to = lanes_up_to(blocks);
+        const int total = __builtin_amdgcn_readlane(up_to, 63);
+        if (item < base + total) {
+            const int at = __popcll(__ballot(base + up_to <= item));
+            out.seq = s0 + at;
+            out.blocks = __builtin_amdgcn_readlane(blocks, at);
+            out.block = item - (base + __builtin_amdgcn_readlane(up_to, at) - out.blocks);
+            out.rows = SeqRows{__builtin_amdgcn_readlane(r.first, at), __builtin_amdgcn_readlane(r.n, at), __builtin_amdgcn_readlane(r.len, at)};
+            return true;
+        }
+        base += total;
+    }
+    return false;
+}
+// Items that a grid has to have, as far as the host knows.
+inline int64_t block_items(int64_t seqs, int64_t rows, int64_t max_new, int64_t group, int64_t size) {
+    const int64_t each = seqs * ((max_new * group + size - 1) / size), all = rows * group / size + seqs;
+    return each < all ? each : all;
 }
 
 #endif

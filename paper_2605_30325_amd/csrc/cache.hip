@@ -66,7 +66,7 @@ template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) v
     RowBlock rb;
     if (!find_block(a.c, 1, 1 << a.log_tb, blockIdx.x, rb)) return;
     const int s = rb.seq, i0 = rb.block << a.log_tb;
-    const SeqRows sr = seq_rows(a.c, s);
+    const SeqRows sr = rb.rows;
     const int n = min(min(sr.n, a.c.max_new) - i0, 1 << a.log_tb);
     const int row0 = sr.first + i0, p0 = sr.len - sr.n + i0, page_mask = (1 << a.c.log_page) - 1;
     if ((int)threadIdx.x < n) {

@@ -73,8 +73,8 @@ __device__ __forceinline__ bool attn_block_of(const CacheAttnArgs& a, int size, 
     if (!a.per_seq) return find_block(a.c, a.group, size, item, out);
     out.seq = item / a.per_seq;
     out.block = item % a.per_seq;
-    const SeqRows sr = seq_rows(a.c, out.seq);
-    out.blocks = (min(sr.n, a.c.max_new) * a.group + size - 1) / size;
+    out.rows = seq_rows(a.c, out.seq);
+    out.blocks = (min(out.rows.n, a.c.max_new) * a.group + size - 1) / size;
     return out.block < out.blocks;
 }
 

@@ -375,7 +375,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__((64 * KeysTile
     RowBlock block;
     if (!attn_block_of(a, kRows, blockIdx.x / a.c.kv_heads, block)) return;
     const int head = blockIdx.x % a.c.kv_heads, r0 = block.block * kRows;
-    const SeqRows sr = seq_rows(a.c, block.seq);
+    const SeqRows sr = block.rows;
     const int n = min(sr.n, a.c.max_new), r_end = min(n * a.group, r0 + kRows);
     const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, 32);
     const int32_t* table = a.c.table + block.seq * a.c.table_stride;

@@ -151,10 +151,11 @@ __device__ __forceinline__ void attn_mask(const AttnRow<kBf16, D>& st, f32x16& s
     }
 }
 
-// 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.
+// 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.  check: values may be not
+// finite at keys that some row does not see (a product with a p of zero would be NaN).
 template <bool kBf16, int D>
 __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16, D>& st, uint32_t k, uint32_t v, int key0, uint32_t exists,
-                                           bool full, int hh) {
+                                           bool full, bool check, int hh) {
     constexpr int NB = D / 32, kRowB = AttnTile<kBf16, D>::kRowB;
     f32x16 s = attn_scores<kBf16, D>(st, k);
     if (!full) attn_mask<kBf16, D>(st, s, key0, exists, a.sinks, hh);
@@ -176,7 +177,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[kk][e] = (__bf16)s[8 * kk + e];
-        if (full || attn_finite<D>(v)) {
+        if (!check || attn_finite<D>(v)) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -193,7 +194,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
             return *(lds_f32_ptr)(uintptr_t)((v ^ (uint32_t)(nb << 7)) + (8 * (i >> 2) + (i & 3)) * kRowB);
         };
         bool plain = true;
-        if (!full) {
+        if (check) {
             f32x16 z;
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.0f;
@@ -407,12 +408,6 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             }
         }
     }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st.o[nb][i] = 0.0f;
-    st.ref = -INFINITY;
-    st.sub = st.l = 0.0f;
     const int wave_lo = __builtin_amdgcn_readlane(st.lo, 0), wave_hi = __builtin_amdgcn_readlane(st.hi, 31);       // some row sees
     const int wave_lo_max = __builtin_amdgcn_readlane(st.lo, 31), wave_hi_min = __builtin_amdgcn_readlane(st.hi, 0);   // every row sees
 
@@ -468,6 +463,18 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         v_at = (uint32_t)(4 * hh * kRowB + 4 * l31 + (hh << 7));
     }
 
+    // Twice at most.  Values that are not finite at keys that exist are taken to be seen by all rows, or by none; where one turns up in
+    // the sums, the workgroup does all of it again and looks at every tile that some row does not see whole.  (To look at once
+    // costs as much as half of such a tile's products.)  Behind the sequence's end and in holes anything may lie: there it looks.
+    float* ml = reinterpret_cast<float*>(smem + kAttnRows * Sh::kOutRowB);   // [128], and a flag of each wave before
+    float l = 0.0f;
+    for (bool careful = false;;) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[nb][i] = 0.0f;
+    st.ref = -INFINITY;
+    st.sub = st.l = 0.0f;
     int slot = 0, at = 0;
     if (t_beg < t_end) {
         look_up(t_beg);
@@ -532,17 +539,34 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         for (int c = 0; c < kKeyTile / 32; ++c) {
             const int key = key0 + 32 * c;
             const uint32_t ex = (exists >> (2 * c)) & 3u;
-            if (some(key, 32, ex))
-                attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, all(key, 32, ex), hh);
+            if (some(key, 32, ex)) {
+                const bool full = all(key, 32, ex);
+                attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, full,
+                                     !full && (careful || ex != 3u || key + 32 > sr.len), hh);
+            }
         }
         ++t;
         slot ^= 1;
     }
 
-    // Results.  A lane holds channels 32 nb + 8 j + 4 hh + 0..3 of its row.
-    const float l = sum_with_other_half(st.l);
+    l = sum_with_other_half(st.l);
+    if (careful) break;
+    float odd = 0.0f * l;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(st.o[nb][i], 0.0f, odd);
     __syncthreads();
-    float* ml = reinterpret_cast<float*>(smem + kAttnRows * Sh::kOutRowB);   // [128]
+    if (lane == 0) ml[wave] = 0.0f;
+    if (odd != 0.0f) ml[wave] = 1.0f;   // NaN
+    __syncthreads();
+    if (ml[0] + ml[1] + ml[2] + ml[3] == 0.0f) break;
+    careful = true;
+    __syncthreads();
+    }
+
+    // Results.  A lane holds channels 32 nb + 8 j + 4 hh + 0..3 of its row.
+    __syncthreads();
     char* orow = smem + (wave * 32 + l31) * Sh::kOutRowB;
     if (part >= 0) {   // [part][row][D] sums, then [part][row] reference and l
         if (w0 + l31 < r_end) {
@@ -591,7 +615,7 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_att
     extern __shared__ __align__(1024) char smem[];
     RowBlock rb;
     if (!attn_block_of(a, kAttnRows, blockIdx.x / a.c.kv_heads, rb)) return;
-    const SeqRows sr = seq_rows(a.c, rb.seq);
+    const SeqRows sr = rb.rows;
     const int rows = min(sr.n, a.c.max_new) * a.group;
     const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
     const int r_end = min(rows, r0 + kAttnRows);
