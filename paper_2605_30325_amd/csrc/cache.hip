@@ -39,8 +39,10 @@ CacheArgs cache_args(const veda_cache* c, const veda_cache_batch* b) {
     return a;
 }
 
-veda_status check_rows(const veda_cache* c, int32_t rows, int32_t heads, const void* p, veda_strides s, bool distinct) {
+veda_status check_rows(const veda_cache* c, int32_t rows, int32_t heads, const void* p, veda_strides& s, bool distinct) {
     const int es = c->dtype == VEDA_BF16 ? 2 : 4, d = c->head_dim;
+    if (rows == 1) s.n = 0;
+    if (heads == 1) s.h = 0;
     if (!p || s.h < 0 || s.n < 0) return VEDA_ERR_INVALID_ARG;
     if (distinct && ((rows > 1 && s.n < d) || (heads > 1 && s.h < d))) return VEDA_ERR_INVALID_ARG;
     if (!aligned16(p) || (s.h * es) % 16 || (s.n * es) % 16) return VEDA_ERR_UNSUPPORTED;
@@ -148,7 +150,7 @@ extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_b
     if (st == VEDA_OK && q_heads) st = veda::check_rows(c, b->rows, q_heads, q, sq, false);
     if (st == VEDA_OK && q_heads) st = veda::check_rows(c, b->rows, q_heads, q_out, sq_out, true);
     if (st != VEDA_OK) return st;
-    if (q_heads && q == q_out && ((b->rows > 1 && sq.n != sq_out.n) || (q_heads > 1 && sq.h != sq_out.h))) return VEDA_ERR_INVALID_ARG;
+    if (q_heads && q == q_out && (sq.n != sq_out.n || sq.h != sq_out.h)) return VEDA_ERR_INVALID_ARG;
     if (rope) {
         int device = -1;
         VEDA_HIP_TRY(hipGetDevice(&device));
@@ -199,7 +201,7 @@ extern "C" veda_status veda_cache_copy_pages(const veda_cache* c, const int32_t*
     if (n > veda::kCopyPairsShort) {
         try {
             note.assign((size_t)c->pages, 0);
-        } catch (const std::bad_alloc&) {
+        } catch (const std::exception&) {
             return veda::hip_fail(hipErrorOutOfMemory, "veda_cache_copy_pages");
         }
     }

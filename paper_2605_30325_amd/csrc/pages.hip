@@ -25,7 +25,7 @@ veda_status veda_pages_create(int32_t pages, int32_t page_tokens, int32_t max_se
     try {
         *out = new veda_pages{veda::PageBook(pages, page_tokens, max_seqs, max_pages)};
         return VEDA_OK;
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         return veda::hip_fail(hipErrorOutOfMemory, "veda_pages_create");
     }
 }
@@ -59,7 +59,7 @@ veda_status veda_pages_compact(veda_pages* p, int32_t* copies, int32_t capacity,
     if (!p || !n_copies) return VEDA_ERR_INVALID_ARG;
     try {
         return told(p->book.compact(copies, capacity, n_copies), "veda_pages_compact");
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         return veda::hip_fail(hipErrorOutOfMemory, "veda_pages_compact");
     }
 }

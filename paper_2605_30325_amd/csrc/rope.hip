@@ -88,7 +88,7 @@ extern "C" veda_status veda_rope_create(const veda_rope_config* c, veda_rope** o
         e = hipGetDevice(&r->device);
         if (e == hipSuccess) e = hipMalloc((void**)&r->d_turns, turns.size() * sizeof(double));
         if (e == hipSuccess) e = hipMemcpy(r->d_turns, turns.data(), turns.size() * sizeof(double), hipMemcpyHostToDevice);
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         e = hipErrorOutOfMemory;
     }
     if (e != hipSuccess) {
@@ -123,10 +123,14 @@ extern "C" veda_status veda_rope_apply(const veda_rope* rope, veda_dtype dtype, 
     if (!x || !y || !positions) return VEDA_ERR_INVALID_ARG;
     const int d = rope->cfg.head_dim, es = dtype == VEDA_BF16 ? 2 : 4;
     if (position_stride < 0 || (position_stride > 0 && position_stride < (int64_t)tokens * rope->cfg.axes)) return VEDA_ERR_INVALID_ARG;
+    // an axis of one entry has no stride, whatever it is given as
+    if (batch == 1) sx.b = sy.b = 0;
+    if (heads == 1) sx.h = sy.h = 0;
+    if (tokens == 1) sx.n = sy.n = 0;
     if (sx.b < 0 || sx.h < 0 || sx.n < 0 || sy.b < 0 || sy.h < 0 || sy.n < 0) return VEDA_ERR_INVALID_ARG;
     // different rows of y must be different bytes
     if ((tokens > 1 && sy.n < d) || (heads > 1 && sy.h < d) || (batch > 1 && sy.b < d)) return VEDA_ERR_INVALID_ARG;
-    if (x == y && ((tokens > 1 && sx.n != sy.n) || (heads > 1 && sx.h != sy.h) || (batch > 1 && sx.b != sy.b))) return VEDA_ERR_INVALID_ARG;
+    if (x == y && (sx.n != sy.n || sx.h != sy.h || sx.b != sy.b)) return VEDA_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(y) || (sx.b * es) % 16 || (sx.h * es) % 16 || (sx.n * es) % 16 || (sy.b * es) % 16 ||
         (sy.h * es) % 16 || (sy.n * es) % 16)
         return VEDA_ERR_UNSUPPORTED;

@@ -753,8 +753,9 @@ class Cache:
             k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
         inner = (page_tokens * head_dim, head_dim, 1)
         for t in (k, v):
-            _need(t is not None and tuple(t.shape) == shape and t.dtype == dtype and t.stride()[1:] == inner and t.device == k.device and
-                  t.stride(0) == k.stride(0), "Cache", f"k and v must be {dtype} {list(shape)} with close rows, heads and tokens")
+            _need(t is not None and tuple(t.shape) == shape and t.dtype == dtype and t.device == k.device and
+                  all(a == b or n == 1 for n, a, b in zip(shape[1:], t.stride()[1:], inner)) and (pages == 1 or t.stride(0) == k.stride(0)),
+                  "Cache", f"k and v must be {dtype} {list(shape)} with close rows, heads and tokens")
         self.k, self.v = k, v
         self.pages, self.page_tokens, self.kv_heads, self.head_dim, self.dtype = int(pages), int(page_tokens), int(kv_heads), int(head_dim), dtype
         stride = k.stride(0) if pages > 1 else 0
@@ -932,7 +933,7 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
     if rope is not None:
         b["q"] = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))
     else:
-        veda_cache_append(cache, batch, k, v)
+        veda_cache_append(cache, batch, k, v, None, positions)
     need = veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])
     if "ws" not in b or b["ws"].numel() < need:
         b["ws"] = torch.empty(need, dtype=torch.uint8, device=q.device)

@@ -480,6 +480,31 @@ def test_append_refuses_what_does_not_fit():
         veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.1, lse=torch.zeros((t.rows, 4), device=dev()))
 
 
+def test_axes_of_one_entry_have_no_stride():
+    # one row, one head: strides of such axes can be anything, and are not looked at
+    t = Setup([1], [40], 1, 1, 64, BF16, seed=23, tail=0)
+    want, _ = check_attention(t)
+    odd = lambda x, *strides: torch.as_strided(x.contiguous(), x.shape, strides)
+    q, k, v = odd(t.q, 3, 5, 1), odd(t.qkv[:, 1:2], 1, 7, 1), odd(t.qkv[:, 2:], 9, 1, 1)
+    out, _ = veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.125, out=odd(torch.zeros(1, 1, 64, dtype=BF16, device=dev()), 11, 1, 1))
+    assert torch.equal(out, want)
+    veda.veda_cache_append(t.cache, t.batch, k, v, q=q, q_out=odd(torch.zeros(1, 1, 64, dtype=BF16, device=dev()), 3, 2, 1))
+    assert torch.equal(t.k[t.table[0, 2], :, 8], k[0]) and torch.equal(t.v[t.table[0, 2], :, 8], v[0])
+    x = torch.as_strided(normal((64,), BF16, 1), (1, 1, 1, 64), (3, 5, 7, 1))
+    rope = make_rope(64, (64,), True)
+    want, bound = rotated(x, torch.tensor([[[5]]]), (64,), True)
+    close(veda.veda_rope_apply(rope, x, torch.tensor([5], dtype=torch.int32, device=dev())), want, bound, BF16)
+    one = normal((1, 16, 64), F32, 3)
+    cache = veda.Cache(1, 16, 1, 64, F32, k=torch.as_strided(one, (1, 1, 16, 64), (3, 5, 64, 1)), v=one[:, None])
+    assert cache.pages == 1
+
+
+def test_one_attention_call_of_a_step_refuses_positions_without_a_rope():
+    t = Setup([4], [8], 4, 2, 64, F32, seed=24)
+    with pytest.raises(veda.VedaError):
+        veda.veda_cache_attention(t.cache, t.batch, t.q, t.qkv[:, 4:6], t.qkv[:, 6:], 0.125, positions=torch.zeros((t.rows, 1), dtype=torch.int32, device=dev()))
+
+
 # ---- copies of pages ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,d,hk,page", [(BF16, 64, 1, 16), (F32, 128, 3, 64), (BF16, 128, 12, 256)])
