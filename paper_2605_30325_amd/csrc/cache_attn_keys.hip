@@ -21,9 +21,7 @@ template <bool kBf16, int D> struct KeysTile {
     static constexpr int kSegLoads = kSegRows * kRowB / 1024;     // 1 KB each
     static constexpr int kSegs = 32 / kSegRows;
     static constexpr int kSlot = 64 * kRowB;                      // 32 rows of K, 32 rows of V
-    static constexpr int kWaves = kBf16 || D == 64 ? 2 : 1;       // 64 KB of LDS (bf16, d = 64: 32): at least two workgroups to a compute unit
     static constexpr int kOutRowB = D * 4 + 16;                   // a row of the sums in LDS
-    static constexpr int kLds = 2 * kWaves * kSlot;
     static constexpr int kLoads = 2 * kSegs * kSegLoads;          // of a tile
     static constexpr int kDepth = kLoads <= 16 ? 3 : 2;           // slots of a wave that shares: loads run kDepth - 1 tiles ahead
     // 16-byte chunk c of row r lies at chunk c ^ swizzle: operand reads of a wave then fall into different banks.
@@ -364,14 +362,22 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)x >> 32), lane) << 32);
 }
 
-// Short caches: a workgroup for each (block of rows, key head), whose waves take its tiles in turn.
-template <bool kBf16, int D, int RB> __global__ __launch_bounds__((64 * KeysTile<kBf16, D>::kWaves)) void cache_attn_keys_kernel(CacheAttnArgs a) {
+// Short caches: a workgroup for each (block of rows, key head), whose waves take its tiles in turn.  With few workgroups latency counts:
+// eight waves (fp32, d = 128: four) with a slot each, so that all of a cache of 256 keys, half of one of 512, is asked for at once.  With
+// more than there are compute units two waves with two slots, so that workgroups start while others end.  Two waves / eight, us: one
+// fp32 token over 257 keys, 12 heads of 64, 12.3 / 9.1; bf16, d = 128, 64 workgroups of 501 keys 12.4 / 10.4, 512 of 401 21.3 / 25, 4096
+// of 101 54 / 88; fp32, d = 64, 768 of 401 44 / 40.
+template <bool kBf16, int D, bool kMany> struct KeysGroup {
+    static constexpr int kWaves = kMany ? 2 : kBf16 || D == 64 ? 8 : 4, kSlots = kMany ? 2 : 1;
+};
+template <bool kBf16, int D, int RB, bool kMany>
+__global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cache_attn_keys_kernel(CacheAttnArgs a) {
     typedef KeysTile<kBf16, D> T;
-    constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4, kWaves = T::kWaves;
+    constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4, kWaves = KeysGroup<kBf16, D, kMany>::kWaves, kSlots = KeysGroup<kBf16, D, kMany>::kSlots;
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KeysLane<kBf16, D> ln(lane);
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * 2 * T::kSlot;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * kSlots * T::kSlot;
     RowBlock block;
     if (!attn_block_of(a, kRows, blockIdx.x / a.c.kv_heads, block)) return;
     const int head = blockIdx.x % a.c.kv_heads, r0 = block.block * kRows;
@@ -402,15 +408,15 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__((64 * KeysTile
     }
     KeysRow<kBf16, D, RB> st;
     const KeysSeen see = keys_rows<kBf16, D, RB>(a, st, sr, n, head, r0, r_end, ln.l15, ln.g);
-    for (int t = wave; t < tiles.count; t += kWaves, slot ^= 1) {
+    for (int t = wave; t < tiles.count; t += kWaves) {
         const uint32_t exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
         const bool more = t + kWaves < tiles.count;
         if (++at == 64 && more) {
             look_up(t + kWaves);
             at = 0;
         }
-        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the other slot has been read
-        if (more) {
+        if (kSlots == 2 && more) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the other slot has been read
             load(at, slot ^ 1);
             wait_vmcnt<T::kLoads>();
         } else {
@@ -418,6 +424,11 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__((64 * KeysTile
         }
         asm volatile("" ::: "memory");
         keys_step<kBf16, D, RB>(a, st, see, ln, lds + slot * T::kSlot, tiles.at(t) * 32, exists);
+        if (kSlots == 1 && more) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            load(at, 0);
+        }
+        if (kSlots == 2) slot ^= 1;
     }
 
     // Sums of the waves, put together row by row.  A lane holds channels 16 c + 4 g + 0..3 of its row.
@@ -674,13 +685,23 @@ int attn_keys_workers(bool bf16, int d) {
     return 256 * (fit < 4 ? fit : 4);
 }
 
+template <bool kBf16, int D, int RB, bool kMany> static veda_status launch_short(const CacheAttnArgs& a, hipStream_t s) {
+    typedef KeysGroup<kBf16, D, kMany> G;
+    constexpr int kSums = G::kWaves * 16 * RB * (KeysTile<kBf16, D>::kOutRowB + 8), kTiles = G::kWaves * G::kSlots * KeysTile<kBf16, D>::kSlot;
+    constexpr int kLds = kTiles > kSums ? kTiles : kSums;
+    static_assert(kLds <= 160 * 1024, "what a compute unit has");
+    auto kern = cache_attn_keys_kernel<kBf16, D, RB, kMany>;
+    if (kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.items * a.c.kv_heads)), dim3(64 * G::kWaves), kLds, s, a);
+    return launch_status("veda_cache_attn_fwd");
+}
+
 template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheAttnArgs& a, hipStream_t s) {
-    typedef KeysTile<kBf16, D> T;
-    static_assert(T::kWaves * 16 * RB * (T::kOutRowB + 8) <= T::kLds, "the sums fit the slots");
-    static_assert(T::kLds <= 64 * 1024, "no more dynamic LDS than a launch may have without asking");
+    static_assert(keys_slots<kBf16, D>() <= 64 * 1024, "what a launch may have without asking");
     if (!a.workers) {
-        hipLaunchKernelGGL((cache_attn_keys_kernel<kBf16, D, RB>), dim3((unsigned)(a.items * a.c.kv_heads)), dim3(64 * T::kWaves), T::kLds, s, a);
-        return launch_status("veda_cache_attn_fwd");
+        if constexpr (kBf16)
+            if (a.items * a.c.kv_heads > 256) return launch_short<kBf16, D, RB, true>(a, s);
+        return launch_short<kBf16, D, RB, false>(a, s);
     }
     hipLaunchKernelGGL((cache_attn_share_kernel<kBf16, D, RB>), dim3((unsigned)a.workers), dim3(64), (keys_slots<kBf16, D>()), s, a);
     veda_status st = launch_status("veda_cache_attn_fwd");
