@@ -403,8 +403,8 @@ veda_status veda_rope_create(const veda_rope_config*, veda_rope** out);
 void veda_rope_destroy(veda_rope*);   /* NULL is allowed */
 /* freq: host, rot / 2 radians per position; amplitude: host, one value.  Either may be NULL. */
 veda_status veda_rope_frequencies(const veda_rope*, double* freq, double* amplitude);
-/* x, y       device, [batch][heads][tokens][head_dim] with strides sx, sy; y == x (with equal strides) rotates in place, other
- *            overlaps are not allowed.
+/* x, y       device, [batch][heads][tokens][head_dim] with strides sx, sy (batch up to 65535); y == x (with equal strides) rotates
+ *            in place, other overlaps are not allowed.
  * positions  device i32 [batch][tokens][axes], any sign; position_stride elements from a sample to the next (0: all alike).
  * transpose  0: rotate; 1: apply the transposed matrix, which turns the gradient of y into that of x (the rotation back, times
  *            A once more, not divided by it). */
@@ -456,8 +456,8 @@ typedef struct { int32_t block, window, sinks; } veda_visible;
  *            kv_heads, up to 32 * kv_heads: query head h reads key head h / (q_heads / kv_heads)
  * out        device, the same shape, strides so; not to overlap q.  A row that sees no key gets zeros.
  * lse        optional device fp32 [q_heads][rows]: natural-log sum of exp of the visible logits, -inf where there are none
- * workspace  device, 16-byte aligned, veda_cache_attn_workspace_bytes() (0 for most calls with many rows: NULL is allowed then);
- *            contents undefined after.  Calls that may overlap need one each.
+ * workspace  device, 16-byte aligned, veda_cache_attn_workspace_bytes() (0 for short caches and for many blocks of rows: NULL is
+ *            allowed then); contents undefined after.  Calls that may overlap need one each.
  * bf16: products on bf16 MFMA with fp32 accumulation, softmax in fp32 (logits scaled there, Q is not rounded again), P rounded to
  * bf16 before P V.  f32: products on fp32 MFMA.  Values behind a sequence's end, in holes and at keys that a row does not see
  * do not reach that row, whatever they are (infinities and NaN too). */
@@ -467,7 +467,7 @@ veda_status veda_cache_attn_fwd(const veda_cache*, const veda_cache_batch*, int3
                                 void* workspace, size_t workspace_bytes, void* stream);
 /* Copies pages inside both pools.  pairs: host i32 [n][2] = (from, to), as if copied one after the other in this order (a page
  * may appear any number of times); numbers outside [0, pages) are refused.  Pairs that do not touch each other's pages share a
- * launch, up to 448 of them. */
+ * launch, up to 448 of them.  They are read before the call returns: a captured call copies the same pages when it is replayed. */
 veda_status veda_cache_copy_pages(const veda_cache*, const int32_t* pairs, int64_t n, void* stream);
 
 /* Which page belongs to which sequence: a host object, no device memory, not thread-safe.  Pages are counted: a forked sequence

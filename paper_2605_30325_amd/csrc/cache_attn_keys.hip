@@ -1,14 +1,18 @@
 // Attention over the paged cache, few rows for each key head (single tokens and small chunks).
 //
-// Memory bounds it: every key and value is read once for at most 32 rows, so the work is to keep loads in flight on all compute
-// units until the last of them is done.  The query heads that share a key head are put together as in cache_attn_rows.hip, 16 rows
-// to a product of 16 x 16 (K rows x query rows, and V channels x query rows).  Every wave walks key tiles of its own, 32 keys each, through
-// two slots of LDS that direct loads fill one tile ahead: no barrier in the loop, and the waves' sums are put together at the end.
+// O = sum_j p_j v_j / l with p_j = 2^(s_j - ref), l = sum_j p_j: sums over any keys can be formed apart and added once they are brought to a
+// common reference.  Memory bounds it: every key and value is read once for at most 32 rows, so the work is to keep loads in flight on
+// all compute units until the last of them is done.  The query heads that share a key head are put together as in cache_attn_rows.hip, 16
+// rows to a product of 16 x 16 (K rows x query rows, and V channels x query rows): with 32 x 32 products, half or more of them padding, fp32
+// tokens waited for the matrix cores (257 keys, 12 heads of 64: 18.6 us instead of 12.3).  A wave walks key tiles of its own, 32 keys each, that direct
+// loads put into its slots of LDS: no barrier in the loop, the compiler's waits only for what the wave itself has read.
 //
-// Keys are shared out evenly.  All tiles of all (sequence, key head) lie in one row of numbers, and each of the workgroups that fit the card at once
-// takes an equal part of it, whatever sequences that cuts: the pieces of a cut sequence go to the workspace as unfinished sums, at
-// most two a workgroup, and cache_attn_join_parts_kernel puts them together.  64 sequences of 1..8192 keys, 8 key heads: a workgroup for each (sequence,
-// key head) waits for the longest (4.6-5.2 TB/s); ...
+// Long caches are shared out evenly.  The tiles of all sequences lie in one row of numbers; each of the waves that run at once takes one key
+// head of an equal part of it, whatever sequences that cuts, and the heads of a part are neighbours: they read the same pages at the same
+// time, which is worth a tenth of the bandwidth.  The pieces of a cut sequence go to the workspace as unfinished sums, at most two a wave,
+// and cache_attn_join_parts_kernel puts them together.  d = 128, bf16, 8 key heads: 64 caches of 8192 keys 353 us (6.1 TB/s); 64 of 1..8192
+// keys 195 us (5.5 TB/s; a workgroup for each sequence and head waits for the longest: 208-235); one of 131,101 keys 105 us (5.1 TB/s), of
+// 400,001 283 us (5.8).
 #include "cache_attn.h"
 
 namespace veda {
@@ -468,7 +472,9 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cac
 }
 
 // Long caches: every wave is a workgroup and takes one key head of an equal part [now, end) of the common row of tiles, sequence by
-// sequence.  Loads run one tile ahead across their ends, so a change of sequence costs the new rows' loads and no more.
+// sequence.  Loads run kDepth - 1 tiles ahead across their ends, so a change of sequence costs the new rows' loads and no more.  (Two slots
+// instead of three: 64 even caches of 8192 keys 376 us instead of 353; a workgroup of several waves that stops at every end: 82 us instead
+// of 53 for ten ragged caches of 12 heads.)
 template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache_attn_share_kernel(CacheAttnArgs a) {
     typedef KeysTile<kBf16, D> T;
     constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4;

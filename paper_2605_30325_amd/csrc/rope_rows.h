@@ -4,7 +4,8 @@
 // y0 = A (x0 cos - x1 sin), y1 = A (x0 sin + x1 cos) for every pair of channels: 2 bytes moved for each flop or so, so memory
 // bounds it, and everything here serves 16-byte accesses and few instructions between them.  The angle of a pair is the same
 // for all heads of a token: a workgroup takes a block of tokens with as many heads as there are, puts A cos and A sin of the
-// block into LDS once and streams the heads' rows past them.
+// block into LDS once and streams the heads' rows past them.  32,760 tokens x 40 heads of 128 channels, bf16, three axes: 136 us = 4.9 TB/s
+// (a large copy: 5.0); a chunk of 4680 x 36 rows into the cache 18 us = 4.8 TB/s.
 #pragma once
 
 #include "veda_internal.h"
