@@ -454,7 +454,7 @@ typedef struct { int32_t block, window, sinks; } veda_visible;
 /* Attention of the new rows over the cache (their own keys included, so append first).
  * q          device, [rows][q_heads][head_dim], strides sq (s.n from row to row, s.h from head to head); q_heads a multiple of
  *            kv_heads, up to 32 * kv_heads: query head h reads key head h / (q_heads / kv_heads)
- * out        device, the same shape, strides so; not to overlap q.  A row that sees no key gets zeros.
+ * out        device, the same shape, strides so; not to overlap q (refused where it begins at q).  A row that sees no key gets zeros.
  * lse        optional device fp32 [q_heads][rows]: natural-log sum of exp of the visible logits, -inf where there are none
  * workspace  device, 16-byte aligned, veda_cache_attn_workspace_bytes() (0 for short caches and for many blocks of rows: NULL is
  *            allowed then); contents undefined after.  Calls that may overlap need one each.
@@ -483,7 +483,8 @@ const int32_t* veda_pages_table(const veda_pages*);              /* host [max_se
 int32_t veda_pages_length(const veda_pages*, int32_t seq);       /* tokens; -1 on bad args                             */
 int32_t veda_pages_free_count(const veda_pages*);                /* pages that nobody holds; -1 on bad args            */
 /* Makes the sequence `tokens` (>= its length) long: pages for the new tokens, and pages of its own in place of shared ones that
- * the new tokens fall into (at most one, so one copy).  Too few free pages: VEDA_ERR_WORKSPACE. */
+ * the new tokens fall into (at most one, so one copy).  Too few free pages: VEDA_ERR_WORKSPACE.  A sequence that was cut inside an
+ * evicted page cannot grow (cut it to the page's start first): the page's first tokens are gone, a new one would pass off anything as them. */
 veda_status veda_pages_extend(veda_pages*, int32_t seq, int32_t tokens, int32_t* copies, int32_t capacity, int32_t* n_copies);
 veda_status veda_pages_fork(veda_pages*, int32_t from, int32_t to);         /* `to` must be empty (length 0)               */
 veda_status veda_pages_truncate(veda_pages*, int32_t seq, int32_t tokens);  /* keeps the first tokens; 0 frees the sequence */

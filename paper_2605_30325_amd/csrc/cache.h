@@ -74,11 +74,22 @@ __device__ __forceinline__ bool find_block(const CacheArgs& c, int group, int si
     }
     return false;
 }
+// Item -> block of rows: by division where the grid has per_seq for every sequence, else (0) by what the sequences hold.
+__device__ __forceinline__ bool block_of(const CacheArgs& c, int group, int size, int per_seq, int item, RowBlock& out) {
+    if (!per_seq) return find_block(c, group, size, item, out);
+    out.seq = item / per_seq;
+    out.block = item % per_seq;
+    out.rows = seq_rows(c, out.seq);
+    out.blocks = (int)(((int64_t)min(out.rows.n, c.max_new) * group + size - 1) / size);
+    return out.block < out.blocks;
+}
 // Items that a grid has to have, as far as the host knows.
 inline int64_t block_items(int64_t seqs, int64_t rows, int64_t max_new, int64_t group, int64_t size) {
     const int64_t each = seqs * ((max_new * group + size - 1) / size), all = rows * group / size + seqs;
     return each < all ? each : all;
 }
+// Whether few of `uniform` blocks, the longest sequence's for each, can be empty, so that there is no need to search for those that are not.
+inline bool blocks_even(int64_t uniform, int64_t items) { return uniform <= items + items / 4; }
 
 #endif
 

@@ -56,7 +56,7 @@ struct AppendArgs {
     char* q_out;
     int64_t sq_h, sq_n, so_h, so_n, sk_h, sk_n, sv_h, sv_n;   // bytes
     const int32_t* positions;   // null: the position in the sequence
-    int32_t q_heads, head_dim, units, log_tb, hb;
+    int32_t q_heads, head_dim, units, log_tb, hb, per_seq;
     RowOrder order;
 };
 
@@ -66,7 +66,7 @@ template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) v
     extern __shared__ float2 cs[];
     __shared__ int page_s[16];
     RowBlock rb;
-    if (!find_block(a.c, 1, 1 << a.log_tb, blockIdx.x, rb)) return;
+    if (!block_of(a.c, 1, 1 << a.log_tb, a.per_seq, blockIdx.x, rb)) return;
     const int s = rb.seq, i0 = rb.block << a.log_tb;
     const SeqRows sr = rb.rows;
     const int n = min(min(sr.n, a.c.max_new) - i0, 1 << a.log_tb);
@@ -169,9 +169,15 @@ extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_b
     a.units = veda::rope_units(a.rope, c->head_dim, chunk, chunks);
     veda::rope_blocks(a.c.max_new, b->seqs, heads, &a.log_tb, &a.hb);
     a.order = veda::row_order(sk.h < sk.n);
-    const int64_t gx = veda::block_items(b->seqs, b->rows, a.c.max_new, 1, (int64_t)1 << a.log_tb);
-    const int64_t gy = (heads + a.hb - 1) / a.hb;
-    if (gx >= (int64_t)1 << 31 || gy > 65535) return VEDA_ERR_UNSUPPORTED;
+    const int64_t each = ((int64_t)a.c.max_new + (1 << a.log_tb) - 1) >> a.log_tb, uniform = b->seqs * each, gy = (heads + a.hb - 1) / a.hb;
+    int64_t gx = veda::block_items(b->seqs, b->rows, a.c.max_new, 1, (int64_t)1 << a.log_tb);
+    a.per_seq = 0;
+    if (veda::blocks_even(uniform, gx)) {
+        gx = uniform;
+        a.per_seq = (int32_t)each;
+    }
+    // a grid has less than 2^32 threads; and the search adds up 64 sequences' blocks in 32 bits
+    if (gx >= 1 << 24 || gy > 65535 || each >= 1 << 24) return VEDA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)gx, (unsigned)gy);
     const size_t lds = (size_t)a.rope.half * sizeof(float2) << a.log_tb;
     const hipStream_t s = (hipStream_t)stream;

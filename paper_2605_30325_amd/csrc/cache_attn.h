@@ -14,7 +14,7 @@ struct CacheAttnArgs {
     int64_t sq_h, sq_n, so_h, so_n;   // bytes
     int32_t q_heads, group;           // group: query heads of a key head
     int64_t items;                    // blocks of rows of one key head, at most
-    int32_t per_seq;                  // blocks of rows of every sequence, or 0: numbered by find_block
+    int32_t per_seq;                  // see block_of
     int32_t workers;                  // workgroups that share all keys evenly, or 0: one for each block of rows and key head
     int32_t part_rows;                // rows of a block's unfinished sums in the workspace
     int32_t block, window, sinks;
@@ -66,16 +66,6 @@ __device__ __forceinline__ AttnTiles tiles_seen(const CacheAttnArgs& a, const Se
     t.rest = max(t.first, lo / size);
     t.count = t.first + max(0, (hi + size - 1) / size - t.rest);
     return t;
-}
-
-// Item -> block of rows: by division where the grid has as many for every sequence, else by what the sequences hold.
-__device__ __forceinline__ bool attn_block_of(const CacheAttnArgs& a, int size, int item, RowBlock& out) {
-    if (!a.per_seq) return find_block(a.c, a.group, size, item, out);
-    out.seq = item / a.per_seq;
-    out.block = item % a.per_seq;
-    out.rows = seq_rows(a.c, out.seq);
-    out.blocks = (min(out.rows.n, a.c.max_new) * a.group + size - 1) / size;
-    return out.block < out.blocks;
 }
 
 // `total` tiles in equal parts: part p is [begin(p), begin(p + 1)).

@@ -21,6 +21,7 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
     cut.items = block_items(b->seqs, b->rows, max_new, group, cut.size);
     int64_t keys = (int64_t)b->max_pages * c->page_tokens;
+    const bool countable = uniform <= 1024 && uniform * (keys / 32 + 8) < (int64_t)1 << 31;   // tiles; whatever the window, so that it never asks for more workspace
     if (vis.window) {   // what the rows of a block can see at most
         const int64_t span = (int64_t)vis.window + vis.sinks + (vis.block ? vis.block : 0) + kAttnRows;
         keys = keys < span ? keys : span;
@@ -32,10 +33,10 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     // against the 20 us that counting and joining take (12 heads, us without / with: 1280 rows on 34,000 keys 530 / 250, 3840 872 / 799,
     // 4680 985 / 1021; causal prompts of 1280 tokens 31 / 36, of 3840 82 / 106; fp32, 449 rows x 12 heads on 2000 keys 302 / 77).
     const int64_t fit = few ? attn_keys_workers(bf16, c->head_dim) : attn_rows_workers(), groups = uniform * c->kv_heads;
-    const bool share = keys > (few || !bf16 ? 512 : 4096) && uniform * (keys / 32 + 8) < (int64_t)1 << 31 &&
-                       (few ? uniform <= 1024 && groups <= 8 * fit : uniform <= 256 && 5 * groups < 4 * fit);
+    const bool share = keys > (few || !bf16 ? 512 : 4096) && countable &&
+                       (few ? groups <= 8 * fit : uniform <= 256 && 5 * groups < 4 * fit);
     if (share) cut.workers = (int32_t)(fit < c->kv_heads ? c->kv_heads : fit / c->kv_heads * c->kv_heads);
-    if (share || uniform <= cut.items + cut.items / 4) {   // few blocks can be empty: no search for those that are not
+    if (share || blocks_even(uniform, cut.items)) {
         cut.items = uniform;
         cut.per_seq = (int32_t)each;
     }
@@ -73,6 +74,7 @@ extern "C" veda_status veda_cache_attn_fwd(const veda_cache* c, const veda_cache
     st = veda::check_rows(c, b->rows, q_heads, q, sq, false);
     if (st == VEDA_OK) st = veda::check_rows(c, b->rows, q_heads, out, so, true);
     if (st != VEDA_OK) return st;
+    if (q == out) return VEDA_ERR_INVALID_ARG;   // a row may be read after its result has been written
     const veda::AttnCut cut = veda::attn_cut(c, b, q_heads, vis);
     const size_t need = veda::attn_workspace(c, cut);
     if (need > 0) {
@@ -91,8 +93,9 @@ extern "C" veda_status veda_cache_attn_fwd(const veda_cache* c, const veda_cache
     a.scale_log2 = softmax_scale * veda::kLog2e;
     a.part = (float*)workspace;
     const bool bf16 = c->dtype == VEDA_BF16;
-    if (cut.items * c->kv_heads >= (int64_t)1 << 31 || (int64_t)a.c.max_new * a.group >= (int64_t)1 << 30 ||
-        (cut.workers && cut.size < veda::kAttnRows && (int64_t)b->rows * q_heads >= (int64_t)1 << 31))
+    // a grid has less than 2^32 threads: 512 to a workgroup, or to eight rows of a query head
+    if (cut.items * c->kv_heads >= (int64_t)1 << 23 || (int64_t)a.c.max_new * a.group >= (int64_t)1 << 30 ||
+        (cut.workers && cut.size < veda::kAttnRows && (int64_t)b->rows * q_heads >= (int64_t)1 << 26))
         return VEDA_ERR_UNSUPPORTED;
     const hipStream_t s = (hipStream_t)stream;
     return cut.size < veda::kAttnRows ? veda::launch_cache_attn_keys(a, bf16, c->head_dim, s) : veda::launch_cache_attn_rows(a, bf16, c->head_dim, s);

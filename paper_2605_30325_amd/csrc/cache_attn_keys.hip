@@ -383,7 +383,7 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cac
     const KeysLane<kBf16, D> ln(lane);
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * kSlots * T::kSlot;
     RowBlock block;
-    if (!attn_block_of(a, kRows, blockIdx.x / a.c.kv_heads, block)) return;
+    if (!block_of(a.c, a.group, kRows, a.per_seq, blockIdx.x / a.c.kv_heads, block)) return;
     const int head = blockIdx.x % a.c.kv_heads, r0 = block.block * kRows;
     const SeqRows sr = block.rows;
     const int n = min(sr.n, a.c.max_new), r_end = min(n * a.group, r0 + kRows);
@@ -713,7 +713,7 @@ template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheA
     veda_status st = launch_status("veda_cache_attn_fwd");
     if (st != VEDA_OK) return st;
     const int64_t joins = (int64_t)a.c.rows * a.q_heads;
-    if (a.workers / a.c.kv_heads > 8 * a.c.seqs) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 8>), dim3((unsigned)joins), dim3(512), 0, s, a);
+    if (a.workers / a.c.kv_heads > 8 * a.c.seqs && joins < 1 << 23) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 8>), dim3((unsigned)joins), dim3(512), 0, s, a);
     else hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 1>), dim3((unsigned)((joins + 7) / 8)), dim3(512), 0, s, a);
     return launch_status("veda_cache_attn_fwd");
 }

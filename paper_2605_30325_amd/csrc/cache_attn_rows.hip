@@ -624,7 +624,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
 template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnArgs a) {
     extern __shared__ __align__(1024) char smem[];
     RowBlock rb;
-    if (!attn_block_of(a, kAttnRows, blockIdx.x / a.c.kv_heads, rb)) return;
+    if (!block_of(a.c, a.group, kAttnRows, a.per_seq, blockIdx.x / a.c.kv_heads, rb)) return;
     const SeqRows sr = rb.rows;
     const int rows = min(sr.n, a.c.max_new) * a.group;
     const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most

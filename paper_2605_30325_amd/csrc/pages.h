@@ -36,15 +36,13 @@ class PageBook {
         const bool open = tokens > old && old % page_tokens_ != 0;
         const int32_t last = open ? row[have - 1] : -1;
         const bool own = last >= 0 && holders_[(size_t)last] > 1;     // shared: a page of its own, copied
-        const bool gone = open && last < 0;                           // evicted with tokens to come: a new page, nothing to copy
-        if (want - have + own + gone > free_count() || (own && (capacity < 1 || !copies))) return kNoRoom;
-        if (own || gone) {
+        if (open && last < 0) return kBadArg;                         // evicted, then cut open: its first tokens are gone
+        if (want - have + own > free_count() || (own && (capacity < 1 || !copies))) return kNoRoom;
+        if (own) {
             const int32_t p = take();
-            if (own) {
-                copies[0] = last;
-                copies[1] = p;
-                --holders_[(size_t)last];
-            }
+            copies[0] = last;
+            copies[1] = p;
+            --holders_[(size_t)last];
             row[have - 1] = p;
         }
         for (int32_t i = have; i < want; ++i) row[i] = take();

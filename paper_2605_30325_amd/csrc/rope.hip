@@ -150,8 +150,9 @@ extern "C" veda_status veda_rope_apply(const veda_rope* rope, veda_dtype dtype, 
     veda::rope_blocks(tokens, batch, heads, &a.log_tb, &a.hb);
     a.order = veda::row_order(sx.h < sx.n);
     const int64_t head_groups = ((int64_t)heads + a.hb - 1) / a.hb;
-    if (head_groups > 65535 || batch > 65535) return VEDA_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)(((int64_t)tokens + (1 << a.log_tb) - 1) >> a.log_tb), (unsigned)head_groups, (unsigned)batch);
+    const int64_t gx = ((int64_t)tokens + (1 << a.log_tb) - 1) >> a.log_tb;
+    if (gx >= 1 << 24 || head_groups > 65535 || batch > 65535) return VEDA_ERR_UNSUPPORTED;   // a grid has less than 2^32 threads
+    const dim3 grid((unsigned)gx, (unsigned)head_groups, (unsigned)batch);
     const size_t lds = (size_t)a.rope.half * sizeof(float2) << a.log_tb;
     const hipStream_t s = (hipStream_t)stream;
     if (dtype == VEDA_BF16 && chunks) hipLaunchKernelGGL((veda::rope_kernel<uint16_t, true>), grid, dim3(veda::kRopeThreads), lds, s, a);

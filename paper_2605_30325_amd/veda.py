@@ -228,6 +228,10 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # current_stream() makes an object first: 2 us of a call's 12
 
 
+def _stream_of(dev: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -675,6 +679,7 @@ class Rope:
         self.handle = None
         if not 1 <= len(dims) <= 3:
             raise VedaError(VEDA_ERR_INVALID_ARG, "Rope", "axis_dim must name 1 to 3 axes")
+        _ints("Rope", head_dim, *dims)
         cfg = veda_rope_config(head_dim, len(dims), (C.c_int32 * 3)(*dims), pairs, scaling, base, factor, trained_len, beta_fast, beta_slow,
                                amplitude)
         h = C.c_void_p()
@@ -710,9 +715,16 @@ def _need(ok: bool, where: str, what: str):
         _refuse(where, what)
 
 
+def _ints(where: str, *values: int):
+    """ctypes cuts numbers off at 32 bits without a word."""
+    for x in values:
+        if not -(1 << 31) <= x < 1 << 31:
+            _refuse(where, f"{x} does not fit 32 bits")
+
+
 def _on(dev: torch.device, where: str):
     """The kernels run on the current device, so that is where the tensors have to be."""
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+    if dev.type != "cuda" or dev.index != torch._C._cuda_getDevice():
         _refuse(where, f"tensors on {dev}, which is not the current device")
 
 
@@ -720,6 +732,8 @@ def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Opt
     """Rotates x [batch, heads, N, d] by positions i32 [batch or 1, N, axes] (or [N], one axis) into y (x itself: in place).
     transpose=True turns the gradient of the result into the gradient of x."""
     w, dev = "veda_rope_apply", x.device
+    if rope.handle is None:
+        _refuse(w, "the rope is closed")
     if x.dim() != 4 or x.shape[3] != rope.head_dim or (x.stride(3) != 1 and x.numel()):
         _refuse(w, "x must be [batch, heads, N, head_dim] with unit channel stride")
     _on(dev, w)
@@ -738,7 +752,7 @@ def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Opt
     sx, sy = x.stride(), y.stride()
     _check(load().veda_rope_apply(rope.handle, _dtype_code(x.dtype), b, h, n, x.data_ptr(), veda_strides(sx[0], sx[1], sx[2]),
                                   positions.data_ptr(), 0 if positions.shape[0] == 1 else n * rope.axes, int(transpose), y.data_ptr(),
-                                  veda_strides(sy[0], sy[1], sy[2]), _stream()), w)
+                                  veda_strides(sy[0], sy[1], sy[2]), _stream_of(dev)), w)
     return y
 
 
@@ -754,8 +768,9 @@ class Cache:
         inner = (page_tokens * head_dim, head_dim, 1)
         for t in (k, v):
             _need(t is not None and tuple(t.shape) == shape and t.dtype == dtype and t.device == k.device and
-                  all(a == b or n == 1 for n, a, b in zip(shape[1:], t.stride()[1:], inner)) and (pages == 1 or t.stride(0) == k.stride(0)),
-                  "Cache", f"k and v must be {dtype} {list(shape)} with close rows, heads and tokens")
+                  all(a == b or n == 1 for n, a, b in zip(shape[1:], t.stride()[1:], inner)) and
+                  (pages == 1 or t.stride(0) == k.stride(0) >= kv_heads * page_tokens * head_dim),
+                  "Cache", f"k and v must be {dtype} {list(shape)} with close rows, heads and tokens, and pages apart")
         self.k, self.v = k, v
         self.pages, self.page_tokens, self.kv_heads, self.head_dim, self.dtype = int(pages), int(page_tokens), int(kv_heads), int(head_dim), dtype
         stride = k.stride(0) if pages > 1 else 0
@@ -770,8 +785,9 @@ class CacheBatch:
 
     def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor, max_new: int):
         seqs = page_table.shape[0]
-        _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and (page_table.stride(1) == 1 or page_table.shape[1] == 1), "CacheBatch",
-              "page_table must be i32 [seqs, max_pages]")
+        _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and (page_table.stride(1) == 1 or page_table.shape[1] == 1) and
+              (seqs < 2 or page_table.stride(0) >= page_table.shape[1]), "CacheBatch", "page_table must be i32 [seqs, max_pages], a row for each sequence")
+        _ints("CacheBatch", max_new)
         for t, n in ((kv_len, seqs), (q_start, seqs + 1)):
             _need(tuple(t.shape) == (n,) and t.dtype == torch.int32 and t.is_contiguous() and t.device == page_table.device, "CacheBatch",
                   "kv_len and q_start must be contiguous i32 [seqs] and [seqs + 1] where the page table is")
@@ -798,6 +814,8 @@ def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch
     positions i32 [rows, axes]; without them the position in the sequence (ropes of one axis)."""
     w, rows = "veda_cache_append", k.shape[0]
     _on(cache.device, w)
+    if rope is not None and rope.handle is None:    # which the library would take for no rope
+        _refuse(w, "the rope is closed")
     sk, sv = _rows(cache, k, rows, w, "k"), _rows(cache, v, rows, w, "v")
     if k.shape[1] != cache.kv_heads or v.shape[1] != cache.kv_heads:
         _refuse(w, "k and v must have the cache's heads")
@@ -817,7 +835,7 @@ def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch
         _refuse(w, "positions must be contiguous i32 [rows, axes of rope]")
     bs = batch.struct(rows)
     _check(load().veda_cache_append(cache._ref, C.byref(bs), k.data_ptr(), sk, v.data_ptr(), sv, 0 if q is None else q.shape[1], _ptr(q), sq,
-                                    _ptr(q_out), so, None if rope is None else rope.handle, _ptr(positions), _stream()), w)
+                                    _ptr(q_out), so, None if rope is None else rope.handle, _ptr(positions), _stream_of(cache.device)), w)
     return q_out
 
 
@@ -835,6 +853,8 @@ def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softma
     in buffers given, and undefined in buffers made here."""
     w, rows, heads = "veda_cache_attn_fwd", q.shape[0], q.shape[1]
     _on(cache.device, w)
+    if not (0 <= block <= 1 << 30 and 0 <= window <= 1 << 30 and 0 <= sinks <= 1 << 30):
+        _refuse(w, "block, window and sinks must be 0 .. 2^30")
     sq = _rows(cache, q, rows, w, "q")
     if batch.page_table.device != cache.device:
         _refuse(w, "the batch must be where the cache is")
@@ -852,17 +872,22 @@ def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softma
     if workspace is None:
         need = int(lib.veda_cache_attn_workspace_bytes(cache._ref, ref, heads))
         workspace = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
+    elif workspace.device != cache.device or not workspace.is_contiguous():
+        _refuse(w, "the workspace must be contiguous and where the cache is")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.veda_cache_attn_fwd(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, veda_visible(block, window, sinks), out.data_ptr(), so,
-                                   _ptr(lse), _ptr(workspace) or None, nbytes, _stream()), w)
+                                   _ptr(lse), _ptr(workspace) or None, nbytes, _stream_of(cache.device)), w)
     return out, lse
 
 
 def veda_cache_copy_pages(cache: Cache, pairs):
     """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
     _on(cache.device, "veda_cache_copy_pages")
-    p = np.ascontiguousarray(pairs, np.int32).reshape(-1, 2)
-    _check(load().veda_cache_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream()), "veda_cache_copy_pages")
+    p = np.asarray(pairs)
+    if p.dtype != np.int32:
+        _need(p.size == 0 or (p.dtype.kind in "iu" and 0 <= p.min() and p.max() < 1 << 31), "veda_cache_copy_pages", "pairs must be page numbers [n, 2]")
+    p = np.ascontiguousarray(p, np.int32).reshape(-1, 2)
+    _check(load().veda_cache_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream_of(cache.device)), "veda_cache_copy_pages")
 
 
 class Pages:
@@ -872,10 +897,12 @@ class Pages:
     def __init__(self, pages: int, page_tokens: int, max_seqs: int, max_pages: int):
         h = C.c_void_p()
         self.handle = None
+        _ints("Pages", pages, page_tokens, max_seqs, max_pages)
         _check(load().veda_pages_create(pages, page_tokens, max_seqs, max_pages, C.byref(h)), "veda_pages_create")
         self.handle, self.pages, self.page_tokens, self.max_seqs, self.max_pages = h, pages, page_tokens, max_seqs, max_pages
 
     def _copies(self, name: str, capacity: int, *args):
+        _ints(name, *args)
         buf, n = np.empty((capacity, 2), np.int32), C.c_int32()
         _book(getattr(load(), name)(self.handle, *args, buf.ctypes.data_as(C.c_void_p), capacity, C.byref(n)), name)
         return buf[:n.value]
@@ -886,6 +913,7 @@ class Pages:
         return np.ctypeslib.as_array(t, (self.max_seqs, self.max_pages)).copy()
 
     def length(self, seq: int) -> int:
+        _ints("veda_pages_length", seq)
         return int(load().veda_pages_length(self.handle, seq))
 
     def free_count(self) -> int:
@@ -895,12 +923,15 @@ class Pages:
         return self._copies("veda_pages_extend", 1, seq, tokens)
 
     def fork(self, source: int, target: int):
+        _ints("veda_pages_fork", source, target)
         _book(load().veda_pages_fork(self.handle, source, target), "veda_pages_fork")
 
     def truncate(self, seq: int, tokens: int = 0):
+        _ints("veda_pages_truncate", seq, tokens)
         _book(load().veda_pages_truncate(self.handle, seq, tokens), "veda_pages_truncate")
 
     def evict(self, seq: int, first: int, last: int):
+        _ints("veda_pages_evict", seq, first, last)
         _book(load().veda_pages_evict(self.handle, seq, first, last), "veda_pages_evict")
 
     def compact(self) -> np.ndarray:
@@ -928,14 +959,16 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
                          positions: Optional[torch.Tensor] = None, block: int = 1, window: int = 0, sinks: int = 0,
                          buffers: Optional[dict] = None):
     """One attention call of a streaming step: q and k rotated, k and v appended, attention of the new rows over the cache.
-    Returns (out [rows, q_heads, d], buffers); `buffers` (optional dict) is filled on the first call and reused afterwards."""
-    b = {} if buffers is None else buffers
+    Returns (out [rows, q_heads, d], buffers); `buffers` (optional dict) is filled on the first call and reused afterwards, by calls
+    of the same rows, heads and table (a captured call writes to them whenever it is replayed, so they are never exchanged for others)."""
+    w, b = "veda_cache_attention", {} if buffers is None else buffers
+    if "ws" in b and (b["out"].shape != q.shape or b["ws"].numel() < veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])):
+        _refuse(w, "these buffers were made for a call of other sizes")
     if rope is not None:
         b["q"] = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))
     else:
         veda_cache_append(cache, batch, k, v, None, positions)
-    need = veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])
-    if "ws" not in b or b["ws"].numel() < need:
-        b["ws"] = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if "ws" not in b:
+        b["ws"] = torch.empty(veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0]), dtype=torch.uint8, device=q.device)
     b["out"], _ = veda_cache_attn_fwd(cache, batch, q if rope is None else b["q"], softmax_scale, block, window, sinks, b.get("out"), workspace=b["ws"])
     return b["out"], b

@@ -55,7 +55,7 @@ def _append(lib, cache, batch, **more):
 
 def _attend(lib, cache, batch, **more):
     s = veda.veda_strides(0, 128, 512)
-    f = dict(q_heads=4, q=AT, sq=s, scale=0.1, visible=veda.veda_visible(1, 0, 0), out=AT, so=s, lse=None, workspace=AT, workspace_bytes=1 << 30)
+    f = dict(q_heads=4, q=AT, sq=s, scale=0.1, visible=veda.veda_visible(1, 0, 0), out=2 * AT, so=s, lse=None, workspace=AT, workspace_bytes=1 << 30)
     f.update(more)
     return lib.veda_cache_attn_fwd(None if cache is None else C.byref(cache), None if batch is None else C.byref(batch), *f.values(), None)
 
@@ -98,6 +98,7 @@ def test_append_refusals(lib, more, status):
     (dict(visible=veda.veda_visible(-1, 0, 0)), INVALID), (dict(visible=veda.veda_visible(1, -1, 0)), INVALID),
     (dict(visible=veda.veda_visible(1, 0, -1)), INVALID), (dict(visible=veda.veda_visible((1 << 30) + 1, 0, 0)), INVALID),
     (dict(so=veda.veda_strides(0, 128, 120)), INVALID), (dict(sq=veda.veda_strides(0, 128, 516)), UNSUPPORTED), (dict(out=AT + 8), UNSUPPORTED),
+    (dict(out=AT), INVALID),     # where q is
 ])
 def test_attention_refusals(lib, more, status):
     assert _attend(lib, _cache(), _batch(), **more) == status
@@ -116,6 +117,13 @@ def test_attention_workspace_refusals(lib):
         need = lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(many), 4)
         assert need > 0 and _attend(lib, c, many, workspace_bytes=need - 1) == WORKSPACE
     assert lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(_batch(max_pages=8, table_stride=8)), 4) == 0
+
+
+def test_grids_beyond_2_32_threads_are_refused(lib):
+    assert _append(lib, _cache(), _batch(seqs=1, rows=1 << 28, max_new=1 << 28)) == UNSUPPORTED
+    assert _append(lib, _cache(), _batch(seqs=1 << 24, rows=1 << 24, max_new=1)) == UNSUPPORTED
+    assert _attend(lib, _cache(kv_heads=4), _batch(seqs=1 << 21, rows=1 << 21, max_new=1)) == UNSUPPORTED
+    assert _attend(lib, _cache(), _batch(seqs=1, rows=1 << 26, max_new=1, max_pages=4096, table_stride=4096)) == UNSUPPORTED
 
 
 def test_empty_calls_do_nothing(lib):
@@ -188,12 +196,13 @@ class Model:
         free = self.free()
         need = -(-tokens // self.page) - len(row)
         open_page = tokens > self.length[s] and self.length[s] % self.page
-        fresh = open_page and (row[-1] is None or self.held(row[-1]) > 1)
+        if open_page and row[-1] is None:
+            return INVALID
+        fresh = open_page and self.held(row[-1]) > 1
         if need + bool(fresh) > len(free):
-            return None
+            return WORKSPACE
         if fresh:
-            if row[-1] is not None:
-                copies.append((row[-1], free[0]))
+            copies.append((row[-1], free[0]))
             row[-1] = free.pop(0)
         row += free[:need]
         self.rows[s], self.length[s] = row, tokens
@@ -214,11 +223,11 @@ def test_page_book_against_a_model(lib, seed, page):
         if op == "extend":
             tokens = min(width * page, n + rng.choice([0, 1, page - 1, page, 2 * page + 3]))
             want = model.extend(s, tokens)
-            if want is None:
+            if not isinstance(want, list):
                 refused["extend"] += 1
                 with pytest.raises(veda.VedaError) as e:
                     book.extend(s, tokens)
-                assert e.value.status == WORKSPACE and np.array_equal(book.table(), before) and book.length(s) == n
+                assert e.value.status == want and np.array_equal(book.table(), before) and book.length(s) == n
             else:
                 assert [tuple(x) for x in book.extend(s, tokens).tolist()] == want
         elif op == "fork":
@@ -287,6 +296,20 @@ def test_page_book_refusals(lib):
     assert [tuple(x) for x in book.compact().tolist()] == [(2, 1)]
 
 
+def test_a_sequence_cut_inside_an_evicted_page_cannot_grow(lib):
+    book = veda.Pages(8, 16, 1, 4)
+    book.extend(0, 40)
+    book.evict(0, 0, 32)
+    book.truncate(0, 20)
+    before = book.table()
+    with pytest.raises(veda.VedaError) as e:
+        book.extend(0, 21)
+    assert e.value.status == INVALID and np.array_equal(book.table(), before) and book.length(0) == 20
+    assert book.extend(0, 20).size == 0     # as long as it was: nothing to write
+    book.truncate(0, 16)
+    assert book.extend(0, 30).size == 0 and book.table()[0].tolist() == [-1, 0, -1, -1]
+
+
 # ---- the binding --------------------------------------------------------------------------------------------------------
 
 def test_binding_refuses_before_the_library(monkeypatch, lib):
@@ -301,6 +324,17 @@ def test_binding_refuses_before_the_library(monkeypatch, lib):
     for bad in ((table.long(), length, start), (table, length[:1], start), (table, length, start[:2]), (table.T.contiguous().T, length, start)):
         with pytest.raises(veda.VedaError):
             veda.CacheBatch(*bad, 1)
+    with pytest.raises(veda.VedaError, match="a row for each"):      # one row for all of them
+        veda.CacheBatch(table[:1].expand(2, 4), length, start, 1)
+    veda.CacheBatch(table[:1].expand(1, 4), length[:1], start[:2], 1)
+    for many in (1 << 31, 1 << 32, -(1 << 32)):
+        with pytest.raises(veda.VedaError, match="32 bits"):
+            veda.CacheBatch(table, length, start, many)
+    one = torch.zeros(1, 2, 16, 64)
+    with pytest.raises(veda.VedaError, match="pages apart"):         # one page for all of them
+        veda.Cache(4, 16, 2, 64, torch.float32, k=one.expand(4, 2, 16, 64), v=one.expand(4, 2, 16, 64))
+    with pytest.raises(veda.VedaError, match="32 bits"):
+        veda.Pages(4, 16, 1 << 32, 1)
     cache, batch = veda.Cache(4, 16, 2, 64, torch.float32, device="cpu"), veda.CacheBatch(table, length, start, 1)
     x = torch.zeros(3, 2, 64)
     with pytest.raises(veda.VedaError, match="current device"):
@@ -309,3 +343,14 @@ def test_binding_refuses_before_the_library(monkeypatch, lib):
         veda.veda_cache_attn_fwd(cache, batch, x, 0.1)
     with pytest.raises(veda.VedaError, match="current device"):
         veda.veda_cache_copy_pages(cache, [(0, 1)])
+
+
+def test_numbers_are_not_cut_off_at_32_bits(lib):
+    book = veda.Pages(8, 16, 2, 4)
+    book.extend(0, 20)
+    far = 1 << 32
+    for call in (lambda: book.extend(far, 40), lambda: book.extend(0, far + 40), lambda: book.fork(far, 1), lambda: book.fork(0, far + 1),
+                 lambda: book.truncate(far, 0), lambda: book.truncate(0, far), lambda: book.evict(far, 0, 16), lambda: book.length(far)):
+        with pytest.raises(veda.VedaError, match="32 bits"):
+            call()
+    assert book.length(0) == 20 and book.length(1) == 0

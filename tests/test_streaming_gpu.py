@@ -505,6 +505,59 @@ def test_one_attention_call_of_a_step_refuses_positions_without_a_rope():
         veda.veda_cache_attention(t.cache, t.batch, t.q, t.qkv[:, 4:6], t.qkv[:, 6:], 0.125, positions=torch.zeros((t.rows, 1), dtype=torch.int32, device=dev()))
 
 
+def test_buffers_serve_calls_of_one_size():
+    t = Setup([4], [100], 4, 2, 64, BF16, seed=25, tail=0)
+    q, k, v = t.q, t.qkv[:, 4:6], t.qkv[:, 6:]
+    out, b = veda.veda_cache_attention(t.cache, t.batch, q, k, v, 0.125)
+    first, held = out.clone(), dict(b)
+    pools = t.k.clone(), t.v.clone()
+    wide = veda.CacheBatch(torch.nn.functional.pad(t.batch.page_table, (0, 4096), value=-1), t.batch.kv_len, t.batch.q_start, 4)
+    assert veda.veda_cache_attn_workspace_bytes(t.cache, wide, 4, 4) > b["ws"].numel()
+    for batch, rows in ((wide, 4), (t.batch, 3)):
+        with pytest.raises(veda.VedaError, match="other sizes"):
+            veda.veda_cache_attention(t.cache, batch, q[:rows], k[:rows], v[:rows], 0.125, buffers=b)
+    assert all(b[x] is held[x] for x in held) and torch.equal(t.k, pools[0]) and torch.equal(t.v, pools[1])
+    again, _ = veda.veda_cache_attention(t.cache, t.batch, q, k, v, 0.125, buffers=b)
+    assert again is out and torch.equal(again, first)
+
+
+def test_attention_refuses_buffers_and_numbers_that_do_not_fit():
+    t = Setup([4], [600], 4, 2, 64, F32, seed=26)
+    need = veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, 4, t.rows)
+    scratch = torch.empty(max(need, 16) * 2, dtype=torch.uint8)
+    for more in (dict(workspace=scratch), dict(workspace=scratch.to(dev())[::2]), dict(window=(1 << 32) + 5), dict(block=1 << 32), dict(sinks=1 << 40, window=1), dict(out=t.q)):
+        with pytest.raises(veda.VedaError):
+            veda.veda_cache_attn_fwd(t.cache, t.batch, t.q, 0.1, **more)
+    for pairs in (np.asarray([[1 << 32, 0]]), [[0.0, 1.0]], np.asarray([[0, -1]])):
+        with pytest.raises(veda.VedaError):
+            veda.veda_cache_copy_pages(t.cache, pairs)
+
+
+def test_closed_ropes_are_refused():
+    t = Setup([4], [8], 4, 2, 64, F32, seed=27)
+    rope = make_rope(64, (64,), True)
+    rope.close()
+    with pytest.raises(veda.VedaError, match="closed"):      # not: no rope
+        veda.veda_cache_append(t.cache, t.batch, t.qkv[:, 4:6], t.qkv[:, 6:], rope)
+    with pytest.raises(veda.VedaError, match="closed"):
+        veda.veda_rope_apply(rope, t.q[None], torch.zeros((1, 4, 1), dtype=torch.int32, device=dev()))
+
+
+@pytest.mark.parametrize("lens", [[3] * 200, [0, 40, 0, 0, 1, 17] * 30, [300] + [0] * 130])
+def test_append_to_many_sequences(lens):
+    # even and uneven numbers of new rows: blocks of rows found by division and by counting
+    t = Setup(lens, [5] * len(lens), 2, 1, 64, BF16, seed=28)
+    k, v = normal((t.rows, 1, 64), BF16, 1), normal((t.rows, 1, 64), BF16, 2)
+    want_k, want_v = t.k.clone(), t.v.clone()
+    table, start = t.table.tolist(), t.start.tolist()
+    for s, n in enumerate(lens):
+        for i in range(n):
+            page, at = table[s][(5 + i) // t.cache.page_tokens], (5 + i) % t.cache.page_tokens
+            want_k[page, :, at], want_v[page, :, at] = k[start[s] + i], v[start[s] + i]
+    veda.veda_cache_append(t.cache, t.batch, k, v)
+    assert torch.equal(t.k, want_k) and torch.equal(t.v, want_v)
+
+
 # ---- copies of pages ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,d,hk,page", [(BF16, 64, 1, 16), (F32, 128, 3, 64), (BF16, 128, 12, 256)])
