@@ -8,6 +8,7 @@
 // (a large copy: 5.0); a chunk of 4680 x 36 rows into the cache 18 us = 4.8 TB/s.
 #pragma once
 
+#include "store.h"
 #include "veda_internal.h"
 
 struct veda_rope {

@@ -47,13 +47,6 @@ template <> struct Chunk<uint32_t> {  // fp32: 4 channels per 16 bytes
     }
 };
 
-// 16 bytes that no later instruction of the kernel reads: not kept in the die's L2, where they would only push out what is still
-// to be read.
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-__device__ __forceinline__ void store_through(void* p, uint4 v) {
-    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
-}
-
 // Token of slot l of a tile whose slot 0 is token n0 (a real slot).
 __device__ __forceinline__ int token_from(const HeadGeom& g, int n0, int l, int H, int W) {
     const int lw = l & (g.pw - 1), lh = (l >> g.log_pw) & (g.ph - 1), lt = l >> g.log_phw;
