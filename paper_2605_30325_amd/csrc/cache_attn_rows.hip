@@ -17,6 +17,7 @@
 // some do, and as long again as two of them for the set-up and the results.  fp32 (v_mfma_f32_32x32x2_f32): 2464 rows x 12 heads on 2000 keys, causal, 0.35 ms,
 // matrix pipes 73 % busy, 102 TFLOP/s on visible keys of the 154 that a large product reaches.
 #include "cache_attn.h"
+#include "store.h"
 
 namespace veda {
 
@@ -377,7 +378,7 @@ template <bool kBf16, int D> struct AttnShape {
     static constexpr int kKeyTile = kBf16 ? 64 : 32;          // keys of a tile: one segment of loads a wave
     static constexpr int kSlot = 2 * kKeyTile * T::kRowB;     // K tile, V tile
     static constexpr int kOutRowB = T::kRowB + 16;            // a row of the results in LDS
-    static constexpr int kOutB = kAttnRows * (kOutRowB + 4);
+    static constexpr int kOutB = kAttnRows * (kOutRowB + 4 + 8);   // and its lse, and where it goes
     static constexpr int kLds = 2 * kSlot > kOutB ? 2 * kSlot : kOutB;
 };
 
@@ -401,11 +402,11 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     const bool active = w0 < rows;
     const int r = min(w0 + l31, rows - 1);
     AttnRow<kBf16, D> st;
+    const char* q = a.q + (int64_t)(sr.first + r / a.group) * a.sq_n + (int64_t)(head * a.group + r % a.group) * a.sq_h;
     {
         const Seen v = seen_by(a, sr, n, r);
         st.lo = v.lo;
         st.hi = v.hi;
-        const char* q = a.q + (int64_t)(sr.first + r / a.group) * a.sq_n + (int64_t)(head * a.group + r % a.group) * a.sq_h;
         if constexpr (kBf16) {
 #pragma unroll
             for (int t = 0; t < D / 16; ++t) st.qb[t] = *reinterpret_cast<const bf16x8*>(q + 32 * t + 16 * hh);
@@ -606,12 +607,20 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
                 *reinterpret_cast<f32x4v*>(orow + ch * 4) = f32x4v{st.o[nb][4 * j] * inv, st.o[nb][4 * j + 1] * inv, st.o[nb][4 * j + 2] * inv, st.o[nb][4 * j + 3] * inv};
             }
         }
+    char** to = reinterpret_cast<char**>(ml + kAttnRows);
     if (hh == 0) ml[wave * 32 + l31] = attn_lse(st.ref, l);
+    if (tid < r_end - r0) {
+        const int at_row = r0 + tid;
+        to[tid] = a.out + (int64_t)(sr.first + at_row / a.group) * a.so_n + (int64_t)(head * a.group + at_row % a.group) * a.so_h;
+    }
     __syncthreads();
-    for (int i = tid; i < (r_end - r0) * T::kChunks; i += 256) {
-        const int rr = i / T::kChunks, c = i % T::kChunks, at_row = r0 + rr;
-        char* o = a.out + (int64_t)(sr.first + at_row / a.group) * a.so_n + (int64_t)(head * a.group + at_row % a.group) * a.so_h;
-        *reinterpret_cast<uint4*>(o + 16 * c) = *reinterpret_cast<const uint4*>(smem + rr * Sh::kOutRowB + 16 * c);
+    // Past the caches, and rows' places found once each: prompts as above 328 us instead of 336.
+    int me = tid;
+    asm volatile("" : "+v"(me));   // or the sharing kernel keeps what follows from it in registers, from piece to piece
+#pragma unroll
+    for (int j = 0; j < kAttnRows * T::kChunks / 256; ++j) {
+        const int rr = (j * 256 + me) / T::kChunks, c = me % T::kChunks;
+        if (rr < r_end - r0) store_through(to[rr] + 16 * c, *reinterpret_cast<const uint4*>(smem + rr * Sh::kOutRowB + 16 * c));
     }
     if (a.lse && tid < r_end - r0) {
         const int at_row = r0 + tid;
