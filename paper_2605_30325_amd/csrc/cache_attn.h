@@ -79,7 +79,9 @@ struct TileShare {
 // Launches: blocks of 128 rows (cache_attn_rows.hip), and blocks of 16 or 32 (cache_attn_keys.hip); and the workgroups of either that
 // run at once on the card's 256 compute units.
 constexpr int kAttnRows = 128;
-int attn_rows_workers();
+constexpr int kRowsShareItems = 256;   // blocks of rows that can be shared out, at most
+int attn_rows_places();
+int attn_rows_workers(bool bf16);
 veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);
 int attn_keys_workers(bool bf16, int d);
 veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);   // a.part_rows: rows of a block

@@ -630,6 +630,18 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
     if (n == 1) return;   // one workgroup had it all (with W = 8 the same for all waves)
     const float2* ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * D);
     auto part_row = [&](int j) { return (2 * ((int64_t)(w0 + j) * a.c.kv_heads + qh / a.group) + (j == 0 ? 1 : 0)) * kRows + row; };
+    float2 m[4];
+    float x[4][V];
+    auto get = [&](int j0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t at = part_row(min(j0 + W * j, n - 1));
+            m[j] = ml[at];
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[j][c] = a.part[at * D + V * lane + c];
+        }
+    };
+    get(w);   // on their way while the common reference is found
     float ref = -INFINITY;
     for (int j = lane; j < n; j += 64) ref = fmaxf(ref, ml[part_row(j)].x);
 #pragma unroll
@@ -638,15 +650,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
 #pragma unroll
     for (int c = 0; c < V; ++c) o[c] = 0.0f;
     for (int j0 = w; j0 < n; j0 += 4 * W) {
-        float2 m[4];
-        float x[4][V];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t at = part_row(min(j0 + W * j, n - 1));
-            m[j] = ml[at];
-#pragma unroll
-            for (int c = 0; c < V; ++c) x[j][c] = a.part[at * D + V * lane + c];
-        }
+        if (j0 != w) get(j0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (j0 + W * j >= n || m[j].y == 0.0f) continue;

@@ -646,8 +646,10 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_att
 // card at once, all with the same number of tiles, `level`.  Of every block's list the first whole multiples of `level` go to workgroups of
 // their own: piece k of every block walks the same tiles of its head at the same time, out of the dies' L2.  (Pieces that
 // merely lie one behind the other, each beginning where the last one ended, do not: 12 heads of 37 blocks, 444 on 512 places, 1.04 ms instead of
-// 0.90 with a workgroup for each.)  What is left of the lists is laid end to end and shared by the other workgroups.  Every workgroup counts
-// the blocks' tiles itself, 64 at a time.
+// 0.90 with a workgroup for each.)  What is left of the lists is laid end to end and shared by the other workgroups, where every piece counts
+// for kPiece tiles more: what its set-up and its sums' way to the workspace take (fp32, 1057 rows x 12 heads in 28 blocks on 2000 keys, with 0 / 2 / 5:
+// 142 / 117 / 116 us, 449 rows 64 / 64 / 71; bf16, 2560 rows x 12 heads on 34,000 keys with 0 / 1 / 3: 531 / 491 / 492, 3840 rows 729 / 734 /
+// 752).  Every workgroup counts the blocks' tiles itself.
 template <int kTile> __device__ __forceinline__ int rows_tiles_of(const CacheAttnArgs& a, int item) {
     if (item >= a.items) return 0;
     const SeqRows sr = seq_rows(a.c, item / a.per_seq);
@@ -665,32 +667,53 @@ template <int D> __device__ __forceinline__ int4* rows_cuts(const CacheAttnArgs&
 }
 
 template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
-    constexpr int kTile = AttnShape<kBf16, D>::kKeyTile;
+    constexpr int kTile = AttnShape<kBf16, D>::kKeyTile, kPiece = kBf16 ? 1 : 2;
     extern __shared__ __align__(1024) char smem[];
+    auto rest_units = [](int tiles) { return tiles ? tiles + kPiece : 0; };
     const int lane = threadIdx.x & 63, head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads, parts = a.workers / a.c.kv_heads;
     auto sum = [&](int x) { return __builtin_amdgcn_readlane(lanes_up_to(x), 63); };
-    int total = 0, fulls = 0;
-    for (int i0 = 0; i0 < a.items; i0 += 64) total += sum(rows_tiles_of<kTile>(a, i0 + lane));
-    const int level = max(kRowsShareTiles, (total + parts - 1) / parts);
-    for (int i0 = 0; i0 < a.items; i0 += 64) fulls += sum(rows_tiles_of<kTile>(a, i0 + lane) / level);
-    const TileShare rests(total - fulls * level, parts - fulls, 1);
+    int counts[kRowsShareItems / 64];
+    int total = 0;
+#pragma unroll
+    for (int k = 0; k < kRowsShareItems / 64; ++k) {
+        counts[k] = 64 * k < a.items ? rows_tiles_of<kTile>(a, 64 * k + lane) : 0;
+        total += sum(counts[k]);
+    }
+    int level = max(kRowsShareTiles, (total + parts - 1) / parts), fulls, units;
+    for (;; level += (level + 15) / 16) {
+        int f = 0, u = 0;
+#pragma unroll
+        for (int k = 0; k < kRowsShareItems / 64; ++k) {
+            f += counts[k] / level;
+            u += rest_units(counts[k] % level);
+        }
+        fulls = sum(f);
+        units = sum(u);
+        if (fulls + (units + level + kPiece - 1) / (level + kPiece) <= parts) break;
+    }
+    const TileShare rests(units, parts - fulls, 1);
     const bool full = mine < fulls;
     const int q = full ? -1 : mine - fulls;
-    if (!full && (rests.total == 0 || q >= rests.parts)) return;
-    // the block: of the whole multiples, number `mine`; of what is left, the one that tile `now` of it falls into
-    int now = full ? 0 : rests.begin(q), end = full ? 1 : rests.begin(q + 1), item = 0, first_full = 0, first_rest = 0;
-    for (int i0 = 0; i0 < a.items; i0 += 64) {
-        const int count = rows_tiles_of<kTile>(a, i0 + lane), f = count / level, r = count - f * level, up_f = lanes_up_to(f), up_r = lanes_up_to(r);
-        const int all_f = __builtin_amdgcn_readlane(up_f, 63), all_r = __builtin_amdgcn_readlane(up_r, 63);
-        if (full ? mine < first_full + all_f : now < first_rest + all_r) {
-            const int at = __popcll(__ballot(full ? first_full + up_f <= mine : first_rest + up_r <= now));
-            item = i0 + at;
+    if (!full && (units == 0 || q >= rests.parts)) return;
+    // the block: of the whole multiples, number `mine`; of what is left, the one that unit `now` of it falls into
+    int now = full ? 0 : rests.begin(q), item = 0, first_full = 0, first_unit = 0;
+    const int end = full ? 1 : rests.begin(q + 1);
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < kRowsShareItems / 64; ++k) {
+        const int f = counts[k] / level, u = rest_units(counts[k] % level), up_f = lanes_up_to(f), up_u = lanes_up_to(u);
+        const int all_f = __builtin_amdgcn_readlane(up_f, 63), all_u = __builtin_amdgcn_readlane(up_u, 63);
+        if (found) continue;
+        found = full ? mine < first_full + all_f : now < first_unit + all_u;
+        if (found) {
+            const int at = __popcll(__ballot(full ? first_full + up_f <= mine : first_unit + up_u <= now));
+            item = 64 * k + at;
             first_full += __builtin_amdgcn_readlane(up_f, at) - __builtin_amdgcn_readlane(f, at);
-            first_rest += __builtin_amdgcn_readlane(up_r, at) - __builtin_amdgcn_readlane(r, at);
-            break;
+            first_unit += __builtin_amdgcn_readlane(up_u, at) - __builtin_amdgcn_readlane(u, at);
+        } else {
+            first_full += all_f;
+            first_unit += all_u;
         }
-        first_full += all_f;
-        first_rest += all_r;
     }
     for (bool again = false; now < end && item < a.items; ++item) {
         const int seq = item / a.per_seq;
@@ -699,21 +722,22 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_att
         if (r0 >= rows) continue;
         const int r_end = min(rows, r0 + kAttnRows);
         const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, kTile);
-        const int count = max(1, tiles.count), f = count / level, rest = count - f * level;
-        // tiles of this piece, and whether it is the block's first
-        const int t_beg = full ? (mine - first_full) * level : f * level + now - first_rest, t_end = full ? t_beg + level : min(count, t_beg + end - now);
+        const int count = max(1, tiles.count), f = count / level, rest = count - f * level, next_unit = first_unit + rest_units(rest);
+        // tiles of this piece
+        const int t_beg = full ? (mine - first_full) * level : f * level + max(0, now - first_unit - kPiece);
+        const int t_end = full ? t_beg + level : f * level + max(0, min(end, next_unit) - first_unit - kPiece);
         if (t_end > t_beg) {
             const bool whole = t_beg == 0 && t_end == count;
             if (t_beg == 0 && threadIdx.x == 0) {   // whole multiples: how many, from which workgroup on; then the others
-                const int q0 = rest ? rests.owner(first_rest) : 0, q1 = rest ? rests.owner(first_rest + rest - 1) : -1;
+                const int q0 = rest ? rests.owner(first_unit + kPiece) : 0, q1 = rest ? rests.owner(next_unit - 1) : -1;
                 rows_cuts<D>(a)[item * a.c.kv_heads + head] = int4{whole ? 0 : f, first_full, whole ? 0 : q1 - q0 + 1, q0};
             }
             if (again) __syncthreads();   // the last piece's results have left the slots
             rows_piece<kBf16, D>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
             again = true;
         }
-        now += t_end - t_beg;
-        first_rest += rest;
+        now = full ? end : max(now, min(end, next_unit));
+        first_unit = next_unit;
         first_full += f;
     }
 }
@@ -809,8 +833,11 @@ template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs&
     return launch_status("veda_cache_attn_fwd");
 }
 
-// Two to a compute unit, by LDS and registers alike.
-int attn_rows_workers() { return 512; }
+// Two workgroups fit a compute unit, by LDS and registers alike.  bf16 shares among so many: one's products run while the other waits.  fp32
+// products leave no such gaps, and half the workgroups have half the unfinished sums to write and join (12 heads on 4 key heads, d = 128, us
+// with 512 / 256: 449 rows on 2000 keys 72 / 63, on 8300 194 / 195, 129 rows on 3100 56 / 45; bf16, 1280 rows on 34,000 keys 285 / 368).
+int attn_rows_places() { return 512; }
+int attn_rows_workers(bool bf16) { return bf16 ? 512 : 256; }
 
 veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) {
     if (bf16) return d == 128 ? launch_rows<true, 128>(a, s) : launch_rows<true, 64>(a, s);
