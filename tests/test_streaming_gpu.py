@@ -364,6 +364,26 @@ def test_long_caches_are_split(dtype, d, n, hq, hk):
     check_attention(t, block=0)
 
 
+@pytest.mark.parametrize("dtype,heads,new", [(F32, 300, [40]), (F32, 130, [0, 40, 1]), (BF16, 800, [1, 0, 1]), (F32, 800, [1])])
+def test_more_key_heads_than_workgroups_that_share(dtype, heads, new):
+    t = Setup(new, [560] * len(new), heads, heads, 64, dtype, seed=29)
+    assert veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, heads, t.rows) > 0
+    check_attention(t)
+
+
+@pytest.mark.parametrize("new,past,shared", [
+    ([300, 5, 0, 129, 260, 1, 77, 128], [900, 0, 40, 3000, 700, 2100, 1, 513], True), ([128] * 9, [640] * 9, True),
+    ([40] * 30 + [600], [30] * 30 + [2000], True),
+    ([40] * 63 + [600], [30] * 63 + [2000], False),      # 320 blocks, most of them empty: as they are
+])
+def test_uneven_blocks(new, past, shared):
+    # whole multiples, rests of many blocks in one workgroup, blocks that see no more than themselves
+    t = Setup(new, past, 2, 2, 64, F32, seed=30)
+    assert (veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, 2, t.rows) > 0) == shared
+    check_attention(t)
+    check_attention(t, block=64, window=700, sinks=20)
+
+
 def test_pools_beyond_4_gib():
     # 16 KB a page and head: 150,000 pages of each pool are 4.9 GB, and the sequence lies at both ends
     pages, page, hk, d = 150000, 64, 2, 128
