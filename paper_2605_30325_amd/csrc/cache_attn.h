@@ -54,17 +54,20 @@ __device__ __forceinline__ float attn_decode(float code) {
 __device__ __forceinline__ float attn_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ float attn_lse(float ref, float l) { return (ref + __log2f(l)) * kLn2; }
 
-// Tiles of `size` keys that some row of a block sees: [0, first) (tokens that stay visible) and [rest, end), as one list.
+// Tiles of `size` keys that some row of a block sees, as one list: those of the tokens that stay visible, from token 0 on, then those of the
+// window, from its first key on, down to a multiple of 16: no 16 keys lie in two pages, and that is all that the loads ask for (tiles
+// from multiples of their size on: half a tile more, prompts of up to 4096 tokens with a window of 1024 326 us instead of 320, of 256 149 instead of 144).
 struct AttnTiles {
-    int first, rest, count;
-    __device__ __forceinline__ int at(int t) const { return t < first ? t : rest + t - first; }
+    int size, first, rest, count;   // first: tiles of the one kind; rest: where the others begin
+    __device__ __forceinline__ int at(int t) const { return t < first ? t * size : rest + (t - first) * size; }   // its first key
 };
 __device__ __forceinline__ AttnTiles tiles_seen(const CacheAttnArgs& a, const SeqRows& sr, int n, int r_first, int r_last, int size) {
     const int lo = seen_by(a, sr, n, r_first).lo, hi = seen_by(a, sr, n, r_last).hi;   // both grow from row to row
     AttnTiles t;
+    t.size = size;
     t.first = a.window ? (min(a.sinks, hi) + size - 1) / size : 0;
-    t.rest = max(t.first, lo / size);
-    t.count = t.first + max(0, (hi + size - 1) / size - t.rest);
+    t.rest = max(t.first * size, lo & ~15);
+    t.count = t.first + max(0, (hi - t.rest + size - 1) / size);
     return t;
 }
 

@@ -399,7 +399,7 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cac
         there = 0;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
-            there |= (keys_from(a.c, table, mine < tiles.count ? sr.len : 0, head_b, T::kRowB, tiles.at(mine) * 32 + 16 * b, from[b]) ? 1u : 0u) << b;
+            there |= (keys_from(a.c, table, mine < tiles.count ? sr.len : 0, head_b, T::kRowB, tiles.at(mine) + 16 * b, from[b]) ? 1u : 0u) << b;
     };
     auto load = [&](int at, int slot) {
         const int64_t f[2] = {lane_value(from[0], at), lane_value(from[1], at)};
@@ -427,7 +427,7 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cac
             wait_vmcnt<0>();
         }
         asm volatile("" ::: "memory");
-        keys_step<kBf16, D, RB>(a, st, see, ln, lds + slot * T::kSlot, tiles.at(t) * 32, exists);
+        keys_step<kBf16, D, RB>(a, st, see, ln, lds + slot * T::kSlot, tiles.at(t), exists);
         if (kSlots == 1 && more) {
             __builtin_amdgcn_s_waitcnt(0xc07f);
             load(at, 0);
@@ -526,7 +526,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
                 const int32_t* table = a.c.table + ahead.seq * a.c.table_stride;
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
-                    there |= (keys_from(a.c, table, t < ahead.tiles.count ? ahead.sr.len : 0, head_b, T::kRowB, ahead.tiles.at(t) * 32 + 16 * b, from[b]) ? 1u : 0u) << b;
+                    there |= (keys_from(a.c, table, t < ahead.tiles.count ? ahead.sr.len : 0, head_b, T::kRowB, ahead.tiles.at(t) + 16 * b, from[b]) ? 1u : 0u) << b;
             }
             if (last >= min(x + 64, end)) break;
             enter(ahead, ahead.seq + 1, last);
@@ -563,7 +563,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
             else if (asked - now == 2) wait_vmcnt<T::kLoads>();
             else wait_vmcnt<0>();
             asm volatile("" ::: "memory");
-            keys_step<kBf16, D, RB>(a, st, see, ln, lds + slot * T::kSlot, here.tiles.at(now - here.first) * 32, ex[0]);
+            keys_step<kBf16, D, RB>(a, st, see, ln, lds + slot * T::kSlot, here.tiles.at(now - here.first), ex[0]);
             slot = slot + 1 == T::kDepth ? 0 : slot + 1;
 #pragma unroll
             for (int j = 0; j + 1 < T::kDepth; ++j) ex[j] = ex[j + 1];

@@ -13,7 +13,7 @@
 //
 // What bounds it: the matrix cores, and the power they draw.  4680 rows x 12 heads on 34,320 keys, d = 128, bf16: 0.91-0.95 ms from box to box =
 // 1.04-1.09 PFLOP/s (a large matrix product reaches 1.22); matrix pipes 55 % busy at 1.87 GHz, 63 % on the compute units that hold two workgroups
-// (444 on 512 places).  Prompts of 1..4096 tokens, G = 4, window 1024: 0.33 ms = 0.79 PFLOP/s; about 15 tiles of 64 keys that all rows see, four that
+// (444 on 512 places).  Prompts of 1..4096 tokens, G = 4, window 1024: 0.32 ms = 0.81 PFLOP/s; about 15 tiles of 64 keys that all rows see, three that
 // some do, and as long again as two of them for the set-up and the results.  fp32 (v_mfma_f32_32x32x2_f32): 2464 rows x 12 heads on 2000 keys, causal, 0.35 ms,
 // matrix pipes 73 % busy, 102 TFLOP/s on visible keys of the 154 that a large product reaches.
 #include "cache_attn.h"
@@ -437,7 +437,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     int32_t page = 0;                          // of the wave's segment
     uint32_t there = 0;                        // which of the groups exist
     auto look_up = [&](int t) {
-        const int mine = t + lane, tok = tiles.at(mine) * kKeyTile;
+        const int mine = t + lane, tok = tiles.at(mine);
         there = 0;
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
@@ -451,7 +451,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     // asks for the wave's segment of tile t, number `at` of the pages looked up
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
         const int row = wave * T::kSegRows, id = __builtin_amdgcn_readlane(page, at);
-        const int64_t from = id * a.c.page_b + head_b + ((tiles.at(t) * kKeyTile + row) & page_mask) * kRowB;
+        const int64_t from = id * a.c.page_b + head_b + ((tiles.at(t) + row) & page_mask) * kRowB;
         const uint32_t to = lds + slot * Sh::kSlot + row * kRowB;
         uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
 #pragma unroll
@@ -502,7 +502,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     // Tile t has landed in its slot and everyone has read the other one; look-up of the next.
     auto arrive = [&]() __attribute__((always_inline)) {
         exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
-        key0 = tiles.at(t) * kKeyTile;
+        key0 = tiles.at(t);
         more = t + 1 < t_end;
         if (++at == 64 && more) {
             look_up(t + 1);
