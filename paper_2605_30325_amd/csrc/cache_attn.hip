@@ -29,11 +29,13 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     // Shared out evenly where a block can have more keys than a workgroup's least part is worth and the blocks are too few to level out by
     // themselves: in a few rounds of workgroups the last one, or the longest, leaves compute units idle.  Every workgroup then counts
     // through all blocks, 64 at a time: up to 1024 of 16 or 32 rows, which are a sequence each, 256 of 128 rows.  Those are left as they are
-    // where a workgroup for each fills four fifths of a round or comes in several rounds, and in bf16 where a block's walk is not long
-    // against the 20 us that counting and joining take (12 heads, us without / with: 1280 rows on 34,000 keys 530 / 250, 3840 872 / 734,
-    // 4680 985 / 1021; causal prompts of 1280 tokens 31 / 36, of 3840 82 / 106; fp32, 449 rows x 12 heads on 2000 keys 302 / 63).
+    // where a workgroup for each fills four fifths of a round or comes in several rounds, and where a block's walk is not long against
+    // what counting and joining take, 10-20 us and, in bf16, more the more blocks there are (d = 128, us without / with: 256 rows of 4 heads on
+    // 456 keys 16 / 19, 756 21 / 20, 3756 72 / 23, 1024 rows of 12 heads, causal, on 1524 keys 38 / 40, 2524 56 / 44, 2133 rows of 12 on
+    // 3633 keys 72 / 84, 1280 rows on 34,000 530 / 250, 3840 872 / 734, 4680 985 / 1021; fp32, 100 rows of 12 on 160 keys 28 / 30, 200 38 / 30, 300 51 /
+    // 30, 449 rows on 2000 302 / 63).
     const int64_t fit = few ? attn_keys_workers(bf16, c->head_dim) : attn_rows_workers(bf16), groups = uniform * c->kv_heads;
-    const bool share = keys > (few || !bf16 ? 512 : 4096) && countable &&
+    const bool share = keys > (few ? 512 : bf16 ? 512 + 16 * groups : 192) && countable &&
                        (few ? groups <= 8 * fit : uniform <= kRowsShareItems && 5 * groups < 4 * attn_rows_places());
     if (share) cut.workers = (int32_t)(fit < c->kv_heads ? c->kv_heads : fit / c->kv_heads * c->kv_heads);
     if (share || blocks_even(uniform, cut.items)) {
