@@ -21,7 +21,7 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
     cut.items = block_items(b->seqs, b->rows, max_new, group, cut.size);
     int64_t keys = (int64_t)b->max_pages * c->page_tokens;
-    const bool countable = uniform <= 1024 && uniform * (keys / 32 + 8) < (int64_t)1 << 31;   // tiles; whatever the window, so that it never asks for more workspace
+    const bool countable = uniform <= 1024 && uniform * (keys / 16 + 8) < (int64_t)1 << 31;   // tiles; whatever the window, so that it never asks for more workspace
     if (vis.window) {   // what the rows of a block can see at most
         const int64_t span = (int64_t)vis.window + vis.sinks + (vis.block ? vis.block : 0) + kAttnRows;
         keys = keys < span ? keys : span;

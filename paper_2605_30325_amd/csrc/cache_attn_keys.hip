@@ -4,7 +4,7 @@
 // common reference.  Memory bounds it: every key and value is read once for at most 32 rows, so the work is to keep loads in flight on
 // all compute units until the last of them is done.  The query heads that share a key head are put together as in cache_attn_rows.hip, 16
 // rows to a product of 16 x 16 (K rows x query rows, and V channels x query rows): with 32 x 32 products, half or more of them padding, fp32
-// tokens waited for the matrix cores (257 keys, 12 heads of 64: 18.6 us instead of 12.3).  A wave walks key tiles of its own, 32 keys each, that direct
+// tokens waited for the matrix cores (257 keys, 12 heads of 64: 18.6 us instead of 12.3).  A wave walks key tiles of its own, 16 or 32 keys, that direct
 // loads put into its slots of LDS: no barrier in the loop, the compiler's waits only for what the wave itself has read.
 //
 // Long caches are shared out evenly.  The tiles of all sequences lie in one row of numbers; each of the waves that run at once takes one key
@@ -23,11 +23,15 @@ template <bool kBf16, int D> struct KeysTile {
     static constexpr int kRowB = D * (kBf16 ? 2 : 4), kChunks = kRowB / 16;
     static constexpr int kSegRows = kBf16 ? 16 : 8;               // rows of a group of loads: never across a page's end
     static constexpr int kSegLoads = kSegRows * kRowB / 1024;     // 1 KB each
-    static constexpr int kSegs = 32 / kSegRows;
-    static constexpr int kSlot = 64 * kRowB;                      // 32 rows of K, 32 rows of V
+    // Keys of a tile: as many as leave a compute unit's LDS room for three waves with three slots each (fp32, d = 128, with 32 / 16 keys, us:
+    // 64 caches of 4096 keys of 8 heads 505 / 445, 33 of up to 2095 of 7 heads 71 / 58, one of 257 of 12 heads, by eight waves, 14.4 / 11.7).
+    static constexpr int kKeys = kBf16 || D == 64 ? 32 : 16;
+    static constexpr int kGroups = kKeys / 16;
+    static constexpr int kSegs = kKeys / kSegRows;
+    static constexpr int kSlot = 2 * kKeys * kRowB;               // rows of K, rows of V
     static constexpr int kOutRowB = D * 4 + 16;                   // a row of the sums in LDS
     static constexpr int kLoads = 2 * kSegs * kSegLoads;          // of a tile
-    static constexpr int kDepth = kLoads <= 16 ? 3 : 2;           // slots of a wave that shares: loads run kDepth - 1 tiles ahead
+    static constexpr int kDepth = 3;                              // slots of a wave that shares: loads run two tiles ahead
     // 16-byte chunk c of row r lies at chunk c ^ swizzle: operand reads of a wave then fall into different banks.
     __device__ static int k_swizzle(int r) { return kBf16 ? (D == 128 ? r & 15 : (r >> 1) & 7) : r & 7; }
     __device__ static int v_swizzle(int r) { return kBf16 ? (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1) : ((r >> 2) & 3) << 2; }
@@ -58,16 +62,18 @@ template <int D> __device__ __forceinline__ float keys_v32(uint32_t v, int c, in
     return *(lds_f32_ptr)(uintptr_t)((v ^ (uint32_t)(c << 6)) + (16 * b + i) * (D * 4));
 }
 
-// 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit b = keys 16 b .. 16 b + 15 exist.
+// A tile of keys from key0 on for one wave.  full: every row sees all of them.  exists: bit b = keys 16 b .. 16 b + 15 exist.
 template <bool kBf16, int D, int RB>
 __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16, D, RB>& st, uint32_t k, uint32_t v, int key0, uint32_t exists,
                                           bool full, int g) {
-    constexpr int kRowB = KeysTile<kBf16, D>::kRowB, C = D / 16;
-    f32x4v s[RB][2];
+    constexpr int kRowB = KeysTile<kBf16, D>::kRowB, C = D / 16, B = KeysTile<kBf16, D>::kGroups;
+    f32x4v s[RB][B];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb][0] = s[rb][1] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < B; ++b) s[rb][b] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
         if constexpr (kBf16) {
 #pragma unroll
             for (int t = 0; t < D / 32; ++t) {
@@ -92,7 +98,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
     for (int rb = 0; rb < RB; ++rb) {
         if (!full) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < B; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = key0 + 16 * b + 4 * g + i;
@@ -100,9 +106,11 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
                     s[rb][b][i] = seen ? s[rb][b][i] : -INFINITY;
                 }
         }
-        float m = fmaxf(s[rb][0][0], s[rb][1][0]);
+        float m = s[rb][0][0];
 #pragma unroll
-        for (int i = 1; i < 4; ++i) m = fmaxf(m, fmaxf(s[rb][0][i], s[rb][1][i]));
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = fmaxf(m, s[rb][b][i]);
         mx[rb] = m * a.scale_log2;
         grown = grown || mx[rb] > st.ref[rb] + kAttnSlack;
     }
@@ -125,7 +133,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
     for (int rb = 0; rb < RB; ++rb) {
         float sum = 0.0f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[rb][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][b][i], a.scale_log2, st.sub[rb]));
@@ -146,7 +154,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
             for (int c = 0; c < C; ++c) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys_v<D>(v, c), zero, z, 0, 0, 0);
         } else {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < B; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -164,7 +172,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
             }
         } else {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < B; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -197,7 +205,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
                 }
             } else {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < B; ++b)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float x = keys_v32<D>(v, c, b, i), y = attn_code(x);
@@ -234,19 +242,19 @@ template <bool kBf16> __device__ __forceinline__ void keys_store(char* dst, f32x
 }
 
 // Tiles of a sequence in the common row (one that has rows but sees nothing counts as one).
-__device__ __forceinline__ int keys_tiles_of(const CacheAttnArgs& a, int s) {
+__device__ __forceinline__ int keys_tiles_of(const CacheAttnArgs& a, int s, int size) {
     const SeqRows sr = seq_rows(a.c, s);
     const int n = min(sr.n, a.c.max_new);
-    return n == 0 ? 0 : max(1, tiles_seen(a, sr, n, 0, n * a.group - 1, 32).count);
+    return n == 0 ? 0 : max(1, tiles_seen(a, sr, n, 0, n * a.group - 1, size).count);
 }
 constexpr int kShareTiles = 8;    // least part of a workgroup: shorter ones are over before their set-up is paid for
 // The first 64 sequences' tiles by lane, and the sum over all.
 struct KeysCount {
-    int mine, up_to, total;
-    __device__ __forceinline__ explicit KeysCount(const CacheAttnArgs& a) : total(0) {
+    int size, mine, up_to, total;
+    __device__ __forceinline__ KeysCount(const CacheAttnArgs& a, int size_) : size(size_), total(0) {
         for (int s0 = (a.c.seqs - 1) & ~63; s0 >= 0; s0 -= 64) {
             const int s = s0 + (threadIdx.x & 63);
-            mine = s < a.c.seqs ? keys_tiles_of(a, s) : 0;
+            mine = s < a.c.seqs ? keys_tiles_of(a, s, size) : 0;
             up_to = lanes_up_to(mine);
             total += __builtin_amdgcn_readlane(up_to, 63);
         }
@@ -259,7 +267,7 @@ __device__ __forceinline__ void keys_find(const CacheAttnArgs& a, const KeysCoun
     for (int s0 = 0; s0 < a.c.seqs; s0 += 64) {
         if (s0) {
             const int s = s0 + (threadIdx.x & 63);
-            mine = s < a.c.seqs ? keys_tiles_of(a, s) : 0;
+            mine = s < a.c.seqs ? keys_tiles_of(a, s, count.size) : 0;
             up_to = lanes_up_to(mine);
         }
         const int here = __builtin_amdgcn_readlane(up_to, 63);
@@ -292,10 +300,10 @@ template <bool kBf16, int D> struct KeysLane {
         } else {
             v_at = (uint32_t)(4 * g * T::kRowB + 4 * l15 + (g << 6));
         }
-        v_at += 32 * T::kRowB;
+        v_at += T::kKeys * T::kRowB;
     }
     // Asks for a tile: from[b] is where its 16 keys number b begin in either pool.
-    __device__ __forceinline__ void load(const CacheArgs& c, const int64_t (&from)[2], uint32_t lds) const {
+    __device__ __forceinline__ void load(const CacheArgs& c, const int64_t (&from)[T::kGroups], uint32_t lds) const {
 #pragma unroll
         for (int sg = 0; sg < T::kSegs; ++sg) {
             const int row = sg * T::kSegRows;
@@ -307,7 +315,7 @@ template <bool kBf16, int D> struct KeysLane {
                 v[j] = v_off ^ T::v_step(sg, j);
             }
             dma16_group_to_lds<T::kSegLoads>(lds + row * T::kRowB, c.k + at, k);
-            dma16_group_to_lds<T::kSegLoads>(lds + (32 + row) * T::kRowB, c.v + at, v);
+            dma16_group_to_lds<T::kSegLoads>(lds + (T::kKeys + row) * T::kRowB, c.v + at, v);
         }
     }
 };
@@ -355,8 +363,10 @@ __device__ __forceinline__ bool keys_from(const CacheArgs& c, const int32_t* tab
 template <bool kBf16, int D, int RB>
 __device__ __forceinline__ void keys_step(const CacheAttnArgs& a, KeysRow<kBf16, D, RB>& st, const KeysSeen& see, const KeysLane<kBf16, D>& ln, uint32_t lds,
                                           int key0, uint32_t exists) {
-    if (key0 >= see.hi || (key0 + 32 <= see.lo && key0 >= a.sinks) || exists == 0) return;
-    const bool full = key0 + 32 <= see.hi_all && (key0 >= see.lo_all || key0 + 32 <= a.sinks) && exists == 3u;
+    typedef KeysTile<kBf16, D> T;
+    const int end = key0 + T::kKeys;
+    if (key0 >= see.hi || (end <= see.lo && key0 >= a.sinks) || exists == 0) return;
+    const bool full = end <= see.hi_all && (key0 >= see.lo_all || end <= a.sinks) && exists == (1u << T::kGroups) - 1;
     keys_tile<kBf16, D, RB>(a, st, lds + ln.k_at, lds + ln.v_at, key0, exists, full, ln.g);
 }
 
@@ -367,17 +377,17 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
 }
 
 // Short caches: a workgroup for each (block of rows, key head), whose waves take its tiles in turn.  With few workgroups latency counts:
-// eight waves (fp32, d = 128: four) with a slot each, so that all of a cache of 256 keys, half of one of 512, is asked for at once.  With
+// eight waves (32 fp32 rows of 128: four, or their registers do not do) with a slot each, so that all of a cache of 256 keys, half of one of 512, is asked for at once.  With
 // more than there are compute units two waves with two slots, so that workgroups start while others end.  Two waves / eight, us: one
 // fp32 token over 257 keys, 12 heads of 64, 12.3 / 9.1; bf16, d = 128, 64 workgroups of 501 keys 12.4 / 10.4, 512 of 401 21.3 / 25, 4096
 // of 101 54 / 88; fp32, d = 64, 768 of 401 44 / 40.
-template <bool kBf16, int D, bool kMany> struct KeysGroup {
-    static constexpr int kWaves = kMany ? 2 : kBf16 || D == 64 ? 8 : 4, kSlots = kMany ? 2 : 1;
+template <bool kBf16, int D, int RB, bool kMany> struct KeysGroup {
+    static constexpr int kWaves = kMany ? 2 : kBf16 || D == 64 || RB == 1 ? 8 : 4, kSlots = kMany ? 2 : 1;
 };
 template <bool kBf16, int D, int RB, bool kMany>
-__global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cache_attn_keys_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__((64 * KeysGroup<kBf16, D, RB, kMany>::kWaves)) void cache_attn_keys_kernel(CacheAttnArgs a) {
     typedef KeysTile<kBf16, D> T;
-    constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4, kWaves = KeysGroup<kBf16, D, kMany>::kWaves, kSlots = KeysGroup<kBf16, D, kMany>::kSlots;
+    constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4, kWaves = KeysGroup<kBf16, D, RB, kMany>::kWaves, kSlots = KeysGroup<kBf16, D, RB, kMany>::kSlots;
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KeysLane<kBf16, D> ln(lane);
@@ -387,22 +397,24 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, kMany>::kWaves)) void cac
     const int head = blockIdx.x % a.c.kv_heads, r0 = block.block * kRows;
     const SeqRows sr = block.rows;
     const int n = min(sr.n, a.c.max_new), r_end = min(n * a.group, r0 + kRows);
-    const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, 32);
+    const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, T::kKeys);
     const int32_t* table = a.c.table + block.seq * a.c.table_stride;
     const int64_t head_b = (int64_t)head * T::kRowB << a.c.log_page;
 
     // Places of the wave's next 64 tiles, one tile a lane: looked up together, so that no step waits for the table.
-    int64_t from[2] = {0, 0};
+    int64_t from[T::kGroups] = {};
     uint32_t there = 0;
     auto look_up = [&](int t) {
         const int mine = t + lane * kWaves;
         there = 0;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < T::kGroups; ++b)
             there |= (keys_from(a.c, table, mine < tiles.count ? sr.len : 0, head_b, T::kRowB, tiles.at(mine) + 16 * b, from[b]) ? 1u : 0u) << b;
     };
     auto load = [&](int at, int slot) {
-        const int64_t f[2] = {lane_value(from[0], at), lane_value(from[1], at)};
+        int64_t f[T::kGroups];
+#pragma unroll
+        for (int b = 0; b < T::kGroups; ++b) f[b] = lane_value(from[b], at);
         ln.load(a.c, f, lds + slot * T::kSlot);
     };
     int slot = 0, at = 0;
@@ -482,7 +494,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
     const int lane = threadIdx.x;
     const KeysLane<kBf16, D> ln(lane);
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const KeysCount count(a);
+    const KeysCount count(a, T::kKeys);
     const TileShare share(count.total, a.workers / a.c.kv_heads, kShareTiles);
     const int head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads;
     if (mine >= share.parts || share.total == 0) return;
@@ -502,7 +514,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
             p.sr = seq_rows(a.c, p.seq);
             const int n = min(p.sr.n, a.c.max_new);
             if (n == 0) continue;
-            p.tiles = tiles_seen(a, p.sr, n, 0, n * a.group - 1, 32);
+            p.tiles = tiles_seen(a, p.sr, n, 0, n * a.group - 1, T::kKeys);
             p.each = max(1, p.tiles.count);
             return;
         }
@@ -515,7 +527,9 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
     }
     ahead = here;
     // Places of the next 64 tiles, one tile a lane, whichever sequences they belong to.
-    int64_t from[2] = {head_b, head_b};
+    int64_t from[T::kGroups];
+#pragma unroll
+    for (int b = 0; b < T::kGroups; ++b) from[b] = head_b;
     uint32_t there = 0;
     auto look_up = [&](int x) {
         const int at = x + lane;
@@ -525,7 +539,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
             if (t >= 0 && at < last && at < end) {
                 const int32_t* table = a.c.table + ahead.seq * a.c.table_stride;
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < T::kGroups; ++b)
                     there |= (keys_from(a.c, table, t < ahead.tiles.count ? ahead.sr.len : 0, head_b, T::kRowB, ahead.tiles.at(t) + 16 * b, from[b]) ? 1u : 0u) << b;
             }
             if (last >= min(x + 64, end)) break;
@@ -541,7 +555,9 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
             look_up(asked);
             at = 0;
         }
-        const int64_t f[2] = {lane_value(from[0], at), lane_value(from[1], at)};
+        int64_t f[T::kGroups];
+#pragma unroll
+        for (int b = 0; b < T::kGroups; ++b) f[b] = lane_value(from[b], at);
         e = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
         ln.load(a.c, f, lds + ask_slot * T::kSlot);
         ask_slot = ask_slot + 1 == T::kDepth ? 0 : ask_slot + 1;
@@ -559,7 +575,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
         for (; now < stop; ++now) {
             __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the slot to fill has been read
             ask(ex[T::kDepth - 1]);
-            if (T::kDepth == 3 && asked - now == 3) wait_vmcnt<(T::kDepth - 1) * T::kLoads & 63>();
+            if (asked - now == 3) wait_vmcnt<2 * T::kLoads>();
             else if (asked - now == 2) wait_vmcnt<T::kLoads>();
             else wait_vmcnt<0>();
             asm volatile("" ::: "memory");
@@ -611,7 +627,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
         const int s = s0 + lane;
         int mine = 0, i = -1;
         if (s < a.c.seqs) {
-            mine = keys_tiles_of(a, s);
+            mine = keys_tiles_of(a, s, KeysTile<kBf16, D>::kKeys);
             const SeqRows sr = seq_rows(a.c, s);
             if (token >= sr.first && token - sr.first < min(sr.n, a.c.max_new)) i = token - sr.first;
         }
@@ -696,7 +712,7 @@ int attn_keys_workers(bool bf16, int d) {
 }
 
 template <bool kBf16, int D, int RB, bool kMany> static veda_status launch_short(const CacheAttnArgs& a, hipStream_t s) {
-    typedef KeysGroup<kBf16, D, kMany> G;
+    typedef KeysGroup<kBf16, D, RB, kMany> G;
     constexpr int kSums = G::kWaves * 16 * RB * (KeysTile<kBf16, D>::kOutRowB + 8), kTiles = G::kWaves * G::kSlots * KeysTile<kBf16, D>::kSlot;
     constexpr int kLds = kTiles > kSums ? kTiles : kSums;
     static_assert(kLds <= 160 * 1024, "what a compute unit has");
