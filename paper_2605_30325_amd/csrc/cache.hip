@@ -167,6 +167,7 @@ extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_b
     a.q_heads = q_heads; a.head_dim = c->head_dim;
     const bool chunks = veda::rope_in_chunks(a.rope, chunk);
     a.units = veda::rope_units(a.rope, c->head_dim, chunk, chunks);
+    a.rope.through = veda::rope_whole_lines(a.rope, c->head_dim, es);
     veda::rope_blocks(a.c.max_new, b->seqs, heads, &a.log_tb, &a.hb);
     a.order = veda::row_order(sk.h < sk.n);
     const int64_t each = ((int64_t)a.c.max_new + (1 << a.log_tb) - 1) >> a.log_tb, uniform = b->seqs * each, gy = (heads + a.hb - 1) / a.hb;

@@ -147,6 +147,7 @@ extern "C" veda_status veda_rope_apply(const veda_rope* rope, veda_dtype dtype, 
     const int chunk = 16 / es;
     const bool chunks = veda::rope_in_chunks(a.rope, chunk);
     a.units = veda::rope_units(a.rope, d, chunk, chunks);
+    a.rope.through = veda::rope_whole_lines(a.rope, d, es);
     veda::rope_blocks(tokens, batch, heads, &a.log_tb, &a.hb);
     a.order = veda::row_order(sx.h < sx.n);
     const int64_t head_groups = ((int64_t)heads + a.hb - 1) / a.hb;
