@@ -16,6 +16,7 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     AttnCut cut{};
     const int64_t max_new = b->max_new < b->rows ? b->max_new : b->rows, group = q_heads / c->kv_heads, rows = max_new * group;
     const bool bf16 = c->dtype == VEDA_BF16, few = rows <= 32;
+    const int d = c->head_dim;
     cut.size = rows <= 16 ? 16 : rows <= 32 ? 32 : kAttnRows;
     cut.part_rows = few ? cut.size : rows < kAttnRows ? (int32_t)rows : kAttnRows;
     const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
@@ -35,7 +36,14 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     // 3633 keys 72 / 84, 1280 rows on 34,000 530 / 250, 3840 872 / 734, 4680 985 / 1021; fp32, 100 rows of 12 on 160 keys 28 / 30, 200 38 / 30, 300 51 /
     // 30, 449 rows on 2000 302 / 63).
     const int64_t fit = few ? attn_keys_workers(bf16, c->head_dim) : attn_rows_workers(bf16), groups = uniform * c->kv_heads;
-    const bool share = keys > (few ? 512 : bf16 ? 512 + 16 * groups : 192) && countable &&
+    // Few rows: long walks wait for memory, so eight waves a workgroup go through short caches about as fast as all that the card can hold, and
+    // the joining is saved; in fp32, where products take longer, the more so the more workgroups there are (single tokens of 4 query heads a key
+    // head, d = 128, us without / with: bf16, one cache of 6 heads, 700 keys 11 / 17, 2500 16 / 17, 4000 23 / 17; 32 ragged ones of 8 heads
+    // up to 2500 27 / 36; 64, by two waves, up to 1000 28 / 33, 2500 68 / 63; fp32, one of 6 heads, 700 keys 20 / 24, 1500 35 / 24, 32 of 8 up to
+    // 1500 42 / 47; d = 64, one of 6 heads 1500 21 / 23, 2500 30 / 23).
+    const int64_t grown = (d == 64 ? 1536 : 768) + 8 * groups;
+    const int64_t short_few = bf16 ? (groups <= 256 ? 2560 : 1536) : grown < 4096 ? grown : 4096;
+    const bool share = keys > (few ? short_few : bf16 ? 512 + 16 * groups : 192) && countable &&
                        (few ? groups <= 8 * fit : uniform <= kRowsShareItems && 5 * groups < 4 * attn_rows_places());
     if (share) cut.workers = (int32_t)(fit < c->kv_heads ? c->kv_heads : fit / c->kv_heads * c->kv_heads);
     if (share || blocks_even(uniform, cut.items)) {

@@ -365,10 +365,23 @@ def test_long_caches_are_split(dtype, d, n, hq, hk):
 
 
 @pytest.mark.parametrize("dtype,heads,new", [(F32, 300, [40]), (F32, 130, [0, 40, 1]), (BF16, 800, [1, 0, 1]), (F32, 800, [1])])
-def test_more_key_heads_than_workgroups_that_share(dtype, heads, new):
+def test_many_key_heads(dtype, heads, new):
+    # 300: more than workgroups that share; single tokens: a workgroup for each
     t = Setup(new, [560] * len(new), heads, heads, 64, dtype, seed=29)
-    assert veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, heads, t.rows) > 0
+    assert (veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, heads, t.rows) > 0) == (max(new) > 32)
     check_attention(t)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("seqs,far", [(70, 0), (130, 100), (65, 64)])
+def test_many_sequences_shared(dtype, d, seqs, far):
+    # counted 64 at a time; one long sequence, at the beginning, in the middle or at the end
+    past = [(37 * i) % 90 for i in range(seqs)]
+    past[far] = 6000
+    t = Setup([i % 3 for i in range(seqs)], past, 4, 2, d, dtype, seed=31)
+    assert veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, 4, t.rows) > 0
+    check_attention(t)
+    check_attention(t, window=4500, sinks=10)
 
 
 @pytest.mark.parametrize("new,past,shared", [
