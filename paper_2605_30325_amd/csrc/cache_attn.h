@@ -16,7 +16,7 @@ struct CacheAttnArgs {
     int64_t items;                    // blocks of rows of one key head, at most
     int32_t per_seq;                  // see block_of
     int32_t workers;                  // workgroups that share all keys evenly, or 0: one for each block of rows and key head
-    int32_t part_rows;                // rows of a block's unfinished sums in the workspace
+    int32_t part_rows;                // rows of a block's unfinished sums in the workspace, even
     int32_t block, window, sinks;
     float scale_log2;                 // softmax_scale * log2(e)
     float* part;                      // unfinished sums, and their references and l (see the kernels)

@@ -18,7 +18,8 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
     const bool bf16 = c->dtype == VEDA_BF16, few = rows <= 32;
     const int d = c->head_dim;
     cut.size = rows <= 16 ? 16 : rows <= 32 ? 32 : kAttnRows;
-    cut.part_rows = few ? cut.size : rows < kAttnRows ? (int32_t)rows : kAttnRows;
+    // Even, so that the sums of a block, part_rows * (d + 2) floats, are whole 16 bytes: the list of cuts behind them is read 16 bytes at a time.
+    cut.part_rows = few ? cut.size : rows < kAttnRows ? (int32_t)(rows + 1) & ~1 : kAttnRows;
     const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
     cut.items = block_items(b->seqs, b->rows, max_new, group, cut.size);
     int64_t keys = (int64_t)b->max_pages * c->page_tokens;

@@ -119,6 +119,22 @@ def test_attention_workspace_refusals(lib):
     assert lib.veda_cache_attn_workspace_bytes(C.byref(c), C.byref(_batch(max_pages=8, table_stride=8)), 4) == 0
 
 
+@pytest.mark.parametrize("dtype", [veda.VEDA_F32, veda.VEDA_BF16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_workspaces_hold_whole_16_bytes(lib, dtype, d):
+    # sums of odd numbers of rows and key heads come before a list that is read 16 bytes at a time: what lies before it, and so the whole,
+    # has to be a multiple of 16
+    shared = 0
+    for kv_heads in range(1, 13):
+        for rows in range(33, 128):
+            for seqs in (1, 3):
+                b = _batch(seqs=seqs, rows=seqs * rows, max_new=rows, max_pages=4096, table_stride=4096)
+                need = lib.veda_cache_attn_workspace_bytes(C.byref(_cache(kv_heads=kv_heads, dtype=dtype, head_dim=d)), C.byref(b), kv_heads)
+                shared += need > 0
+                assert need % 16 == 0, (kv_heads, rows, seqs)
+    assert shared > 1000
+
+
 def test_grids_beyond_2_32_threads_are_refused(lib):
     assert _append(lib, _cache(), _batch(seqs=1, rows=1 << 28, max_new=1 << 28)) == UNSUPPORTED
     assert _append(lib, _cache(), _batch(seqs=1 << 24, rows=1 << 24, max_new=1)) == UNSUPPORTED

@@ -397,6 +397,16 @@ def test_uneven_blocks(new, past, shared):
     check_attention(t, block=64, window=700, sinks=20)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows,seqs", [(33, 1), (35, 3), (127, 1)])
+def test_odd_numbers_of_rows_shared(dtype, d, rows, seqs):
+    # odd numbers of rows, key heads and sequences: what is written behind the unfinished sums keeps its alignment
+    t = Setup([rows] * seqs, [1500] * seqs, 1, 1, d, dtype, page=64, seed=32)
+    assert veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, 1, t.rows) > 0
+    check_attention(t)
+    check_attention(t, window=900, sinks=5)
+
+
 def test_pools_beyond_4_gib():
     # 16 KB a page and head: 150,000 pages of each pool are 4.9 GB, and the sequence lies at both ends
     pages, page, hk, d = 150000, 64, 2, 128
