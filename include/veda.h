@@ -374,7 +374,9 @@ veda_status veda_output_sqerr(const veda_plan*, const void* a, veda_strides sa, 
 /* ---- streaming generation: rotary positions, and a paged cache of earlier chunks' keys and values ------------------
  * A generator that makes a clip chunk by chunk rotates the newest chunk's Q and K, appends K and V to a cache and attends to
  * that cache.  These calls take the conventions above (device buffers and workspaces are the caller's, only kernels are
- * enqueued, equal inputs give equal bytes); head_dim in {64, 128} for the cache, f32 and bf16. */
+ * enqueued, equal inputs give equal bytes); head_dim in {64, 128} for the cache, f32 and bf16.  Rows that a call writes through strides
+ * (y, q_out, out) must not have elements in common: such strides are refused (VEDA_ERR_INVALID_ARG; VEDA_ERR_UNSUPPORTED where no axis order
+ * nests and there are too many rows to tell). */
 
 /* Rotary positions: pair p of a row's channels, of axis a, is turned by the angle position[a] * freq[p]:
  *   y0 = A (x0 cos - x1 sin),  y1 = A (x0 sin + x1 cos).

@@ -17,7 +17,7 @@ struct CacheArgs {
 veda_status check_cache(const veda_cache* c);
 veda_status check_batch(const veda_cache* c, const veda_cache_batch* b);   // after check_cache
 CacheArgs cache_args(const veda_cache* c, const veda_cache_batch* b);
-// A tensor of rows [rows][heads][head_dim] in the caller's memory: aligned, strides of 16 bytes, and (distinct) no two rows the same bytes.
+// A tensor of rows [rows][heads][head_dim] in the caller's memory: aligned, strides of 16 bytes, and (distinct) no two rows with a byte in common.
 // An axis of one entry has no stride, whatever it is given as: s.n or s.h becomes 0.
 veda_status check_rows(const veda_cache* c, int32_t rows, int32_t heads, const void* p, veda_strides& s, bool distinct);
 

@@ -1,6 +1,7 @@
 // The paged cache: checks, appending the newest rows, copies of pages.
 #include "cache.h"
 #include "rope_rows.h"
+#include "rows_apart.h"
 
 namespace veda {
 
@@ -44,7 +45,10 @@ veda_status check_rows(const veda_cache* c, int32_t rows, int32_t heads, const v
     if (rows == 1) s.n = 0;
     if (heads == 1) s.h = 0;
     if (!p || s.h < 0 || s.n < 0) return VEDA_ERR_INVALID_ARG;
-    if (distinct && ((rows > 1 && s.n < d) || (heads > 1 && s.h < d))) return VEDA_ERR_INVALID_ARG;
+    if (distinct) {
+        const RowsApart apart = rows_apart({rows, s.n}, {heads, s.h}, {1, 0}, d);
+        if (apart != RowsApart::kApart) return apart == RowsApart::kShare ? VEDA_ERR_INVALID_ARG : VEDA_ERR_UNSUPPORTED;
+    }
     if (!aligned16(p) || (s.h * es) % 16 || (s.n * es) % 16) return VEDA_ERR_UNSUPPORTED;
     return VEDA_OK;
 }

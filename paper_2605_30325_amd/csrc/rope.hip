@@ -3,6 +3,7 @@
 #include <new>
 
 #include "rope_rows.h"
+#include "rows_apart.h"
 
 namespace veda {
 
@@ -128,8 +129,8 @@ extern "C" veda_status veda_rope_apply(const veda_rope* rope, veda_dtype dtype, 
     if (heads == 1) sx.h = sy.h = 0;
     if (tokens == 1) sx.n = sy.n = 0;
     if (sx.b < 0 || sx.h < 0 || sx.n < 0 || sy.b < 0 || sy.h < 0 || sy.n < 0) return VEDA_ERR_INVALID_ARG;
-    // different rows of y must be different bytes
-    if ((tokens > 1 && sy.n < d) || (heads > 1 && sy.h < d) || (batch > 1 && sy.b < d)) return VEDA_ERR_INVALID_ARG;
+    const veda::RowsApart apart = veda::rows_apart({tokens, sy.n}, {heads, sy.h}, {batch, sy.b}, d);
+    if (apart != veda::RowsApart::kApart) return apart == veda::RowsApart::kShare ? VEDA_ERR_INVALID_ARG : VEDA_ERR_UNSUPPORTED;
     if (x == y && (sx.n != sy.n || sx.h != sy.h || sx.b != sy.b)) return VEDA_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(y) || (sx.b * es) % 16 || (sx.h * es) % 16 || (sx.n * es) % 16 || (sy.b * es) % 16 ||
         (sy.h * es) % 16 || (sy.n * es) % 16)

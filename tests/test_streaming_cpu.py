@@ -2,6 +2,7 @@
 a plain model of it."""
 import ctypes as C
 import random
+import subprocess
 
 import numpy as np
 import pytest
@@ -102,6 +103,58 @@ def test_append_refusals(lib, more, status):
 ])
 def test_attention_refusals(lib, more, status):
     assert _attend(lib, _cache(), _batch(), **more) == status
+
+
+# (rows, heads), strides (row, head) of a result with d = 128, and whether two of its rows share bytes
+LAID_OUT = [
+    ((10, 4), (128, 128), True), ((10, 4), (256, 128), True), ((10, 4), (384, 128), True), ((10, 4), (512, 128), False), ((10, 4), (128, 1280), False),
+    ((10, 4), (128, 1152), True), ((10, 4), (504, 128), True), ((10, 4), (1280, 256), False), ((10, 4), (136, 272), True), ((1, 4), (0, 128), False),
+    ((2, 4), (128, 256), False),      # in turn: rows 0 and 1 of head 0, then of head 1
+    ((10, 4), (384, 256), True),      # row 2 of head 0 is row 0 of head 3
+    ((2, 3), (384, 256), False),      # 0 256 512, 384 640 896: each its own place, no axis within the other
+    ((3, 3), (384, 256), False), ((3, 4), (384, 256), True), ((3, 3), (376, 256), True), ((2, 4), (1 << 40, 128), False),
+]
+
+
+@pytest.mark.parametrize("shape,strides,share", LAID_OUT)
+def test_results_on_top_of_each_other_are_refused(lib, shape, strides, share):
+    # strides that are not refused lead to the next check, which refuses the address: nothing is launched
+    rows, heads = shape
+    s = veda.veda_strides(0, strides[1], strides[0])
+    near = veda.veda_strides(0, 128, 128 * heads)
+    c = _cache(kv_heads=1)
+    b = _batch(seqs=1, rows=rows, max_new=rows)
+    one = veda.veda_strides(0, 128, 128)
+    want = INVALID if share else UNSUPPORTED
+    assert _attend(lib, c, b, q_heads=heads, q=AT, sq=near, out=AT * 2 + 8, so=s) == want
+    assert _append(lib, c, b, sk=one, sv=one, q_heads=heads, q=AT, sq=near, q_out=AT * 2 + 8, so=s) == want
+
+
+def test_rows_apart_against_all_their_elements(tmp_path):
+    """Three axes, by marking every element of every row; the header has no HIP in it."""
+    src, exe = tmp_path / "apart.cpp", tmp_path / "apart"
+    src.write_text("""
+#include <cstdio>
+#include "rows_apart.h"
+int main() {
+    long long v[7];
+    while (std::scanf("%lld %lld %lld %lld %lld %lld %lld", v, v + 1, v + 2, v + 3, v + 4, v + 5, v + 6) == 7)
+        std::printf("%d\\n", (int)veda::rows_apart({v[0], v[1]}, {v[2], v[3]}, {v[4], v[5]}, v[6]));
+}
+""")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", str(veda.LIB_PATH.parent / "csrc"), str(src), "-o", str(exe)], check=True)
+    rng, cases, want = random.Random(3), [], []
+    for _ in range(4000):
+        d = rng.choice([4, 8])
+        axes = [(rng.randint(1, 5), 2 * rng.randint(0, 24) if rng.random() < 0.7 else d * rng.randint(1, 9)) for _ in range(3)]
+        at = [i * axes[0][1] + j * axes[1][1] + k * axes[2][1] + e
+              for i in range(axes[0][0]) for j in range(axes[1][0]) for k in range(axes[2][0]) for e in range(d)]
+        cases.append(" ".join(str(x) for a in axes for x in a) + f" {d}")
+        want.append(int(len(set(at)) < len(at)))
+    cases += ["1073741824 128 4096 192 1 0 128", "65535 1000 65535 1001 65535 1002 64", "2 4611686018427387904 1000000 64 32768 9223372036854775800 64"]
+    want += [1, 2, 0]
+    got = subprocess.run([str(exe)], input="\n".join(cases), capture_output=True, text=True, check=True).stdout.split()
+    assert [int(x) for x in got] == want and 1000 < sum(want) < 3000
 
 
 def test_attention_workspace_refusals(lib):

@@ -162,6 +162,20 @@ def test_rope_refuses_what_does_not_fit():
         veda.veda_rope_apply(rope, x.double(), pos)
 
 
+def test_rope_refuses_rows_that_share_bytes():
+    rope = make_rope(64, (64,), True)
+    x, pos = normal((2, 3, 4, 64), F32, 0), torch.arange(4, dtype=torch.int32, device=dev())
+    room = torch.zeros(4096, device=dev())
+    for strides in ((64, 64, 64), (768, 64, 64), (64, 256, 64), (128, 128, 256), (192, 256, 128), (512, 256, 96)):
+        with pytest.raises(veda.VedaError):
+            veda.veda_rope_apply(rope, x, pos, torch.as_strided(room, x.shape, (*strides, 1)))
+    assert not bool(room.any())
+    want = veda.veda_rope_apply(rope, x, pos)
+    for strides in ((192, 64, 384), (64, 512, 128), (2048, 192, 320)):      # others than [b, h, n]; the last: one axis not within the other
+        y = veda.veda_rope_apply(rope, x, pos, torch.as_strided(room, x.shape, (*strides, 1)))
+        assert torch.equal(y, want)
+
+
 # ---- the cache ----------------------------------------------------------------------------------------------------------
 
 class Setup:
