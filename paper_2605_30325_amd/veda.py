@@ -845,19 +845,32 @@ def veda_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, q_heads: in
     return int(load().veda_cache_attn_workspace_bytes(cache._ref, C.byref(bs), q_heads))
 
 
+def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int, window: int, sinks: int, w: str) -> veda_strides:
+    """Refuses what the library would refuse, of everything but the buffers; q's strides."""
+    _on(cache.device, w)
+    if not (0 <= block <= 1 << 30 and 0 <= window <= 1 << 30 and 0 <= sinks <= 1 << 30):
+        _refuse(w, "block, window and sinks must be 0 .. 2^30")
+    if not 0.0 < softmax_scale < float("inf"):
+        _refuse(w, "softmax_scale must be positive and finite")
+    sq, heads = _rows(cache, q, q.shape[0], w, "q"), q.shape[1]
+    if heads < 1 or heads % cache.kv_heads:
+        _refuse(w, f"{heads} query heads on {cache.kv_heads} key heads")
+    if heads > 32 * cache.kv_heads:
+        raise VedaError(VEDA_ERR_UNSUPPORTED, w, "more than 32 query heads to a key head")
+    if batch.page_table.device != cache.device:
+        _refuse(w, "the batch must be where the cache is")
+    return sq
+
+
 def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
                         workspace: Optional[torch.Tensor] = None):
     """Attention of the new rows q [rows, q_heads, d] over the cache.  block, window, sinks: which keys a row sees (veda_visible: block 1
     causal, 0 everything).  Returns (out [rows, q_heads, d], lse fp32 [q_heads, rows] or None); rows of no sequence are left as they are
     in buffers given, and undefined in buffers made here."""
-    w, rows, heads = "veda_cache_attn_fwd", q.shape[0], q.shape[1]
-    _on(cache.device, w)
-    if not (0 <= block <= 1 << 30 and 0 <= window <= 1 << 30 and 0 <= sinks <= 1 << 30):
-        _refuse(w, "block, window and sinks must be 0 .. 2^30")
-    sq = _rows(cache, q, rows, w, "q")
-    if batch.page_table.device != cache.device:
-        _refuse(w, "the batch must be where the cache is")
+    w = "veda_cache_attn_fwd"
+    sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)
+    rows, heads = q.shape[0], q.shape[1]
     if out is None:
         out = torch.empty((rows, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
     so = _rows(cache, out, rows, w, "out")
@@ -960,15 +973,27 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
                          buffers: Optional[dict] = None):
     """One attention call of a streaming step: q and k rotated, k and v appended, attention of the new rows over the cache.
     Returns (out [rows, q_heads, d], buffers); `buffers` (optional dict) is filled on the first call and reused afterwards, by calls
-    of the same rows, heads and table (a captured call writes to them whenever it is replayed, so they are never exchanged for others)."""
+    of the same rows, heads and table (a captured call writes to them whenever it is replayed, so they are never exchanged for others).
+    A call that is refused appends nothing and leaves the buffers as they were."""
     w, b = "veda_cache_attention", {} if buffers is None else buffers
-    if "ws" in b and (b["out"].shape != q.shape or b["ws"].numel() < veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])):
-        _refuse(w, "these buffers were made for a call of other sizes")
+    sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)     # before K and V are written
+    es = q.element_size()
+    if rope is None and (q.data_ptr() % 16 or any(n > 1 and s * es % 16 for n, s in ((q.shape[0], sq.n), (q.shape[1], sq.h)))):
+        raise VedaError(VEDA_ERR_UNSUPPORTED, w, "rows of q must begin at multiples of 16 bytes")
+    need = veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])
+    if "out" in b:
+        out, ws = b["out"], b["ws"]
+        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or ws.numel() < need:
+            _refuse(w, "these buffers were made for a call of other sizes")
+    else:
+        out, ws = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(need, dtype=torch.uint8, device=q.device)
+    turned = None
     if rope is not None:
-        b["q"] = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))
+        turned = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))
     else:
         veda_cache_append(cache, batch, k, v, None, positions)
-    if "ws" not in b:
-        b["ws"] = torch.empty(veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0]), dtype=torch.uint8, device=q.device)
-    b["out"], _ = veda_cache_attn_fwd(cache, batch, q if rope is None else b["q"], softmax_scale, block, window, sinks, b.get("out"), workspace=b["ws"])
-    return b["out"], b
+    veda_cache_attn_fwd(cache, batch, q if rope is None else turned, softmax_scale, block, window, sinks, out, workspace=ws)
+    b.update(out=out, ws=ws)
+    if rope is not None:
+        b["q"] = turned
+    return out, b

@@ -414,6 +414,81 @@ def test_binding_refuses_before_the_library(monkeypatch, lib):
         veda.veda_cache_copy_pages(cache, [(0, 1)])
 
 
+class Recorder:
+    """Stands for the library: notes the calls and says that all went well, or what it is told to."""
+
+    def __init__(self):
+        self.calls, self.attn = [], OK
+
+    def veda_cache_append(self, *args):
+        self.calls.append("append")
+        return OK
+
+    def veda_cache_attn_workspace_bytes(self, *args):
+        return 64
+
+    def veda_cache_attn_fwd(self, *args):
+        self.calls.append("attend")
+        return self.attn
+
+    def veda_status_string(self, status):
+        return b"status"
+
+    def veda_last_error(self):
+        return b""
+
+
+def _step(monkeypatch):
+    rec = Recorder()
+    monkeypatch.setattr(veda, "load", lambda: rec)
+    monkeypatch.setattr(veda, "_on", lambda dev, where: None)
+    monkeypatch.setattr(veda, "_stream_of", lambda dev: 0)
+    cache = veda.Cache(4, 16, 2, 64, torch.float32, device="cpu")
+    batch = veda.CacheBatch(torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), 3)
+    q, k, v = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64), torch.zeros(3, 2, 64)
+    return rec, lambda **more: veda.veda_cache_attention(cache, batch, **{**dict(q=q, k=k, v=v, softmax_scale=0.1), **more})
+
+
+@pytest.mark.parametrize("bad", [
+    dict(softmax_scale=0.0), dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(window=-1), dict(sinks=1 << 31),
+    dict(block=-2), dict(q=torch.zeros(3, 3, 64)), dict(q=torch.zeros(3, 66, 64)), dict(q=torch.zeros(3, 4, 32)),
+    dict(q=torch.zeros(3, 0, 64)), dict(q=torch.zeros(3, 4, 64, dtype=torch.bfloat16)),
+    dict(q=torch.zeros(3 * 4 * 64 + 1)[1:].view(3, 4, 64)), dict(q=torch.zeros(3, 4, 66)[..., :64]), dict(q=torch.zeros(4, 64)),
+], ids=lambda bad: "-".join(f"{k}-{tuple(v.shape) if torch.is_tensor(v) else v}" for k, v in bad.items()))
+def test_a_refused_first_call_of_a_step_leaves_everything_as_it_was(monkeypatch, bad):
+    rec, step = _step(monkeypatch)
+    b = {}
+    with pytest.raises(veda.VedaError):
+        step(buffers=b, **bad)
+    assert b == {} and rec.calls == []       # nothing appended either
+    out, same = step(buffers=b)
+    assert same is b and b["out"] is out and rec.calls == ["append", "attend"]
+    assert step(buffers=b)[0] is out
+
+
+def test_a_failed_first_call_of_a_step_leaves_the_buffers_as_they_were(monkeypatch):
+    rec, step = _step(monkeypatch)
+    b = {}
+    rec.attn = veda.VEDA_ERR_HIP
+    with pytest.raises(veda.VedaError):
+        step(buffers=b)
+    assert b == {}
+    rec.attn = OK
+    out, _ = step(buffers=b)
+    assert step(buffers=b)[0] is out
+
+
+def test_a_later_call_of_a_step_that_does_not_fit_its_buffers_appends_nothing(monkeypatch):
+    rec, step = _step(monkeypatch)
+    b = {}
+    step(buffers=b)
+    held, rec.calls = dict(b), []
+    for bad in (dict(q=torch.zeros(3, 2, 64)), dict(softmax_scale=0.0), dict(q=torch.zeros(3, 4, 64).bfloat16())):
+        with pytest.raises(veda.VedaError):
+            step(buffers=b, **bad)
+    assert rec.calls == [] and b.keys() == held.keys() and all(b[x] is held[x] for x in held)
+
+
 def test_numbers_are_not_cut_off_at_32_bits(lib):
     book = veda.Pages(8, 16, 2, 4)
     book.extend(0, 20)

@@ -578,6 +578,21 @@ def test_buffers_serve_calls_of_one_size():
     assert again is out and torch.equal(again, first)
 
 
+def test_a_refused_first_call_leaves_buffers_that_serve_the_next():
+    t = Setup([4], [100], 4, 2, 64, BF16, seed=34, tail=0)
+    q, k, v, b = t.q, t.qkv[:, 4:6], t.qkv[:, 6:], {}
+    pools = t.k.clone(), t.v.clone()
+    for bad in (dict(softmax_scale=-1.0), dict(softmax_scale=0.1, window=-1)):
+        with pytest.raises(veda.VedaError):
+            veda.veda_cache_attention(t.cache, t.batch, q, k, v, buffers=b, **bad)
+    with pytest.raises(veda.VedaError):
+        veda.veda_cache_attention(t.cache, t.batch, q[:, :3], k, v, 0.125, buffers=b)
+    assert b == {} and torch.equal(t.k, pools[0]) and torch.equal(t.v, pools[1])
+    out, _ = veda.veda_cache_attention(t.cache, t.batch, q, k, v, 0.125, buffers=b)
+    want, _ = veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.125)
+    assert torch.equal(out, want)
+
+
 def test_attention_refuses_buffers_and_numbers_that_do_not_fit():
     t = Setup([4], [600], 4, 2, 64, F32, seed=26)
     need = veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, 4, t.rows)
