@@ -668,6 +668,8 @@ def veda_attention(plan: Plan, q, k, v, phi_q: Mlp, phi_k: Mlp, k_per_head, scor
 
 
 # ---- streaming generation: rotary positions, a paged cache and the attention over it -------------------------------------
+# As everywhere in this binding no graph is formed (generation needs no gradients), with the exception of veda_rope_apply, whose gradient
+# the library has.
 
 class Rope:
     """veda_rope handle: the frequencies of one rotary scheme, on the current device.
@@ -730,8 +732,12 @@ def _on(dev: torch.device, where: str):
 
 def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Optional[torch.Tensor] = None, transpose: bool = False):
     """Rotates x [batch, heads, N, d] by positions i32 [batch or 1, N, axes] (or [N], one axis) into y (x itself: in place).
-    transpose=True turns the gradient of the result into the gradient of x."""
+    transpose=True turns the gradient of the result into the gradient of x.  Where x requires a gradient the result carries one (and its
+    backward pass makes that call); a y that is given is then refused, as no graph leads through it."""
     w, dev = "veda_rope_apply", x.device
+    if torch.is_grad_enabled() and (x.requires_grad or (y is not None and y.requires_grad)):
+        _need(y is None, w, "y is given and a gradient is required: leave y out, or call under torch.no_grad()")
+        return _Turn.apply(x, rope, positions, transpose)
     if rope.handle is None:
         _refuse(w, "the rope is closed")
     if x.dim() != 4 or x.shape[3] != rope.head_dim or (x.stride(3) != 1 and x.numel()):
@@ -754,6 +760,23 @@ def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Opt
                                   positions.data_ptr(), 0 if positions.shape[0] == 1 else n * rope.axes, int(transpose), y.data_ptr(),
                                   veda_strides(sy[0], sy[1], sy[2]), _stream_of(dev)), w)
     return y
+
+
+class _Turn(torch.autograd.Function):
+    """The rotation is linear, so its gradient is the transposed rotation of the result's; and the other way round."""
+
+    @staticmethod
+    def forward(ctx, x, rope, positions, transpose):
+        ctx.rope, ctx.transpose = rope, transpose
+        ctx.save_for_backward(positions)
+        return veda_rope_apply(rope, x, positions, transpose=transpose)
+
+    @staticmethod
+    def backward(ctx, g):
+        es = g.element_size()
+        if g.stride(3) != 1 or g.data_ptr() % 16 or any(n > 1 and s * es % 16 for n, s in zip(g.shape[:3], g.stride())):
+            g = g.clone(memory_format=torch.contiguous_format)     # a sum's gradient has no strides at all
+        return veda_rope_apply(ctx.rope, g, ctx.saved_tensors[0], transpose=not ctx.transpose), None, None, None
 
 
 class Cache:

@@ -148,6 +148,53 @@ def test_rope_gradient():
         assert bool(((slope - dx[..., c].double()).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("transpose", [False, True])
+def test_rope_gradient_through_autograd(dtype, transpose):
+    rope = make_rope(64, (24, 8), False, scaling="linear", factor=4.0)
+    b, h, n = 2, 3, 17
+    leaf = normal((b, n, h, 64), dtype, 1).requires_grad_()
+    pos = (torch.arange(n * 2, dtype=torch.int32, device=dev()) * 131).view(1, n, 2)
+    x = leaf.transpose(1, 2)
+    y = veda.veda_rope_apply(rope, x, pos, transpose=transpose)
+    with torch.no_grad():
+        plain = veda.veda_rope_apply(rope, x, pos, transpose=transpose)
+        assert not plain.requires_grad and torch.equal(plain, y) and y.requires_grad
+    odd = torch.empty(b * h * n * 64 + 1, dtype=dtype, device=dev())[1:].view(b, h, n, 64).copy_(normal((b, h, n, 64), dtype, 4))
+    grads = [normal((b, h, n, 64), dtype, 2), normal((b, n, h, 64), dtype, 3).transpose(1, 2), torch.ones((), dtype=dtype, device=dev()).expand(b, h, n, 64),
+             normal((b, h, 64, n), dtype, 5).transpose(2, 3), odd]      # dense, other orders, no strides at all, an odd address
+    for g in grads:
+        (got,) = torch.autograd.grad(y, leaf, g, retain_graph=True)
+        want = veda.veda_rope_apply(rope, g.clone(memory_format=torch.contiguous_format), pos, transpose=not transpose)
+        assert torch.equal(got.transpose(1, 2), want)
+        exact, bound = rotated(g, pos[:, None], (24, 8), False, not transpose, scaling="linear", factor=4.0)
+        close(got.transpose(1, 2), exact, bound, dtype)
+    # one head for all: its gradient is the sum over them
+    one = normal((b, 1, n, 64), F32, 6).requires_grad_()
+    g = normal((b, h, n, 64), F32, 7)
+    (got,) = torch.autograd.grad(veda.veda_rope_apply(rope, one.expand(b, h, n, 64), pos, transpose=transpose), one, g)
+    exact, bound = rotated(g, pos[:, None], (24, 8), False, not transpose, scaling="linear", factor=4.0)
+    close(got, exact.sum(1, keepdim=True), bound.sum(1, keepdim=True) + 3 * 2.0 ** -24 * exact.abs().sum(1, keepdim=True), F32)
+    # the gradient's own gradient is the rotation again
+    v = normal((b, h, n, 64), dtype, 8).requires_grad_()
+    (first,) = torch.autograd.grad(veda.veda_rope_apply(rope, x, pos, transpose=transpose), leaf, v, create_graph=True)
+    (second,) = torch.autograd.grad(first, v, normal((b, n, h, 64), dtype, 9))
+    assert torch.equal(second, veda.veda_rope_apply(rope, normal((b, n, h, 64), dtype, 9).transpose(1, 2), pos, transpose=transpose))
+
+
+def test_rope_into_a_given_tensor_has_no_graph():
+    rope = make_rope(64, (64,), True)
+    x, pos = normal((1, 2, 5, 64), F32, 0).requires_grad_(), torch.arange(5, dtype=torch.int32, device=dev())
+    y = torch.zeros((1, 2, 5, 64), device=dev())
+    for args in ((x, y), (x, x), (y, x)):
+        with pytest.raises(veda.VedaError, match="gradient"):
+            veda.veda_rope_apply(rope, args[0], pos, args[1])
+    with torch.no_grad():
+        want = veda.veda_rope_apply(rope, x, pos)
+        assert torch.equal(veda.veda_rope_apply(rope, x, pos, y), want) and not y.requires_grad
+    assert torch.equal(veda.veda_rope_apply(rope, x.detach(), pos, y), want)
+
+
 def test_rope_refuses_what_does_not_fit():
     rope = make_rope(64, (24, 20, 20), False)
     x, pos = normal((2, 3, 10, 64), F32, 0), torch.zeros((2, 10, 3), dtype=torch.int32, device=dev())
