@@ -457,7 +457,9 @@ typedef struct { int32_t block, window, sinks; } veda_visible;
  * q          device, [rows][q_heads][head_dim], strides sq (s.n from row to row, s.h from head to head); q_heads a multiple of
  *            kv_heads, up to 32 * kv_heads: query head h reads key head h / (q_heads / kv_heads)
  * out        device, the same shape, strides so; not to overlap q (refused where it begins at q).  A row that sees no key gets zeros.
- * lse        optional device fp32 [q_heads][rows]: natural-log sum of exp of the visible logits, -inf where there are none
+ *            A row with a logit that is NaN or +inf, and one whose visible logits are all -inf (0 / 0), gets NaN.
+ * lse        optional device fp32 [q_heads][rows]: natural-log sum of exp of the visible logits, -inf where there are none or all are -inf, NaN
+ *            where one is NaN or +inf
  * workspace  device, 16-byte aligned, veda_cache_attn_workspace_bytes() (0 for short caches and for many blocks of rows: NULL is
  *            allowed then); contents undefined after.  Calls that may overlap need one each.
  * bf16: products on bf16 MFMA with fp32 accumulation, softmax in fp32 (logits scaled there, Q is not rounded again), P rounded to

@@ -50,8 +50,26 @@ __device__ __forceinline__ float attn_decode(float code) {
     return (code > 128.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
 }
 
-// Sums of the softmax over no key are 0: such a row gives zeros and -inf.
-__device__ __forceinline__ float attn_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+// Whether row r of a sequence sees a key that exists.
+__device__ __forceinline__ bool attn_sees(const CacheAttnArgs& a, int seq, int r) {
+    const SeqRows sr = seq_rows(a.c, seq);
+    const Seen v = seen_by(a, sr, min(sr.n, a.c.max_new), r);
+    const int32_t* table = a.c.table + seq * a.c.table_stride;
+    const int sinks = min(a.sinks, v.hi);
+    bool found = false;
+    for (int tok = sinks > 0 ? 0 : v.lo; tok < v.hi && !found;) {
+        const int id = table[tok >> a.c.log_page], next = ((tok >> a.c.log_page) + 1) << a.c.log_page;
+        found = id >= 0 && id < a.c.pages;
+        tok = next < sinks ? next : max(next, v.lo);
+    }
+    return found;
+}
+// 1 / l.  All weights are 0 where a row sees no key, which gives zeros and -inf, and where all its logits are -inf: 0 / 0, NaN.  Their sum
+// does not tell these apart, so there, and only there, the table is looked through.
+__device__ __forceinline__ float attn_inverse(const CacheAttnArgs& a, int seq, int r, float l) {
+    if (l != 0.0f) return 1.0f / l;
+    return attn_sees(a, seq, r) ? __builtin_nanf("") : 0.0f;
+}
 __device__ __forceinline__ float attn_lse(float ref, float l) { return (ref + __log2f(l)) * kLn2; }
 
 // Tiles of `size` keys that some row of a block sees, as one list: those of the tokens that stay visible, from token 0 on, then those of the

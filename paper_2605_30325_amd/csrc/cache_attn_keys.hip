@@ -478,7 +478,7 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, RB, kMany>::kWaves)) void
         }
         const int64_t token = sr.first + row / a.group;
         const int qh = head * a.group + row % a.group;
-        keys_store<kBf16>(a.out + token * a.so_n + (int64_t)qh * a.so_h + ch * kEs, o * attn_inverse(l));
+        keys_store<kBf16>(a.out + token * a.so_n + (int64_t)qh * a.so_h + ch * kEs, o * attn_inverse(a, block.seq, row, l));
         if (a.lse && ch == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(ref, l);
     }
 }
@@ -602,7 +602,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
             const int64_t token = sr.first + row / a.group;
             const int qh = head * a.group + row % a.group;
             char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h + 4 * ln.g * kEs;
-            const float inv = attn_inverse(l);
+            const float inv = attn_inverse(a, here.seq, row, l);
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) keys_store<kBf16>(dst + 16 * c * kEs, st.o[rb][c] * inv);
             if (a.lse && ln.g == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(st.ref[rb], l);
@@ -622,7 +622,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
     const bool is_row = item < (int64_t)a.c.rows * a.q_heads;
     const int token = is_row ? (int)(item / a.q_heads) : -1, qh = (int)(item % a.q_heads);
     // the row's sequence, and its tiles
-    int first = 0, each = 0, row = 0, total = 0;
+    int first = 0, each = 0, row = 0, total = 0, seq = 0;
     for (int s0 = 0; s0 < a.c.seqs; s0 += 64) {
         const int s = s0 + lane;
         int mine = 0, i = -1;
@@ -638,6 +638,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
             each = __builtin_amdgcn_readlane(mine, at);
             first = total + __builtin_amdgcn_readlane(up_to, at) - each;
             row = __builtin_amdgcn_readlane(i, at) * a.group + qh % a.group;
+            seq = s0 + at;
         }
         total += __builtin_amdgcn_readlane(up_to, 63);
     }
@@ -692,7 +693,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
             for (int c = 0; c < V; ++c) o[c] += sums[x][V * lane + c];
         }
     }
-    const float inv = attn_inverse(l);
+    const float inv = attn_inverse(a, seq, row, l);
     char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h;
 #pragma unroll
     for (int c = 0; c < V; ++c) {

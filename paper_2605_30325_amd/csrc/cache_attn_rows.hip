@@ -592,7 +592,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         }
         return;
     }
-    const float inv = attn_inverse(l);
+    const float inv = attn_inverse(a, seq, r, l);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -809,8 +809,8 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
 #pragma unroll
         for (int c = 0; c < V; ++c) y[c] += sums[w][wave][V * lane + c];
     }
-    const float inv = attn_inverse(lsum);
     const int row = item % a.per_seq * kAttnRows + r0 + wave, qh = head * a.group + row % a.group;
+    const float inv = attn_inverse(a, item / a.per_seq, row, lsum);
     const int64_t token = sr.first + row / a.group;
     char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h;
 #pragma unroll

@@ -405,6 +405,54 @@ def test_bad_queries_and_keys_that_are_seen(dtype, n):
     assert torch.equal(out, clean)
 
 
+def plain_row(t, s, i, h, q, scale, block=1, window=0, sinks=0):
+    """Row i of sequence s, query head h, by the formula in 64 bits with all that infinities do there: (out, lse)."""
+    tok, k, v = t.keys(s)
+    p = t.len[s] - t.new[s] + i
+    e = (p // block + 1) * block if block else t.len[s]
+    seen = (tok < e) & ((tok >= e - window) | (tok < sinks) if window else tok >= 0)
+    g = h // (t.hq // t.hk)
+    x = k[seen, g] @ q[int(t.start[s]) + i, h].double().cpu() * scale
+    pr = torch.softmax(x, 0)
+    return pr @ v[seen, g], torch.logsumexp(x, 0)
+
+
+ALL = [(1, 60), (3, 60), (1, 6000), (70, 60), (70, 1500), (333, 10)]      # new rows and cached tokens: every kernel, and shared walks
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,past", ALL)
+def test_logits_that_are_all_minus_infinity(dtype, d, n, past):
+    # the softmax over them is 0 / 0; a row that sees no key at all gives zeros
+    t = Setup([n, 1, 0, 2], [past, 5, 0, 40], 2, 1, d, dtype, page=32, seed=35, holes=[(3, 0, -1), (3, 1, -1)])
+    q = t.q.clone()
+    q[:, 0, 0], q[:, 1, 0] = 1.0, -1.0
+    clean, clean_lse = check_attention(t, q=q)
+    for page in range(-(-(past + n) // 32)):
+        t.k[t.table[0, page], :, :, 0] = -math.inf                 # every key of the first sequence: head 0 is repelled, head 1 attracted
+    out, lse = clean.clone(), clean_lse.clone()
+    veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.125, out=out, lse=lse)
+    assert bool(torch.isnan(out[:n, 0]).all()) and bool((lse[0, :n] == -math.inf).all())
+    assert bool(torch.isnan(out[:n, 1]).all()) and bool(torch.isnan(lse[1, :n]).all())
+    assert bool((out[n + 1:n + 3] == 0).all()) and bool((lse[:, n + 1:n + 3] == -math.inf).all())
+    # nothing but the first token is seen: the rows of head 0 are its value
+    first = t.table[0, 0]
+    t.k[first, :, 0, 0] = 0.5
+    q[:, 1] = q[:, 0]
+    veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.125, out=out, lse=lse)
+    want, want_lse = plain_row(t, 0, n - 1, 0, q, 0.125)
+    # one weight, divided by itself: a few roundings on its way through products, joining and division; its logit is a sum of d products
+    bound = 2.0 ** -20 * want.abs()
+    close(out[:n], want.expand(n, 2, d), bound.expand(n, 2, d), dtype)
+    big = 0.125 * (q[n - 1, 0].abs().double() @ t.k[first, 0, 0].abs().double()).item()
+    assert (lse[0, n - 1].double().cpu() - want_lse).abs() <= (d + 8) * 2.0 ** -24 * big + 2.0 ** -20
+    # a window over the repelling ones alone, and one that leaves the first token
+    veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.125, window=50, out=out, lse=lse)
+    assert bool(torch.isnan(out[n - 1]).all()) and bool((lse[:, n - 1] == -math.inf).all())
+    veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.125, window=50, sinks=1, out=out, lse=lse)
+    close(out[n - 1], want.expand(2, d), bound.expand(2, d), dtype)
+
+
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 def test_large_logits(dtype, d):
     # queries forty times as large: one key takes almost all; the reference moves often
