@@ -40,14 +40,18 @@ __device__ __forceinline__ Seen seen_by(const CacheAttnArgs& a, const SeqRows& s
     return {a.window ? max(0, e - a.window) : 0, min(e, sr.len)};
 }
 
-// A value that is not finite reaches the rows that see it, and no others, as a count: 1 for +inf, 128 for -inf, 129 for NaN, of at
-// most 32 keys, so a sum of them says which there were.
+// A value that is not finite reaches the rows that see its key, and no others, as a count: 1 for +inf, 128 for -inf, 129 for NaN, of at
+// most 32 keys, so a sum of them says which there were.  Times 2^14 where the weight has come out as 0: 0 times infinity, NaN, as
+// the product itself gives in tiles that all rows see.
+constexpr float kCodeNothing = 16384.0f;
 __device__ __forceinline__ float attn_code(float x) {
     return (x < INFINITY ? 0.0f : 1.0f) + (x > -INFINITY ? 0.0f : 128.0f);
 }
+__device__ __forceinline__ float attn_times(float p, bool seen) { return p > 0.0f ? 1.0f : seen ? kCodeNothing : 0.0f; }
 __device__ __forceinline__ float attn_decode(float code) {
     const float down = floorf(code * (1.0f / 128.0f));
-    return (code > 128.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+    const float sum = (code > 128.0f * down ? INFINITY : 0.0f) + (down > 0.0f ? -INFINITY : 0.0f);
+    return code >= kCodeNothing ? __builtin_nanf("") : sum;
 }
 
 // Whether row r of a sequence sees a key that exists.

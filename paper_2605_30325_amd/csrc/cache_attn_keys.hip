@@ -92,6 +92,10 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
             }
         }
     }
+    auto seen = [&](int rb, int b, int i) __attribute__((always_inline)) {
+        const int key = key0 + 16 * b + 4 * g + i;
+        return key < st.hi[rb] && (key >= st.lo[rb] || key < a.sinks) && ((exists >> b) & 1u);
+    };
     float mx[RB];
     bool grown = false;
 #pragma unroll
@@ -100,11 +104,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
 #pragma unroll
             for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = key0 + 16 * b + 4 * g + i;
-                    const bool seen = key < st.hi[rb] && (key >= st.lo[rb] || key < a.sinks) && ((exists >> b) & 1u);
-                    s[rb][b][i] = seen ? s[rb][b][i] : -INFINITY;
-                }
+                for (int i = 0; i < 4; ++i) s[rb][b][i] = seen(rb, b, i) ? s[rb][b][i] : -INFINITY;
         }
         float m = s[rb][0][0];
 #pragma unroll
@@ -199,7 +199,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
                 for (int rb = 0; rb < RB; ++rb) {
                     bf16x8 on;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) on[e] = (__bf16)((float)p[rb][e] > 0.0f ? 1.0f : 0.0f);
+                    for (int e = 0; e < 8; ++e) on[e] = (__bf16)attn_times((float)p[rb][e], seen(rb, e / 4, e % 4));
                     st.o[rb][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[rb], st.o[rb][c], 0, 0, 0);
                     code[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, on, code[rb], 0, 0, 0);
                 }
@@ -212,7 +212,7 @@ __device__ __forceinline__ void keys_tile(const CacheAttnArgs& a, KeysRow<kBf16,
 #pragma unroll
                         for (int rb = 0; rb < RB; ++rb) {
                             st.o[rb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(y == 0.0f ? x : 0.0f, s[rb][b][i], st.o[rb][c], 0, 0, 0);
-                            code[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(y, s[rb][b][i] > 0.0f ? 1.0f : 0.0f, code[rb], 0, 0, 0);
+                            code[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(y, attn_times(s[rb][b][i], seen(rb, b, i)), code[rb], 0, 0, 0);
                         }
                     }
             }
@@ -471,8 +471,7 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, RB, kMany>::kWaves)) void
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float m = ml[2 * (w * kRows + rr)], lw = ml[2 * (w * kRows + rr) + 1];
-            if (lw == 0.0f) continue;
-            const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - ref);   // -inf: the sum is NaN
+            const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - ref);   // -inf: the sums are 0 or NaN
             l += f * lw;
             o += f * *reinterpret_cast<const f32x4v*>(smem + (w * kRows + rr) * T::kOutRowB + ch * 4);
         }
@@ -670,8 +669,8 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
         if (j0 != w) get(j0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (j0 + W * j >= n || m[j].y == 0.0f) continue;
-            const float f = m[j].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j].x - ref);   // -inf: the sum is NaN
+            if (j0 + W * j >= n) continue;
+            const float f = m[j].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j].x - ref);   // -inf: the sums are 0 or NaN
             l += f * m[j].y;
 #pragma unroll
             for (int c = 0; c < V; ++c) o[c] += f * x[j][c];

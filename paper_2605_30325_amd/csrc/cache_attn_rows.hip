@@ -108,8 +108,8 @@ template <int D> __device__ __forceinline__ bool attn_finite(uint32_t v) {
     return !__any(t != 0.0f);   // NaN != 0
 }
 
-// O^T += V^T P^T of 32 keys some of whose values are not finite: those reach the rows whose p there is not zero.
-template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& st, uint32_t v, const bf16x8 (&p)[2]) {
+// O^T += V^T P^T of 32 keys some of whose values are not finite: those reach the rows that see their keys (bit i: register i's).
+template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& st, uint32_t v, const bf16x8 (&p)[2], uint32_t seen) {
     constexpr int NB = D / 32;
     f32x16 o[NB];   // indexed as the loop goes, so it lies in memory: this path must not cost the others registers
 #pragma unroll
@@ -126,7 +126,7 @@ template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& 
             for (int e = 0; e < 8; ++e) {
                 y[e] = (__bf16)attn_code((float)x[e]);
                 x[e] = (float)y[e] == 0.0f ? x[e] : (__bf16)0.0f;
-                on[e] = (__bf16)((float)p[kk][e] > 0.0f ? 1.0f : 0.0f);
+                on[e] = (__bf16)attn_times((float)p[kk][e], (seen >> (8 * kk + e)) & 1u);
             }
             sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[kk], sum, 0, 0, 0);
             code = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, on, code, 0, 0, 0);
@@ -160,6 +160,17 @@ __device__ __forceinline__ void attn_mask(const AttnRow<kBf16, D>& st, f32x16& s
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (exists >> (i >> 3)) & 1u ? s[i] : -INFINITY;
     }
+}
+
+// Bit i: the lane's row sees the key of register i.
+template <bool kBf16, int D> __device__ __forceinline__ uint32_t attn_seen(const AttnRow<kBf16, D>& st, int key0, uint32_t exists, int sinks, int hh) {
+    uint32_t seen = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int key = key0 + 4 * hh + 8 * (i >> 2) + (i & 3);
+        seen |= (key < st.hi && (key >= st.lo || key < sinks) && ((exists >> (i >> 3)) & 1u) ? 1u : 0u) << i;
+    }
+    return seen;
 }
 
 // 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.  check: values may be not
@@ -197,7 +208,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
                     if (nb & 1) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
                 }
         } else {
-            attn_careful<D>(st, v, p);
+            attn_careful<D>(st, v, p, attn_seen<kBf16, D>(st, key0, exists, a.sinks, hh));
         }
     } else {
         // step i takes keys 8 (i / 4) + i % 4 of either lane half: register i is the operand
@@ -238,6 +249,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
+            const uint32_t seen = attn_seen<kBf16, D>(st, key0, exists, a.sinks, hh);
             f32x16 o[NB];   // in memory, as above
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) o[nb] = st.o[nb];
@@ -250,7 +262,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
                 for (int i = 0; i < 16; ++i) {
                     const float x = operand(i, nb), y = attn_code(x);
                     sum = __builtin_amdgcn_mfma_f32_32x32x2f32(y == 0.0f ? x : 0.0f, s[i], sum, 0, 0, 0);
-                    code = __builtin_amdgcn_mfma_f32_32x32x2f32(y, s[i] > 0.0f ? 1.0f : 0.0f, code, 0, 0, 0);
+                    code = __builtin_amdgcn_mfma_f32_32x32x2f32(y, attn_times(s[i], (seen >> i) & 1u), code, 0, 0, 0);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum[i] += attn_decode(code[i]);
@@ -785,8 +797,7 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            if (m[r].y == 0.0f) continue;
-            const float f = m[r].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[r].x - ref[r]);   // -inf: the sum is NaN
+            const float f = m[r].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[r].x - ref[r]);   // -inf: the sums are 0 or NaN
             l[r] += f * m[r].y;
 #pragma unroll
             for (int c = 0; c < V; ++c) o[r][c] += f * x[r][c];

@@ -454,6 +454,81 @@ def test_logits_that_are_all_minus_infinity(dtype, d, n, past):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,past", ALL)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_bad_values_that_are_seen(dtype, d, n, past, bad):
+    """At keys in tiles that every row sees and in tiles that some do not, with weights of ordinary size and with weights that are 0 in
+    fp32: the rows that see one are never finite there, and as the formula says where the weight is more than 2^-100; all else keeps its bytes."""
+    t = Setup([n, 2], [past, 9], 2, 1, d, dtype, page=32, seed=36)
+    last = past + n - 1
+    q = t.q.clone()
+    q[:, :, 0] = 1.0
+    for far in (0.0, -3000.0):               # the logit falls by a hundred or two: a weight of e^-375 at d = 64, and less
+        for key in sorted({3, past - 2, past, last}):
+            page, at = t.table[0, key // 32], key % 32
+            kept = t.k[page, 0, at].clone()
+            t.k[page, 0, at, 0] = far
+            clean, clean_lse = check_attention(t, q=q)
+            good = t.v[page, 0, at, 5].clone()
+            t.v[page, 0, at, 5] = bad
+            out, lse = veda.veda_cache_attn_fwd(t.cache, t.batch, q, 1.0 / math.sqrt(d), out=clean.clone(), lse=clean_lse.clone())
+            first = max(0, key - past)                       # rows from here on see it
+            assert torch.equal(out[:first], clean[:first]) and torch.equal(out[n:], clean[n:]) and torch.equal(lse, clean_lse)
+            keep = [c for c in range(d) if c != 5]
+            assert torch.equal(out[:, :, keep], clean[:, :, keep])
+            hit = out[first:n, :, 5].float()
+            assert not bool(torch.isfinite(hit).any()), (far, key)
+            if far == 0.0 and math.isinf(bad):
+                assert bool((hit == bad).all())
+            if math.isnan(bad):
+                assert bool(torch.isnan(hit).all())
+            t.v[page, 0, at, 5], t.k[page, 0, at] = good, kept
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,past", ALL)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_bad_keys_that_are_seen(dtype, d, n, past, bad):
+    """A logit of -inf is a weight of 0, one of +inf or NaN makes the row NaN.  Rows of the same sequence that do not see the key stay within
+    their bounds, not at their bytes: all rows of a wave move their references where one has outgrown its own, and the quotient
+    sum p v / sum p is the same for any reference only up to the roundings that the bounds count (exponential, sums, rescalings)."""
+    t = Setup([n, 2], [past, 9], 2, 1, d, dtype, page=32, seed=37)
+    last = past + n - 1
+    q = t.q.clone()
+    q[:, 0, 0], q[:, 1, 0] = 1.0, -1.0
+    for key in sorted({3, past - 2, past, last}):
+        page, at = t.table[0, key // 32], key % 32
+        kept = t.k[page, 0, at].clone()
+        clean, clean_lse = check_attention(t, q=q)
+        formula, formula_lse, ob, lb = attention(t, q, 1.0 / math.sqrt(d), 1, 0, 0)
+        t.k[page, 0, at, 0] = bad
+        out, lse = veda.veda_cache_attn_fwd(t.cache, t.batch, q, 1.0 / math.sqrt(d), out=clean.clone(), lse=clean_lse.clone())
+        first = max(0, key - past)
+        assert torch.equal(out[n:], clean[n:]) and torch.equal(lse[:, n:], clean_lse[:, n:])        # the other sequence
+        if first:
+            close(out[:first], formula[:first], ob[:first], dtype)
+            assert bool(((lse[:, :first].double().cpu() - formula_lse[:, :first]).abs() <= lb[:, :first]).all())
+        for h in range(2):
+            if math.isnan(bad) or (bad > 0) == (h == 0):
+                assert bool(torch.isnan(out[first:n, h]).all()) and bool(torch.isnan(lse[h, first:n]).all())
+                continue
+            for i in {first, n - 1}:
+                want, want_lse = plain_row(t, 0, i, h, q, 1.0 / math.sqrt(d))
+                tok, k, v = t.keys(0)
+                seen = (tok <= past + i) & (tok != key)
+                if not bool(seen.any()):
+                    continue
+                k, v, qr = k[seen, 0], v[seen, 0], q[i, h].double().cpu()
+                mean = torch.softmax(k @ qr / math.sqrt(d), 0) @ v.abs()
+                big = (k.abs() @ qr.abs()).max().item() / math.sqrt(d)
+                delta, count = (d + 8) * 2.0 ** -24 * big + 2.0 ** -22, int(seen.sum())
+                bound = mean * (2 * delta + 2 * (count + 64) * 2.0 ** -24 + (2.0 ** -8 if dtype == BF16 else 0.0)) * 1.01
+                close(out[i, h], want, bound, dtype)
+                assert abs(lse[h, i].item() - want_lse.item()) <= delta + (count + 64) * 2.0 ** -24 + 2.0 ** -21 * abs(want_lse.item())
+        t.k[page, 0, at] = kept
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 def test_large_logits(dtype, d):
     # queries forty times as large: one key takes almost all; the reference moves often
     t = Setup([5, 140], [400, 100], 4, 2, d, dtype, page=64, seed=11, gain=40.0)
