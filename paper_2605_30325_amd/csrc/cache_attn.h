@@ -55,8 +55,7 @@ __device__ __forceinline__ float attn_decode(float code) {
 }
 
 // Whether row r of a sequence sees a key that exists.
-__device__ __forceinline__ bool attn_sees(const CacheAttnArgs& a, int seq, int r) {
-    const SeqRows sr = seq_rows(a.c, seq);
+__device__ __forceinline__ bool attn_sees(const CacheAttnArgs& a, int seq, const SeqRows& sr, int r) {
     const Seen v = seen_by(a, sr, min(sr.n, a.c.max_new), r);
     const int32_t* table = a.c.table + seq * a.c.table_stride;
     const int sinks = min(a.sinks, v.hi);
@@ -70,9 +69,9 @@ __device__ __forceinline__ bool attn_sees(const CacheAttnArgs& a, int seq, int r
 }
 // 1 / l.  All weights are 0 where a row sees no key, which gives zeros and -inf, and where all its logits are -inf: 0 / 0, NaN.  Their sum
 // does not tell these apart, so there, and only there, the table is looked through.
-__device__ __forceinline__ float attn_inverse(const CacheAttnArgs& a, int seq, int r, float l) {
+__device__ __forceinline__ float attn_inverse(const CacheAttnArgs& a, int seq, const SeqRows& sr, int r, float l) {
     if (l != 0.0f) return 1.0f / l;
-    return attn_sees(a, seq, r) ? __builtin_nanf("") : 0.0f;
+    return attn_sees(a, seq, sr, r) ? __builtin_nanf("") : 0.0f;
 }
 __device__ __forceinline__ float attn_lse(float ref, float l) { return (ref + __log2f(l)) * kLn2; }
 

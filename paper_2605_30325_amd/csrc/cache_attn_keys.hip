@@ -477,7 +477,7 @@ __global__ __launch_bounds__((64 * KeysGroup<kBf16, D, RB, kMany>::kWaves)) void
         }
         const int64_t token = sr.first + row / a.group;
         const int qh = head * a.group + row % a.group;
-        keys_store<kBf16>(a.out + token * a.so_n + (int64_t)qh * a.so_h + ch * kEs, o * attn_inverse(a, block.seq, row, l));
+        keys_store<kBf16>(a.out + token * a.so_n + (int64_t)qh * a.so_h + ch * kEs, o * attn_inverse(a, block.seq, sr, row, l));
         if (a.lse && ch == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(ref, l);
     }
 }
@@ -601,7 +601,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64) void cache
             const int64_t token = sr.first + row / a.group;
             const int qh = head * a.group + row % a.group;
             char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h + 4 * ln.g * kEs;
-            const float inv = attn_inverse(a, here.seq, row, l);
+            const float inv = attn_inverse(a, here.seq, sr, row, l);
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) keys_store<kBf16>(dst + 16 * c * kEs, st.o[rb][c] * inv);
             if (a.lse && ln.g == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(st.ref[rb], l);
@@ -692,7 +692,7 @@ template <bool kBf16, int D, int RB, int W> __global__ __launch_bounds__(512) vo
             for (int c = 0; c < V; ++c) o[c] += sums[x][V * lane + c];
         }
     }
-    const float inv = attn_inverse(a, seq, row, l);
+    const float inv = l != 0.0f ? 1.0f / l : attn_inverse(a, seq, seq_rows(a.c, seq), row, l);
     char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h;
 #pragma unroll
     for (int c = 0; c < V; ++c) {

@@ -165,7 +165,7 @@ __device__ __forceinline__ void attn_mask(const AttnRow<kBf16, D>& st, f32x16& s
 // Bit i: the lane's row sees the key of register i.
 template <bool kBf16, int D> __device__ __forceinline__ uint32_t attn_seen(const AttnRow<kBf16, D>& st, int key0, uint32_t exists, int sinks, int hh) {
     uint32_t seen = 0;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < 16; ++i) {
         const int key = key0 + 4 * hh + 8 * (i >> 2) + (i & 3);
         seen |= (key < st.hi && (key >= st.lo || key < sinks) && ((exists >> (i >> 3)) & 1u) ? 1u : 0u) << i;
@@ -604,7 +604,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         }
         return;
     }
-    const float inv = attn_inverse(a, seq, r, l);
+    const float inv = attn_inverse(a, seq, sr, r, l);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -821,7 +821,7 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
         for (int c = 0; c < V; ++c) y[c] += sums[w][wave][V * lane + c];
     }
     const int row = item % a.per_seq * kAttnRows + r0 + wave, qh = head * a.group + row % a.group;
-    const float inv = attn_inverse(a, item / a.per_seq, row, lsum);
+    const float inv = attn_inverse(a, item / a.per_seq, sr, row, lsum);
     const int64_t token = sr.first + row / a.group;
     char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h;
 #pragma unroll
