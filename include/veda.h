@@ -462,8 +462,9 @@ typedef struct { int32_t block, window, sinks; } veda_visible;
  *            where one is NaN or +inf
  * workspace  device, 16-byte aligned, veda_cache_attn_workspace_bytes() (0 for short caches and for many blocks of rows: NULL is
  *            allowed then); contents undefined after.  Calls that may overlap need one each.
- * bf16: products on bf16 MFMA with fp32 accumulation, softmax in fp32 (logits scaled there, Q is not rounded again), P rounded to
- * bf16 before P V.  f32: products on fp32 MFMA.  Values behind a sequence's end, in holes and at keys that a row does not see
+ * bf16: products on bf16 MFMA with fp32 accumulation, softmax in fp32 (logits scaled there, Q is not rounded again).  P V takes P in two
+ * bf16 parts (2^-15 of a weight off at most) where no sequence has more than 32 rows of a key head, min(max_new, rows) * q_heads /
+ * kv_heads; in larger blocks P is rounded to bf16 once (2^-8).  f32: products on fp32 MFMA.  Values behind a sequence's end, in holes and at keys that a row does not see
  * do not reach that row, whatever they are (infinities and NaN too).  One that is not finite at a key that a row sees makes that row's
  * channel infinite (NaN where both signs or a NaN are seen); where the key's weight is less than 2^-100 of the row's largest it
  * may be NaN instead (a weight of 0 times infinity). */

@@ -537,6 +537,21 @@ def test_large_logits(dtype, d):
     check_attention(t, scale=3.0)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,past,hq,hk", [([1] * 3, [0, 37, 700], 4, 2), ([1] * 300, [90] * 300, 1, 1), ([1, 1], [6000, 20], 5, 1),
+                                            ([3, 1], [500, 30], 8, 1), ([3, 2], [6000, 100], 16, 2)])
+def test_weights_of_few_rows_are_not_rounded_to_bf16(d, new, past, hq, hk):
+    """Up to 32 rows of a key head: a weight goes into its product in two bf16 parts.  The first lies below it by at most a step, 2^-7
+    of it, and that is rounded by half a step: 2^-15 of the weight, where one part alone is off by 2^-8."""
+    t = Setup(new, past, hq, hk, d, BF16, page=32, seed=38)
+    out, _ = check_attention(t)
+    want, _, ob, _ = attention(t, t.q, 1.0 / math.sqrt(d), 1, 0, 0)
+    real, t.v = t.v, t.v.abs()                      # the mean of |v|, of which the bound counts 1.01 * 2^-8
+    mean, _, _, _ = attention(t, t.q, 1.0 / math.sqrt(d), 1, 0, 0)
+    t.v, used = real, int(t.start[-1])
+    close(out[:used], want[:used], (ob - 1.01 * (2.0 ** -8 - 2.0 ** -15) * mean)[:used], BF16)
+
+
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 @pytest.mark.parametrize("n,hq,hk", [(1, 3, 1), (3, 8, 2), (40, 4, 1)])
 def test_long_caches_are_split(dtype, d, n, hq, hk):
