@@ -70,14 +70,16 @@ constexpr int kRopeThreads = 256;
 
 // A cos and A sin of tokens 0..n-1 of a block, [token][pair]; pos(t, axis) is a token's position.
 // The product position * turns is formed in 64 bits and only its fraction kept: fp32 would be off by a radian's part at
-// positions of 2^20 already.
+// positions of 2^20 already.  What the fraction loses as fp32, up to 2^-26 of a turn, 1.6 half steps of a sine near 1, is put back to first order.
 template <typename Pos> __device__ __forceinline__ void rope_angles(const RopeArgs& a, int n, Pos pos, float2* cs) {
     for (int i = threadIdx.x; i < n * a.half; i += kRopeThreads) {
         const int t = i / a.half, p = i % a.half;
         const double turns = (double)pos(t, p < a.end0 ? 0 : p < a.end1 ? 1 : 2) * a.turns[p];
+        const double part = turns - rint(turns);
         float s, c;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-        cs[i] = float2{a.amplitude * c, a.sign * a.amplitude * s};
+        sincospif(2.0f * (float)part, &s, &c);
+        const float rest = 6.2831853f * (float)(part - (double)(float)part);
+        cs[i] = float2{a.amplitude * (c - s * rest), a.sign * a.amplitude * (s + c * rest)};
     }
 }
 

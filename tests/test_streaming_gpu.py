@@ -105,6 +105,26 @@ def test_rope_against_the_formula(dtype, halves, d, dims):
             close(y, want, bound, dtype, f"{b}x{h}x{n} from {first}")
 
 
+def test_rope_angles_are_not_rounded_to_fp32():
+    """Pairs (1, 0) become (cos, sin).  A fraction of a turn that is rounded to fp32 turns them by 2 pi times what that loses, which the
+    errors then follow: their slope on it is 1, and 0 where nothing is lost (the other roundings know nothing of it: 100,000 errors of
+    about a half step each leave 0.01)."""
+    rope = make_rope(128, (128,), False)
+    f, _ = rope.frequencies()
+    n = 1600
+    pos = (torch.arange(n, dtype=torch.int32) * 7919 % 65536).view(1, n, 1)
+    x = torch.zeros(1, 1, n, 128, device=dev())
+    x[..., 0::2] = 1.0
+    y = veda.veda_rope_apply(rope, x, pos.to(dev()))[0, 0].double().cpu().numpy()
+    turns = pos.view(n, 1).numpy().astype(np.float64) * (f / 6.283185307179586476925286766559)
+    part = turns - np.rint(turns)
+    lost = 2 * math.pi * (part - part.astype(np.float32).astype(np.float64))
+    c, s = np.cos(2 * math.pi * part), np.sin(2 * math.pi * part)
+    err = np.stack([y[:, 0::2] - c, y[:, 1::2] - s])
+    follows = np.stack([s * lost, -c * lost])
+    assert abs((err * follows).sum() / (follows ** 2).sum()) < 0.25
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_rope_strides_sharing_and_in_place(dtype):
     rope = make_rope(64, (32,), True)
