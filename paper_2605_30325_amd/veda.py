@@ -8,6 +8,7 @@ kernels.  There is no fallback: if the library is missing or a call fails, this 
 from __future__ import annotations
 
 import ctypes as C
+import math
 from pathlib import Path
 from typing import Optional, Sequence, Tuple
 
@@ -735,7 +736,7 @@ def veda_rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Opt
     transpose=True turns the gradient of the result into the gradient of x.  Where x requires a gradient the result carries one (and its
     backward pass makes that call); a y that is given is then refused, as no graph leads through it."""
     w, dev = "veda_rope_apply", x.device
-    if torch.is_grad_enabled() and (x.requires_grad or (y is not None and y.requires_grad)):
+    if (x.requires_grad or (y is not None and y.requires_grad)) and torch.is_grad_enabled():
         _need(y is None, w, "y is given and a gradient is required: leave y out, or call under torch.no_grad()")
         return _Turn.apply(x, rope, positions, transpose)
     if rope.handle is None:
@@ -873,7 +874,7 @@ def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: 
     _on(cache.device, w)
     if not (0 <= block <= 1 << 30 and 0 <= window <= 1 << 30 and 0 <= sinks <= 1 << 30):
         _refuse(w, "block, window and sinks must be 0 .. 2^30")
-    if not 0.0 < softmax_scale < float("inf"):
+    if not 0.0 < softmax_scale < math.inf:
         _refuse(w, "softmax_scale must be positive and finite")
     sq, heads = _rows(cache, q, q.shape[0], w, "q"), q.shape[1]
     if heads < 1 or heads % cache.kv_heads:
