@@ -947,14 +947,19 @@ class Pages:
     def table(self) -> np.ndarray:
         """A copy of the table, i32 [max_seqs, max_pages], -1 where there is no page."""
         t = load().veda_pages_table(self.handle)
+        _need(bool(t), "veda_pages_table", "the book is closed")
         return np.ctypeslib.as_array(t, (self.max_seqs, self.max_pages)).copy()
 
     def length(self, seq: int) -> int:
         _ints("veda_pages_length", seq)
-        return int(load().veda_pages_length(self.handle, seq))
+        n = int(load().veda_pages_length(self.handle, seq))
+        _need(n >= 0, "veda_pages_length", f"no sequence {seq}")
+        return n
 
     def free_count(self) -> int:
-        return int(load().veda_pages_free_count(self.handle))
+        n = int(load().veda_pages_free_count(self.handle))
+        _need(n >= 0, "veda_pages_free_count", "the book is closed")
+        return n
 
     def extend(self, seq: int, tokens: int) -> np.ndarray:
         return self._copies("veda_pages_extend", 1, seq, tokens)

@@ -498,3 +498,15 @@ def test_numbers_are_not_cut_off_at_32_bits(lib):
         with pytest.raises(veda.VedaError, match="32 bits"):
             call()
     assert book.length(0) == 20 and book.length(1) == 0
+
+
+def test_books_say_no_to_sequences_that_are_not_theirs(lib):
+    book = veda.Pages(8, 16, 2, 4)
+    for seq in (-1, 2, 1 << 20):
+        with pytest.raises(veda.VedaError):      # a length of -1 would go on into the next sum
+            book.length(seq)
+    assert book.length(1) == 0
+    book.close()
+    for call in (book.table, book.free_count, lambda: book.length(0), lambda: book.extend(0, 1), lambda: book.truncate(0), book.compact):
+        with pytest.raises(veda.VedaError):
+            call()
