@@ -921,6 +921,8 @@ def veda_cache_copy_pages(cache: Cache, pairs):
     """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
     _on(cache.device, "veda_cache_copy_pages")
     p = np.asarray(pairs)
+    if p.size and not (p.shape[1] == 2 if p.ndim == 2 else p.ndim == 1 and p.size % 2 == 0):     # sources and targets as two rows, say
+        _refuse("veda_cache_copy_pages", "pairs must be page numbers [n, 2]")
     if p.dtype != np.int32:
         _need(p.size == 0 or (p.dtype.kind in "iu" and 0 <= p.min() and p.max() < 1 << 31), "veda_cache_copy_pages", "pairs must be page numbers [n, 2]")
     p = np.ascontiguousarray(p, np.int32).reshape(-1, 2)

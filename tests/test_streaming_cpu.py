@@ -510,3 +510,27 @@ def test_books_say_no_to_sequences_that_are_not_theirs(lib):
     for call in (book.table, book.free_count, lambda: book.length(0), lambda: book.extend(0, 1), lambda: book.truncate(0), book.compact):
         with pytest.raises(veda.VedaError):
             call()
+
+
+def test_copies_are_pairs(monkeypatch, lib):
+    monkeypatch.setattr(veda, "_on", lambda dev, where: None)
+    monkeypatch.setattr(veda, "_stream_of", lambda dev: 0)
+    cache, seen = veda.Cache(8, 16, 2, 64, torch.float32, device="cpu"), []
+
+    class Listed(Recorder):
+        def veda_cache_copy_pages(self, ref, at, n, stream):
+            seen.append(np.ctypeslib.as_array(C.cast(at, C.POINTER(C.c_int32)), (n, 2)).tolist() if n else [])
+            return OK
+
+    rec = Listed()
+    monkeypatch.setattr(veda, "load", lambda: rec)
+    for pairs in ([[1, 2], [3, 4]], np.asarray([[1, 2], [3, 4]]), [1, 2, 3, 4]):
+        veda.veda_cache_copy_pages(cache, pairs)
+        assert seen.pop() == [[1, 2], [3, 4]]
+    for none in ([], np.zeros((0, 2), np.int32)):
+        veda.veda_cache_copy_pages(cache, none)
+        assert seen.pop() == []
+    for bad in ([[1, 2, 3, 4], [5, 6, 7, 0]], [1, 2, 3], [[[1, 2]]], 5, np.zeros((2, 3), np.int32)):      # the first: sources and targets
+        with pytest.raises(veda.VedaError, match="pairs"):
+            veda.veda_cache_copy_pages(cache, bad)
+    assert seen == []
