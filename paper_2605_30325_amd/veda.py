@@ -682,7 +682,7 @@ class Rope:
         self.handle = None
         if not 1 <= len(dims) <= 3:
             raise VedaError(VEDA_ERR_INVALID_ARG, "Rope", "axis_dim must name 1 to 3 axes")
-        _ints("Rope", head_dim, *dims)
+        _ints("Rope", head_dim, *dims, pairs, scaling)
         cfg = veda_rope_config(head_dim, len(dims), (C.c_int32 * 3)(*dims), pairs, scaling, base, factor, trained_len, beta_fast, beta_slow,
                                amplitude)
         h = C.c_void_p()
@@ -865,6 +865,7 @@ def veda_cache_append(cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch
 
 def veda_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, q_heads: int, rows: int) -> int:
     """Bytes of scratch for veda_cache_attn_fwd on buffers of `rows` rows."""
+    _ints("veda_cache_attn_workspace_bytes", q_heads, rows)
     bs = batch.struct(rows)
     return int(load().veda_cache_attn_workspace_bytes(cache._ref, C.byref(bs), q_heads))
 

@@ -534,3 +534,16 @@ def test_copies_are_pairs(monkeypatch, lib):
         with pytest.raises(veda.VedaError, match="pairs"):
             veda.veda_cache_copy_pages(cache, bad)
     assert seen == []
+
+
+def test_counts_and_kinds_are_not_cut_off_either(monkeypatch, lib):
+    cache = veda.Cache(4, 16, 2, 64, torch.float32, device="cpu")
+    batch = veda.CacheBatch(torch.zeros(1, 4096, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), 3)
+    assert veda.veda_cache_attn_workspace_bytes(cache, batch, 4, 3) > 0
+    for q_heads, rows in (((1 << 32) + 4, 3), (4, (1 << 32) + 3)):
+        with pytest.raises(veda.VedaError, match="32 bits"):
+            veda.veda_cache_attn_workspace_bytes(cache, batch, q_heads, rows)
+    monkeypatch.setattr(veda, "load", lambda: pytest.fail("the library was called"))
+    for more in (dict(pairs=1 << 32), dict(scaling=1 << 32)):
+        with pytest.raises(veda.VedaError, match="32 bits"):
+            veda.Rope(64, 64, **more)
