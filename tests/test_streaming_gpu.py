@@ -1032,3 +1032,34 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for i, o in enumerate(got):
         assert torch.equal(o[:3], calls[i % 2][1])
+
+
+@pytest.mark.parametrize("dtype,d,seqs,new,past", [
+    (BF16, 128, 2, 1, 200), (BF16, 64, 300, 1, 90), (F32, 128, 2, 3, 300), (F32, 64, 40, 1, 300), (F32, 128, 2, 40, 100), (F32, 128, 2, 100, 1500),
+    (F32, 64, 1, 3, 6000), (BF16, 64, 2, 33, 1200), (BF16, 128, 3, 90, 90)])
+def test_every_form_of_the_attention_captured(dtype, d, seqs, new, past):
+    # short and shared walks of few and of many rows; those that ask for more LDS than a launch has without asking among them
+    t = Setup([new] * seqs, [past] * seqs, 4, 2, d, dtype, page=32, seed=39)
+    ws = torch.empty(veda.veda_cache_attn_workspace_bytes(t.cache, t.batch, 4, t.rows), dtype=torch.uint8, device=dev())
+    q, out, lse = t.q.clone(), torch.zeros((t.rows, 4, d), dtype=dtype, device=dev()), torch.zeros((4, t.rows), device=dev())
+
+    def call():
+        veda.veda_cache_attn_fwd(t.cache, t.batch, q, 0.1, window=past - 7, sinks=9, out=out, lse=lse, workspace=ws)
+
+    call()
+    torch.cuda.synchronize()
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+        call()
+    for i in range(3):
+        q.copy_(normal(q.shape, dtype, 60 + i))
+        t.batch.kv_len.copy_(torch.tensor([past + new - 5 * i] * seqs, dtype=torch.int32))
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        out.zero_()
+        lse.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(got_lse, lse) and bool(torch.isfinite(got).all()) and bool(got.float().abs().sum() > 0)
