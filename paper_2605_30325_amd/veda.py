@@ -1013,12 +1013,14 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
     if rope is None and (q.data_ptr() % 16 or any(n > 1 and s * es % 16 for n, s in ((q.shape[0], sq.n), (q.shape[1], sq.h)))):
         raise VedaError(VEDA_ERR_UNSUPPORTED, w, "rows of q must begin at multiples of 16 bytes")
     need = veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])
-    if "out" in b:
-        out, ws = b["out"], b["ws"]
-        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or ws.numel() < need:
-            _refuse(w, "these buffers were made for a call of other sizes")
-    else:
-        out, ws = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(need, dtype=torch.uint8, device=q.device)
+    out, ws = b.get("out"), b.get("ws")
+    if (out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device) or
+            ws is not None and ws.numel() * ws.element_size() < need):
+        _refuse(w, "these buffers were made for a call of other sizes")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
     turned = None
     if rope is not None:
         turned = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))

@@ -489,6 +489,20 @@ def test_a_later_call_of_a_step_that_does_not_fit_its_buffers_appends_nothing(mo
     assert rec.calls == [] and b.keys() == held.keys() and all(b[x] is held[x] for x in held)
 
 
+def test_some_buffers_of_a_step_may_be_the_callers(monkeypatch):
+    rec, step = _step(monkeypatch)
+    for mine in (dict(out=torch.zeros(3, 4, 64)), dict(ws=torch.empty(80, dtype=torch.uint8)), dict(ws=torch.empty(16))):
+        b = dict(mine)
+        out, _ = step(buffers=b)
+        assert out is b["out"] and set(b) == {"out", "ws"} and all(b[x] is mine[x] for x in mine)
+        assert step(buffers=b)[0] is out
+    rec.calls = []
+    for small in (dict(ws=torch.empty(63, dtype=torch.uint8)), dict(out=torch.zeros(3, 4, 64).bfloat16()), dict(out=torch.zeros(2, 4, 64))):
+        with pytest.raises(veda.VedaError, match="other sizes"):
+            step(buffers=dict(small))
+    assert rec.calls == []
+
+
 def test_numbers_are_not_cut_off_at_32_bits(lib):
     book = veda.Pages(8, 16, 2, 4)
     book.extend(0, 20)
