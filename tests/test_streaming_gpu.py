@@ -202,6 +202,35 @@ def test_rope_gradient_through_autograd(dtype, transpose):
     assert torch.equal(second, veda.veda_rope_apply(rope, normal((b, n, h, 64), dtype, 9).transpose(1, 2), pos, transpose=transpose))
 
 
+def test_rope_and_its_gradient_captured():
+    # leaves of the graph's own: no eager graph of theirs lives while it is captured
+    rope = make_rope(64, (64,), True)
+    pos = torch.arange(33, dtype=torch.int32, device=dev())
+    g = normal((2, 3, 33, 64), BF16, 1)
+
+    def both(x, g):
+        y = veda.veda_rope_apply(rope, x, pos)
+        return y, torch.autograd.grad(y, x, g)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(normal((2, 3, 33, 64), BF16, 2).requires_grad_(), g)
+    torch.cuda.synchronize()
+    x = normal((2, 3, 33, 64), BF16, 3).requires_grad_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, dx = both(x, g)
+    y = y.detach()
+    for i in range(3):
+        with torch.no_grad():
+            x.copy_(normal(x.shape, BF16, 10 + i))
+        g.copy_(normal(g.shape, BF16, 20 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, veda.veda_rope_apply(rope, x.detach(), pos)) and torch.equal(dx, veda.veda_rope_apply(rope, g, pos, transpose=True))
+
+
 def test_rope_into_a_given_tensor_has_no_graph():
     rope = make_rope(64, (64,), True)
     x, pos = normal((1, 2, 5, 64), F32, 0).requires_grad_(), torch.arange(5, dtype=torch.int32, device=dev())
