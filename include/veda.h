@@ -464,10 +464,12 @@ typedef struct { int32_t block, window, sinks; } veda_visible;
  *            allowed then); contents undefined after.  Calls that may overlap need one each.
  * bf16: products on bf16 MFMA with fp32 accumulation, softmax in fp32 (logits scaled there, Q is not rounded again).  P V takes P in two
  * bf16 parts (2^-15 of a weight off at most) where no sequence has more than 32 rows of a key head, min(max_new, rows) * q_heads /
- * kv_heads; in larger blocks P is rounded to bf16 once (2^-8).  f32: products on fp32 MFMA.  Values behind a sequence's end, in holes and at keys that a row does not see
- * do not reach that row, whatever they are (infinities and NaN too).  One that is not finite at a key that a row sees makes that row's
- * channel infinite (NaN where both signs or a NaN are seen); where the key's weight is less than 2^-100 of the row's largest it
- * may be NaN instead (a weight of 0 times infinity). */
+ * kv_heads; in larger blocks P is rounded to bf16 once (2^-8).  f32: products on fp32 MFMA.
+ * Values behind a sequence's end, in holes and at keys that a row does not see do not reach that row, whatever they are (infinities and
+ * NaN too).  One that is not finite at a key that a row sees makes that row's channel infinite (NaN where both signs or a NaN are
+ * seen); where the key's weight is less than 2^-100 of the row's largest it may be NaN instead (a weight of 0 times infinity).
+ * How a call is cut up follows the most rows that a sequence may have and the most keys that max_pages has room for, for all sequences
+ * alike: a table much wider than its sequences, or single tokens beside long prompts, cost time (two calls on the same cache are fine). */
 size_t veda_cache_attn_workspace_bytes(const veda_cache*, const veda_cache_batch*, int32_t q_heads);
 veda_status veda_cache_attn_fwd(const veda_cache*, const veda_cache_batch*, int32_t q_heads, const void* q, veda_strides sq,
                                 float softmax_scale, veda_visible visible, void* out, veda_strides so, float* lse,

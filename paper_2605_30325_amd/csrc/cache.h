@@ -50,7 +50,7 @@ __device__ __forceinline__ SeqRows seq_rows(const CacheArgs& c, int s) {
 
 // Work items: every sequence's rows in blocks (of `size`, where a token counts as `group` rows), sequence by sequence.  Only the
 // device knows the sequences' lengths; a grid of the longest's blocks for each of them is mostly empty where they are ragged, and an empty
-// workgroup costs its launch: prompts of 4096 rows and less, 8192 workgroups of which 4176 empty, 527 us instead
+// workgroup costs its launch: prompts of 4096 rows and less, 8192 workgroups of which 4168 empty, 527 us instead
 // of 352 with the items numbered as here.  Returns false for numbers beyond the last item.
 struct RowBlock { int seq, block, blocks; SeqRows rows; };   // block of blocks of its sequence
 __device__ __forceinline__ bool find_block(const CacheArgs& c, int group, int size, int item, RowBlock& out) {

@@ -28,13 +28,16 @@ static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t 
         const int64_t span = (int64_t)vis.window + vis.sinks + (vis.block ? vis.block : 0) + kAttnRows;
         keys = keys < span ? keys : span;
     }
+    // A batch is cut in one way, by the most rows that a sequence may have and the most keys that the table's width holds: a single token beside a
+    // long prompt is a block of 128 rows (512 rows on 8192 keys and 63 ragged tokens 249 us, 98 and 186 apart; 4096 rows and a token on
+    // 131,101 keys 2252 us, 135 and 105 apart: such are better two calls).
     // Shared out evenly where a block can have more keys than a workgroup's least part is worth and the blocks are too few to level out by
     // themselves: in a few rounds of workgroups the last one, or the longest, leaves compute units idle.  Every workgroup then counts
     // through all blocks, 64 at a time: up to 1024 of 16 or 32 rows, which are a sequence each, 256 of 128 rows.  Those are left as they are
     // where a workgroup for each fills four fifths of a round or comes in several rounds, and where a block's walk is not long against
     // what counting and joining take, 10-20 us and, in bf16, more the more blocks there are (d = 128, us without / with: 256 rows of 4 heads on
     // 456 keys 16 / 19, 756 21 / 20, 3756 72 / 23, 1024 rows of 12 heads, causal, on 1524 keys 38 / 40, 2524 56 / 44, 2133 rows of 12 on
-    // 3633 keys 72 / 84, 1280 rows on 34,000 530 / 250, 3840 872 / 734, 4680 985 / 1021; fp32, 100 rows of 12 on 160 keys 28 / 30, 200 38 / 30, 300 51 /
+    // 3633 keys 72 / 84, 1280 rows on 34,000 530 / 278-304 from box to box, 3840 872 / 734, 4680 985 / 1021; fp32, 100 rows of 12 on 160 keys 28 / 30, 200 38 / 30, 300 51 /
     // 30, 449 rows on 2000 302 / 63).
     const int64_t fit = few ? attn_keys_workers(bf16, c->head_dim) : attn_rows_workers(bf16), groups = uniform * c->kv_heads;
     // Few rows: long walks wait for memory, so eight waves a workgroup go through short caches about as fast as all that the card can hold, and

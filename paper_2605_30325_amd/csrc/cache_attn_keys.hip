@@ -10,8 +10,8 @@
 // Long caches are shared out evenly.  The tiles of all sequences lie in one row of numbers; each of the waves that run at once takes one key
 // head of an equal part of it, whatever sequences that cuts, and the heads of a part are neighbours: they read the same pages at the same
 // time, which is worth a tenth of the bandwidth.  The pieces of a cut sequence go to the workspace as unfinished sums, at most two a wave,
-// and cache_attn_join_parts_kernel puts them together.  d = 128, bf16, 8 key heads: 64 caches of 8192 keys 353 us (6.1 TB/s); 64 of 1..8192
-// keys 195 us (5.5 TB/s; a workgroup for each sequence and head waits for the longest: 208-235); one of 131,101 keys 105 us (5.1 TB/s), of
+// and cache_attn_join_parts_kernel puts them together.  d = 128, bf16, 8 key heads: 64 caches of 8192 keys 353-371 us from box to box (5.8-6.1 TB/s); 64 of 1..8192
+// keys 192-196 us (5.5 TB/s; a workgroup for each sequence and head waits for the longest: 208-235); one of 131,101 keys 105 us (5.1 TB/s), of
 // 400,001 283 us (5.8).
 #include "cache_attn.h"
 

@@ -5,15 +5,16 @@
 // its accumulators run over keys, the running maximum and sum of the softmax stay in registers, and P^T is the second product's operand
 // as it stands.  The reference of the exponentials follows the maximum only when that has outgrown it by 2^8: any reference gives the same
 // quotient.  Logits are scaled in fp32 on their way into the exponential, so Q is not rounded again; P is rounded to bf16 for its product
-// (half a step, 2^-8 of each weight, and independent from key to key), l sums the weights before that.
+// (half a step, 2^-8 of each weight, and independent from key to key; a second part, as few rows have it, would be half as many matrix
+// instructions again where these bound the kernel), l sums the weights before that.
 //
 // A workgroup takes 128 rows, 32 a wave; its four waves load a tile of keys together (straight into LDS, one tile ahead, 64 KB for two
 // tiles of 64 keys at d = 128, so two workgroups to a compute unit) and each attends to all of it.  K and V lie token by token as they
 // were appended: rows of K are operands as they stand, V is transposed by gfx950's transposing LDS reads.
 //
-// What bounds it: the matrix cores, and the power they draw.  4680 rows x 12 heads on 34,320 keys, d = 128, bf16: 0.91-0.95 ms from box to box =
-// 1.04-1.09 PFLOP/s (a large matrix product reaches 1.22); matrix pipes 55 % busy at 1.87 GHz, 63 % on the compute units that hold two workgroups
-// (444 on 512 places).  Prompts of 1..4096 tokens, G = 4, window 1024: 0.32 ms = 0.81 PFLOP/s; about 15 tiles of 64 keys that all rows see, three that
+// What bounds it: the matrix cores, and the power they draw.  4680 rows x 12 heads on 34,320 keys, d = 128, bf16: 0.90-0.95 ms from box to box =
+// 1.04-1.10 PFLOP/s (a large matrix product reaches 1.22); matrix pipes 55 % busy at 1.9 GHz, 63 % on the compute units that hold two workgroups
+// (444 on 512 places).  Prompts of 1..4096 tokens, G = 4, window 1024: 0.30-0.33 ms = 0.79-0.87 PFLOP/s; about 15 tiles of 64 keys that all rows see, three that
 // some do, and as long again as two of them for the set-up and the results.  fp32 (v_mfma_f32_32x32x2_f32): 2464 rows x 12 heads on 2000 keys, causal, 0.35 ms,
 // matrix pipes 73 % busy, 102 TFLOP/s on visible keys of the 154 that a large product reaches.
 #include "cache_attn.h"
