@@ -695,12 +695,12 @@ def _stepped(case, st):
         if not 0 <= s < len(length) or s in have_left:
             kept.append(None)
             continue
+        have_left.add(s)
         keep = min(keep, length[s])
         fits = 0 <= grow <= limit and keep + grow <= width * page and 0 <= a <= b <= keep
         if not fits or (grow and keep % page and table[s, keep // page] < 0):
             kept.append(None)
             continue
-        have_left.add(s)
         kept.append(keep)
         for x in list(range(-(-keep // page), -(-length[s] // page))) + list(range(-(-a // page), b // page)):
             if table[s, x] >= 0:
