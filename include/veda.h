@@ -479,6 +479,39 @@ veda_status veda_cache_attn_fwd(const veda_cache*, const veda_cache_batch*, int3
  * launch, up to 448 of them.  They are read before the call returns: a captured call copies the same pages when it is replayed. */
 veda_status veda_cache_copy_pages(const veda_cache*, const int32_t* pairs, int64_t n, void* stream);
 
+/* ---- a cache held in 4 bits ------------------------------------------------------------------------------------------
+ * The cache of one layer with every 32 channels of a row as 32 codes of 4 bits and a power of two, 4.25 bits a value:
+ *   value = +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^(s - 127),   code = 8 * sign + number of the magnitude,   s = a byte for the 32 channels.
+ * Rounding (veda_packed_append): 2^(s - 127) is the least power with max|x| < 7 * 2^(s - 127), s within 2..252, and a code the nearest of
+ * the eight (ties to the even number, beyond 6 is 6, the sign is kept, of zeros too): off by 2^(s - 127) at most, 2/7 of the block's largest
+ * magnitude (2^126 from 7 * 2^125 on).  32 channels with one that is not finite: s = 255 and codes 0, which stand for NaN.
+ * A page holds, for every key head, the codes [page_tokens][head_dim / 2], channel 2i in the low and 2i + 1 in the high half of a byte,
+ * and behind them the bytes s [page_tokens][head_dim / 32].  All conventions of the cache above hold. */
+typedef struct {
+    int32_t pages;                /* pages of each pool                                                             */
+    int32_t page_tokens;          /* 16, 32, 64, 128 or 256                                                         */
+    int32_t kv_heads, head_dim;   /* kv_heads 1..1024, head_dim 64 or 128                                           */
+    veda_dtype dtype;             /* of the rows that go in and of the queries and results                          */
+    int64_t page_stride;          /* bytes from a page to the next, a multiple of 16; 0: pages lie close            */
+    void *k, *v;                  /* device, 16-byte aligned                                                        */
+} veda_packed_cache;
+/* veda_cache_append with rounding.  K is turned in 64 bits and rounded once, to 4 bits: no code depends on an order of operations.
+ * k_out, v_out  optional (each may be NULL), [rows][kv_heads][head_dim] of the cache's dtype: the new rows as the cache now stands for
+ *            them (bf16 holds such values exactly); not to overlap k and v (refused where they begin there).  Rows that write nothing into
+ *            the cache are left as they were. */
+veda_status veda_packed_append(const veda_packed_cache*, const veda_cache_batch*, const void* k, veda_strides sk, const void* v,
+                               veda_strides sv, int32_t q_heads, const void* q, veda_strides sq, void* q_out, veda_strides sq_out,
+                               const veda_rope* rope, const int32_t* positions, void* k_out, veda_strides sk_out, void* v_out,
+                               veda_strides sv_out, void* stream);
+/* veda_cache_attn_fwd over what the cache stands for: the same masks, results and errors.  A page's bytes may be anything where no row
+ * sees them.  bf16: a channel whose 32 are NaN at a key that a row sees is NaN. */
+size_t veda_packed_attn_workspace_bytes(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads);
+veda_status veda_packed_attn_fwd(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads, const void* q, veda_strides sq,
+                                 float softmax_scale, veda_visible visible, void* out, veda_strides so, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+/* veda_cache_copy_pages for the pools of a packed cache. */
+veda_status veda_packed_copy_pages(const veda_packed_cache*, const int32_t* pairs, int64_t n, void* stream);
+
 /* Which page belongs to which sequence: a host object, no device memory, not thread-safe.  Pages are counted: a forked sequence
  * shares its parent's pages, and the calls that come to write a shared page or move one tell which pages to copy.
  * Free pages are given out lowest number first.
@@ -501,6 +534,53 @@ veda_status veda_pages_truncate(veda_pages*, int32_t seq, int32_t tokens);  /* k
 veda_status veda_pages_evict(veda_pages*, int32_t seq, int32_t first, int32_t last);
 /* Moves pages down so that those in use are the lowest numbers: one copy for each page moved, no page copied to twice. */
 veda_status veda_pages_compact(veda_pages*, int32_t* copies, int32_t capacity, int32_t* n_copies);
+
+/* The page book on the GPU, for steps that the host does not look at (a captured loop): the same rules without shared pages.  An object
+ * in the caller's memory; all zeros are an empty book. */
+typedef struct {
+    int32_t pages;                /* up to 2^19                                                                     */
+    int32_t page_tokens;          /* max_pages * page_tokens up to 2^30                                             */
+    int32_t max_seqs, max_pages;  /* sequences (up to 8192), and pages of one                                       */
+    int32_t* table;               /* device [max_seqs][max_pages]: pages of a sequence; what lies behind its last page is not read */
+    int32_t* length;              /* device [max_seqs]: tokens                                                      */
+    uint32_t* used;               /* device [(pages + 31) / 32]: bit p % 32 of word p / 32 is set while page p is held */
+} veda_device_pages;
+/* What a step asks for.  Request i is about sequence seq[i]: it keeps its first keep[i] tokens, gives back the pages that lie wholly in
+ * [evict[i][0], evict[i][1]) of those, and grows by grow[i] tokens.  All arrays are read on the device. */
+typedef struct {
+    int32_t seqs;                 /* requests, 0..8192                                                              */
+    int32_t rows;                 /* rows that there is room for, >= 0: positions, row_seq and slots have as many   */
+    int32_t max_new;              /* no request grows by more than this, >= 0                                       */
+    int32_t axes;                 /* 1: a row's position is its token's number; 3: (t, h, w) = (p / (H W), p / W % H, p % W) */
+    int32_t frame_h, frame_w;     /* H and W, >= 1 (axes 3)                                                         */
+    const int32_t* seq;           /* device [seqs], or NULL: request i is about sequence i                          */
+    const int32_t* keep;          /* device [seqs], or NULL: all tokens stay (as where keep is no less than the length) */
+    const int32_t* evict;         /* device [seqs][2], or NULL: nothing is evicted                                  */
+    const int32_t* grow;          /* device [seqs]                                                                  */
+} veda_step;
+/* What the calls of the step need (veda_cache_batch; rows and positions of the appends), written for every request; any of the last
+ * three may be NULL.  Rows behind the last request's are left as they were. */
+typedef struct {
+    int64_t table_stride;         /* entries from a request to the next, >= max_pages                               */
+    int32_t* page_table;          /* device [seqs][table_stride]: the sequence's pages, -1 behind its last one      */
+    int32_t* kv_len;              /* device [seqs]: tokens, the new ones among them                                 */
+    int32_t* q_start;             /* device [seqs + 1]: first row of every request                                  */
+    int32_t* status;              /* device [seqs]: VEDA_STEP_*                                                     */
+    int32_t* positions;           /* device [rows][axes]                                                            */
+    int32_t* row_seq;             /* device [rows]: the row's request                                               */
+    int64_t* slots;               /* device [rows]: page * page_tokens + place in it                                */
+} veda_step_tables;
+enum {
+    VEDA_STEP_SERVED = 0,
+    VEDA_STEP_REFUSED = 1,        /* changes nothing, and has kv_len 0 and no rows: no such sequence (padding of a batch: -1), one that an
+                                   * earlier request is about, grow outside 0..max_new or beyond max_pages pages, evict not within the tokens
+                                   * kept, or growing in an evicted page                                            */
+    VEDA_STEP_NO_ROOM = 2         /* cut and evicted, but not grown                                                 */
+};
+/* First all requests give back (whether they are served or not), then they grow in their order, from the lowest free pages on; the first for
+ * which pages or rows do not suffice and all behind it that would grow have no room.  The call is two kernels, or one where little is written,
+ * and equal inputs give equal bytes; calls on the same book must not overlap. */
+veda_status veda_pages_step(const veda_device_pages*, const veda_step*, const veda_step_tables*, void* stream);
 
 const char* veda_status_string(veda_status);
 /* Text of the last HIP error seen by this thread inside the library ("" if none). */

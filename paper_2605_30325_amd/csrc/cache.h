@@ -21,6 +21,9 @@ CacheArgs cache_args(const veda_cache* c, const veda_cache_batch* b);
 // An axis of one entry has no stride, whatever it is given as: s.n or s.h becomes 0.
 veda_status check_rows(const veda_cache* c, int32_t rows, int32_t heads, const void* p, veda_strides& s, bool distinct);
 
+// Copies pages of `bytes` (a multiple of 16) inside both pools; see veda_cache_copy_pages.
+veda_status copy_pages(char* k, char* v, int64_t page_b, int64_t bytes, int32_t pages, const int32_t* pairs, int64_t n, hipStream_t s, const char* what);
+
 #if defined(__HIPCC__)
 
 // Sum over the lanes up to and with this one, by DPP; all 64 lanes take part.

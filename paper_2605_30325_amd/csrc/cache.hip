@@ -137,6 +137,64 @@ template <int N> __global__ __launch_bounds__(256) void copy_pages_kernel(CopyAr
         if (c0 + j * 256 < a.chunks) store_through(dst + c0 + j * 256, x[j]);
 }
 
+veda_status copy_pages(char* k, char* v, int64_t page_b, int64_t bytes, int32_t pages, const int32_t* pairs, int64_t n, hipStream_t s, const char* what) {
+    if (n < 0 || (n > 0 && !pairs)) return VEDA_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < 2 * n; ++i)
+        if (pairs[i] < 0 || pairs[i] >= pages) return VEDA_ERR_INVALID_ARG;
+    if (n == 0) return VEDA_OK;
+    CopyArgs<kCopyPairs> a;
+    a.k = k; a.v = v; a.page_b = page_b;
+    a.chunks = (int32_t)(bytes / 16);
+    const unsigned gx = (unsigned)((a.chunks + 256 * kCopyChunks - 1) / (256 * kCopyChunks));
+    // A launch ends where the next pair touches what its pairs write, or writes what they read: stream order then gives the
+    // order of the list.  Long lists keep a note for every page (bit 0 read, bit 1 written by the open launch), short ones look back.
+    std::vector<uint8_t> note;
+    if (n > kCopyPairsShort) {
+        try {
+            note.assign((size_t)pages, 0);
+        } catch (const std::exception&) {
+            return hip_fail(hipErrorOutOfMemory, what);
+        }
+    }
+    int m = 0;
+    auto launch = [&]() -> veda_status {
+        if (m == 0) return VEDA_OK;
+        if (m <= kCopyPairsShort) {
+            CopyArgs<kCopyPairsShort> b;
+            b.k = a.k; b.v = a.v; b.page_b = a.page_b; b.chunks = a.chunks;
+            for (int i = 0; i < kCopyPairsShort; ++i)
+                for (int j = 0; j < 2; ++j) b.pair[i][j] = i < m ? a.pair[i][j] : 0;
+            hipLaunchKernelGGL((copy_pages_kernel<kCopyPairsShort>), dim3(gx, (unsigned)m, 2), dim3(256), 0, s, b);
+        } else {
+            hipLaunchKernelGGL((copy_pages_kernel<kCopyPairs>), dim3(gx, (unsigned)m, 2), dim3(256), 0, s, a);
+        }
+        if (!note.empty())
+            for (int i = 0; i < m; ++i) note[a.pair[i][0]] = note[a.pair[i][1]] = 0;
+        m = 0;
+        return launch_status(what);
+    };
+    for (int64_t i = 0; i < n; ++i) {
+        const int32_t from = pairs[2 * i], to = pairs[2 * i + 1];
+        if (from == to) continue;
+        bool touches = m == kCopyPairs;
+        if (!note.empty()) touches = touches || (note[from] & 2) || note[to];
+        else
+            for (int j = 0; j < m; ++j) touches = touches || a.pair[j][1] == from || a.pair[j][1] == to || a.pair[j][0] == to;
+        if (touches) {
+            const veda_status st = launch();
+            if (st != VEDA_OK) return st;
+        }
+        a.pair[m][0] = from;
+        a.pair[m][1] = to;
+        ++m;
+        if (!note.empty()) {
+            note[from] |= 1;
+            note[to] |= 2;
+        }
+    }
+    return launch();
+}
+
 }  // namespace veda
 
 extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_batch* b, const void* k, veda_strides sk, const void* v,
@@ -194,63 +252,9 @@ extern "C" veda_status veda_cache_append(const veda_cache* c, const veda_cache_b
 }
 
 extern "C" veda_status veda_cache_copy_pages(const veda_cache* c, const int32_t* pairs, int64_t n, void* stream) {
-    veda_status st = veda::check_cache(c);
+    const veda_status st = veda::check_cache(c);
     if (st != VEDA_OK) return st;
-    if (n < 0 || (n > 0 && !pairs)) return VEDA_ERR_INVALID_ARG;
-    for (int64_t i = 0; i < 2 * n; ++i)
-        if (pairs[i] < 0 || pairs[i] >= c->pages) return VEDA_ERR_INVALID_ARG;
-    if (n == 0) return VEDA_OK;
     const veda::CacheArgs ca = veda::cache_args(c, nullptr);
-    veda::CopyArgs<veda::kCopyPairs> a;
-    a.k = ca.k; a.v = ca.v; a.page_b = ca.page_b;
-    a.chunks = (int32_t)((int64_t)c->kv_heads * c->page_tokens * c->head_dim * (c->dtype == VEDA_BF16 ? 2 : 4) / 16);
-    const unsigned gx = (unsigned)((a.chunks + 256 * veda::kCopyChunks - 1) / (256 * veda::kCopyChunks));
-    const hipStream_t s = (hipStream_t)stream;
-    // A launch ends where the next pair touches what its pairs write, or writes what they read: stream order then gives the
-    // order of the list.  Long lists keep a note for every page (bit 0 read, bit 1 written by the open launch), short ones look back.
-    std::vector<uint8_t> note;
-    if (n > veda::kCopyPairsShort) {
-        try {
-            note.assign((size_t)c->pages, 0);
-        } catch (const std::exception&) {
-            return veda::hip_fail(hipErrorOutOfMemory, "veda_cache_copy_pages");
-        }
-    }
-    int m = 0;
-    auto launch = [&]() -> veda_status {
-        if (m == 0) return VEDA_OK;
-        if (m <= veda::kCopyPairsShort) {
-            veda::CopyArgs<veda::kCopyPairsShort> b;
-            b.k = a.k; b.v = a.v; b.page_b = a.page_b; b.chunks = a.chunks;
-            for (int i = 0; i < veda::kCopyPairsShort; ++i)
-                for (int j = 0; j < 2; ++j) b.pair[i][j] = i < m ? a.pair[i][j] : 0;
-            hipLaunchKernelGGL((veda::copy_pages_kernel<veda::kCopyPairsShort>), dim3(gx, (unsigned)m, 2), dim3(256), 0, s, b);
-        } else {
-            hipLaunchKernelGGL((veda::copy_pages_kernel<veda::kCopyPairs>), dim3(gx, (unsigned)m, 2), dim3(256), 0, s, a);
-        }
-        if (!note.empty())
-            for (int i = 0; i < m; ++i) note[a.pair[i][0]] = note[a.pair[i][1]] = 0;
-        m = 0;
-        return veda::launch_status("veda_cache_copy_pages");
-    };
-    for (int64_t i = 0; i < n; ++i) {
-        const int32_t from = pairs[2 * i], to = pairs[2 * i + 1];
-        if (from == to) continue;
-        bool touches = m == veda::kCopyPairs;
-        if (!note.empty()) touches = touches || (note[from] & 2) || note[to];
-        else
-            for (int j = 0; j < m; ++j) touches = touches || a.pair[j][1] == from || a.pair[j][1] == to || a.pair[j][0] == to;
-        if (touches) {
-            st = launch();
-            if (st != VEDA_OK) return st;
-        }
-        a.pair[m][0] = from;
-        a.pair[m][1] = to;
-        ++m;
-        if (!note.empty()) {
-            note[from] |= 1;
-            note[to] |= 2;
-        }
-    }
-    return launch();
+    const int64_t bytes = (int64_t)c->kv_heads * c->page_tokens * c->head_dim * (c->dtype == VEDA_BF16 ? 2 : 4);
+    return veda::copy_pages(ca.k, ca.v, ca.page_b, bytes, c->pages, pairs, n, (hipStream_t)stream, "veda_cache_copy_pages");
 }

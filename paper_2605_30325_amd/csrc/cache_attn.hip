@@ -1,6 +1,7 @@
 // Attention of the newest rows of every sequence over its paged cache, O = softmax(q K^T scale over the visible keys) V: the C entry points
 // and how a call is cut into workgroups.
 #include "cache_attn.h"
+#include "packed.h"
 
 namespace veda {
 
@@ -12,12 +13,12 @@ struct AttnCut {
     int32_t part_rows;
     int64_t items;
 };
-static AttnCut attn_cut(const veda_cache* c, const veda_cache_batch* b, int32_t q_heads, veda_visible vis) {
+static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch* b, int32_t q_heads, veda_visible vis) {
     AttnCut cut{};
     const int64_t max_new = b->max_new < b->rows ? b->max_new : b->rows, group = q_heads / c->kv_heads, rows = max_new * group;
-    const bool bf16 = c->dtype == VEDA_BF16, few = rows <= 32;
+    const bool bf16 = c->dtype == VEDA_BF16, few = rows <= 32 && !packed;
     const int d = c->head_dim;
-    cut.size = rows <= 16 ? 16 : rows <= 32 ? 32 : kAttnRows;
+    cut.size = !few ? kAttnRows : rows <= 16 ? 16 : 32;
     // Even, so that the sums of a block, part_rows * (d + 2) floats, are whole 16 bytes: the list of cuts behind them is read 16 bytes at a time.
     cut.part_rows = few ? cut.size : rows < kAttnRows ? (int32_t)(rows + 1) & ~1 : kAttnRows;
     const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
@@ -67,11 +68,55 @@ static veda_status check_heads(const veda_cache* c, int32_t q_heads) {
     return q_heads / c->kv_heads > 32 ? VEDA_ERR_UNSUPPORTED : VEDA_OK;
 }
 
+// Workspace of a call on a cache of these rows (c), checked already.
+static size_t attn_bytes(const veda_cache* c, bool packed, const veda_cache_batch* b, int32_t q_heads) {
+    if (check_batch(c, b) != VEDA_OK || check_heads(c, q_heads) != VEDA_OK) return 0;
+    return attn_workspace(c, attn_cut(c, packed, b, q_heads, veda_visible{0, 0, 0}));
+}
+// The call on a cache of these rows, checked already; pools: what its kernels see.
+static veda_status attend(const veda_cache* c, const CacheArgs& pools, bool packed, const veda_cache_batch* b, int32_t q_heads, const void* q, veda_strides sq,
+                          float softmax_scale, veda_visible vis, void* out, veda_strides so, float* lse, void* workspace, size_t workspace_bytes,
+                          hipStream_t s) {
+    veda_status st = check_heads(c, q_heads);
+    if (st != VEDA_OK) return st;
+    if (!(softmax_scale > 0.0f) || !(softmax_scale < INFINITY)) return VEDA_ERR_INVALID_ARG;
+    constexpr int32_t kMost = 1 << 30;
+    if (vis.block < 0 || vis.window < 0 || vis.sinks < 0 || vis.block > kMost || vis.window > kMost || vis.sinks > kMost) return VEDA_ERR_INVALID_ARG;
+    if (b->seqs == 0 || b->rows == 0 || b->max_new == 0) return VEDA_OK;
+    st = check_rows(c, b->rows, q_heads, q, sq, false);
+    if (st == VEDA_OK) st = check_rows(c, b->rows, q_heads, out, so, true);
+    if (st != VEDA_OK) return st;
+    if (q == out) return VEDA_ERR_INVALID_ARG;   // a row may be read after its result has been written
+    const AttnCut cut = attn_cut(c, packed, b, q_heads, vis);
+    const size_t need = attn_workspace(c, cut);
+    if (need > 0) {
+        if (!workspace) return VEDA_ERR_INVALID_ARG;
+        if (workspace_bytes < need) return VEDA_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return VEDA_ERR_UNSUPPORTED;
+    }
+    const int es = c->dtype == VEDA_BF16 ? 2 : 4;
+    CacheAttnArgs a;
+    a.c = pools;
+    a.q = (const char*)q; a.out = (char*)out; a.lse = lse;
+    a.sq_h = sq.h * es; a.sq_n = sq.n * es; a.so_h = so.h * es; a.so_n = so.n * es;
+    a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
+    a.items = cut.items; a.per_seq = cut.per_seq; a.workers = cut.workers; a.part_rows = cut.part_rows;
+    a.block = vis.block; a.window = vis.window; a.sinks = vis.window ? vis.sinks : 0;
+    a.scale_log2 = softmax_scale * kLog2e;
+    a.part = (float*)workspace;
+    const bool bf16 = c->dtype == VEDA_BF16;
+    // a grid has less than 2^32 threads: 512 to a workgroup, or to eight rows of a query head
+    if (cut.items * c->kv_heads >= (int64_t)1 << 23 || (int64_t)a.c.max_new * a.group >= (int64_t)1 << 30 ||
+        (cut.workers && cut.size < kAttnRows && (int64_t)b->rows * q_heads >= (int64_t)1 << 26))
+        return VEDA_ERR_UNSUPPORTED;
+    if (packed) return launch_packed_attn_rows(a, bf16, c->head_dim, s);
+    return cut.size < kAttnRows ? launch_cache_attn_keys(a, bf16, c->head_dim, s) : launch_cache_attn_rows(a, bf16, c->head_dim, s);
+}
+
 }  // namespace veda
 
 extern "C" size_t veda_cache_attn_workspace_bytes(const veda_cache* c, const veda_cache_batch* b, int32_t q_heads) {
-    if (veda::check_cache(c) != VEDA_OK || veda::check_batch(c, b) != VEDA_OK || veda::check_heads(c, q_heads) != VEDA_OK) return 0;
-    return veda::attn_workspace(c, veda::attn_cut(c, b, q_heads, veda_visible{0, 0, 0}));
+    return veda::check_cache(c) == VEDA_OK ? veda::attn_bytes(c, false, b, q_heads) : 0;
 }
 
 extern "C" veda_status veda_cache_attn_fwd(const veda_cache* c, const veda_cache_batch* b, int32_t q_heads, const void* q, veda_strides sq,
@@ -79,38 +124,25 @@ extern "C" veda_status veda_cache_attn_fwd(const veda_cache* c, const veda_cache
                                            void* workspace, size_t workspace_bytes, void* stream) {
     veda_status st = veda::check_cache(c);
     if (st == VEDA_OK) st = veda::check_batch(c, b);
-    if (st == VEDA_OK) st = veda::check_heads(c, q_heads);
     if (st != VEDA_OK) return st;
-    if (!(softmax_scale > 0.0f) || !(softmax_scale < INFINITY)) return VEDA_ERR_INVALID_ARG;
-    constexpr int32_t kMost = 1 << 30;
-    if (vis.block < 0 || vis.window < 0 || vis.sinks < 0 || vis.block > kMost || vis.window > kMost || vis.sinks > kMost) return VEDA_ERR_INVALID_ARG;
-    if (b->seqs == 0 || b->rows == 0 || b->max_new == 0) return VEDA_OK;
-    st = veda::check_rows(c, b->rows, q_heads, q, sq, false);
-    if (st == VEDA_OK) st = veda::check_rows(c, b->rows, q_heads, out, so, true);
+    return veda::attend(c, veda::cache_args(c, b), false, b, q_heads, q, sq, softmax_scale, vis, out, so, lse, workspace, workspace_bytes,
+                        (hipStream_t)stream);
+}
+
+extern "C" size_t veda_packed_attn_workspace_bytes(const veda_packed_cache* c, const veda_cache_batch* b, int32_t q_heads) {
+    if (veda::check_packed(c) != VEDA_OK) return 0;
+    const veda_cache as = veda::packed_rows(c);
+    return veda::attn_bytes(&as, true, b, q_heads);
+}
+
+extern "C" veda_status veda_packed_attn_fwd(const veda_packed_cache* c, const veda_cache_batch* b, int32_t q_heads, const void* q, veda_strides sq,
+                                            float softmax_scale, veda_visible vis, void* out, veda_strides so, float* lse,
+                                            void* workspace, size_t workspace_bytes, void* stream) {
+    veda_status st = veda::check_packed(c);
     if (st != VEDA_OK) return st;
-    if (q == out) return VEDA_ERR_INVALID_ARG;   // a row may be read after its result has been written
-    const veda::AttnCut cut = veda::attn_cut(c, b, q_heads, vis);
-    const size_t need = veda::attn_workspace(c, cut);
-    if (need > 0) {
-        if (!workspace) return VEDA_ERR_INVALID_ARG;
-        if (workspace_bytes < need) return VEDA_ERR_WORKSPACE;
-        if (!veda::aligned16(workspace)) return VEDA_ERR_UNSUPPORTED;
-    }
-    const int es = c->dtype == VEDA_BF16 ? 2 : 4;
-    veda::CacheAttnArgs a;
-    a.c = veda::cache_args(c, b);
-    a.q = (const char*)q; a.out = (char*)out; a.lse = lse;
-    a.sq_h = sq.h * es; a.sq_n = sq.n * es; a.so_h = so.h * es; a.so_n = so.n * es;
-    a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
-    a.items = cut.items; a.per_seq = cut.per_seq; a.workers = cut.workers; a.part_rows = cut.part_rows;
-    a.block = vis.block; a.window = vis.window; a.sinks = vis.window ? vis.sinks : 0;
-    a.scale_log2 = softmax_scale * veda::kLog2e;
-    a.part = (float*)workspace;
-    const bool bf16 = c->dtype == VEDA_BF16;
-    // a grid has less than 2^32 threads: 512 to a workgroup, or to eight rows of a query head
-    if (cut.items * c->kv_heads >= (int64_t)1 << 23 || (int64_t)a.c.max_new * a.group >= (int64_t)1 << 30 ||
-        (cut.workers && cut.size < veda::kAttnRows && (int64_t)b->rows * q_heads >= (int64_t)1 << 26))
-        return VEDA_ERR_UNSUPPORTED;
-    const hipStream_t s = (hipStream_t)stream;
-    return cut.size < veda::kAttnRows ? veda::launch_cache_attn_keys(a, bf16, c->head_dim, s) : veda::launch_cache_attn_rows(a, bf16, c->head_dim, s);
+    const veda_cache as = veda::packed_rows(c);
+    st = veda::check_batch(&as, b);
+    if (st != VEDA_OK) return st;
+    return veda::attend(&as, veda::packed_args(c, b), true, b, q_heads, q, sq, softmax_scale, vis, out, so, lse, workspace, workspace_bytes,
+                        (hipStream_t)stream);
 }

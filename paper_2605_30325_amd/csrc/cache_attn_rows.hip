@@ -18,6 +18,7 @@
 // some do, and as long again as two of them for the set-up and the results.  fp32 (v_mfma_f32_32x32x2_f32): 2464 rows x 12 heads on 2000 keys, causal, 0.35 ms,
 // matrix pipes 73 % busy, 102 TFLOP/s on visible keys of the 154 that a large product reaches.
 #include "cache_attn.h"
+#include "packed.h"
 #include "store.h"
 
 namespace veda {
@@ -395,12 +396,71 @@ template <bool kBf16, int D> struct AttnShape {
     static constexpr int kLds = 2 * kSlot > kOutB ? 2 * kSlot : kOutB;
 };
 
+// A cache held in 4 bits: the tile's segment of a wave comes into its registers, C channels of one row of K and of V to a lane (their codes
+// and the byte of their 32), and is written to the tile in LDS as the values that it stands for, in the places that direct loads would
+// have put them.  Everything behind is as for a cache of such values.
+template <bool kBf16, int D> struct PackedTile {
+    typedef AttnTile<kBf16, D> T;
+    static constexpr int C = T::kSegRows * D / 64, W = C / 8;    // channels, and words of codes
+    uint32_t k[W], v[W];
+    uint32_t ks, vs;
+    __device__ static int row(int lane) { return lane * C / D; }
+    __device__ static int channel(int lane) { return lane * C % D; }
+    // k_at, v_at: the head's place in the page; tok: the segment's first row in it; page: its tokens.
+    __device__ __forceinline__ void load(const char* k_at, const char* v_at, int tok, int log_page, int lane) {
+        const uint32_t code = (uint32_t)(lane * C / 2), scale = (uint32_t)(lane * C / 32);
+        const int64_t at = (int64_t)tok * (D / 2), s_at = ((int64_t)(D / 2) << log_page) + (int64_t)tok * (D / 32);
+        ks = *reinterpret_cast<const uint8_t*>(k_at + s_at + scale);
+        vs = *reinterpret_cast<const uint8_t*>(v_at + s_at + scale);
+        words(k_at + at + code, k);
+        words(v_at + at + code, v);
+    }
+    __device__ static __forceinline__ void words(const char* p, uint32_t (&w)[W]) {
+        if constexpr (W == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+        } else if constexpr (W == 2) {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            w[0] = x.x; w[1] = x.y;
+        } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+    }
+    // to: the segment's first row of K and of V in LDS.  exists: whether the lane's key does; others become zeros, whatever lies there.
+    __device__ __forceinline__ void store(char* k_to, char* v_to, bool exists, int lane) {
+        const int r = row(lane), c0 = channel(lane);
+        const float kp = packed_power(exists ? ks : 127u), vp = packed_power(exists ? vs : 127u);
+        char* kr = k_to + r * T::kRowB;
+        char* vr = v_to + r * T::kRowB;
+        const int kx = T::k_swizzle(r), vx = T::v_swizzle(r);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const uint32_t kw = exists ? k[i] : 0u, vw = exists ? v[i] : 0u;
+            if constexpr (kBf16) {
+                const int c = c0 / 8 + i;
+                *reinterpret_cast<uint4*>(kr + ((c ^ kx) << 4)) = packed_bf16(kw, kp);
+                *reinterpret_cast<uint4*>(vr + ((c ^ vx) << 4)) = packed_bf16(vw, vp);
+            } else {
+                uint4 x[2], y[2];
+                packed_f32(kw, kp, x);
+                packed_f32(vw, vp, y);
+                const int c = c0 / 4 + 2 * i;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    *reinterpret_cast<uint4*>(kr + (((c + j) ^ kx) << 4)) = x[j];
+                    *reinterpret_cast<uint4*>(vr + (((c + j) ^ vx) << 4)) = y[j];
+                }
+            }
+        }
+    }
+};
+
 // Pieces that unfinished sums can come in, at most (see the sharing kernel).
 __device__ __forceinline__ int64_t rows_pieces(const CacheAttnArgs& a) { return 2 * (int64_t)a.workers + a.items * a.c.kv_heads; }
 
 // Tiles t_beg .. t_end - 1 of those that rows r0 .. r_end - 1 of a sequence see, for one key head.  part: where the unfinished sums go,
 // or -1 if these are all the tiles.
-template <bool kBf16, int D>
+template <bool kBf16, int D, bool kPacked>
 __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, int seq, const SeqRows& sr, int r0, int r_end, int head,
                                            const AttnTiles& tiles, int t_beg, int t_end, int64_t part) {
     typedef AttnShape<kBf16, D> Sh;
@@ -441,7 +501,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     const uint32_t k_off0 = (uint32_t)(load_row * kRowB + ((load_c ^ T::k_swizzle(load_row)) << 4));
     const uint32_t v_off0 = (uint32_t)(load_row * kRowB + ((load_c ^ T::v_swizzle(load_row)) << 4));
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const int64_t head_b = (int64_t)head * kRowB << a.c.log_page;
+    const int64_t head_b = (int64_t)head * (kPacked ? D / 2 + D / 32 : kRowB) << a.c.log_page;
     const int page_mask = (1 << a.c.log_page) - 1;
     const int32_t* table = a.c.table + seq * a.c.table_stride;
 
@@ -462,8 +522,14 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         }
     };
     // asks for the wave's segment of tile t, number `at` of the pages looked up
+    PackedTile<kBf16, D> raw;
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
         const int row = wave * T::kSegRows, id = __builtin_amdgcn_readlane(page, at);
+        if constexpr (kPacked) {
+            const int64_t from = id * a.c.page_b + head_b;
+            raw.load(a.c.k + from, a.c.v + from, (tiles.at(t) + row) & page_mask, a.c.log_page, lane);
+            return;
+        }
         const int64_t from = id * a.c.page_b + head_b + ((tiles.at(t) + row) & page_mask) * kRowB;
         const uint32_t to = lds + slot * Sh::kSlot + row * kRowB;
         uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
@@ -521,6 +587,11 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             look_up(t + 1);
             at = 0;
         }
+        if constexpr (kPacked) {
+            const int row = wave * T::kSegRows, key = key0 + row + PackedTile<kBf16, D>::row(lane);
+            char* to = smem + slot * Sh::kSlot + row * kRowB;
+            raw.store(to, to + kKeyTile * kRowB, ((exists >> (row / 16)) & 1u) && key < sr.len, lane);
+        }
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the other slot has been read
         wait_vmcnt<0>();
         asm volatile("" ::: "memory");
@@ -566,7 +637,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             if (some(key, 32, ex)) {
                 const bool full = all(key, 32, ex);
                 attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, full,
-                                     !full && (careful || ex != 3u || key + 32 > sr.len), hh);
+                                     !full && (careful || (!kPacked && (ex != 3u || key + 32 > sr.len))), hh);
             }
         }
         ++t;
@@ -643,7 +714,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
 
 // A workgroup for each (block of rows, key head).  Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of
 // a head meet in few L2 caches.
-template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnArgs a) {
+template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnArgs a) {
     extern __shared__ __align__(1024) char smem[];
     RowBlock rb;
     if (!block_of(a.c, a.group, kAttnRows, a.per_seq, blockIdx.x / a.c.kv_heads, rb)) return;
@@ -652,7 +723,7 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_att
     const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
     const int r_end = min(rows, r0 + kAttnRows);
     const AttnTiles tiles = tiles_seen(a, sr, min(sr.n, a.c.max_new), r0, r_end - 1, AttnShape<kBf16, D>::kKeyTile);
-    rows_piece<kBf16, D>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
+    rows_piece<kBf16, D, kPacked>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
 }
 
 // Where there are few blocks, a workgroup for each leaves compute units idle, so their tiles are dealt out to as many workgroups as fit the
@@ -679,7 +750,7 @@ template <int D> __device__ __forceinline__ int4* rows_cuts(const CacheAttnArgs&
     return reinterpret_cast<int4*>(a.part + rows_pieces(a) * a.part_rows * (D + 2));
 }
 
-template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
+template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
     constexpr int kTile = AttnShape<kBf16, D>::kKeyTile, kPiece = kBf16 ? 1 : 2;
     extern __shared__ __align__(1024) char smem[];
     auto rest_units = [](int tiles) { return tiles ? tiles + kPiece : 0; };
@@ -746,7 +817,7 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256, 2) void cache_att
                 rows_cuts<D>(a)[item * a.c.kv_heads + head] = int4{whole ? 0 : f, first_full, whole ? 0 : q1 - q0 + 1, q0};
             }
             if (again) __syncthreads();   // the last piece's results have left the slots
-            rows_piece<kBf16, D>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
+            rows_piece<kBf16, D, kPacked>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
             again = true;
         }
         now = full ? end : max(now, min(end, next_unit));
@@ -834,15 +905,15 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
     if (a.lse && lane == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(top, lsum);
 }
 
-template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs& a, hipStream_t s) {
+template <bool kBf16, int D, bool kPacked> static veda_status launch_rows(const CacheAttnArgs& a, hipStream_t s, const char* what) {
     typedef AttnShape<kBf16, D> Sh;
-    auto kern = a.workers ? cache_attn_rows_share_kernel<kBf16, D> : cache_attn_rows_kernel<kBf16, D>;
+    auto kern = a.workers ? cache_attn_rows_share_kernel<kBf16, D, kPacked> : cache_attn_rows_kernel<kBf16, D, kPacked>;
     if (Sh::kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds));
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.workers ? a.workers : a.items * a.c.kv_heads)), dim3(256), Sh::kLds, s, a);
-    const veda_status st = launch_status("veda_cache_attn_fwd");
+    const veda_status st = launch_status(what);
     if (st != VEDA_OK || !a.workers) return st;
     hipLaunchKernelGGL((cache_attn_rows_join_kernel<kBf16, D>), dim3((unsigned)(a.items * a.c.kv_heads), (unsigned)((a.part_rows + 3) / 4)), dim3(256), 0, s, a);
-    return launch_status("veda_cache_attn_fwd");
+    return launch_status(what);
 }
 
 // Two workgroups fit a compute unit, by LDS and registers alike.  bf16 shares among so many: one's products run while the other waits.  fp32
@@ -851,9 +922,11 @@ template <bool kBf16, int D> static veda_status launch_rows(const CacheAttnArgs&
 int attn_rows_places() { return 512; }
 int attn_rows_workers(bool bf16) { return bf16 ? 512 : 256; }
 
-veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) {
-    if (bf16) return d == 128 ? launch_rows<true, 128>(a, s) : launch_rows<true, 64>(a, s);
-    return d == 128 ? launch_rows<false, 128>(a, s) : launch_rows<false, 64>(a, s);
+template <bool kPacked> static veda_status launch_rows_any(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s, const char* what) {
+    if (bf16) return d == 128 ? launch_rows<true, 128, kPacked>(a, s, what) : launch_rows<true, 64, kPacked>(a, s, what);
+    return d == 128 ? launch_rows<false, 128, kPacked>(a, s, what) : launch_rows<false, 64, kPacked>(a, s, what);
 }
+veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) { return launch_rows_any<false>(a, bf16, d, s, "veda_cache_attn_fwd"); }
+veda_status launch_packed_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s) { return launch_rows_any<true>(a, bf16, d, s, "veda_packed_attn_fwd"); }
 
 }  // namespace veda

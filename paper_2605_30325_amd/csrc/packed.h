@@ -1,0 +1,41 @@
+// The paged cache held in 4 bits, as its kernels see it, and the checks that its calls share.  Not part of the public ABI.
+//
+// 32 channels are 32 codes of 4 bits (E2M1) and a byte s: gfx950 converts a pair of codes to bf16 or fp32, times 2^(s - 127), in one
+// instruction and exactly (all 16 codes under all 256 bytes agree with the definition; s = 255 gives NaN), and rounds a pair of fp32 to
+// codes as the definition says (1,038,256 numbers, all borders between codes and their neighbours among them).
+#pragma once
+
+#include "cache.h"
+
+namespace veda {
+
+veda_status check_packed(const veda_packed_cache* c);
+veda_cache packed_rows(const veda_packed_cache* c);                             // a cache of the same rows, for the checks of batches and row tensors
+CacheArgs packed_args(const veda_packed_cache* c, const veda_cache_batch* b);   // page_b: bytes of a packed page
+inline int64_t packed_head_bytes(const veda_packed_cache* c) { return (int64_t)c->page_tokens * (c->head_dim / 2 + c->head_dim / 32); }
+
+#if defined(__HIPCC__)
+
+__device__ __forceinline__ float packed_power(uint32_t s) { return __uint_as_float(s << 23); }   // 2^(s - 127) as the conversions take it
+
+// Eight codes, channel i in bits 4 i.. of w, as values.
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2v;
+typedef __attribute__((ext_vector_type(2))) float f32x2p;
+__device__ __forceinline__ uint4 packed_bf16(uint32_t w, float power) {
+    uint4 x;
+    x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 0));
+    x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 1));
+    x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 2));
+    x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 3));
+    return x;
+}
+__device__ __forceinline__ void packed_f32(uint32_t w, float power, uint4 (&x)[2]) {
+    const f32x2p a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, power, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, power, 1);
+    const f32x2p c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, power, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, power, 3);
+    x[0] = uint4{__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(b[0]), __float_as_uint(b[1])};
+    x[1] = uint4{__float_as_uint(c[0]), __float_as_uint(c[1]), __float_as_uint(d[0]), __float_as_uint(d[1])};
+}
+
+#endif
+
+}  // namespace veda

@@ -30,6 +30,7 @@ VEDA_PRODUCTS_FP32, VEDA_PRODUCTS_SPLIT = 1, 2
 VEDA_CHAINS_MATRIX, VEDA_CHAINS_VECTOR = 1, 2
 VEDA_ROPE_INTERLEAVED, VEDA_ROPE_HALVES = 0, 1
 VEDA_ROPE_PLAIN, VEDA_ROPE_LINEAR, VEDA_ROPE_NTK, VEDA_ROPE_BY_PARTS = range(4)
+VEDA_STEP_SERVED, VEDA_STEP_REFUSED, VEDA_STEP_NO_ROOM = range(3)
 
 EXPORTS = (
     "veda_plan_create", "veda_plan_destroy", "veda_plan_set_option", "veda_plan_chain_unit", "veda_plan_tiles", "veda_plan_tile_offset",
@@ -44,8 +45,9 @@ EXPORTS = (
     "veda_tile_recall", "veda_output_sqerr",
     "veda_rope_create", "veda_rope_destroy", "veda_rope_frequencies", "veda_rope_apply",
     "veda_cache_append", "veda_cache_attn_workspace_bytes", "veda_cache_attn_fwd", "veda_cache_copy_pages",
+    "veda_packed_append", "veda_packed_attn_workspace_bytes", "veda_packed_attn_fwd", "veda_packed_copy_pages",
     "veda_pages_create", "veda_pages_destroy", "veda_pages_table", "veda_pages_length", "veda_pages_free_count", "veda_pages_extend",
-    "veda_pages_fork", "veda_pages_truncate", "veda_pages_evict", "veda_pages_compact",
+    "veda_pages_fork", "veda_pages_truncate", "veda_pages_evict", "veda_pages_compact", "veda_pages_step",
     "veda_status_string", "veda_last_error",
 )
 
@@ -84,6 +86,24 @@ class veda_rope_config(C.Structure):
 class veda_cache(C.Structure):
     _fields_ = [("pages", C.c_int32), ("page_tokens", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int),
                 ("page_stride", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class veda_packed_cache(C.Structure):
+    _fields_ = veda_cache._fields_
+
+
+class veda_device_pages(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("page_tokens", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32),
+                ("table", C.c_void_p), ("length", C.c_void_p), ("used", C.c_void_p)]
+
+
+class veda_step(C.Structure):
+    _fields_ = [("seqs", C.c_int32), ("rows", C.c_int32), ("max_new", C.c_int32), ("axes", C.c_int32), ("frame_h", C.c_int32),
+                ("frame_w", C.c_int32), ("seq", C.c_void_p), ("keep", C.c_void_p), ("evict", C.c_void_p), ("grow", C.c_void_p)]
+
+
+class veda_step_tables(C.Structure):
+    _fields_ = [("table_stride", C.c_int64)] + [(n, C.c_void_p) for n in ("page_table", "kv_len", "q_start", "status", "positions", "row_seq", "slots")]
 
 
 class veda_cache_batch(C.Structure):
@@ -191,6 +211,17 @@ def load():
     L.veda_cache_attn_fwd.restype = C.c_int
     L.veda_cache_copy_pages.argtypes = [cache, vp, i64, vp]
     L.veda_cache_copy_pages.restype = C.c_int
+    packed = C.POINTER(veda_packed_cache)
+    L.veda_packed_append.argtypes = [packed, *L.veda_cache_append.argtypes[1:-1], vp, veda_strides, vp, veda_strides, vp]
+    L.veda_packed_append.restype = C.c_int
+    L.veda_packed_attn_workspace_bytes.argtypes = [packed, batch, i32]
+    L.veda_packed_attn_workspace_bytes.restype = C.c_size_t
+    L.veda_packed_attn_fwd.argtypes = [packed, *L.veda_cache_attn_fwd.argtypes[1:]]
+    L.veda_packed_attn_fwd.restype = C.c_int
+    L.veda_packed_copy_pages.argtypes = [packed, vp, i64, vp]
+    L.veda_packed_copy_pages.restype = C.c_int
+    L.veda_pages_step.argtypes = [C.POINTER(veda_device_pages), C.POINTER(veda_step), C.POINTER(veda_step_tables), vp]
+    L.veda_pages_step.restype = C.c_int
     L.veda_pages_create.argtypes = [i32, i32, i32, i32, C.POINTER(vp)]
     L.veda_pages_create.restype = C.c_int
     L.veda_pages_destroy.argtypes = [vp]
@@ -803,6 +834,38 @@ class Cache:
         self._ref = C.byref(self._struct)
 
 
+class PackedCache:
+    """One layer's paged cache in 4 bits: pools k, v u8 [pages, kv_heads, page_tokens * (d / 2 + d / 32)], made here unless given (views
+    with a larger page stride are fine).  dtype: of the rows that go in, of queries and of results."""
+
+    def __init__(self, pages: int, page_tokens: int, kv_heads: int, head_dim: int, dtype: torch.dtype, device="cuda",
+                 k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+        _ints("PackedCache", pages, page_tokens, kv_heads, head_dim)
+        run = page_tokens * (head_dim // 2 + head_dim // 32)
+        shape = (pages, kv_heads, run)
+        if k is None and v is None:
+            k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        for t in (k, v):
+            _need(t is not None and tuple(t.shape) == shape and t.dtype == torch.uint8 and t.device == k.device and
+                  all(a == b or n == 1 for n, a, b in zip(shape[1:], t.stride()[1:], (run, 1))) and
+                  (pages == 1 or t.stride(0) == k.stride(0) >= kv_heads * run),
+                  "PackedCache", f"k and v must be uint8 {list(shape)} with close bytes and heads, and pages apart")
+        self.k, self.v = k, v
+        self.pages, self.page_tokens, self.kv_heads, self.head_dim, self.dtype = int(pages), int(page_tokens), int(kv_heads), int(head_dim), dtype
+        stride = k.stride(0) if pages > 1 else 0
+        self.device = k.device
+        self._struct = veda_packed_cache(self.pages, self.page_tokens, self.kv_heads, self.head_dim, _dtype_code(dtype), stride, _ptr(k), _ptr(v))
+        self._ref = C.byref(self._struct)
+
+    def codes(self, pool: torch.Tensor) -> torch.Tensor:
+        """The codes of k or v, a view u8 [pages, kv_heads, page_tokens, d / 2]: channel 2i in the low, 2i + 1 in the high half of a byte."""
+        return pool[:, :, :self.page_tokens * (self.head_dim // 2)].unflatten(2, (self.page_tokens, self.head_dim // 2))
+
+    def scales(self, pool: torch.Tensor) -> torch.Tensor:
+        """The bytes s of k or v, a view u8 [pages, kv_heads, page_tokens, d / 32]: 32 channels are their codes times 2^(s - 127)."""
+        return pool[:, :, self.page_tokens * (self.head_dim // 2):].unflatten(2, (self.page_tokens, self.head_dim // 32))
+
+
 class CacheBatch:
     """The sequences of a call: page_table i32 [seqs, max_pages], kv_len i32 [seqs], q_start i32 [seqs + 1] on the GPU (read when the
     kernels run), max_new: the most new tokens of any sequence."""
@@ -870,6 +933,13 @@ def veda_cache_attn_workspace_bytes(cache: Cache, batch: CacheBatch, q_heads: in
     return int(load().veda_cache_attn_workspace_bytes(cache._ref, C.byref(bs), q_heads))
 
 
+def veda_packed_attn_workspace_bytes(cache: PackedCache, batch: CacheBatch, q_heads: int, rows: int) -> int:
+    """Bytes of scratch for veda_packed_attn_fwd on buffers of `rows` rows."""
+    _ints("veda_packed_attn_workspace_bytes", q_heads, rows)
+    bs = batch.struct(rows)
+    return int(load().veda_packed_attn_workspace_bytes(cache._ref, C.byref(bs), q_heads))
+
+
 def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int, window: int, sinks: int, w: str) -> veda_strides:
     """Refuses what the library would refuse, of everything but the buffers; q's strides."""
     _on(cache.device, w)
@@ -918,16 +988,96 @@ def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softma
     return out, lse
 
 
-def veda_cache_copy_pages(cache: Cache, pairs):
-    """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
-    _on(cache.device, "veda_cache_copy_pages")
+def veda_packed_append(cache: PackedCache, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                       positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                       k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """veda_cache_append into a cache held in 4 bits.  k_out, v_out [rows, kv_heads, d]: the rows as the cache then stands for them."""
+    w, rows = "veda_packed_append", k.shape[0]
+    _on(cache.device, w)
+    _need(isinstance(cache, PackedCache), w, "the cache is not held in 4 bits")
+    if rope is not None and rope.handle is None:    # which the library would take for no rope
+        _refuse(w, "the rope is closed")
+    sk, sv = _rows(cache, k, rows, w, "k"), _rows(cache, v, rows, w, "v")
+    none = veda_strides(0, 0, 0)
+    sko, svo = (none if t is None else _rows(cache, t, rows, w, name) for t, name in ((k_out, "k_out"), (v_out, "v_out")))
+    for t in (k, v, k_out, v_out):
+        if t is not None and t.shape[1] != cache.kv_heads:
+            _refuse(w, "k, v, k_out and v_out must have the cache's heads")
+    if batch.page_table.device != cache.device:
+        _refuse(w, "the batch must be where the cache is")
+    sq = so = none
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty((rows, q.shape[1], cache.head_dim), dtype=cache.dtype, device=cache.device)
+        sq, so = _rows(cache, q, rows, w, "q"), _rows(cache, q_out, rows, w, "q_out")
+        if q.shape[1] != q_out.shape[1]:
+            _refuse(w, "q and q_out must have the same heads")
+    else:
+        _need(q_out is None, w, "q_out without q")
+    if positions is not None and (rope is None or tuple(positions.shape) != (rows, rope.axes) or positions.dtype != torch.int32 or
+                                  positions.device != cache.device or not positions.is_contiguous()):
+        _refuse(w, "positions must be contiguous i32 [rows, axes of rope]")
+    bs = batch.struct(rows)
+    _check(load().veda_packed_append(cache._ref, C.byref(bs), k.data_ptr(), sk, v.data_ptr(), sv, 0 if q is None else q.shape[1], _ptr(q), sq,
+                                     _ptr(q_out), so, None if rope is None else rope.handle, _ptr(positions), _ptr(k_out), sko, _ptr(v_out), svo,
+                                     _stream_of(cache.device)), w)
+    return q_out
+
+
+def veda_packed_attn_fwd(cache: PackedCache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                        workspace: Optional[torch.Tensor] = None):
+    """veda_cache_attn_fwd over a cache held in 4 bits: the same arguments and results."""
+    w = "veda_packed_attn_fwd"
+    _need(isinstance(cache, PackedCache), w, "the cache is not held in 4 bits")
+    sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)
+    rows, heads = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty((rows, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+    so = _rows(cache, out, rows, w, "out")
+    if out.shape[1] != heads:
+        _refuse(w, "out must have q's heads")
+    if want_lse and lse is None:
+        lse = torch.empty((heads, rows), dtype=torch.float32, device=cache.device)
+    if lse is not None and (tuple(lse.shape) != (heads, rows) or lse.dtype != torch.float32 or lse.device != cache.device or not lse.is_contiguous()):
+        _refuse(w, "lse must be contiguous fp32 [q_heads, rows]")
+    bs = batch.struct(rows)
+    lib, ref = load(), C.byref(bs)
+    if workspace is None:
+        need = int(lib.veda_packed_attn_workspace_bytes(cache._ref, ref, heads))
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
+    elif workspace.device != cache.device or not workspace.is_contiguous():
+        _refuse(w, "the workspace must be contiguous and where the cache is")
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.veda_packed_attn_fwd(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, veda_visible(block, window, sinks), out.data_ptr(), so,
+                                   _ptr(lse), _ptr(workspace) or None, nbytes, _stream_of(cache.device)), w)
+    return out, lse
+
+
+def _pairs(pairs, w: str) -> np.ndarray:
     p = np.asarray(pairs)
     if p.size and not (p.shape[1] == 2 if p.ndim == 2 else p.ndim == 1 and p.size % 2 == 0):     # sources and targets as two rows, say
-        _refuse("veda_cache_copy_pages", "pairs must be page numbers [n, 2]")
+        _refuse(w, "pairs must be page numbers [n, 2]")
     if p.dtype != np.int32:
-        _need(p.size == 0 or (p.dtype.kind in "iu" and 0 <= p.min() and p.max() < 1 << 31), "veda_cache_copy_pages", "pairs must be page numbers [n, 2]")
-    p = np.ascontiguousarray(p, np.int32).reshape(-1, 2)
-    _check(load().veda_cache_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream_of(cache.device)), "veda_cache_copy_pages")
+        _need(p.size == 0 or (p.dtype.kind in "iu" and 0 <= p.min() and p.max() < 1 << 31), w, "pairs must be page numbers [n, 2]")
+    return np.ascontiguousarray(p, np.int32).reshape(-1, 2)
+
+
+def veda_cache_copy_pages(cache: Cache, pairs):
+    """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
+    w = "veda_cache_copy_pages"
+    _on(cache.device, w)
+    p = _pairs(pairs, w)
+    _check(load().veda_cache_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream_of(cache.device)), w)
+
+
+def veda_packed_copy_pages(cache: PackedCache, pairs):
+    """veda_cache_copy_pages for a cache held in 4 bits."""
+    w = "veda_packed_copy_pages"
+    _on(cache.device, w)
+    _need(isinstance(cache, PackedCache), w, "the cache is not held in 4 bits")
+    p = _pairs(pairs, w)
+    _check(load().veda_packed_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream_of(cache.device)), w)
 
 
 class Pages:
@@ -1000,10 +1150,76 @@ def _book(status: int, where: str):
     _check(status, where)
 
 
+class DevicePages:
+    """A page book on the GPU (veda_device_pages): table i32 [max_seqs, max_pages], length i32 [max_seqs], used i32 [(pages + 31) / 32],
+    made here (empty) unless given."""
+
+    def __init__(self, pages: int, page_tokens: int, max_seqs: int, max_pages: int, device="cuda", table: Optional[torch.Tensor] = None,
+                 length: Optional[torch.Tensor] = None, used: Optional[torch.Tensor] = None):
+        _ints("DevicePages", pages, page_tokens, max_seqs, max_pages)
+        _need(min(pages, page_tokens, max_seqs, max_pages) >= 1, "DevicePages", "a book has pages, tokens to a page, sequences and pages of one")
+        shapes = ((max_seqs, max_pages), (max_seqs,), ((pages + 31) // 32,))
+        self.table, self.length, self.used = (torch.zeros(n, dtype=torch.int32, device=device) if t is None else t
+                                              for t, n in zip((table, length, used), shapes))
+        self.device = self.table.device
+        for t, n in zip((self.table, self.length, self.used), shapes):
+            _need(tuple(t.shape) == n and t.dtype == torch.int32 and t.device == self.device and t.is_contiguous(), "DevicePages",
+                  f"table, length and used must be contiguous i32 {list(shapes[0])}, {list(shapes[1])}, {list(shapes[2])}")
+        self.pages, self.page_tokens, self.max_seqs, self.max_pages = int(pages), int(page_tokens), int(max_seqs), int(max_pages)
+        self._struct = veda_device_pages(self.pages, self.page_tokens, self.max_seqs, self.max_pages, _ptr(self.table), _ptr(self.length), _ptr(self.used))
+        self._ref = C.byref(self._struct)
+
+
+class StepTables:
+    """What veda_pages_step writes for up to `rows` new rows of `seqs` requests, of which none grows by more than max_new; made here unless given.
+    axes, frame (H, W): what `positions` are.  `batch` is the CacheBatch of the step's calls, on row buffers of `rows` rows."""
+
+    def __init__(self, book: DevicePages, seqs: int, rows: int, max_new: int, axes: int = 1, frame: Tuple[int, int] = (1, 1),
+                 page_table: Optional[torch.Tensor] = None, kv_len: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, row_seq: Optional[torch.Tensor] = None,
+                 slots: Optional[torch.Tensor] = None):
+        w, dev = "StepTables", book.device
+        _ints(w, seqs, rows, max_new, axes, *frame)
+        _need(seqs >= 0 and rows >= 0 and axes in (1, 3), w, "seqs and rows are not negative, axes are 1 or 3")
+
+        def take(t, shape, dtype):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=dev)
+            _need(tuple(t.shape) == shape and t.dtype == dtype and t.device == dev and t.is_contiguous(), w, f"a table must be contiguous {dtype} {list(shape)}")
+            return t
+
+        i32 = torch.int32
+        self.page_table, self.kv_len = take(page_table, (seqs, book.max_pages), i32), take(kv_len, (seqs,), i32)
+        self.q_start, self.status = take(q_start, (seqs + 1,), i32), take(status, (seqs,), i32)
+        self.positions, self.row_seq = take(positions, (rows, axes), i32), take(row_seq, (rows,), i32)
+        self.slots = take(slots, (rows,), torch.int64)
+        self.seqs, self.rows, self.max_new, self.axes, self.frame, self.max_pages, self.device = seqs, rows, int(max_new), axes, tuple(frame), book.max_pages, dev
+        self.batch = CacheBatch(self.page_table, self.kv_len, self.q_start, max_new)
+        self._struct = veda_step_tables(book.max_pages, *(_ptr(t) for t in (self.page_table, self.kv_len, self.q_start, self.status, self.positions,
+                                                                            self.row_seq, self.slots)))
+        self._ref = C.byref(self._struct)
+
+
+def veda_pages_step(book: DevicePages, out: StepTables, grow: torch.Tensor, seq: Optional[torch.Tensor] = None, keep: Optional[torch.Tensor] = None,
+                    evict: Optional[torch.Tensor] = None) -> StepTables:
+    """One step of the book: request i keeps the first keep[i] tokens of sequence seq[i] (all; sequence i), gives back the pages wholly within
+    evict[i] = (first, last) of them (none) and grows by grow[i]; all i32 on the GPU, read when the kernels run.  Fills and returns `out`."""
+    w = "veda_pages_step"
+    _on(book.device, w)
+    _need(out.max_pages == book.max_pages and out.device == book.device, w, "the tables were made for another book")
+    n = out.seqs
+    for t, shape in ((grow, (n,)), (seq, (n,)), (keep, (n,)), (evict, (n, 2))):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != torch.int32 or t.device != book.device or not t.is_contiguous()):
+            _refuse(w, f"grow, seq and keep must be contiguous i32 [{n}], evict [{n}, 2], where the book is")
+    step = veda_step(n, out.rows, out.max_new, out.axes, *out.frame, _ptr(seq), _ptr(keep), _ptr(evict), _ptr(grow))
+    _check(load().veda_pages_step(book._ref, C.byref(step), out._ref, _stream_of(book.device)), w)
+    return out
+
+
 def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale: float, rope: Optional[Rope] = None,
                          positions: Optional[torch.Tensor] = None, block: int = 1, window: int = 0, sinks: int = 0,
                          buffers: Optional[dict] = None):
-    """One attention call of a streaming step: q and k rotated, k and v appended, attention of the new rows over the cache.
+    """One attention call of a streaming step: q and k rotated, k and v appended, attention of the new rows over the cache (a Cache or a PackedCache).
     Returns (out [rows, q_heads, d], buffers); `buffers` (optional dict) is filled on the first call and reused afterwards, by calls
     of the same rows, heads and table (a captured call writes to them whenever it is replayed, so they are never exchanged for others).
     A call that is refused appends nothing and leaves the buffers as they were."""
@@ -1012,7 +1228,9 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
     es = q.element_size()
     if rope is None and (q.data_ptr() % 16 or any(n > 1 and s * es % 16 for n, s in ((q.shape[0], sq.n), (q.shape[1], sq.h)))):
         raise VedaError(VEDA_ERR_UNSUPPORTED, w, "rows of q must begin at multiples of 16 bytes")
-    need = veda_cache_attn_workspace_bytes(cache, batch, q.shape[1], q.shape[0])
+    append, attend, room = ((veda_packed_append, veda_packed_attn_fwd, veda_packed_attn_workspace_bytes) if isinstance(cache, PackedCache) else
+                            (veda_cache_append, veda_cache_attn_fwd, veda_cache_attn_workspace_bytes))
+    need = room(cache, batch, q.shape[1], q.shape[0])
     out, ws = b.get("out"), b.get("ws")
     if (out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != q.device) or
             ws is not None and ws.numel() * ws.element_size() < need):
@@ -1023,10 +1241,10 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)
     turned = None
     if rope is not None:
-        turned = veda_cache_append(cache, batch, k, v, rope, positions, q, b.get("q"))
+        turned = append(cache, batch, k, v, rope, positions, q, b.get("q"))
     else:
-        veda_cache_append(cache, batch, k, v, None, positions)
-    veda_cache_attn_fwd(cache, batch, q if rope is None else turned, softmax_scale, block, window, sinks, out, workspace=ws)
+        append(cache, batch, k, v, None, positions)
+    attend(cache, batch, q if rope is None else turned, softmax_scale, block, window, sinks, out, workspace=ws)
     b.update(out=out, ws=ws)
     if rope is not None:
         b["q"] = turned
