@@ -484,7 +484,8 @@ veda_status veda_cache_copy_pages(const veda_cache*, const int32_t* pairs, int64
  *   value = +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^(s - 127),   code = 8 * sign + number of the magnitude,   s = a byte for the 32 channels.
  * Rounding (veda_packed_append): 2^(s - 127) is the least power with max|x| < 7 * 2^(s - 127), s within 2..252, and a code the nearest of
  * the eight (ties to the even number, beyond 6 is 6, the sign is kept, of zeros too): off by 2^(s - 127) at most, 2/7 of the block's largest
- * magnitude (2^126 from 7 * 2^125 on).  32 channels with one that is not finite: s = 255 and codes 0, which stand for NaN.
+ * magnitude (2^126 from 7 * 2^125 on).  32 channels with one that is not finite: s = 255 and codes 0, which stand for NaN; so
+ * does every s from 253 on, whatever the codes.
  * A page holds, for every key head, the codes [page_tokens][head_dim / 2], channel 2i in the low and 2i + 1 in the high half of a byte,
  * and behind them the bytes s [page_tokens][head_dim / 32].  All conventions of the cache above hold. */
 typedef struct {
@@ -504,7 +505,9 @@ veda_status veda_packed_append(const veda_packed_cache*, const veda_cache_batch*
                                const veda_rope* rope, const int32_t* positions, void* k_out, veda_strides sk_out, void* v_out,
                                veda_strides sv_out, void* stream);
 /* veda_cache_attn_fwd over what the cache stands for: the same masks, results and errors.  A page's bytes may be anything where no row
- * sees them.  bf16: a channel whose 32 are NaN at a key that a row sees is NaN. */
+ * sees them.  A block of K that stands for NaN makes the rows that see its key NaN, one of V its 32 channels of those rows, and neither touches
+ * others.  f32: Q and the weights enter the products in three bf16 parts that hold all their bits (the cache's values are exact in bf16), sums are
+ * in fp32; f32 rows in blocks of more than 32 take fp32 products. */
 size_t veda_packed_attn_workspace_bytes(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads);
 veda_status veda_packed_attn_fwd(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads, const void* q, veda_strides sq,
                                  float softmax_scale, veda_visible visible, void* out, veda_strides so, float* lse,

@@ -108,6 +108,8 @@ int attn_rows_places();
 int attn_rows_workers(bool bf16);
 veda_status launch_cache_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);
 veda_status launch_packed_attn_rows(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);   // over a cache held in 4 bits
+int packed_keys_workers(bool bf16, int d, int size);   // size: rows of a block
+veda_status launch_packed_attn_keys(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);
 int attn_keys_workers(bool bf16, int d);
 veda_status launch_cache_attn_keys(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s);   // a.part_rows: rows of a block
 

@@ -16,9 +16,9 @@ struct AttnCut {
 static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch* b, int32_t q_heads, veda_visible vis) {
     AttnCut cut{};
     const int64_t max_new = b->max_new < b->rows ? b->max_new : b->rows, group = q_heads / c->kv_heads, rows = max_new * group;
-    const bool bf16 = c->dtype == VEDA_BF16, few = rows <= 32 && !packed;
+    const bool bf16 = c->dtype == VEDA_BF16, few = rows <= 32;
     const int d = c->head_dim;
-    cut.size = !few ? kAttnRows : rows <= 16 ? 16 : 32;
+    cut.size = rows <= 16 ? 16 : rows <= 32 ? 32 : kAttnRows;
     // Even, so that the sums of a block, part_rows * (d + 2) floats, are whole 16 bytes: the list of cuts behind them is read 16 bytes at a time.
     cut.part_rows = few ? cut.size : rows < kAttnRows ? (int32_t)(rows + 1) & ~1 : kAttnRows;
     const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
@@ -40,7 +40,7 @@ static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch
     // 456 keys 16 / 19, 756 21 / 20, 3756 72 / 23, 1024 rows of 12 heads, causal, on 1524 keys 38 / 40, 2524 56 / 44, 2133 rows of 12 on
     // 3633 keys 72 / 84, 1280 rows on 34,000 530 / 278-304 from box to box, 3840 872 / 734, 4680 985 / 1021; fp32, 100 rows of 12 on 160 keys 28 / 30, 200 38 / 30, 300 51 /
     // 30, 449 rows on 2000 302 / 63).
-    const int64_t fit = few ? attn_keys_workers(bf16, c->head_dim) : attn_rows_workers(bf16), groups = uniform * c->kv_heads;
+    const int64_t fit = !few ? attn_rows_workers(bf16) : packed ? packed_keys_workers(bf16, d, cut.size) : attn_keys_workers(bf16, d), groups = uniform * c->kv_heads;
     // Few rows: long walks wait for memory, so eight waves a workgroup go through short caches about as fast as all that the card can hold, and
     // the joining is saved; in fp32, where products take longer, the more so the more workgroups there are (single tokens of 4 query heads a key
     // head, d = 128, us without / with: bf16, one cache of 6 heads, 700 keys 11 / 17, 2500 16 / 17, 4000 23 / 17; 32 ragged ones of 8 heads
@@ -109,7 +109,7 @@ static veda_status attend(const veda_cache* c, const CacheArgs& pools, bool pack
     if (cut.items * c->kv_heads >= (int64_t)1 << 23 || (int64_t)a.c.max_new * a.group >= (int64_t)1 << 30 ||
         (cut.workers && cut.size < kAttnRows && (int64_t)b->rows * q_heads >= (int64_t)1 << 26))
         return VEDA_ERR_UNSUPPORTED;
-    if (packed) return launch_packed_attn_rows(a, bf16, c->head_dim, s);
+    if (packed) return cut.size < kAttnRows ? launch_packed_attn_keys(a, bf16, c->head_dim, s) : launch_packed_attn_rows(a, bf16, c->head_dim, s);
     return cut.size < kAttnRows ? launch_cache_attn_keys(a, bf16, c->head_dim, s) : launch_cache_attn_rows(a, bf16, c->head_dim, s);
 }
 

@@ -429,7 +429,7 @@ template <bool kBf16, int D> struct PackedTile {
     // to: the segment's first row of K and of V in LDS.  exists: whether the lane's key does; others become zeros, whatever lies there.
     __device__ __forceinline__ void store(char* k_to, char* v_to, bool exists, int lane) {
         const int r = row(lane), c0 = channel(lane);
-        const float kp = packed_power(exists ? ks : 127u), vp = packed_power(exists ? vs : 127u);
+        const float kp = packed_power_of(exists ? ks : 127u), vp = packed_power_of(exists ? vs : 127u);
         char* kr = k_to + r * T::kRowB;
         char* vr = v_to + r * T::kRowB;
         const int kx = T::k_swizzle(r), vx = T::v_swizzle(r);

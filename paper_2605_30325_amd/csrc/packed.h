@@ -16,7 +16,9 @@ inline int64_t packed_head_bytes(const veda_packed_cache* c) { return (int64_t)c
 
 #if defined(__HIPCC__)
 
-__device__ __forceinline__ float packed_power(uint32_t s) { return __uint_as_float(s << 23); }   // 2^(s - 127) as the conversions take it
+constexpr uint32_t kPackedNan = 253;   // bytes from here on stand for NaN
+__device__ __forceinline__ float packed_power(uint32_t s) { return __uint_as_float(s << 23); }   // 2^(s - 127) as the conversions take it; 255: NaN
+__device__ __forceinline__ float packed_power_of(uint32_t s) { return packed_power(s >= kPackedNan ? 255u : s); }   // of a byte from the pool
 
 // Eight codes, channel i in bits 4 i.. of w, as values.
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2v;
