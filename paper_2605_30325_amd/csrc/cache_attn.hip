@@ -5,6 +5,17 @@
 
 namespace veda {
 
+// Keys up to which few rows of a packed cache are left to a workgroup for each block and key head: eight waves up to 256 of them, four up to 768, two
+// beyond, as many as run at once.  Sharing has 10 us of its own (what every wave looks up before it starts) and 5 of joining; the waves of a workgroup
+// go through their tiles one after the other.  Single tokens of 4 query heads a key head, us apart / shared: bf16, d = 128, one cache of 6 heads, 2000
+// keys 17 / 19, 3000 22 / 19; 32 of 8, 3000 23 / 28, 7000 44 / 39; 64 of 8, 2000 26 / 32, 4500 52 / 45; 128 of 8, 1200 32 / 40, 3000 65 / 58; d = 64, 32 of 8, 4500 24 /
+// 35, 64 of 8, 3000 28 / 30, 4500 39 / 34; fp32, d = 128, one of 6, 2000 20 / 21, 3000 26 / 21, 64 of 8, 2000 32 / 36, 3000 47 / 45.
+static int64_t packed_short(bool bf16, int d, int64_t groups) {
+    if (groups <= 256) return d == 64 ? 2700 + 20 * groups : bf16 ? 2400 + 10 * groups : 2200 + 8 * groups;
+    if (groups <= 768) return d == 64 ? 3600 : bf16 ? 2800 : 2000;
+    return (d == 64 || bf16 ? 1400 : 1000) + groups * 3 / 5;
+}
+
 // How a call is cut up.
 struct AttnCut {
     int32_t size;       // rows of a block: 16 or 32 where a key head has no more rows than that for any sequence, else 128
@@ -47,7 +58,7 @@ static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch
     // up to 2500 27 / 36; 64, by two waves, up to 1000 28 / 33, 2500 68 / 63; fp32, one of 6 heads, 700 keys 20 / 24, 1500 35 / 24, 32 of 8 up to
     // 1500 42 / 47; d = 64, one of 6 heads 1500 21 / 23, 2500 30 / 23).
     const int64_t grown = (d == 64 ? 1536 : 768) + 8 * groups;
-    const int64_t short_few = bf16 ? (groups <= 256 ? 2560 : 1536) : grown < 4096 ? grown : 4096;
+    const int64_t short_few = packed ? packed_short(bf16, d, groups) : bf16 ? (groups <= 256 ? 2560 : 1536) : grown < 4096 ? grown : 4096;
     const bool share = keys > (few ? short_few : bf16 ? 512 + 16 * groups : 192) && countable &&
                        (few ? groups <= 8 * fit : uniform <= kRowsShareItems && 5 * groups < 4 * attn_rows_places());
     if (share) cut.workers = (int32_t)(fit < c->kv_heads ? c->kv_heads : fit / c->kv_heads * c->kv_heads);

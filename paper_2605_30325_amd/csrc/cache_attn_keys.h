@@ -113,12 +113,14 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
 }
 
 // Puts the unfinished sums of a (row, query head) together; rows that one workgroup had whole have none.  W waves for each: one
-// where there are about as many sequences as parts, eight (four loads in flight each) for few long sequences, cut into many.
-template <bool kBf16, int D, int RB, int W, int kKeys> __global__ __launch_bounds__(512) void cache_attn_join_parts_kernel(CacheAttnArgs a) {
+// where there are about as many sequences as parts, more for few long sequences, cut into many; kAhead loads in flight each.
+template <bool kBf16, int D, int RB, int W, int kKeys, int kAhead, int kLeast> __global__ __launch_bounds__((W > 8 ? 64 * W : 512)) void cache_attn_join_parts_kernel(CacheAttnArgs a) {
     constexpr int kRows = 16 * RB, V = D / 64;
     __shared__ float sums[W][D + 2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, w = wave % W;
-    const int64_t item = (int64_t)blockIdx.x * (8 / W) + wave / W;
+    int64_t item;
+    if constexpr (W > 8) item = blockIdx.x;
+    else item = (int64_t)blockIdx.x * (8 / W) + wave / W;
     const bool is_row = item < (int64_t)a.c.rows * a.q_heads;
     const int token = is_row ? (int)(item / a.q_heads) : -1, qh = (int)(item % a.q_heads);
     // the row's sequence, and its tiles
@@ -142,16 +144,16 @@ template <bool kBf16, int D, int RB, int W, int kKeys> __global__ __launch_bound
         }
         total += __builtin_amdgcn_readlane(up_to, 63);
     }
-    const TileShare share(total, a.workers / a.c.kv_heads, kShareTiles);
+    const TileShare share(total, a.workers / a.c.kv_heads, kLeast);
     const int w0 = each ? share.owner(first) : 0, n = each ? share.owner(first + each - 1) - w0 + 1 : 1;
     if (n == 1) return;   // one workgroup had it all (with W = 8 the same for all waves)
     const float2* ml = reinterpret_cast<const float2*>(a.part + (int64_t)2 * a.workers * kRows * D);
     auto part_row = [&](int j) { return (2 * ((int64_t)(w0 + j) * a.c.kv_heads + qh / a.group) + (j == 0 ? 1 : 0)) * kRows + row; };
-    float2 m[4];
-    float x[4][V];
+    float2 m[kAhead];
+    float x[kAhead][V];
     auto get = [&](int j0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kAhead; ++j) {
             const int64_t at = part_row(min(j0 + W * j, n - 1));
             m[j] = ml[at];
 #pragma unroll
@@ -160,16 +162,26 @@ template <bool kBf16, int D, int RB, int W, int kKeys> __global__ __launch_bound
     };
     get(w);   // on their way while the common reference is found
     float ref = -INFINITY;
-    for (int j = lane; j < n; j += 64) ref = fmaxf(ref, ml[part_row(j)].x);
+    if constexpr (kAhead > 4) {
+        for (int j = lane; j < n; j += 256) {
+            float far[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) far[i] = ml[part_row(min(j + 64 * i, n - 1))].x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ref = fmaxf(ref, far[i]);
+        }
+    } else {
+        for (int j = lane; j < n; j += 64) ref = fmaxf(ref, ml[part_row(j)].x);
+    }
 #pragma unroll
     for (int x = 32; x >= 1; x >>= 1) ref = fmaxf(ref, __shfl_xor(ref, x));
     float l = 0.0f, o[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) o[c] = 0.0f;
-    for (int j0 = w; j0 < n; j0 += 4 * W) {
+    for (int j0 = w; j0 < n; j0 += kAhead * W) {
         if (j0 != w) get(j0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kAhead; ++j) {
             if (j0 + W * j >= n) continue;
             const float f = m[j].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j].x - ref);   // -inf: the sums are 0 or NaN
             l += f * m[j].y;

@@ -553,8 +553,8 @@ template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheA
     veda_status st = launch_status("veda_cache_attn_fwd");
     if (st != VEDA_OK) return st;
     const int64_t joins = (int64_t)a.c.rows * a.q_heads;
-    if (a.workers / a.c.kv_heads > 8 * a.c.seqs && joins < 1 << 23) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 8, KeysTile<kBf16, D>::kKeys>), dim3((unsigned)joins), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 1, KeysTile<kBf16, D>::kKeys>), dim3((unsigned)((joins + 7) / 8)), dim3(512), 0, s, a);
+    if (a.workers / a.c.kv_heads > 8 * a.c.seqs && joins < 1 << 23) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 8, KeysTile<kBf16, D>::kKeys, 4, kShareTiles>), dim3((unsigned)joins), dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 1, KeysTile<kBf16, D>::kKeys, 4, kShareTiles>), dim3((unsigned)((joins + 7) / 8)), dim3(512), 0, s, a);
     return launch_status("veda_cache_attn_fwd");
 }
 

@@ -13,11 +13,19 @@
 
 namespace veda {
 
-template <int D> struct PackedKeys {
-    static constexpr int kKeys = 32, W = D / 32;         // keys of a tile; words of codes a lane has of 16 keys
+template <int D, int G> struct PackedKeys {
+    // Keys of a tile in groups of 16, and the least tiles of a share.
+    static constexpr int kKeys = 16 * G, kLeast = 16 / G;
+    static constexpr int W = D / 32;                     // words of codes a lane has of 16 keys
     static constexpr int kRowB = D / 2, kScaleB = D / 32;
     static constexpr int kSlot = kKeys * D * 2;          // V in LDS
     static constexpr int kOutRowB = D * 4 + 16;          // a row of the sums in LDS
+    // 16-byte chunk c of V's row r lies at chunk c ^ swizzle: four rows that 16 lanes write a chunk of each quarter of, and eight rows that
+    // 32 lanes read two neighbouring chunks of, then fall into different banks.
+    __device__ static int swizzle(int r) {
+        const int k0 = r & 1, k1 = (r >> 1) & 1, k2 = (r >> 2) & 1;
+        return D == 128 ? k2 << 3 | k0 << 2 | k1 << 1 | k0 : k2 << 2 | k1 << 1 | k1;
+    }
 };
 
 template <bool kBf16, int D, int RB> struct PackedRow {
@@ -27,15 +35,25 @@ template <bool kBf16, int D, int RB> struct PackedRow {
     float ref[RB], sub[RB], l[RB];   // reference of the exponentials (log2 units), 0 or -ref, this lane's sum
     float scale[RB];                 // of the logits
     int lo[RB], hi[RB];              // visible keys
+    uint32_t nan[RB];                // bit i: the i-th quarter of the channels is NaN
+    __device__ __forceinline__ f32x4v sums(int rb, int c) const {      // of channels 16 c + 4 g + 0..3
+        f32x4v x = o[rb][c];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (nan[rb] >> (c / (D / 64))) & 1u ? __builtin_nanf("") : x[i];
+        return x;
+    }
 };
 
 // Waves to a SIMD that the registers are to leave room for.
-template <bool kBf16, int D, int RB> constexpr int packed_waves() { return RB == 2 ? 2 : kBf16 ? (D == 64 ? 4 : 3) : (D == 64 ? 3 : 2); }
+template <bool kBf16, int D, int RB> constexpr int packed_waves() { return RB == 2 ? (kBf16 || D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
+
+// Groups of 16 keys of a tile in the sharing kernel.
+template <bool kBf16, int D, int RB> constexpr int packed_groups() { return RB == 1 ? 4 : 2; }
 
 // A lane's part of a tile: of its K row (l15), and of V, where lane / 4 is the key.
-template <int D> struct PackedRaw {
-    uint32_t k[2][D / 32], v[2][D / 32];
-    uint32_t ks[2], vs[2];
+template <int D, int G> struct PackedRaw {
+    uint32_t k[G][D / 32], v[G][D / 32];
+    uint32_t ks[G], vs[G];
 };
 template <int W> __device__ __forceinline__ void packed_words(const char* p, uint32_t (&w)[W]) {
     if constexpr (W == 4) {
@@ -47,9 +65,8 @@ template <int W> __device__ __forceinline__ void packed_words(const char* p, uin
     }
 }
 
-template <int D> struct PackedLane {
-    typedef PackedKeys<D> P;
-    typedef KeysTile<true, D> T;                         // the layout of bf16 V in LDS
+template <int D, int G> struct PackedLane {
+    typedef PackedKeys<D, G> P;
     uint32_t k_code, k_scale, v_code, v_scale;           // what the lane adds to addresses in a pool
     uint32_t v_to, v_at;                                 // its places in LDS: where its part of V goes, and its operand's
     int lane, l15, g;
@@ -58,17 +75,23 @@ template <int D> struct PackedLane {
         k_scale = (uint32_t)(l15 * P::kScaleB + g * (D / 4) / 32);
         v_code = (uint32_t)(lane * (D / 8));
         v_scale = (uint32_t)((lane >> 2) * P::kScaleB + (lane & 3) * (D / 4) / 32);
-        v_to = (uint32_t)((lane >> 2) * D * 2 + ((((lane & 3) * (D / 32)) ^ T::v_swizzle(lane >> 2)) << 4));
+        v_to = (uint32_t)((lane >> 2) * D * 2 + ((((lane & 3) * (D / 32)) ^ P::swizzle(lane >> 2)) << 4));
         const int key = 4 * g + (l15 >> 2);
-        v_at = (uint32_t)(key * D * 2 + ((((l15 & 3) >> 1) ^ T::v_swizzle(key)) << 4) + 8 * (l15 & 1));
+        v_at = (uint32_t)(key * D * 2 + ((((l15 & 3) >> 1) ^ P::swizzle(key)) << 4) + 8 * (l15 & 1));
+    }
+    // The same place for all lanes, in scalar registers, and what a lane adds to it.
+    __device__ static __forceinline__ const char* at(const char* all, uint32_t lane_part) {
+        uint64_t x = (uint64_t)(uintptr_t)all;
+        asm("" : "+s"(x));
+        return (const char*)(uintptr_t)x + lane_part;
     }
     // base: the head's place in the pools, tok: the first of 16 keys in the page.
-    __device__ __forceinline__ void load(const CacheArgs& c, PackedRaw<D>& r, int b, int64_t base, int tok) const {
+    __device__ __forceinline__ void load(const CacheArgs& c, PackedRaw<D, G>& r, int b, int64_t base, int tok) const {
         const int64_t code = base + tok * P::kRowB, scale = base + ((int64_t)P::kRowB << c.log_page) + tok * P::kScaleB;
-        packed_words<P::W>(c.k + code + k_code, r.k[b]);
-        packed_words<P::W>(c.v + code + v_code, r.v[b]);
-        r.ks[b] = *reinterpret_cast<const uint8_t*>(c.k + scale + k_scale);
-        r.vs[b] = *reinterpret_cast<const uint8_t*>(c.v + scale + v_scale);
+        packed_words<P::W>(at(c.k + code, k_code), r.k[b]);
+        packed_words<P::W>(at(c.v + code, v_code), r.v[b]);
+        r.ks[b] = *reinterpret_cast<const uint8_t*>(at(c.k + scale, k_scale));
+        r.vs[b] = *reinterpret_cast<const uint8_t*>(at(c.v + scale, v_scale));
     }
 };
 
@@ -124,57 +147,87 @@ __device__ __forceinline__ KeysSeen packed_rows_of(const CacheAttnArgs& a, Packe
         for (int c = 0; c < D / 16; ++c) st.o[rb][c] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
         st.ref[rb] = -INFINITY;
         st.sub[rb] = st.l[rb] = 0.0f;
+        st.nan[rb] = 0;
     }
+    // Q is waited for here: left to its first use, in the loop over tiles, the wait would be there, and every tile would wait for the next one's loads.
+#pragma unroll
+    for (int u = 0; u < PackedRow<kBf16, D, RB>::kQ; ++u)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) asm volatile("" : "+v"(st.q[u][rb][t]));
     return {__builtin_amdgcn_readlane(st.lo[0], 0), __builtin_amdgcn_readlane(st.hi[RB - 1], 15), __builtin_amdgcn_readlane(st.lo[RB - 1], 15),
             __builtin_amdgcn_readlane(st.hi[0], 0)};
 }
 
-// A tile of keys from key0 on for one wave; its V goes through LDS at `v`.  exists: bit b = keys 16 b .. 16 b + 15 exist; len: the sequence's tokens.
-template <bool kBf16, int D, int RB>
-__device__ __forceinline__ void packed_tile(const CacheAttnArgs& a, PackedRow<kBf16, D, RB>& st, const KeysSeen& see, const PackedLane<D>& ln, PackedRaw<D>& raw,
-                                            char* smem, uint32_t v, int key0, uint32_t exists, int len) {
-    constexpr int C = D / 16, W = D / 32, kQ = PackedRow<kBf16, D, RB>::kQ, kP = kBf16 ? 2 : 3;
-    const int end = key0 + 32;
-    if (key0 >= see.hi || (end <= see.lo && key0 >= a.sinks) || exists == 0) return;
-    const bool full = end <= see.hi_all && (key0 >= see.lo_all || end <= a.sinks) && exists == 3u;
+// A tile of keys from key0 on for one wave, in two halves between which the next tile's codes are asked for, into the registers that the first
+// half is done with.  exists: bit b = keys 16 b .. 16 b + 15 exist; len: the sequence's tokens.
+template <int G> struct PackedStep {
+    int key0;
+    uint32_t exists;
+    bool some, full, odd;    // some row sees some keys; every row sees all; blocks of V stand for NaN
+    uint64_t nans[G];        // the lanes that have some
+};
+// V goes to its places in LDS (at smem), scores are formed.
+template <bool kBf16, int D, int RB, int G>
+__device__ __forceinline__ void packed_scores(const CacheAttnArgs& a, const PackedRow<kBf16, D, RB>& st, const KeysSeen& see, const PackedLane<D, G>& ln, PackedRaw<D, G>& raw,
+                                              char* smem, int len, PackedStep<G>& step, f32x4v (&s)[RB][G]) {
+    constexpr int W = D / 32, kQ = PackedRow<kBf16, D, RB>::kQ;
+    const int key0 = step.key0, end = key0 + 16 * G;
+    const uint32_t exists = step.exists;
+    step.some = !(key0 >= see.hi || (end <= see.lo && key0 >= a.sinks) || exists == 0);
+    if (!step.some) return;
+    step.full = end <= see.hi_all && (key0 >= see.lo_all || end <= a.sinks) && exists == (1u << G) - 1u;
 
     // V to its places; zeros for keys that do not exist, whatever lies there, and for blocks that stand for NaN (odd, nans: the lanes that have some)
-    const bool odd = __any(max(raw.vs[0], raw.vs[1]) >= kPackedNan);
-    uint64_t nans[2] = {0, 0};
-    if (exists != 3u || end > len || odd) {
+    uint32_t most = 0;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < G; ++b) {
+        most = max(most, raw.vs[b]);
+        step.nans[b] = 0;
+    }
+    step.odd = __any(most >= kPackedNan);
+    if (exists != (1u << G) - 1u || end > len || step.odd) {
+#pragma unroll
+        for (int b = 0; b < G; ++b) {
             const bool there = ((exists >> b) & 1u) && key0 + 16 * b + (ln.lane >> 2) < len, nan = there && raw.vs[b] >= kPackedNan;
-            nans[b] = __ballot(nan);
+            step.nans[b] = __ballot(nan);
 #pragma unroll
             for (int i = 0; i < W; ++i) raw.v[b][i] = there && !nan ? raw.v[b][i] : 0u;
             raw.vs[b] = there && !nan ? raw.vs[b] : 127u;
         }
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < G; ++b)
 #pragma unroll
         for (int i = 0; i < W; ++i)
             *reinterpret_cast<uint4*>(smem + ((ln.v_to ^ (uint32_t)(i << 4)) + b * 16 * D * 2)) = packed_bf16(raw.v[b][i], packed_power(raw.vs[b]));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 
-    f32x4v s[RB][2];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) s[rb][b] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b = 0; b < G; ++b) s[rb][b] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int t = 0; t < W; ++t)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < G; ++b) {
             const bf16x8 x = __builtin_bit_cast(bf16x8, packed_bf16(raw.k[b][t], packed_power_of(raw.ks[b])));
 #pragma unroll
             for (int u = kQ - 1; u >= 0; --u)
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) s[rb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, st.q[u][rb][t], s[rb][b], 0, 0, 0);
         }
-    __builtin_amdgcn_sched_barrier(0);
+}
+// Weights, and their products with V (at v in LDS).
+template <bool kBf16, int D, int RB, int G>
+__device__ __forceinline__ void packed_values(const CacheAttnArgs& a, PackedRow<kBf16, D, RB>& st, const PackedLane<D, G>& ln, uint32_t v, const PackedStep<G>& step,
+                                              f32x4v (&s)[RB][G]) {
+    constexpr int C = D / 16, kP = kBf16 ? 2 : 3;
+    const int key0 = step.key0;
+    const uint32_t exists = step.exists;
+    if (!step.some) return;
     auto seen = [&](int rb, int b, int i) __attribute__((always_inline)) {
         const int key = key0 + 16 * b + 4 * ln.g + i;
         return key < st.hi[rb] && (key >= st.lo[rb] || key < a.sinks) && ((exists >> b) & 1u);
@@ -183,15 +236,15 @@ __device__ __forceinline__ void packed_tile(const CacheAttnArgs& a, PackedRow<kB
     bool grown = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        if (!full) {
+        if (!step.full) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < G; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[rb][b][i] = seen(rb, b, i) ? s[rb][b][i] : -INFINITY;
         }
         float m = s[rb][0][0];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < G; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) m = fmaxf(m, s[rb][b][i]);
         mx[rb] = m * st.scale[rb];
@@ -211,86 +264,85 @@ __device__ __forceinline__ void packed_tile(const CacheAttnArgs& a, PackedRow<kB
             for (int c = 0; c < C; ++c) st.o[rb][c] *= alpha;
         }
     }
-    bf16x8 p[kP][RB];
+    bf16x8 p[G / 2][kP][RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         float sum = 0.0f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < G; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                const int h = b / 2, e = 4 * (b % 2) + i;
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][b][i], st.scale[rb], st.sub[rb]));
                 sum += w;
                 // the first part below the weight, so that what is left of a weight above 0 is above 0 too (keys_part)
-                p[0][rb][4 * b + i] = keys_part(w);
-                const float rest = w - (float)p[0][rb][4 * b + i];
+                p[h][0][rb][e] = keys_part(w);
+                const float rest = w - (float)p[h][0][rb][e];
                 if constexpr (kP == 2) {
-                    p[1][rb][4 * b + i] = (__bf16)rest;
+                    p[h][1][rb][e] = (__bf16)rest;
                 } else {
                     const float second = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
-                    p[1][rb][4 * b + i] = (__bf16)second;
-                    p[kP - 1][rb][4 * b + i] = (__bf16)(rest - second);
+                    p[h][1][rb][e] = (__bf16)second;
+                    p[h][kP - 1][rb][e] = (__bf16)(rest - second);
                 }
             }
         st.l[rb] += sum;
     }
 #pragma unroll
-    for (int c = 0; c < C; c += 2) {   // two at a time, so that a sum's next product is not the one right behind it
-        const bf16x8 x[2] = {keys_v<D>(v, c), keys_v<D>(v, c + 1)};
+    for (int h = 0; h < G / 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 2 * kP * RB; ++j) {
-            const int i = c + j % 2, rb = j / 2 % RB, u = kP - 1 - j / 2 / RB;
-            st.o[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[j % 2], p[u][rb], st.o[rb][i], 0, 0, 0);
+        for (int c = 0; c < C; c += 2) {   // two at a time, so that a sum's next product is not the one right behind it
+            const bf16x8 x[2] = {keys_v<D>(v + h * 32 * D * 2, c), keys_v<D>(v + h * 32 * D * 2, c + 1)};
+#pragma unroll
+            for (int j = 0; j < 2 * kP * RB; ++j) {
+                const int i = c + j % 2, rb = j / 2 % RB, u = kP - 1 - j / 2 / RB;
+                st.o[rb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[j % 2], p[h][u][rb], st.o[rb][i], 0, 0, 0);
+            }
+            if (c % 4 == 2) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
         }
-        if (c % 4 == 2) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
-    }
-    if (odd) {   // NaN for the rows that see such a block's key, and for no others
+    if (step.odd) {   // NaN for the rows that see such a block's key, and for no others
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-            for (uint64_t left = nans[b]; left; left &= left - 1) {
+        for (int b = 0; b < G; ++b)
+#pragma unroll 1
+            for (uint64_t left = step.nans[b]; left; left &= left - 1) {
                 const int from = __ffsll((long long)left) - 1, key = key0 + 16 * b + (from >> 2);
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    const bool sees = key < st.hi[rb] && (key >= st.lo[rb] || key < a.sinks);
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-                        if (c / (C / 4) == (from & 3))
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) st.o[rb][c][i] = sees ? __builtin_nanf("") : st.o[rb][c][i];
-                }
+                for (int rb = 0; rb < RB; ++rb) st.nan[rb] |= key < st.hi[rb] && (key >= st.lo[rb] || key < a.sinks) ? 1u << (from & 3) : 0u;
             }
     }
     asm volatile("" ::: "memory");
 }
 
 // Places of 64 tiles, one tile a lane: looked up together, so that no step waits for the table.
-template <int D> struct PackedPlaces {
-    int64_t base[2];
-    int info;      // which of the two groups of 16 keys exist (bits 0, 1), and their numbers in their pages (bits 8.., 20..)
+template <int D, int G> struct PackedPlaces {
+    int64_t base[G];
+    int info;      // which of the groups of 16 keys exist (bits 0..), and their numbers in their pages (16 at a time: four bits from 8 on)
     __device__ __forceinline__ void find(const CacheArgs& c, const int32_t* table, int len, int64_t head_b, int tok) {
-        int at[2];
         info = 0;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) info |= (packed_from<D>(c, table, len, head_b, tok + 16 * b, base[b], at[b]) ? 1 : 0) << b;
-        info |= at[0] << 8 | at[1] << 20;
+        for (int b = 0; b < G; ++b) {
+            int at;
+            const bool ok = packed_from<D>(c, table, len, head_b, tok + 16 * b, base[b], at);
+            info |= (ok ? 1 << b : 0) | (at >> 4) << (8 + 4 * b);
+        }
     }
     // asks for the tile of lane `at`; returns which keys exist
-    __device__ __forceinline__ uint32_t ask(const CacheArgs& c, const PackedLane<D>& ln, PackedRaw<D>& raw, int at) const {
+    __device__ __forceinline__ uint32_t ask(const CacheArgs& c, const PackedLane<D, G>& ln, PackedRaw<D, G>& raw, int at) const {
         const int x = __builtin_amdgcn_readlane(info, at);
-        ln.load(c, raw, 0, lane_value(base[0], at), (x >> 8) & 0xfff);
-        ln.load(c, raw, 1, lane_value(base[1], at), (x >> 20) & 0xfff);
-        return (uint32_t)x & 3u;
+#pragma unroll
+        for (int b = 0; b < G; ++b) ln.load(c, raw, b, lane_value(base[b], at), (x >> (8 + 4 * b) & 15) << 4);
+        return (uint32_t)x & ((1u << G) - 1u);
     }
 };
 
 // Short caches: a workgroup for each (block of rows, key head), whose waves take its tiles in turn: eight of them, or two where workgroups are more
 // than compute units.
-template <bool kBf16, int D, int RB, int kWaves> __global__ __launch_bounds__(64 * kWaves, 2) void packed_attn_keys_kernel(CacheAttnArgs a) {
-    typedef PackedKeys<D> P;
+template <bool kBf16, int D, int RB, int G, int kWaves> __global__ __launch_bounds__(64 * kWaves, 2) void packed_attn_keys_kernel(CacheAttnArgs a) {
+    typedef PackedKeys<D, G> P;
     constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4;
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const PackedLane<D> ln(lane);
+    const PackedLane<D, G> ln(lane);
     char* mine = smem + wave * P::kSlot;
     const uint32_t v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * P::kSlot + ln.v_at;
     RowBlock block;
@@ -302,8 +354,8 @@ template <bool kBf16, int D, int RB, int kWaves> __global__ __launch_bounds__(64
     const int32_t* table = a.c.table + block.seq * a.c.table_stride;
     const int64_t head_b = (int64_t)head * (P::kRowB + P::kScaleB) << a.c.log_page;
 
-    PackedPlaces<D> places;
-    PackedRaw<D> raw;
+    PackedPlaces<D, G> places;
+    PackedRaw<D, G> raw;
     uint32_t exists = 0;
     if (wave < tiles.count) {
         places.find(a.c, table, sr.len, head_b, tiles.at(min(wave + lane * kWaves, tiles.count - 1)));
@@ -313,8 +365,9 @@ template <bool kBf16, int D, int RB, int kWaves> __global__ __launch_bounds__(64
     const KeysSeen see = packed_rows_of<kBf16, D, RB>(a, st, sr, n, head, r0, r_end, ln.l15, ln.g);
     int at = 0;
     for (int t = wave; t < tiles.count; t += kWaves) {
-        PackedRaw<D> now = raw;
-        const uint32_t ex = exists;
+        PackedStep<G> step{tiles.at(t), exists};
+        f32x4v sc[RB][G];
+        packed_scores<kBf16, D, RB, G>(a, st, see, ln, raw, mine, sr.len, step, sc);
         if (t + kWaves < tiles.count) {
             if (++at == 64) {
                 places.find(a.c, table, sr.len, head_b, tiles.at(min(t + kWaves + lane * kWaves, tiles.count - 1)));
@@ -322,7 +375,7 @@ template <bool kBf16, int D, int RB, int kWaves> __global__ __launch_bounds__(64
             }
             exists = places.ask(a.c, ln, raw, at);
         }
-        packed_tile<kBf16, D, RB>(a, st, see, ln, now, mine, v, tiles.at(t), ex, sr.len);
+        packed_values<kBf16, D, RB, G>(a, st, ln, v, step, sc);
     }
 
     // Sums of the waves, put together row by row.  A lane holds channels 16 c + 4 g + 0..3 of its row.
@@ -333,7 +386,7 @@ template <bool kBf16, int D, int RB, int kWaves> __global__ __launch_bounds__(64
         const int row = wave * kRows + 16 * rb + ln.l15;
         const float l = keys_sum(st.l[rb]);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4v*>(smem + row * P::kOutRowB + (16 * c + 4 * ln.g) * 4) = st.o[rb][c];
+        for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4v*>(smem + row * P::kOutRowB + (16 * c + 4 * ln.g) * 4) = st.sums(rb, c);
         if (ln.g == 0) {
             ml[2 * row] = st.ref[rb];
             ml[2 * row + 1] = l;
@@ -361,15 +414,15 @@ template <bool kBf16, int D, int RB, int kWaves> __global__ __launch_bounds__(64
 }
 
 // Long caches: every wave is a workgroup and takes one key head of an equal part [now, end) of the common row of tiles, sequence by sequence.
-template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64, (packed_waves<kBf16, D, RB>())) void packed_attn_share_kernel(CacheAttnArgs a) {
-    typedef PackedKeys<D> P;
+template <bool kBf16, int D, int RB, int G> __global__ __launch_bounds__(64, (packed_waves<kBf16, D, RB>())) void packed_attn_share_kernel(CacheAttnArgs a) {
+    typedef PackedKeys<D, G> P;
     constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4;
     extern __shared__ __align__(1024) char smem[];
     const int lane = threadIdx.x;
-    const PackedLane<D> ln(lane);
+    const PackedLane<D, G> ln(lane);
     const uint32_t v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + ln.v_at;
     const KeysCount count(a, P::kKeys);
-    const TileShare share(count.total, a.workers / a.c.kv_heads, kShareTiles);
+    const TileShare share(count.total, a.workers / a.c.kv_heads, P::kLeast);
     const int head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads;
     if (mine >= share.parts || share.total == 0) return;
     int now = share.begin(mine);
@@ -401,10 +454,11 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64, (packed_wa
     }
     ahead = here;
     // Places of the next 64 tiles, whichever sequences they belong to.
-    PackedPlaces<D> places;
+    PackedPlaces<D, G> places;
     auto look_up = [&](int x) {
         const int at = x + lane;
-        places.base[0] = places.base[1] = head_b;
+#pragma unroll
+        for (int b = 0; b < G; ++b) places.base[b] = head_b;
         places.info = 0;
         while (ahead.each) {
             const int last = ahead.first + ahead.each, t = at - ahead.first;
@@ -415,7 +469,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64, (packed_wa
         }
     };
     int asked = now, at = 64;
-    PackedRaw<D> raw;
+    PackedRaw<D, G> raw;
     uint32_t exists = 0;
     auto ask = [&]() __attribute__((always_inline)) {
         if (asked >= end) return;
@@ -435,10 +489,11 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64, (packed_wa
         PackedRow<kBf16, D, RB> st;
         const KeysSeen see = packed_rows_of<kBf16, D, RB>(a, st, sr, n, head, 0, rows, ln.l15, ln.g);
         for (; now < stop; ++now) {
-            PackedRaw<D> tile = raw;
-            const uint32_t ex = exists;
+            PackedStep<G> step{here.tiles.at(now - here.first), exists};
+            f32x4v sc[RB][G];
+            packed_scores<kBf16, D, RB, G>(a, st, see, ln, raw, smem, sr.len, step, sc);
             ask();
-            packed_tile<kBf16, D, RB>(a, st, see, ln, tile, smem, v, here.tiles.at(now - here.first), ex, sr.len);
+            packed_values<kBf16, D, RB, G>(a, st, ln, v, step, sc);
         }
         // The sums: finished, or to the workspace, [part][row][D] and then [part][row] reference and l.
         const bool whole = t_beg == 0 && stop == here.first + here.each;
@@ -451,7 +506,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64, (packed_wa
             if (!whole) {
                 float* po = a.part + (part * kRows + row) * D + 4 * ln.g;
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4v*>(po + 16 * c) = st.o[rb][c];
+                for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4v*>(po + 16 * c) = st.sums(rb, c);
                 if (ln.g == 0) *reinterpret_cast<f32x2v*>(a.part + (int64_t)2 * a.workers * kRows * D + (part * kRows + row) * 2) = f32x2v{st.ref[rb], l};
                 continue;
             }
@@ -460,7 +515,7 @@ template <bool kBf16, int D, int RB> __global__ __launch_bounds__(64, (packed_wa
             char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h + 4 * ln.g * kEs;
             const float inv = attn_inverse(a, here.seq, sr, row, l);
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) keys_store<kBf16>(dst + 16 * c * kEs, st.o[rb][c] * inv);
+            for (int c = 0; c < D / 16; ++c) keys_store<kBf16>(dst + 16 * c * kEs, st.sums(rb, c) * inv);
             if (a.lse && ln.g == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(st.ref[rb], l);
         }
         if (now == here.first + here.each) enter(here, here.seq + 1, now);
@@ -474,27 +529,29 @@ int packed_keys_workers(bool bf16, int d, int size) {
     return d == 128 ? packed_fit<false, 128>(size) : packed_fit<false, 64>(size);
 }
 
-template <bool kBf16, int D, int RB, int kWaves> static veda_status launch_short(const CacheAttnArgs& a, hipStream_t s) {
-    typedef PackedKeys<D> P;
+template <bool kBf16, int D, int RB, int G, int kWaves> static veda_status launch_short(const CacheAttnArgs& a, hipStream_t s) {
+    typedef PackedKeys<D, G> P;
     constexpr int kSums = kWaves * 16 * RB * (P::kOutRowB + 8), kTiles = kWaves * P::kSlot, kLds = kTiles > kSums ? kTiles : kSums;
     static_assert(kLds <= 160 * 1024, "what a compute unit has");
-    auto kern = packed_attn_keys_kernel<kBf16, D, RB, kWaves>;
+    auto kern = packed_attn_keys_kernel<kBf16, D, RB, G, kWaves>;
     if (kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.items * a.c.kv_heads)), dim3(64 * kWaves), kLds, s, a);
     return launch_status("veda_packed_attn_fwd");
 }
 
 template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheAttnArgs& a, hipStream_t s) {
+    constexpr int G = packed_groups<kBf16, D, RB>();
     if (!a.workers) {
-        if (a.items * a.c.kv_heads > 256) return launch_short<kBf16, D, RB, 2>(a, s);
-        return launch_short<kBf16, D, RB, 8>(a, s);
+        const int64_t groups = a.items * a.c.kv_heads;
+        if (groups > 768) return launch_short<kBf16, D, RB, 2, 2>(a, s);
+        return groups > 256 ? launch_short<kBf16, D, RB, 2, 4>(a, s) : launch_short<kBf16, D, RB, 2, 8>(a, s);
     }
-    hipLaunchKernelGGL((packed_attn_share_kernel<kBf16, D, RB>), dim3((unsigned)a.workers), dim3(64), (PackedKeys<D>::kSlot), s, a);
+    hipLaunchKernelGGL((packed_attn_share_kernel<kBf16, D, RB, G>), dim3((unsigned)a.workers), dim3(64), (PackedKeys<D, G>::kSlot), s, a);
     veda_status st = launch_status("veda_packed_attn_fwd");
     if (st != VEDA_OK) return st;
     const int64_t joins = (int64_t)a.c.rows * a.q_heads;
-    if (a.workers / a.c.kv_heads > 8 * a.c.seqs && joins < 1 << 23) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 8, 32>), dim3((unsigned)joins), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 1, 32>), dim3((unsigned)((joins + 7) / 8)), dim3(512), 0, s, a);
+    if (a.workers / a.c.kv_heads > 8 * a.c.seqs && joins < 1 << 22) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 16, PackedKeys<D, G>::kKeys, 8, PackedKeys<D, G>::kLeast>), dim3((unsigned)joins), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 1, PackedKeys<D, G>::kKeys, 8, PackedKeys<D, G>::kLeast>), dim3((unsigned)((joins + 7) / 8)), dim3(512), 0, s, a);
     return launch_status("veda_packed_attn_fwd");
 }
 
