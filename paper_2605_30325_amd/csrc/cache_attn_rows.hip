@@ -426,31 +426,42 @@ template <bool kBf16, int D> struct PackedTile {
             w[0] = *reinterpret_cast<const uint32_t*>(p);
         }
     }
-    // to: the segment's first row of K and of V in LDS.  exists: whether the lane's key does; others become zeros, whatever lies there.
-    __device__ __forceinline__ void store(char* k_to, char* v_to, bool exists, int lane) {
+    // Whether the lane's key exists; others become zeros, whatever lies there.
+    __device__ __forceinline__ void only(bool exists) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            k[i] = exists ? k[i] : 0u;
+            v[i] = exists ? v[i] : 0u;
+        }
+        ks = exists ? ks : 127u;
+        vs = exists ? vs : 127u;
+    }
+    // Part I of W: a word of K and of V.  k_to, v_to: the segment's first row of either in LDS.
+    template <int I> __device__ __forceinline__ void store(char* k_to, char* v_to, int lane) const {
         const int r = row(lane), c0 = channel(lane);
-        const float kp = packed_power_of(exists ? ks : 127u), vp = packed_power_of(exists ? vs : 127u);
         char* kr = k_to + r * T::kRowB;
         char* vr = v_to + r * T::kRowB;
         const int kx = T::k_swizzle(r), vx = T::v_swizzle(r);
+        if constexpr (kBf16) {
+            const int c = c0 / 8 + I;
+            *reinterpret_cast<uint4*>(kr + ((c ^ kx) << 4)) = packed_bf16(k[I], packed_power_of(ks));
+            *reinterpret_cast<uint4*>(vr + ((c ^ vx) << 4)) = packed_bf16(v[I], packed_power_of(vs));
+        } else {
+            uint4 x[2], y[2];
+            packed_f32(k[I], packed_power_of(ks), x);
+            packed_f32(v[I], packed_power_of(vs), y);
+            const int c = c0 / 4 + 2 * I;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const uint32_t kw = exists ? k[i] : 0u, vw = exists ? v[i] : 0u;
-            if constexpr (kBf16) {
-                const int c = c0 / 8 + i;
-                *reinterpret_cast<uint4*>(kr + ((c ^ kx) << 4)) = packed_bf16(kw, kp);
-                *reinterpret_cast<uint4*>(vr + ((c ^ vx) << 4)) = packed_bf16(vw, vp);
-            } else {
-                uint4 x[2], y[2];
-                packed_f32(kw, kp, x);
-                packed_f32(vw, vp, y);
-                const int c = c0 / 4 + 2 * i;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    *reinterpret_cast<uint4*>(kr + (((c + j) ^ kx) << 4)) = x[j];
-                    *reinterpret_cast<uint4*>(vr + (((c + j) ^ vx) << 4)) = y[j];
-                }
+            for (int j = 0; j < 2; ++j) {
+                *reinterpret_cast<uint4*>(kr + (((c + j) ^ kx) << 4)) = x[j];
+                *reinterpret_cast<uint4*>(vr + (((c + j) ^ vx) << 4)) = y[j];
             }
+        }
+    }
+    template <int I = 0> __device__ __forceinline__ void store_all(char* k_to, char* v_to, int lane) const {
+        if constexpr (I < W) {
+            store<I>(k_to, v_to, lane);
+            store_all<I + 1>(k_to, v_to, lane);
         }
     }
 };
@@ -521,15 +532,33 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             if (g == wave * T::kSegRows / 16) page = ok ? id : 0;
         }
     };
-    // asks for the wave's segment of tile t, number `at` of the pages looked up
+    // A packed cache: the wave's segment of tile raw_t comes into registers, one tile ahead of the one that goes into LDS.
     PackedTile<kBf16, D> raw;
+    int raw_t = 0, raw_at = 64, raw_key = 0;
+    uint32_t raw_exists = 0, next_exists = 0;
+    auto load_raw = [&]() __attribute__((always_inline)) {
+        if (raw_t >= t_end) return;
+        if (raw_at == 64) {
+            look_up(raw_t);
+            raw_at = 0;
+        }
+        raw_exists = (uint32_t)__builtin_amdgcn_readlane((int)there, raw_at);
+        raw_key = tiles.at(raw_t);
+        const int64_t from = __builtin_amdgcn_readlane(page, raw_at) * a.c.page_b + head_b;
+        raw.load(a.c.k + from, a.c.v + from, (raw_key + wave * T::kSegRows) & page_mask, a.c.log_page, lane);
+        ++raw_at;
+        ++raw_t;
+    };
+    auto open_raw = [&]() __attribute__((always_inline)) {      // before it goes into LDS
+        const int row = wave * T::kSegRows;
+        if (raw_exists != (1u << kGroups) - 1u || raw_key + kKeyTile > sr.len)
+            raw.only(((raw_exists >> (row / 16)) & 1u) && raw_key + row + PackedTile<kBf16, D>::row(lane) < sr.len);
+        next_exists = raw_exists;
+    };
+    auto place = [&](int slot) __attribute__((always_inline)) { return smem + slot * Sh::kSlot + wave * T::kSegRows * kRowB; };
+    // asks for the wave's segment of tile t, number `at` of the pages looked up
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
         const int row = wave * T::kSegRows, id = __builtin_amdgcn_readlane(page, at);
-        if constexpr (kPacked) {
-            const int64_t from = id * a.c.page_b + head_b;
-            raw.load(a.c.k + from, a.c.v + from, (tiles.at(t) + row) & page_mask, a.c.log_page, lane);
-            return;
-        }
         const int64_t from = id * a.c.page_b + head_b + ((tiles.at(t) + row) & page_mask) * kRowB;
         const uint32_t to = lds + slot * Sh::kSlot + row * kRowB;
         uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
@@ -566,7 +595,16 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     st.ref = -INFINITY;
     st.sub = st.l = 0.0f;
     int slot = 0, at = 0;
-    if (t_beg < t_end) {
+    if constexpr (kPacked) {
+        raw_t = t_beg;
+        raw_at = 64;
+        if (t_beg < t_end) {
+            load_raw();
+            open_raw();
+            raw.store_all(place(0), place(0) + kKeyTile * kRowB, lane);
+            load_raw();
+        }
+    } else if (t_beg < t_end) {
         look_up(t_beg);
         load_tile(t_beg, 0, 0);
     }
@@ -580,20 +618,16 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     bool more = false, asked = false, started = false;   // asked: for tile t + 1
     // Tile t has landed in its slot and everyone has read the other one; look-up of the next.
     auto arrive = [&]() __attribute__((always_inline)) {
-        exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
+        if constexpr (kPacked) exists = next_exists;
+        else exists = (uint32_t)__builtin_amdgcn_readlane((int)there, at);
         key0 = tiles.at(t);
         more = t + 1 < t_end;
-        if (++at == 64 && more) {
+        if (!kPacked && ++at == 64 && more) {
             look_up(t + 1);
             at = 0;
         }
-        if constexpr (kPacked) {
-            const int row = wave * T::kSegRows, key = key0 + row + PackedTile<kBf16, D>::row(lane);
-            char* to = smem + slot * Sh::kSlot + row * kRowB;
-            raw.store(to, to + kKeyTile * kRowB, ((exists >> (row / 16)) & 1u) && key < sr.len, lane);
-        }
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the other slot has been read
-        wait_vmcnt<0>();
+        if constexpr (!kPacked) wait_vmcnt<0>();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -611,10 +645,27 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
                 AttnStep<D> step;
                 step.begin(base + k_at, base + v_at + kKeyTile * kRowB);
                 step.template piece<0>(st);
-                if (more) load_tile(t + 1, at, slot ^ 1);
-                step.template piece<1>(st);
-                step.template piece<2>(st);
-                step.template piece<3>(st);
+                if constexpr (kPacked) {
+                    // the next tile's values go to the other slot under block 0's products, which no other instructions of the step ride on (where
+                    // there is no next tile what lies in the registers does, and nobody reads it)
+                    constexpr int W = PackedTile<kBf16, D>::W;
+                    char* k_to = place(slot ^ 1);
+                    char* v_to = k_to + kKeyTile * kRowB;
+                    open_raw();
+                    raw.template store<0>(k_to, v_to, lane);
+                    step.template piece<1>(st);
+                    raw.template store<1>(k_to, v_to, lane);
+                    step.template piece<2>(st);
+                    if constexpr (W == 4) raw.template store<2>(k_to, v_to, lane);
+                    step.template piece<3>(st);
+                    if constexpr (W == 4) raw.template store<3>(k_to, v_to, lane);
+                    load_raw();
+                } else {
+                    if (more) load_tile(t + 1, at, slot ^ 1);
+                    step.template piece<1>(st);
+                    step.template piece<2>(st);
+                    step.template piece<3>(st);
+                }
                 asked = true;
                 if (!step.scores(st, a.scale_log2)) break;
                 step.values(st, a.scale_log2);
@@ -627,7 +678,15 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             if (!left) break;
         }
         const uint32_t base = lds + slot * Sh::kSlot;
-        if (more && !asked) load_tile(t + 1, at, slot ^ 1);
+        if (more && !asked) {
+            if constexpr (kPacked) {
+                open_raw();
+                raw.store_all(place(slot ^ 1), place(slot ^ 1) + kKeyTile * kRowB, lane);
+                load_raw();
+            } else {
+                load_tile(t + 1, at, slot ^ 1);
+            }
+        }
         asked = false;
         started = true;
 #pragma unroll 1
