@@ -100,6 +100,9 @@ struct TileShare {
     __device__ __forceinline__ int owner(int tile) const { return (int)((((int64_t)tile + 1) * parts + total - 1) / total) - 1; }
 };
 
+// Pieces that unfinished sums can come in, at most (see the sharing kernel).
+__device__ __forceinline__ int64_t rows_pieces(const CacheAttnArgs& a) { return 2 * (int64_t)a.workers + a.items * a.c.kv_heads; }
+
 // Launches: blocks of 128 rows (cache_attn_rows.hip), and blocks of 16 or 32 (cache_attn_keys.hip); and the workgroups of either that
 // run at once on the card's 256 compute units.
 constexpr int kAttnRows = 128;

@@ -18,7 +18,7 @@
 // some do, and as long again as two of them for the set-up and the results.  fp32 (v_mfma_f32_32x32x2_f32): 2464 rows x 12 heads on 2000 keys, causal, 0.35 ms,
 // matrix pipes 73 % busy, 102 TFLOP/s on visible keys of the 154 that a large product reaches.
 #include "cache_attn.h"
-#include "packed.h"
+#include "packed_attn_rows.h"
 #include "store.h"
 
 namespace veda {
@@ -396,79 +396,6 @@ template <bool kBf16, int D> struct AttnShape {
     static constexpr int kLds = 2 * kSlot > kOutB ? 2 * kSlot : kOutB;
 };
 
-// A cache held in 4 bits: the tile's segment of a wave comes into its registers, C channels of one row of K and of V to a lane (their codes
-// and the byte of their 32), and is written to the tile in LDS as the values that it stands for, in the places that direct loads would
-// have put them.  Everything behind is as for a cache of such values.
-template <bool kBf16, int D> struct PackedTile {
-    typedef AttnTile<kBf16, D> T;
-    static constexpr int C = T::kSegRows * D / 64, W = C / 8;    // channels, and words of codes
-    uint32_t k[W], v[W];
-    uint32_t ks, vs;
-    __device__ static int row(int lane) { return lane * C / D; }
-    __device__ static int channel(int lane) { return lane * C % D; }
-    // k_at, v_at: the head's place in the page; tok: the segment's first row in it; page: its tokens.
-    __device__ __forceinline__ void load(const char* k_at, const char* v_at, int tok, int log_page, int lane) {
-        const uint32_t code = (uint32_t)(lane * C / 2), scale = (uint32_t)(lane * C / 32);
-        const int64_t at = (int64_t)tok * (D / 2), s_at = ((int64_t)(D / 2) << log_page) + (int64_t)tok * (D / 32);
-        ks = *reinterpret_cast<const uint8_t*>(k_at + s_at + scale);
-        vs = *reinterpret_cast<const uint8_t*>(v_at + s_at + scale);
-        words(k_at + at + code, k);
-        words(v_at + at + code, v);
-    }
-    __device__ static __forceinline__ void words(const char* p, uint32_t (&w)[W]) {
-        if constexpr (W == 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p);
-            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-        } else if constexpr (W == 2) {
-            const uint2 x = *reinterpret_cast<const uint2*>(p);
-            w[0] = x.x; w[1] = x.y;
-        } else {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
-        }
-    }
-    // Whether the lane's key exists; others become zeros, whatever lies there.
-    __device__ __forceinline__ void only(bool exists) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            k[i] = exists ? k[i] : 0u;
-            v[i] = exists ? v[i] : 0u;
-        }
-        ks = exists ? ks : 127u;
-        vs = exists ? vs : 127u;
-    }
-    // Part I of W: a word of K and of V.  k_to, v_to: the segment's first row of either in LDS.
-    template <int I> __device__ __forceinline__ void store(char* k_to, char* v_to, int lane) const {
-        const int r = row(lane), c0 = channel(lane);
-        char* kr = k_to + r * T::kRowB;
-        char* vr = v_to + r * T::kRowB;
-        const int kx = T::k_swizzle(r), vx = T::v_swizzle(r);
-        if constexpr (kBf16) {
-            const int c = c0 / 8 + I;
-            *reinterpret_cast<uint4*>(kr + ((c ^ kx) << 4)) = packed_bf16(k[I], packed_power_of(ks));
-            *reinterpret_cast<uint4*>(vr + ((c ^ vx) << 4)) = packed_bf16(v[I], packed_power_of(vs));
-        } else {
-            uint4 x[2], y[2];
-            packed_f32(k[I], packed_power_of(ks), x);
-            packed_f32(v[I], packed_power_of(vs), y);
-            const int c = c0 / 4 + 2 * I;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                *reinterpret_cast<uint4*>(kr + (((c + j) ^ kx) << 4)) = x[j];
-                *reinterpret_cast<uint4*>(vr + (((c + j) ^ vx) << 4)) = y[j];
-            }
-        }
-    }
-    template <int I = 0> __device__ __forceinline__ void store_all(char* k_to, char* v_to, int lane) const {
-        if constexpr (I < W) {
-            store<I>(k_to, v_to, lane);
-            store_all<I + 1>(k_to, v_to, lane);
-        }
-    }
-};
-
-// Pieces that unfinished sums can come in, at most (see the sharing kernel).
-__device__ __forceinline__ int64_t rows_pieces(const CacheAttnArgs& a) { return 2 * (int64_t)a.workers + a.items * a.c.kv_heads; }
-
 // Tiles t_beg .. t_end - 1 of those that rows r0 .. r_end - 1 of a sequence see, for one key head.  part: where the unfinished sums go,
 // or -1 if these are all the tiles.
 template <bool kBf16, int D, bool kPacked>
@@ -533,7 +460,8 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         }
     };
     // A packed cache: the wave's segment of tile raw_t comes into registers, one tile ahead of the one that goes into LDS.
-    PackedTile<kBf16, D> raw;
+    typedef PackedTile<D, T::kSegRows> Raw;
+    Raw raw;
     int raw_t = 0, raw_at = 64, raw_key = 0;
     uint32_t raw_exists = 0, next_exists = 0;
     auto load_raw = [&]() __attribute__((always_inline)) {
@@ -552,9 +480,10 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     auto open_raw = [&]() __attribute__((always_inline)) {      // before it goes into LDS
         const int row = wave * T::kSegRows;
         if (raw_exists != (1u << kGroups) - 1u || raw_key + kKeyTile > sr.len)
-            raw.only(((raw_exists >> (row / 16)) & 1u) && raw_key + row + PackedTile<kBf16, D>::row(lane) < sr.len);
+            raw.only(((raw_exists >> (row / 16)) & 1u) && raw_key + row + Raw::row(lane) < sr.len);
         next_exists = raw_exists;
     };
+    const int raw_kx = T::k_swizzle(Raw::row(lane)), raw_vx = T::v_swizzle(Raw::row(lane));
     auto place = [&](int slot) __attribute__((always_inline)) { return smem + slot * Sh::kSlot + wave * T::kSegRows * kRowB; };
     // asks for the wave's segment of tile t, number `at` of the pages looked up
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
@@ -601,7 +530,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         if (t_beg < t_end) {
             load_raw();
             open_raw();
-            raw.store_all(place(0), place(0) + kKeyTile * kRowB, lane);
+            raw.store_all(place(0), place(0) + kKeyTile * kRowB, raw_kx, raw_vx, lane);
             load_raw();
         }
     } else if (t_beg < t_end) {
@@ -648,17 +577,17 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
                 if constexpr (kPacked) {
                     // the next tile's values go to the other slot under block 0's products, which no other instructions of the step ride on (where
                     // there is no next tile what lies in the registers does, and nobody reads it)
-                    constexpr int W = PackedTile<kBf16, D>::W;
+                    constexpr int W = Raw::W;
                     char* k_to = place(slot ^ 1);
                     char* v_to = k_to + kKeyTile * kRowB;
                     open_raw();
-                    raw.template store<0>(k_to, v_to, lane);
+                    raw.template store<0>(k_to, v_to, raw_kx, raw_vx, lane);
                     step.template piece<1>(st);
-                    raw.template store<1>(k_to, v_to, lane);
+                    raw.template store<1>(k_to, v_to, raw_kx, raw_vx, lane);
                     step.template piece<2>(st);
-                    if constexpr (W == 4) raw.template store<2>(k_to, v_to, lane);
+                    if constexpr (W == 4) raw.template store<2>(k_to, v_to, raw_kx, raw_vx, lane);
                     step.template piece<3>(st);
-                    if constexpr (W == 4) raw.template store<3>(k_to, v_to, lane);
+                    if constexpr (W == 4) raw.template store<3>(k_to, v_to, raw_kx, raw_vx, lane);
                     load_raw();
                 } else {
                     if (more) load_tile(t + 1, at, slot ^ 1);
@@ -681,7 +610,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         if (more && !asked) {
             if constexpr (kPacked) {
                 open_raw();
-                raw.store_all(place(slot ^ 1), place(slot ^ 1) + kKeyTile * kRowB, lane);
+                raw.store_all(place(slot ^ 1), place(slot ^ 1) + kKeyTile * kRowB, raw_kx, raw_vx, lane);
                 load_raw();
             } else {
                 load_tile(t + 1, at, slot ^ 1);
@@ -771,9 +700,21 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     }
 }
 
+// fp32 rows over a packed cache have a piece of their own (packed_attn_rows.h).
+template <bool kBf16, bool kPacked> constexpr bool rows_split() { return kPacked && !kBf16; }
+template <bool kBf16, bool kPacked> constexpr int rows_threads() { return rows_split<kBf16, kPacked>() ? kSplitThreads : 256; }
+template <bool kBf16, bool kPacked> constexpr int rows_waves() { return rows_split<kBf16, kPacked>() ? kSplitWaves : 2; }
+template <bool kBf16, int D, bool kPacked> constexpr int rows_tile() { return rows_split<kBf16, kPacked>() ? kSplitKeys : AttnShape<kBf16, D>::kKeyTile; }
+template <bool kBf16, int D, bool kPacked>
+__device__ __forceinline__ void rows_piece_of(const CacheAttnArgs& a, char* smem, int seq, const SeqRows& sr, int r0, int r_end, int head,
+                                              const AttnTiles& tiles, int t_beg, int t_end, int64_t part) {
+    if constexpr (rows_split<kBf16, kPacked>()) split_piece<D>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, t_end, part);
+    else rows_piece<kBf16, D, kPacked>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, t_end, part);
+}
+
 // A workgroup for each (block of rows, key head).  Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of
 // a head meet in few L2 caches.
-template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) void cache_attn_rows_kernel(CacheAttnArgs a) {
+template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_threads<kBf16, kPacked>()), (rows_waves<kBf16, kPacked>())) void cache_attn_rows_kernel(CacheAttnArgs a) {
     extern __shared__ __align__(1024) char smem[];
     RowBlock rb;
     if (!block_of(a.c, a.group, kAttnRows, a.per_seq, blockIdx.x / a.c.kv_heads, rb)) return;
@@ -781,8 +722,8 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) 
     const int rows = min(sr.n, a.c.max_new) * a.group;
     const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
     const int r_end = min(rows, r0 + kAttnRows);
-    const AttnTiles tiles = tiles_seen(a, sr, min(sr.n, a.c.max_new), r0, r_end - 1, AttnShape<kBf16, D>::kKeyTile);
-    rows_piece<kBf16, D, kPacked>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
+    const AttnTiles tiles = tiles_seen(a, sr, min(sr.n, a.c.max_new), r0, r_end - 1, rows_tile<kBf16, D, kPacked>());
+    rows_piece_of<kBf16, D, kPacked>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
 }
 
 // Where there are few blocks, a workgroup for each leaves compute units idle, so their tiles are dealt out to as many workgroups as fit the
@@ -809,8 +750,8 @@ template <int D> __device__ __forceinline__ int4* rows_cuts(const CacheAttnArgs&
     return reinterpret_cast<int4*>(a.part + rows_pieces(a) * a.part_rows * (D + 2));
 }
 
-template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
-    constexpr int kTile = AttnShape<kBf16, D>::kKeyTile, kPiece = kBf16 ? 1 : 2;
+template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_threads<kBf16, kPacked>()), (rows_waves<kBf16, kPacked>())) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
+    constexpr int kTile = rows_tile<kBf16, D, kPacked>(), kPiece = kBf16 || kPacked ? 1 : 2;
     extern __shared__ __align__(1024) char smem[];
     auto rest_units = [](int tiles) { return tiles ? tiles + kPiece : 0; };
     const int lane = threadIdx.x & 63, head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads, parts = a.workers / a.c.kv_heads;
@@ -827,6 +768,7 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) 
         int f = 0, u = 0;
 #pragma unroll
         for (int k = 0; k < kRowsShareItems / 64; ++k) {
+            if (kPacked && 64 * k >= a.items) continue;
             f += counts[k] / level;
             u += rest_units(counts[k] % level);
         }
@@ -844,6 +786,7 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) 
     bool found = false;
 #pragma unroll
     for (int k = 0; k < kRowsShareItems / 64; ++k) {
+        if (kPacked && 64 * k >= a.items) continue;
         const int f = counts[k] / level, u = rest_units(counts[k] % level), up_f = lanes_up_to(f), up_u = lanes_up_to(u);
         const int all_f = __builtin_amdgcn_readlane(up_f, 63), all_u = __builtin_amdgcn_readlane(up_u, 63);
         if (found) continue;
@@ -876,7 +819,7 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__(256, 2) 
                 rows_cuts<D>(a)[item * a.c.kv_heads + head] = int4{whole ? 0 : f, first_full, whole ? 0 : q1 - q0 + 1, q0};
             }
             if (again) __syncthreads();   // the last piece's results have left the slots
-            rows_piece<kBf16, D, kPacked>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
+            rows_piece_of<kBf16, D, kPacked>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
             again = true;
         }
         now = full ? end : max(now, min(end, next_unit));
@@ -965,10 +908,10 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
 }
 
 template <bool kBf16, int D, bool kPacked> static veda_status launch_rows(const CacheAttnArgs& a, hipStream_t s, const char* what) {
-    typedef AttnShape<kBf16, D> Sh;
+    constexpr int kLds = rows_split<kBf16, kPacked>() ? split_lds<D>() : AttnShape<kBf16, D>::kLds, kThreads = rows_threads<kBf16, kPacked>();
     auto kern = a.workers ? cache_attn_rows_share_kernel<kBf16, D, kPacked> : cache_attn_rows_kernel<kBf16, D, kPacked>;
-    if (Sh::kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds));
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.workers ? a.workers : a.items * a.c.kv_heads)), dim3(256), Sh::kLds, s, a);
+    if (kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.workers ? a.workers : a.items * a.c.kv_heads)), dim3(kThreads), kLds, s, a);
     const veda_status st = launch_status(what);
     if (st != VEDA_OK || !a.workers) return st;
     hipLaunchKernelGGL((cache_attn_rows_join_kernel<kBf16, D>), dim3((unsigned)(a.items * a.c.kv_heads), (unsigned)((a.part_rows + 3) / 4)), dim3(256), 0, s, a);

@@ -38,6 +38,34 @@ __device__ __forceinline__ void packed_f32(uint32_t w, float power, uint4 (&x)[2
     x[1] = uint4{__float_as_uint(c[0]), __float_as_uint(c[1]), __float_as_uint(d[0]), __float_as_uint(d[1])};
 }
 
+// fp32 as three bf16 parts: the value with its bits cut off at 8, twice, and what is left (8 bits at most).  Only the first part of what is not finite.
+__device__ __forceinline__ void packed_parts(float x, __bf16 (&p)[3]) {
+    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u), r = fabsf(x) < INFINITY ? x - a : 0.0f;
+    const float b = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+    p[0] = (__bf16)(fabsf(x) < INFINITY ? a : x);
+    p[1] = (__bf16)b;
+    p[2] = (__bf16)(r - b);
+}
+
+template <int W> __device__ __forceinline__ void packed_words(const char* p, uint32_t (&w)[W]) {
+    if constexpr (W == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    } else if constexpr (W == 2) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        w[0] = x.x; w[1] = x.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+
+// bf16 V in LDS, rows of D channels, for products of 16 channels: 16-byte chunk c of row r lies at chunk c ^ swizzle.  Four rows that 16 lanes write a chunk of
+// each quarter of, and eight rows that 32 lanes read two neighbouring chunks of, then fall into different banks.
+template <int D> __device__ __forceinline__ int packed_v_swizzle(int r) {
+    const int k0 = r & 1, k1 = (r >> 1) & 1, k2 = (r >> 2) & 1;
+    return D == 128 ? k2 << 3 | k0 << 2 | k1 << 1 | k0 : k2 << 2 | k1 << 1 | k1;
+}
+
 #endif
 
 }  // namespace veda

@@ -20,12 +20,6 @@ template <int D, int G> struct PackedKeys {
     static constexpr int kRowB = D / 2, kScaleB = D / 32;
     static constexpr int kSlot = kKeys * D * 2;          // V in LDS
     static constexpr int kOutRowB = D * 4 + 16;          // a row of the sums in LDS
-    // 16-byte chunk c of V's row r lies at chunk c ^ swizzle: four rows that 16 lanes write a chunk of each quarter of, and eight rows that
-    // 32 lanes read two neighbouring chunks of, then fall into different banks.
-    __device__ static int swizzle(int r) {
-        const int k0 = r & 1, k1 = (r >> 1) & 1, k2 = (r >> 2) & 1;
-        return D == 128 ? k2 << 3 | k0 << 2 | k1 << 1 | k0 : k2 << 2 | k1 << 1 | k1;
-    }
 };
 
 template <bool kBf16, int D, int RB> struct PackedRow {
@@ -55,16 +49,6 @@ template <int D, int G> struct PackedRaw {
     uint32_t k[G][D / 32], v[G][D / 32];
     uint32_t ks[G], vs[G];
 };
-template <int W> __device__ __forceinline__ void packed_words(const char* p, uint32_t (&w)[W]) {
-    if constexpr (W == 4) {
-        const uint4 x = *reinterpret_cast<const uint4*>(p);
-        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-    } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
-        w[0] = x.x; w[1] = x.y;
-    }
-}
-
 template <int D, int G> struct PackedLane {
     typedef PackedKeys<D, G> P;
     uint32_t k_code, k_scale, v_code, v_scale;           // what the lane adds to addresses in a pool
@@ -75,9 +59,9 @@ template <int D, int G> struct PackedLane {
         k_scale = (uint32_t)(l15 * P::kScaleB + g * (D / 4) / 32);
         v_code = (uint32_t)(lane * (D / 8));
         v_scale = (uint32_t)((lane >> 2) * P::kScaleB + (lane & 3) * (D / 4) / 32);
-        v_to = (uint32_t)((lane >> 2) * D * 2 + ((((lane & 3) * (D / 32)) ^ P::swizzle(lane >> 2)) << 4));
+        v_to = (uint32_t)((lane >> 2) * D * 2 + ((((lane & 3) * (D / 32)) ^ packed_v_swizzle<D>(lane >> 2)) << 4));
         const int key = 4 * g + (l15 >> 2);
-        v_at = (uint32_t)(key * D * 2 + ((((l15 & 3) >> 1) ^ P::swizzle(key)) << 4) + 8 * (l15 & 1));
+        v_at = (uint32_t)(key * D * 2 + ((((l15 & 3) >> 1) ^ packed_v_swizzle<D>(key)) << 4) + 8 * (l15 & 1));
     }
     // The same place for all lanes, in scalar registers, and what a lane adds to it.
     __device__ static __forceinline__ const char* at(const char* all, uint32_t lane_part) {
@@ -102,15 +86,6 @@ template <int D> __device__ __forceinline__ bool packed_from(const CacheArgs& c,
     base = ok ? id * c.page_b + head_b : head_b;   // any place in the pool will do
     at = ok ? tok & ((1 << c.log_page) - 1) : 0;
     return ok;
-}
-
-// fp32 as three bf16 parts: the value with its bits cut off at 8, twice, and what is left (8 bits at most).  Only the first part of what is not finite.
-__device__ __forceinline__ void packed_parts(float x, __bf16 (&p)[3]) {
-    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u), r = fabsf(x) < INFINITY ? x - a : 0.0f;
-    const float b = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-    p[0] = (__bf16)(fabsf(x) < INFINITY ? a : x);
-    p[1] = (__bf16)b;
-    p[2] = (__bf16)(r - b);
 }
 
 // The rows of a block: what they see and ask for, and no sums yet.
