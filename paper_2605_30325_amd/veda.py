@@ -957,13 +957,9 @@ def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: 
     return sq
 
 
-def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
-                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
-                        workspace: Optional[torch.Tensor] = None):
-    """Attention of the new rows q [rows, q_heads, d] over the cache.  block, window, sinks: which keys a row sees (veda_visible: block 1
-    causal, 0 everything).  Returns (out [rows, q_heads, d], lse fp32 [q_heads, rows] or None); rows of no sequence are left as they are
-    in buffers given, and undefined in buffers made here."""
-    w = "veda_cache_attn_fwd"
+def _attn_fwd(kind: str, cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int, window: int, sinks: int,
+              out: Optional[torch.Tensor], lse: Optional[torch.Tensor], want_lse: bool, workspace: Optional[torch.Tensor]):
+    w = kind + "_fwd"
     sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)
     rows, heads = q.shape[0], q.shape[1]
     if out is None:
@@ -978,14 +974,23 @@ def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softma
     bs = batch.struct(rows)
     lib, ref = load(), C.byref(bs)
     if workspace is None:
-        need = int(lib.veda_cache_attn_workspace_bytes(cache._ref, ref, heads))
+        need = int(getattr(lib, kind + "_workspace_bytes")(cache._ref, ref, heads))
         workspace = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
     elif workspace.device != cache.device or not workspace.is_contiguous():
         _refuse(w, "the workspace must be contiguous and where the cache is")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.veda_cache_attn_fwd(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, veda_visible(block, window, sinks), out.data_ptr(), so,
-                                   _ptr(lse), _ptr(workspace) or None, nbytes, _stream_of(cache.device)), w)
+    _check(getattr(lib, w)(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, veda_visible(block, window, sinks), out.data_ptr(), so,
+                           _ptr(lse), _ptr(workspace) or None, nbytes, _stream_of(cache.device)), w)
     return out, lse
+
+
+def veda_cache_attn_fwd(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                        workspace: Optional[torch.Tensor] = None):
+    """Attention of the new rows q [rows, q_heads, d] over the cache.  block, window, sinks: which keys a row sees (veda_visible: block 1
+    causal, 0 everything).  Returns (out [rows, q_heads, d], lse fp32 [q_heads, rows] or None); rows of no sequence are left as they are
+    in buffers given, and undefined in buffers made here."""
+    return _attn_fwd("veda_cache_attn", cache, batch, q, softmax_scale, block, window, sinks, out, lse, want_lse, workspace)
 
 
 def veda_packed_append(cache: PackedCache, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
@@ -1025,33 +1030,11 @@ def veda_packed_append(cache: PackedCache, batch: CacheBatch, k: torch.Tensor, v
 
 
 def veda_packed_attn_fwd(cache: PackedCache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int = 1, window: int = 0, sinks: int = 0,
-                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
-                        workspace: Optional[torch.Tensor] = None):
+                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                         workspace: Optional[torch.Tensor] = None):
     """veda_cache_attn_fwd over a cache held in 4 bits: the same arguments and results."""
-    w = "veda_packed_attn_fwd"
-    _need(isinstance(cache, PackedCache), w, "the cache is not held in 4 bits")
-    sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)
-    rows, heads = q.shape[0], q.shape[1]
-    if out is None:
-        out = torch.empty((rows, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
-    so = _rows(cache, out, rows, w, "out")
-    if out.shape[1] != heads:
-        _refuse(w, "out must have q's heads")
-    if want_lse and lse is None:
-        lse = torch.empty((heads, rows), dtype=torch.float32, device=cache.device)
-    if lse is not None and (tuple(lse.shape) != (heads, rows) or lse.dtype != torch.float32 or lse.device != cache.device or not lse.is_contiguous()):
-        _refuse(w, "lse must be contiguous fp32 [q_heads, rows]")
-    bs = batch.struct(rows)
-    lib, ref = load(), C.byref(bs)
-    if workspace is None:
-        need = int(lib.veda_packed_attn_workspace_bytes(cache._ref, ref, heads))
-        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
-    elif workspace.device != cache.device or not workspace.is_contiguous():
-        _refuse(w, "the workspace must be contiguous and where the cache is")
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.veda_packed_attn_fwd(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, veda_visible(block, window, sinks), out.data_ptr(), so,
-                                   _ptr(lse), _ptr(workspace) or None, nbytes, _stream_of(cache.device)), w)
-    return out, lse
+    _need(isinstance(cache, PackedCache), "veda_packed_attn_fwd", "the cache is not held in 4 bits")
+    return _attn_fwd("veda_packed_attn", cache, batch, q, softmax_scale, block, window, sinks, out, lse, want_lse, workspace)
 
 
 def _pairs(pairs, w: str) -> np.ndarray:
