@@ -62,6 +62,7 @@ __global__ __launch_bounds__(kGiveThreads) void pages_give_back_kernel(StepArgs 
         for (int j = threadIdx.x; j < i; j += kGiveThreads) taken = taken || a.step.seq[j] == seq;
     taken = __syncthreads_or(taken);
     const StepAsk k = step_ask(a, i, seq, taken);
+    __syncthreads();    // all threads have read the length
     if (threadIdx.x == 0) {
         a.out.status[i] = k.kept < 0 ? VEDA_STEP_REFUSED : VEDA_STEP_SERVED;
         if (k.kept >= 0) a.book.length[k.seq] = k.kept;
@@ -391,8 +392,8 @@ extern "C" veda_status veda_pages_step(const veda_device_pages* book, const veda
     if (step->seqs > 0 && (!step->grow || !out->page_table || !out->kv_len || !out->status)) return VEDA_ERR_INVALID_ARG;
     if (!step->seq && step->seqs > book->max_seqs) return VEDA_ERR_INVALID_ARG;
     for (const int32_t* in : {step->seq, step->keep, step->evict, step->grow})       // read after others' results are written
-        for (const int32_t* res : {out->page_table, out->kv_len, out->q_start, out->status, out->positions, out->row_seq, book->table, book->length})
-            if (in && in == res) return VEDA_ERR_INVALID_ARG;
+        for (const int32_t* res : {out->page_table, out->kv_len, out->q_start, out->status, out->positions, out->row_seq, book->table, book->length, (int32_t*)book->used})
+            if (in && (in == res || in == (const int32_t*)out->slots)) return VEDA_ERR_INVALID_ARG;
     if (book->pages > 1 << 19 || book->max_seqs > 8192 || step->seqs > 8192 || step->rows > 1 << 30) return VEDA_ERR_UNSUPPORTED;
     if ((int64_t)book->max_pages * book->page_tokens > (int64_t)1 << 30) return VEDA_ERR_UNSUPPORTED;
     const hipStream_t s = (hipStream_t)stream;

@@ -150,6 +150,7 @@ def test_bad_books_are_refused(lib, book, status):
     (dict(seqs=8193), {}, UNSUPPORTED), (dict(rows=(1 << 30) + 1), {}, UNSUPPORTED), ({}, dict(table_stride=7), INVALID), ({}, dict(page_table=None), INVALID),
     ({}, dict(kv_len=None), INVALID), ({}, dict(q_start=None), INVALID), ({}, dict(status=None), INVALID),
     ({}, dict(kv_len=5 * AT), INVALID), ({}, dict(status=7 * AT), INVALID), (dict(keep=2 * AT), {}, INVALID), (dict(seq=8 * AT), {}, INVALID),
+    (dict(evict=3 * AT), {}, INVALID), (dict(grow=14 * AT), {}, INVALID),
 ])
 def test_bad_steps_are_refused(lib, step, out, status):
     assert _step(lib, step=step, out=out) == status
@@ -201,3 +202,20 @@ def test_the_binding_refuses_what_does_not_fit(monkeypatch):
             veda.veda_pages_step(book, out, *args)
     with pytest.raises(veda.VedaError, match="another book"):
         veda.veda_pages_step(veda.DevicePages(40, 16, 2, 5, **cpu), out, torch.zeros(3, dtype=i32))
+
+
+def test_calls_of_the_other_cache_refuse_this_one(lib, monkeypatch):
+    cpu, i32 = dict(device="cpu"), torch.int32
+    packed, plain = veda.PackedCache(4, 16, 2, 64, torch.bfloat16, **cpu), veda.Cache(4, 16, 2, 64, torch.bfloat16, **cpu)
+    batch = veda.CacheBatch(torch.zeros(1, 2, dtype=i32), torch.zeros(1, dtype=i32), torch.zeros(2, dtype=i32), 1)
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    monkeypatch.setattr(veda, "_on", lambda *a: None)
+    monkeypatch.setattr(veda, "_stream_of", lambda *a: 0)
+    for call in (lambda: veda.veda_cache_append(packed, batch, x, x), lambda: veda.veda_cache_attn_fwd(packed, batch, x, 0.1),
+                 lambda: veda.veda_cache_copy_pages(packed, [(0, 1)]), lambda: veda.veda_cache_attn_workspace_bytes(packed, batch, 2, 3)):
+        with pytest.raises(C.ArgumentError):
+            call()
+    for call in (lambda: veda.veda_packed_append(plain, batch, x, x), lambda: veda.veda_packed_attn_fwd(plain, batch, x, 0.1),
+                 lambda: veda.veda_packed_copy_pages(plain, [(0, 1)])):
+        with pytest.raises(veda.VedaError, match="4 bits"):
+            call()

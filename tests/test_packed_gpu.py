@@ -594,6 +594,25 @@ def test_captured_and_on_another_stream(dtype, n, past):
         assert torch.equal(got[:n + 2], want[:n + 2]) and torch.equal(t.cache.k, after[0]) and torch.equal(t.cache.v, after[1])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_captured_calls_that_share_a_workspace(dtype):
+    """Calls of different shapes captured into graphs of their own, on one workspace: replayed in any order on one stream, each gives its own result."""
+    cases = [Packed([n, 2], [past, 40], 8, 2, 128, dtype, page=64, seed=60 + i) for i, (n, past) in enumerate([(1, 6000), (3, 9000), (70, 1500)])]
+    need = max(veda.veda_packed_attn_workspace_bytes(t.cache, t.batch, t.hq, t.rows) for t in cases)
+    work = torch.empty(need, dtype=torch.uint8, device=dev())
+    want = [veda.veda_packed_attn_fwd(t.cache, t.batch, t.q, 0.1)[0] for t in cases]
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in cases], [torch.zeros_like(x) for x in want]
+    for t, g, out in zip(cases, graphs, outs):
+        with torch.cuda.graph(g):
+            veda.veda_packed_attn_fwd(t.cache, t.batch, t.q, 0.1, out=out, workspace=work)
+    for i in (0, 1, 0, 2, 1, 2, 0):
+        outs[i].zero_()
+        graphs[i].replay()
+        work.fill_(255) if i == 1 else None        # what a call leaves in it is of no use to the next
+        used = int(cases[i].start[-1])
+        assert torch.equal(outs[i][:used], want[i][:used]), i
+
+
 def test_one_call_of_a_step_is_its_parts():
     t = Packed([40, 3], [100, 9], 4, 2, 128, BF16, page=32, seed=17)
     x = normal((t.rows, 4, 128), BF16, 3)
@@ -757,6 +776,21 @@ def test_steps_without_lists():
     before = out.slots.clone()
     assert veda.load().veda_pages_step(book._ref, C.byref(step), C.byref(few), None) == veda.VEDA_OK
     assert out.kv_len.tolist() == [n + 1 for n in model.length[:4]] and torch.equal(out.slots, before)
+
+
+def test_long_sequences_go_back_whole():
+    # more entries to give back than a workgroup has threads, from many sequences at once, again and again
+    seqs, width = 40, 700
+    book = veda.DevicePages(seqs * width, 16, seqs, width)
+    t = lambda x: torch.tensor(x, dtype=torch.int32, device=dev())
+    out = veda.StepTables(book, seqs, seqs * width * 16, width * 16)
+    for i in range(20):
+        veda.veda_pages_step(book, out, t([width * 16] * seqs), None, t([0] * seqs))
+        assert out.kv_len.tolist() == [width * 16] * seqs and not out.status.any()
+        assert sorted(out.page_table.flatten().tolist()) == list(range(seqs * width))
+        veda.veda_pages_step(book, out, t([0] * seqs), None, t([i] * seqs))
+        bits = np.unpackbits(book.used.cpu().numpy().view(np.uint8))
+        assert bits.sum() == seqs * -(-i // 16) and out.kv_len.tolist() == [i] * seqs
 
 
 def test_books_with_wild_numbers_stay_inside():
