@@ -103,7 +103,7 @@ struct TileShare {
 // Pieces that unfinished sums can come in, at most (see the sharing kernel).
 __device__ __forceinline__ int64_t rows_pieces(const CacheAttnArgs& a) { return 2 * (int64_t)a.workers + a.items * a.c.kv_heads; }
 
-// Launches: blocks of 128 rows (cache_attn_rows.hip), and blocks of 16 or 32 (cache_attn_keys.hip); and the workgroups of either that
+// Launches: blocks of 128 rows, or 256 (cache_attn_rows.hip; a.part_rows says so), and blocks of 16 or 32 (cache_attn_keys.hip); and the workgroups of either that
 // run at once on the card's 256 compute units.
 constexpr int kAttnRows = 128;
 constexpr int kRowsShareItems = 256;   // blocks of rows that can be shared out, at most

@@ -18,12 +18,19 @@ static int64_t packed_short(bool bf16, int d, int64_t groups) {
 
 // How a call is cut up.
 struct AttnCut {
-    int32_t size;       // rows of a block: 16 or 32 where a key head has no more rows than that for any sequence, else 128
+    int32_t size;       // rows of a block: 16 or 32 where a key head has no more rows than that for any sequence, else 128 or 256
     int32_t per_seq;    // see CacheAttnArgs
     int32_t workers;
     int32_t part_rows;
     int64_t items;
+    size_t bytes;       // of workspace
 };
+// unfinished sums with references and l: two blocks of few rows a workgroup, or the pieces of the others and how they were cut
+static size_t attn_workspace(const veda_cache* c, const AttnCut& cut) {
+    if (!cut.workers) return 0;
+    const size_t block = (size_t)cut.part_rows * (size_t)(c->head_dim + 2) * sizeof(float), groups = (size_t)cut.items * (size_t)c->kv_heads;
+    return cut.size < kAttnRows ? (size_t)2 * cut.workers * block : ((size_t)2 * cut.workers + groups) * block + groups * 16;
+}
 static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch* b, int32_t q_heads, veda_visible vis) {
     AttnCut cut{};
     const int64_t max_new = b->max_new < b->rows ? b->max_new : b->rows, group = q_heads / c->kv_heads, rows = max_new * group;
@@ -32,7 +39,7 @@ static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch
     cut.size = rows <= 16 ? 16 : rows <= 32 ? 32 : kAttnRows;
     // Even, so that the sums of a block, part_rows * (d + 2) floats, are whole 16 bytes: the list of cuts behind them is read 16 bytes at a time.
     cut.part_rows = few ? cut.size : rows < kAttnRows ? (int32_t)(rows + 1) & ~1 : kAttnRows;
-    const int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
+    int64_t each = (rows + cut.size - 1) / cut.size, uniform = b->seqs * each;
     cut.items = block_items(b->seqs, b->rows, max_new, group, cut.size);
     int64_t keys = (int64_t)b->max_pages * c->page_tokens;
     const bool countable = uniform <= 1024 && uniform * (keys / 16 + 8) < (int64_t)1 << 31;   // tiles; whatever the window, so that it never asks for more workspace
@@ -65,18 +72,33 @@ static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch
     const int64_t short_few = packed ? packed_short(bf16, d, groups) : bf16 ? (groups <= 256 ? 2560 : 1536) : grown < 4096 ? grown : 4096;
     const bool share = keys > (few ? short_few : bf16 ? 512 + 16 * groups : 192) && countable &&
                        (few ? groups <= 8 * fit : uniform <= kRowsShareItems && 5 * groups < 4 * attn_rows_places());
-    if (share) cut.workers = (int32_t)(fit < c->kv_heads ? c->kv_heads : fit / c->kv_heads * c->kv_heads);
-    if (share || blocks_even(uniform, cut.items)) {
-        cut.items = uniform;
-        cut.per_seq = (int32_t)each;
+    // bf16 rows of a packed cache, d = 128: blocks of 256 rows, whose eight waves turn a tile's codes into values once where two blocks of 128 do it
+    // twice, but load, begin and end together.  Where that fills no more than a quarter of rows in vain, and walks are long: of two tiles at least
+    // for each workgroup that shares, of 4096 keys in several rounds of workgroups, 10240 in one (causal, or frames of 1560, us with 128 / 256: 12 heads, 4680 rows on
+    // 36,240 keys 1036 / 918, 12,680 385 / 363, 8680 242 / 254, 3840 rows on 35,840 888 / 801, 640 on 32,640 161 / 153, 300 on 32,300 100 / 106, 130 on 3130 30 / 27,
+    // 256 on 1256 29 / 31; 8 sequences of 512 rows of 32 heads on 8, 4512 keys 289 / 271, 512 44 / 46).  d = 64, where a tile has half as much to turn: never (4680 rows
+    // on 8680 keys 170 / 186).
+    auto finish = [&](int64_t at_once) {
+        if (share) cut.workers = (int32_t)(at_once < c->kv_heads ? c->kv_heads : at_once / c->kv_heads * c->kv_heads);
+        if (share || blocks_even(uniform, cut.items)) {
+            cut.items = uniform;
+            cut.per_seq = (int32_t)each;
+        }
+        const size_t bytes = attn_workspace(c, cut);
+        cut.bytes = bytes > cut.bytes ? bytes : cut.bytes;      // of either way: a window that leaves blocks of 128 must not ask for more than none did
+    };
+    finish(fit);
+    const int64_t tall = (rows + 2 * kAttnRows - 1) / (2 * kAttnRows);
+    if (packed && bf16 && d == 128 && rows > kAttnRows && 8 * tall <= 5 * each &&
+        (share ? b->seqs * tall * c->kv_heads * (keys / 64) >= fit : keys >= (groups >= 1024 ? 4096 : 10240) && 5 * groups >= 4 * attn_rows_places())) {
+        cut.size = cut.part_rows = 2 * kAttnRows;
+        cut.per_seq = 0;
+        each = tall;
+        uniform = b->seqs * each;
+        cut.items = block_items(b->seqs, b->rows, max_new, group, cut.size);
+        finish(fit / 2);
     }
     return cut;
-}
-static size_t attn_workspace(const veda_cache* c, const AttnCut& cut) {
-    if (!cut.workers) return 0;
-    // unfinished sums with references and l: two blocks of few rows a workgroup, or the pieces of the others and how they were cut
-    const size_t block = (size_t)cut.part_rows * (size_t)(c->head_dim + 2) * sizeof(float), groups = (size_t)cut.items * (size_t)c->kv_heads;
-    return cut.size < kAttnRows ? (size_t)2 * cut.workers * block : ((size_t)2 * cut.workers + groups) * block + groups * 16;
 }
 static veda_status check_heads(const veda_cache* c, int32_t q_heads) {
     if (q_heads < 1 || q_heads % c->kv_heads) return VEDA_ERR_INVALID_ARG;
@@ -86,7 +108,7 @@ static veda_status check_heads(const veda_cache* c, int32_t q_heads) {
 // Workspace of a call on a cache of these rows (c), checked already.
 static size_t attn_bytes(const veda_cache* c, bool packed, const veda_cache_batch* b, int32_t q_heads) {
     if (check_batch(c, b) != VEDA_OK || check_heads(c, q_heads) != VEDA_OK) return 0;
-    return attn_workspace(c, attn_cut(c, packed, b, q_heads, veda_visible{0, 0, 0}));
+    return attn_cut(c, packed, b, q_heads, veda_visible{0, 0, 0}).bytes;
 }
 // The call on a cache of these rows, checked already; pools: what its kernels see.
 static veda_status attend(const veda_cache* c, const CacheArgs& pools, bool packed, const veda_cache_batch* b, int32_t q_heads, const void* q, veda_strides sq,
@@ -103,10 +125,9 @@ static veda_status attend(const veda_cache* c, const CacheArgs& pools, bool pack
     if (st != VEDA_OK) return st;
     if (q == out) return VEDA_ERR_INVALID_ARG;   // a row may be read after its result has been written
     const AttnCut cut = attn_cut(c, packed, b, q_heads, vis);
-    const size_t need = attn_workspace(c, cut);
-    if (need > 0) {
+    if (cut.bytes > 0) {
         if (!workspace) return VEDA_ERR_INVALID_ARG;
-        if (workspace_bytes < need) return VEDA_ERR_WORKSPACE;
+        if (workspace_bytes < cut.bytes) return VEDA_ERR_WORKSPACE;
         if (!aligned16(workspace)) return VEDA_ERR_UNSUPPORTED;
     }
     const int es = c->dtype == VEDA_BF16 ? 2 : 4;

@@ -387,23 +387,27 @@ template <int D> struct AttnStep {
     }
 };
 
-template <bool kBf16, int D> struct AttnShape {
+// kWaves: of a workgroup, 32 rows each; eight for the long walks of a packed cache, whose tiles are then turned into values for twice the rows.
+template <bool kBf16, int D, int kWaves> struct AttnShape {
     typedef AttnTile<kBf16, D> T;
+    static constexpr int kRows = 32 * kWaves;
     static constexpr int kKeyTile = kBf16 ? 64 : 32;          // keys of a tile: one segment of loads a wave
     static constexpr int kSlot = 2 * kKeyTile * T::kRowB;     // K tile, V tile
     static constexpr int kOutRowB = T::kRowB + 16;            // a row of the results in LDS
-    static constexpr int kOutB = kAttnRows * (kOutRowB + 4 + 8);   // and its lse, and where it goes
+    static constexpr int kOutB = kRows * (kOutRowB + 4 + 8);   // and its lse, and where it goes
     static constexpr int kLds = 2 * kSlot > kOutB ? 2 * kSlot : kOutB;
 };
 
 // Tiles t_beg .. t_end - 1 of those that rows r0 .. r_end - 1 of a sequence see, for one key head.  part: where the unfinished sums go,
 // or -1 if these are all the tiles.
-template <bool kBf16, int D, bool kPacked>
+template <bool kBf16, int D, bool kPacked, int kWaves>
 __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, int seq, const SeqRows& sr, int r0, int r_end, int head,
                                            const AttnTiles& tiles, int t_beg, int t_end, int64_t part) {
-    typedef AttnShape<kBf16, D> Sh;
+    typedef AttnShape<kBf16, D, kWaves> Sh;
     typedef AttnTile<kBf16, D> T;
     constexpr int kRowB = T::kRowB, kKeyTile = Sh::kKeyTile, NB = D / 32;
+    constexpr int kSeg = kPacked ? kKeyTile / kWaves : T::kSegRows;      // rows of a tile that a wave loads, of K and of V
+    static_assert(kSeg * kWaves == kKeyTile, "all of a tile");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l31 = lane & 31, hh = lane >> 5;
     const int n = min(sr.n, a.c.max_new), rows = n * a.group;
@@ -456,11 +460,11 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             const int id = mine < t_end && at < sr.len ? table[at >> a.c.log_page] : -1;
             const bool ok = id >= 0 && id < a.c.pages;
             there |= (ok ? 1u : 0u) << g;
-            if (g == wave * T::kSegRows / 16) page = ok ? id : 0;
+            if (g == wave * kSeg / 16) page = ok ? id : 0;
         }
     };
     // A packed cache: the wave's segment of tile raw_t comes into registers, one tile ahead of the one that goes into LDS.
-    typedef PackedTile<D, T::kSegRows> Raw;
+    typedef PackedTile<D, kSeg> Raw;
     Raw raw;
     int raw_t = 0, raw_at = 64, raw_key = 0;
     uint32_t raw_exists = 0, next_exists = 0;
@@ -473,21 +477,21 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
         raw_exists = (uint32_t)__builtin_amdgcn_readlane((int)there, raw_at);
         raw_key = tiles.at(raw_t);
         const int64_t from = __builtin_amdgcn_readlane(page, raw_at) * a.c.page_b + head_b;
-        raw.load(a.c.k + from, a.c.v + from, (raw_key + wave * T::kSegRows) & page_mask, a.c.log_page, lane);
+        raw.load(a.c.k + from, a.c.v + from, (raw_key + wave * kSeg) & page_mask, a.c.log_page, lane);
         ++raw_at;
         ++raw_t;
     };
     auto open_raw = [&]() __attribute__((always_inline)) {      // before it goes into LDS
-        const int row = wave * T::kSegRows;
+        const int row = wave * kSeg;
         if (raw_exists != (1u << kGroups) - 1u || raw_key + kKeyTile > sr.len)
             raw.only(((raw_exists >> (row / 16)) & 1u) && raw_key + row + Raw::row(lane) < sr.len);
         next_exists = raw_exists;
     };
-    const int raw_kx = T::k_swizzle(Raw::row(lane)), raw_vx = T::v_swizzle(Raw::row(lane));
-    auto place = [&](int slot) __attribute__((always_inline)) { return smem + slot * Sh::kSlot + wave * T::kSegRows * kRowB; };
+    const int raw_kx = T::k_swizzle(wave * kSeg + Raw::row(lane)), raw_vx = T::v_swizzle(wave * kSeg + Raw::row(lane));
+    auto place = [&](int slot) __attribute__((always_inline)) { return smem + slot * Sh::kSlot + wave * kSeg * kRowB; };
     // asks for the wave's segment of tile t, number `at` of the pages looked up
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
-        const int row = wave * T::kSegRows, id = __builtin_amdgcn_readlane(page, at);
+        const int row = wave * kSeg, id = __builtin_amdgcn_readlane(page, at);
         const int64_t from = id * a.c.page_b + head_b + ((tiles.at(t) + row) & page_mask) * kRowB;
         const uint32_t to = lds + slot * Sh::kSlot + row * kRowB;
         uint32_t k_off[T::kSegLoads], v_off[T::kSegLoads];
@@ -514,7 +518,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     // Twice at most.  Values that are not finite at keys that exist are taken to be seen by all rows, or by none; where one turns up in
     // the sums, the workgroup does all of it again and looks at every tile that some row does not see whole.  (To look at once
     // costs as much as half of such a tile's products.)  Behind the sequence's end and in holes anything may lie: there it looks.
-    float* ml = reinterpret_cast<float*>(smem + kAttnRows * Sh::kOutRowB);   // [128], and a flag of each wave before
+    float* ml = reinterpret_cast<float*>(smem + Sh::kRows * Sh::kOutRowB);   // [rows], and a flag of each wave before
     float l = 0.0f;
     for (bool careful = false;;) {
 #pragma unroll
@@ -583,7 +587,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
                     open_raw();
                     raw.template store<0>(k_to, v_to, raw_kx, raw_vx, lane);
                     step.template piece<1>(st);
-                    raw.template store<1>(k_to, v_to, raw_kx, raw_vx, lane);
+                    if constexpr (W >= 2) raw.template store<1>(k_to, v_to, raw_kx, raw_vx, lane);
                     step.template piece<2>(st);
                     if constexpr (W == 4) raw.template store<2>(k_to, v_to, raw_kx, raw_vx, lane);
                     step.template piece<3>(st);
@@ -643,7 +647,10 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     if (lane == 0) ml[wave] = 0.0f;
     if (odd != 0.0f) ml[wave] = 1.0f;   // NaN
     __syncthreads();
-    if (ml[0] + ml[1] + ml[2] + ml[3] == 0.0f) break;
+    float bad = ml[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) bad += ml[w];
+    if (bad == 0.0f) break;
     careful = true;
     __syncthreads();
     }
@@ -679,7 +686,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
                 *reinterpret_cast<f32x4v*>(orow + ch * 4) = f32x4v{st.o[nb][4 * j] * inv, st.o[nb][4 * j + 1] * inv, st.o[nb][4 * j + 2] * inv, st.o[nb][4 * j + 3] * inv};
             }
         }
-    char** to = reinterpret_cast<char**>(ml + kAttnRows);
+    char** to = reinterpret_cast<char**>(ml + Sh::kRows);
     if (hh == 0) ml[wave * 32 + l31] = attn_lse(st.ref, l);
     if (tid < r_end - r0) {
         const int at_row = r0 + tid;
@@ -690,8 +697,8 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     int me = tid;
     asm volatile("" : "+v"(me));   // or the sharing kernel keeps what follows from it in registers, from piece to piece
 #pragma unroll
-    for (int j = 0; j < kAttnRows * T::kChunks / 256; ++j) {
-        const int rr = (j * 256 + me) / T::kChunks, c = me % T::kChunks;
+    for (int j = 0; j < Sh::kRows * T::kChunks / (64 * kWaves); ++j) {
+        const int rr = (j * 64 * kWaves + me) / T::kChunks, c = me % T::kChunks;
         if (rr < r_end - r0) store_through(to[rr] + 16 * c, *reinterpret_cast<const uint4*>(smem + rr * Sh::kOutRowB + 16 * c));
     }
     if (a.lse && tid < r_end - r0) {
@@ -702,28 +709,29 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
 
 // fp32 rows over a packed cache have a piece of their own (packed_attn_rows.h).
 template <bool kBf16, bool kPacked> constexpr bool rows_split() { return kPacked && !kBf16; }
-template <bool kBf16, bool kPacked> constexpr int rows_threads() { return rows_split<kBf16, kPacked>() ? kSplitThreads : 256; }
+template <bool kBf16, bool kPacked, int kWaves> constexpr int rows_threads() { return rows_split<kBf16, kPacked>() ? kSplitThreads : 64 * kWaves; }
 template <bool kBf16, bool kPacked> constexpr int rows_waves() { return rows_split<kBf16, kPacked>() ? kSplitWaves : 2; }
-template <bool kBf16, int D, bool kPacked> constexpr int rows_tile() { return rows_split<kBf16, kPacked>() ? kSplitKeys : AttnShape<kBf16, D>::kKeyTile; }
-template <bool kBf16, int D, bool kPacked>
+template <bool kBf16, int D, bool kPacked> constexpr int rows_tile() { return rows_split<kBf16, kPacked>() ? kSplitKeys : AttnShape<kBf16, D, 4>::kKeyTile; }
+template <bool kBf16, int D, bool kPacked, int kWaves>
 __device__ __forceinline__ void rows_piece_of(const CacheAttnArgs& a, char* smem, int seq, const SeqRows& sr, int r0, int r_end, int head,
                                               const AttnTiles& tiles, int t_beg, int t_end, int64_t part) {
     if constexpr (rows_split<kBf16, kPacked>()) split_piece<D>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, t_end, part);
-    else rows_piece<kBf16, D, kPacked>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, t_end, part);
+    else rows_piece<kBf16, D, kPacked, kWaves>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, t_end, part);
 }
 
 // A workgroup for each (block of rows, key head).  Heads next to each other: workgroups are dealt to the 8 dies in turn, so those of
 // a head meet in few L2 caches.
-template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_threads<kBf16, kPacked>()), (rows_waves<kBf16, kPacked>())) void cache_attn_rows_kernel(CacheAttnArgs a) {
+template <bool kBf16, int D, bool kPacked, int kWaves> __global__ __launch_bounds__((rows_threads<kBf16, kPacked, kWaves>()), (rows_waves<kBf16, kPacked>())) void cache_attn_rows_kernel(CacheAttnArgs a) {
+    constexpr int kRows = 32 * kWaves;
     extern __shared__ __align__(1024) char smem[];
     RowBlock rb;
-    if (!block_of(a.c, a.group, kAttnRows, a.per_seq, blockIdx.x / a.c.kv_heads, rb)) return;
+    if (!block_of(a.c, a.group, kRows, a.per_seq, blockIdx.x / a.c.kv_heads, rb)) return;
     const SeqRows sr = rb.rows;
     const int rows = min(sr.n, a.c.max_new) * a.group;
-    const int r0 = (rb.blocks - 1 - rb.block) * kAttnRows;   // the last rows of a causal sequence see the most
-    const int r_end = min(rows, r0 + kAttnRows);
+    const int r0 = (rb.blocks - 1 - rb.block) * kRows;   // the last rows of a causal sequence see the most
+    const int r_end = min(rows, r0 + kRows);
     const AttnTiles tiles = tiles_seen(a, sr, min(sr.n, a.c.max_new), r0, r_end - 1, rows_tile<kBf16, D, kPacked>());
-    rows_piece_of<kBf16, D, kPacked>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
+    rows_piece_of<kBf16, D, kPacked, kWaves>(a, smem, rb.seq, sr, r0, r_end, blockIdx.x % a.c.kv_heads, tiles, 0, tiles.count, -1);
 }
 
 // Where there are few blocks, a workgroup for each leaves compute units idle, so their tiles are dealt out to as many workgroups as fit the
@@ -734,11 +742,11 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_th
 // for kPiece tiles more: what its set-up and its sums' way to the workspace take (fp32, 1057 rows x 12 heads in 28 blocks on 2000 keys, with 0 / 2 / 5:
 // 142 / 117 / 116 us, 449 rows 64 / 64 / 71; bf16, 2560 rows x 12 heads on 34,000 keys with 0 / 1 / 3: 531 / 491 / 492, 3840 rows 729 / 734 /
 // 752).  Every workgroup counts the blocks' tiles itself.
-template <int kTile> __device__ __forceinline__ int rows_tiles_of(const CacheAttnArgs& a, int item) {
+template <int kTile, int kRows> __device__ __forceinline__ int rows_tiles_of(const CacheAttnArgs& a, int item) {
     if (item >= a.items) return 0;
     const SeqRows sr = seq_rows(a.c, item / a.per_seq);
-    const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = item % a.per_seq * kAttnRows;
-    return r0 >= rows ? 0 : max(1, tiles_seen(a, sr, n, r0, min(rows, r0 + kAttnRows) - 1, kTile).count);
+    const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = item % a.per_seq * kRows;
+    return r0 >= rows ? 0 : max(1, tiles_seen(a, sr, n, r0, min(rows, r0 + kRows) - 1, kTile).count);
 }
 constexpr int kRowsShareTiles = 4;   // least level
 // Number of a piece of unfinished sums: whole multiples by workgroup, the others (block and workgroup both only grow from one to the next)
@@ -750,8 +758,8 @@ template <int D> __device__ __forceinline__ int4* rows_cuts(const CacheAttnArgs&
     return reinterpret_cast<int4*>(a.part + rows_pieces(a) * a.part_rows * (D + 2));
 }
 
-template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_threads<kBf16, kPacked>()), (rows_waves<kBf16, kPacked>())) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
-    constexpr int kTile = rows_tile<kBf16, D, kPacked>(), kPiece = kBf16 || kPacked ? 1 : 2;
+template <bool kBf16, int D, bool kPacked, int kWaves> __global__ __launch_bounds__((rows_threads<kBf16, kPacked, kWaves>()), (rows_waves<kBf16, kPacked>())) void cache_attn_rows_share_kernel(CacheAttnArgs a) {
+    constexpr int kTile = rows_tile<kBf16, D, kPacked>(), kPiece = kBf16 || kPacked ? 1 : 2, kRows = 32 * kWaves;
     extern __shared__ __align__(1024) char smem[];
     auto rest_units = [](int tiles) { return tiles ? tiles + kPiece : 0; };
     const int lane = threadIdx.x & 63, head = blockIdx.x % a.c.kv_heads, mine = blockIdx.x / a.c.kv_heads, parts = a.workers / a.c.kv_heads;
@@ -760,7 +768,7 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_th
     int total = 0;
 #pragma unroll
     for (int k = 0; k < kRowsShareItems / 64; ++k) {
-        counts[k] = 64 * k < a.items ? rows_tiles_of<kTile>(a, 64 * k + lane) : 0;
+        counts[k] = 64 * k < a.items ? rows_tiles_of<kTile, kRows>(a, 64 * k + lane) : 0;
         total += sum(counts[k]);
     }
     int level = max(kRowsShareTiles, (total + parts - 1) / parts), fulls, units;
@@ -804,9 +812,9 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_th
     for (bool again = false; now < end && item < a.items; ++item) {
         const int seq = item / a.per_seq;
         const SeqRows sr = seq_rows(a.c, seq);
-        const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = item % a.per_seq * kAttnRows;
+        const int n = min(sr.n, a.c.max_new), rows = n * a.group, r0 = item % a.per_seq * kRows;
         if (r0 >= rows) continue;
-        const int r_end = min(rows, r0 + kAttnRows);
+        const int r_end = min(rows, r0 + kRows);
         const AttnTiles tiles = tiles_seen(a, sr, n, r0, r_end - 1, kTile);
         const int count = max(1, tiles.count), f = count / level, rest = count - f * level, next_unit = first_unit + rest_units(rest);
         // tiles of this piece
@@ -819,7 +827,7 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_th
                 rows_cuts<D>(a)[item * a.c.kv_heads + head] = int4{whole ? 0 : f, first_full, whole ? 0 : q1 - q0 + 1, q0};
             }
             if (again) __syncthreads();   // the last piece's results have left the slots
-            rows_piece_of<kBf16, D, kPacked>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
+            rows_piece_of<kBf16, D, kPacked, kWaves>(a, smem, seq, sr, r0, r_end, head, tiles, t_beg, min(t_end, tiles.count), whole ? -1 : rows_piece_id(a, parts, full ? mine : item, q, head));
             again = true;
         }
         now = full ? end : max(now, min(end, next_unit));
@@ -829,12 +837,12 @@ template <bool kBf16, int D, bool kPacked> __global__ __launch_bounds__((rows_th
 }
 
 // Puts a cut block's unfinished sums together, four rows a workgroup: its waves take every fourth piece.
-template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_rows_join_kernel(CacheAttnArgs a) {
+template <bool kBf16, int D, int kRows> __global__ __launch_bounds__(256) void cache_attn_rows_join_kernel(CacheAttnArgs a) {
     constexpr int V = D / 64;
     __shared__ float sums[4][4][D + 2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.x % a.c.kv_heads, item = blockIdx.x / a.c.kv_heads;
     const SeqRows sr = seq_rows(a.c, item / a.per_seq);
-    const int block_rows = min(min(sr.n, a.c.max_new) * a.group - item % a.per_seq * kAttnRows, kAttnRows), r0 = 4 * blockIdx.y, rows = min(4, block_rows - r0);
+    const int block_rows = min(min(sr.n, a.c.max_new) * a.group - item % a.per_seq * kRows, kRows), r0 = 4 * blockIdx.y, rows = min(4, block_rows - r0);
     if (rows <= 0) return;
     const int4 cut = rows_cuts<D>(a)[blockIdx.x];
     const int n = cut.x + cut.z, parts = a.workers / a.c.kv_heads;
@@ -894,7 +902,7 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
 #pragma unroll
         for (int c = 0; c < V; ++c) y[c] += sums[w][wave][V * lane + c];
     }
-    const int row = item % a.per_seq * kAttnRows + r0 + wave, qh = head * a.group + row % a.group;
+    const int row = item % a.per_seq * kRows + r0 + wave, qh = head * a.group + row % a.group;
     const float inv = attn_inverse(a, item / a.per_seq, sr, row, lsum);
     const int64_t token = sr.first + row / a.group;
     char* dst = a.out + token * a.so_n + (int64_t)qh * a.so_h;
@@ -907,14 +915,14 @@ template <bool kBf16, int D> __global__ __launch_bounds__(256) void cache_attn_r
     if (a.lse && lane == 0) a.lse[(int64_t)qh * a.c.rows + token] = attn_lse(top, lsum);
 }
 
-template <bool kBf16, int D, bool kPacked> static veda_status launch_rows(const CacheAttnArgs& a, hipStream_t s, const char* what) {
-    constexpr int kLds = rows_split<kBf16, kPacked>() ? split_lds<D>() : AttnShape<kBf16, D>::kLds, kThreads = rows_threads<kBf16, kPacked>();
-    auto kern = a.workers ? cache_attn_rows_share_kernel<kBf16, D, kPacked> : cache_attn_rows_kernel<kBf16, D, kPacked>;
+template <bool kBf16, int D, bool kPacked, int kWaves = 4> static veda_status launch_rows(const CacheAttnArgs& a, hipStream_t s, const char* what) {
+    constexpr int kLds = rows_split<kBf16, kPacked>() ? split_lds<D>() : AttnShape<kBf16, D, kWaves>::kLds, kThreads = rows_threads<kBf16, kPacked, kWaves>();
+    auto kern = a.workers ? cache_attn_rows_share_kernel<kBf16, D, kPacked, kWaves> : cache_attn_rows_kernel<kBf16, D, kPacked, kWaves>;
     if (kLds > 64 * 1024) VEDA_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.workers ? a.workers : a.items * a.c.kv_heads)), dim3(kThreads), kLds, s, a);
     const veda_status st = launch_status(what);
     if (st != VEDA_OK || !a.workers) return st;
-    hipLaunchKernelGGL((cache_attn_rows_join_kernel<kBf16, D>), dim3((unsigned)(a.items * a.c.kv_heads), (unsigned)((a.part_rows + 3) / 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((cache_attn_rows_join_kernel<kBf16, D, 32 * kWaves>), dim3((unsigned)(a.items * a.c.kv_heads), (unsigned)((a.part_rows + 3) / 4)), dim3(256), 0, s, a);
     return launch_status(what);
 }
 
@@ -925,6 +933,8 @@ int attn_rows_places() { return 512; }
 int attn_rows_workers(bool bf16) { return bf16 ? 512 : 256; }
 
 template <bool kPacked> static veda_status launch_rows_any(const CacheAttnArgs& a, bool bf16, int d, hipStream_t s, const char* what) {
+    if constexpr (kPacked)
+        if (bf16 && d == 128 && a.part_rows > kAttnRows) return launch_rows<true, 128, true, 8>(a, s, what);
     if (bf16) return d == 128 ? launch_rows<true, 128, kPacked>(a, s, what) : launch_rows<true, 64, kPacked>(a, s, what);
     return d == 128 ? launch_rows<false, 128, kPacked>(a, s, what) : launch_rows<false, 64, kPacked>(a, s, what);
 }

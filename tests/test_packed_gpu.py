@@ -463,6 +463,69 @@ def test_logits_that_are_all_minus_infinity(dtype, d, n, past):
     assert bool((out[n + 1:n + 3] == 0).all()) and bool((lse[:, n + 1:n + 3] == -math.inf).all())
 
 
+def tall(shared, seed=0):
+    """bf16 rows that are cut into blocks of 256: shared out by walks that span workgroups, or many sequences under a wide table."""
+    if shared:
+        return Packed([64, 3], [6000, 50], 16, 4, 128, BF16, page=64, seed=seed)
+    past = [(37 * i) % 211 for i in range(30)]
+    past[2] = 900
+    return Packed([64 if i % 13 == 2 else i % 3 for i in range(30)], past, 32, 8, 128, BF16, page=64, seed=seed, extra_width=160)
+
+
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("block,window,sinks", [(1, 0, 0), (0, 0, 0), (16, 0, 0), (1, 100, 70), (30, 64, 1)])
+def test_blocks_of_256_rows(shared, block, window, sinks):
+    check(tall(shared, 70), block=block, window=window, sinks=sinks)
+
+
+def test_blocks_of_256_rows_in_several_rounds():
+    # 70 sequences that may have 2048 rows of a key head each, under a table of 5120 keys
+    new, past = [1] * 70, [(53 * i) % 97 for i in range(70)]
+    new[5], new[31], new[69] = 64, 9, 33
+    check(Packed(new, past, 32, 1, 128, BF16, page=64, seed=71, extra_width=80))
+
+
+@pytest.mark.parametrize("key_heads", [1, 3, 5, 7, 12])
+def test_a_window_asks_for_no_more_workspace(key_heads):
+    # the binding gives what a call without a window asks for
+    t = Packed([256, 1], [20000 // key_heads, 3], key_heads, key_heads, 128, BF16, page=256, seed=72)
+    need = veda.veda_packed_attn_workspace_bytes(t.cache, t.batch, t.hq, t.rows)
+    for window in (0, 300, 1000, 2500, 5000, 2 ** 30):
+        out, _ = veda.veda_packed_attn_fwd(t.cache, t.batch, t.q, 0.1, 1, window, 0, workspace=torch.empty(need, dtype=torch.uint8, device=dev()))
+        assert bool(torch.isfinite(out[:257]).all())
+
+
+@pytest.mark.parametrize("shared", [True, False])
+def test_bad_values_in_blocks_of_256_rows(shared):
+    t = tall(shared, 73)
+    s = 0 if shared else 2
+    r0, n, past = int(t.start[s]), t.new[s], t.past[s]
+    clean, clean_lse = check(t)
+    want, want_lse, ob, lb = attention(t, t.q, 1.0 / math.sqrt(128), 1, 0, 0)
+    for key in (3, past - 2, past, past + 40, past + n - 1):
+        page, at, first = t.table[s, key // 64], key % 64, r0 + max(0, key - past)
+        others = torch.ones(t.rows, dtype=torch.bool)
+        others[first:r0 + n] = False
+        vs = t.cache.scales(t.cache.v)[page, :, at]
+        good = vs.clone()
+        vs[:, 2] = 255
+        out, lse = veda.veda_packed_attn_fwd(t.cache, t.batch, t.q, 1.0 / math.sqrt(128), out=clean.clone(), lse=clean_lse.clone())
+        keep = [c for c in range(128) if not 64 <= c < 96]
+        assert torch.equal(out[others], clean[others]) and torch.equal(out[:, :, keep], clean[:, :, keep]) and torch.equal(lse, clean_lse)
+        assert bool(torch.isnan(out[first:r0 + n, :, 64:96]).all())
+        vs.copy_(good)
+        ks = t.cache.scales(t.cache.k)[page, :, at]
+        good = ks.clone()
+        ks[:, 1] = 254
+        out, lse = veda.veda_packed_attn_fwd(t.cache, t.batch, t.q, 1.0 / math.sqrt(128), out=clean.clone(), lse=clean_lse.clone())
+        away = torch.ones(t.rows, dtype=torch.bool)
+        away[r0:r0 + n] = False
+        assert torch.equal(out[away], clean[away]) and bool(torch.isnan(out[first:r0 + n]).all()) and bool(torch.isnan(lse[:, first:r0 + n]).all())
+        if first > r0:
+            close(out[r0:first], want[r0:first], ob[r0:first], BF16)
+        ks.copy_(good)
+
+
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 def test_large_logits(dtype, d):
     t = Packed([5, 140], [400, 100], 4, 2, d, dtype, page=64, seed=11, gain=40.0)
