@@ -58,10 +58,10 @@ static AttnCut attn_cut(const veda_cache* c, bool packed, const veda_cache_batch
     // 456 keys 16 / 19, 756 21 / 20, 3756 72 / 23, 1024 rows of 12 heads, causal, on 1524 keys 38 / 40, 2524 56 / 44, 2133 rows of 12 on
     // 3633 keys 72 / 84, 1280 rows on 34,000 530 / 278-304 from box to box, 3840 872 / 734, 4680 985 / 1021; fp32, 100 rows of 12 on 160 keys 28 / 30, 200 38 / 30, 300 51 /
     // 30, 449 rows on 2000 302 / 63).
-    // fp32 rows of a packed cache: twice the workgroups where they have five tiles each at least, or writing and joining their sums costs more than it
-    // brings (12 heads on 4 key heads, d = 128, us with 512 / 256: up to 333 rows of two sequences on up to 1700 keys 52 / 46, 449 rows on 2449 71 / 77; 2464
-    // rows of 12 heads, causal, on 4464 keys 187 / 256).
-    const bool many = bf16 || (packed && uniform * c->kv_heads * (keys / 64) >= 5 * attn_rows_workers(true));
+    // fp32 rows of a packed cache: at d = 64 two workgroups fit a compute unit, which pays where they have five tiles each at least (12 heads on 4 key
+    // heads, us with 512 / 256: 449 rows of two sequences on 8449 keys 91 / 102, on 2449 43 / 43, 333 rows on 2033 34 / 33; 2464 rows of 12 heads, causal,
+    // on 4464 106 / 129).
+    const bool many = bf16 || (packed && d == 64 && uniform * c->kv_heads * (keys / 64) >= 5 * attn_rows_workers(true));
     const int64_t fit = !few ? attn_rows_workers(many) : packed ? packed_keys_workers(bf16, d, cut.size) : attn_keys_workers(bf16, d), groups = uniform * c->kv_heads;
     // Few rows: long walks wait for memory, so eight waves a workgroup go through short caches about as fast as all that the card can hold, and
     // the joining is saved; in fp32, where products take longer, the more so the more workgroups there are (single tokens of 4 query heads a key

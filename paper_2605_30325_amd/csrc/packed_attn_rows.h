@@ -49,9 +49,12 @@ template <int D, int kRows> struct PackedTile {
 // fp32 rows.  The cache's values are exact in bf16; Q and the weights come as three bf16 parts each, which hold all 24 bits of an fp32 number, so all
 // products are exact and sums are in fp32: three v_mfma_f32_16x16x32_bf16 (48 cycles) stand for eight v_mfma_f32_16x16x4_f32 (256).  A workgroup
 // takes 128 rows, 16 to each of its eight waves: with 32 rows three parts of Q, 96 registers, and the sums, 64, leave no room for the rest
-// (2464 rows x 12 heads, d = 128, causal behind 2000 keys: 420 us, and 530 on the fp32 matrix cores).  Reading a tile from LDS for 16 rows
-// instead of 32 costs twice the reads, which three products for each have the time for.
-constexpr int kSplitThreads = 512, kSplitWaves = 4, kSplitKeys = 64;      // four waves to a SIMD
+// (2464 rows x 12 heads, d = 128, causal behind 2000 keys: 178 us; 420 with 32 rows, and 530 on the fp32 matrix cores).  Reading a tile from LDS
+// for 16 rows instead of 32 costs twice the reads, which three products for each have the time for.  What bounds it: the matrix cores and the
+// vector instructions of the weights alike, 1.3 us each for a tile of a workgroup, which a wave's chain of products, weights and products
+// keeps from overlapping (up to 333 rows of two sequences, 12 heads on 4, up to 2033 keys: 36 us, of which 28 are this walk and 8 the joining).
+constexpr int kSplitThreads = 512, kSplitKeys = 64;
+constexpr int kSplitWaves = 2;      // to a SIMD, at least: both halves of a tile in flight take 160 registers at d = 128, 120 at 64 (with four, spilled: 45 us, not 36)
 template <int D> struct SplitShape {
     static constexpr int kRowB = D * 2, kTile = kSplitKeys * kRowB, kSlot = 2 * kTile + kSplitKeys * 4;      // K, V, and which blocks of V stand for NaN
     __device__ static int k_swizzle(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
@@ -171,7 +174,7 @@ __device__ __forceinline__ void split_piece(const CacheAttnArgs& a, char* smem, 
             load();
         }
         const uint32_t base = lds + slot * Sh::kSlot;
-#pragma unroll 1
+#pragma unroll 2
         for (int h = 0; h < kSplitKeys / 32; ++h) {
             const int key = key0 + 32 * h;
             const uint32_t ex = (exists >> (2 * h)) & 3u;
@@ -179,14 +182,16 @@ __device__ __forceinline__ void split_piece(const CacheAttnArgs& a, char* smem, 
             const bool full = key + 32 <= all_hi && (key >= all_lo || key + 32 <= a.sinks) && ex == 3u;
             f32x4v s[2];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                s[b] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int b = 0; b < 2; ++b) s[b] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const bf16x8 x = *(lds_bf16x8_p)(uintptr_t)(((base + k_at) ^ (uint32_t)(i << 6)) + (32 * h + 16 * b) * kRowB);
+            for (int i = 0; i < D / 32; ++i) {
+                bf16x8 x[2];
 #pragma unroll
-                    for (int u = 2; u >= 0; --u) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[u][i], s[b], 0, 0, 0);
-                }
+                for (int b = 0; b < 2; ++b) x[b] = *(lds_bf16x8_p)(uintptr_t)(((base + k_at) ^ (uint32_t)(i << 6)) + (32 * h + 16 * b) * kRowB);
+#pragma unroll
+                for (int u = 2; u >= 0; --u)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[b], q[u][i], s[b], 0, 0, 0);
             }
             auto sees = [&](int k) __attribute__((always_inline)) { return k < see.hi && (k >= see.lo || k < a.sinks); };
             if (!full) {
@@ -226,7 +231,6 @@ __device__ __forceinline__ void split_piece(const CacheAttnArgs& a, char* smem, 
                 const bf16x8 x[2] = {keys_v<D>(v, c), keys_v<D>(v, c + 1)};
 #pragma unroll
                 for (int j = 0; j < 6; ++j) o[c + j % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[j % 2], p[2 - j / 2], o[c + j % 2], 0, 0, 0);
-                if (c % 4 == 2) __builtin_amdgcn_sched_barrier(0);
             }
             const uint32_t mark = *reinterpret_cast<const uint32_t*>(smem + slot * Sh::kSlot + 2 * Sh::kTile + (32 * h + (lane & 31)) * 4);
 #pragma unroll 1
