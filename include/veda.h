@@ -498,16 +498,16 @@ typedef struct {
 } veda_packed_cache;
 /* veda_cache_append with rounding.  K is turned in 64 bits and rounded once, to 4 bits: no code depends on an order of operations.
  * k_out, v_out  optional (each may be NULL), [rows][kv_heads][head_dim] of the cache's dtype: the new rows as the cache now stands for
- *            them (bf16 holds such values exactly); not to overlap k and v (refused where they begin there).  Rows that write nothing into
- *            the cache are left as they were. */
+ *            them (bf16 holds such values exactly); not to overlap any other of the call's rows (refused where they begin there).  Rows that
+ *            write nothing into the cache are left as they were. */
 veda_status veda_packed_append(const veda_packed_cache*, const veda_cache_batch*, const void* k, veda_strides sk, const void* v,
                                veda_strides sv, int32_t q_heads, const void* q, veda_strides sq, void* q_out, veda_strides sq_out,
                                const veda_rope* rope, const int32_t* positions, void* k_out, veda_strides sk_out, void* v_out,
                                veda_strides sv_out, void* stream);
 /* veda_cache_attn_fwd over what the cache stands for: the same masks, results and errors.  A page's bytes may be anything where no row
  * sees them.  A block of K that stands for NaN makes the rows that see its key NaN, one of V its 32 channels of those rows, and neither touches
- * others.  f32: Q and the weights enter the products in three bf16 parts that hold all their bits (the cache's values are exact in bf16), sums are
- * in fp32; f32 rows in blocks of more than 32 take fp32 products. */
+ * others.  The cache's values are exact in bf16.  f32: Q and the weights enter the products in three bf16 parts that hold all their bits, sums are
+ * in fp32.  bf16: weights enter as bf16, of few rows (32 of a key head at most) in two parts. */
 size_t veda_packed_attn_workspace_bytes(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads);
 veda_status veda_packed_attn_fwd(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads, const void* q, veda_strides sq,
                                  float softmax_scale, veda_visible visible, void* out, veda_strides so, float* lse,
@@ -581,8 +581,8 @@ enum {
     VEDA_STEP_NO_ROOM = 2         /* cut and evicted, but not grown                                                 */
 };
 /* First all requests give back (whether they are served or not), then they grow in their order, from the lowest free pages on; the first for
- * which pages or rows do not suffice and all behind it that would grow have no room.  The call is two kernels, or one where little is written,
- * and equal inputs give equal bytes; calls on the same book must not overlap. */
+ * which pages or rows do not suffice and all behind it that would grow have no room.  The call is three kernels, or one where little is written,
+ * and equal inputs give equal bytes; calls on the same book must not overlap.  Inputs must not lie where results or the book do (refused where they begin there). */
 veda_status veda_pages_step(const veda_device_pages*, const veda_step*, const veda_step_tables*, void* stream);
 
 const char* veda_status_string(veda_status);

@@ -219,8 +219,9 @@ extern "C" veda_status veda_packed_append(const veda_packed_cache* c, const veda
     if (st == VEDA_OK && v_out) st = veda::check_rows(&as, b->rows, c->kv_heads, v_out, sv_out, true);
     if (st != VEDA_OK) return st;
     if (q_heads && q == q_out && (sq.n != sq_out.n || sq.h != sq_out.h)) return VEDA_ERR_INVALID_ARG;
-    if (k_out && (k_out == k || k_out == v || k_out == v_out)) return VEDA_ERR_INVALID_ARG;   // a row is read by several lanes
-    if (v_out && (v_out == k || v_out == v)) return VEDA_ERR_INVALID_ARG;
+    for (const void* to : {k_out, v_out})      // rows are read by several lanes, and other workgroups
+        if (to && (to == k || to == v || to == q || to == q_out)) return VEDA_ERR_INVALID_ARG;
+    if (k_out && k_out == v_out) return VEDA_ERR_INVALID_ARG;
     if (rope) {
         int device = -1;
         VEDA_HIP_TRY(hipGetDevice(&device));

@@ -73,7 +73,8 @@ def test_null_cache_or_batch_is_refused(lib):
     (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(q=None), INVALID), (dict(q_out=None), INVALID), (dict(q_heads=0), INVALID),
     (dict(q_heads=-1), INVALID), (dict(q_heads=40000), UNSUPPORTED), (dict(sk=veda.veda_strides(0, -8, 256)), INVALID),
     (dict(so=veda.veda_strides(0, 128, 64)), INVALID), (dict(sv=veda.veda_strides(0, 128, 260)), UNSUPPORTED), (dict(k=AT + 2), UNSUPPORTED),
-    (dict(k_out=AT), INVALID), (dict(v_out=AT), INVALID), (dict(k_out=3 * AT), INVALID), (dict(k_out=2 * AT + 8), UNSUPPORTED),
+    (dict(k_out=AT), INVALID), (dict(v_out=AT), INVALID), (dict(k_out=3 * AT), INVALID), (dict(v_out=9 * AT, q_out=9 * AT), INVALID),
+    (dict(k_out=9 * AT, q=9 * AT), INVALID), (dict(k_out=2 * AT + 8), UNSUPPORTED),
     (dict(sko=veda.veda_strides(0, 64, 256)), INVALID), (dict(svo=veda.veda_strides(0, 128, 128)), INVALID), (dict(svo=veda.veda_strides(0, 128, 260)), UNSUPPORTED),
 ])
 def test_append_refusals(lib, more, status):
