@@ -17,6 +17,11 @@
 // (444 on 512 places).  Prompts of 1..4096 tokens, G = 4, window 1024: 0.30-0.33 ms = 0.79-0.87 PFLOP/s; about 15 tiles of 64 keys that all rows see, three that
 // some do, and as long again as two of them for the set-up and the results.  fp32 (v_mfma_f32_32x32x2_f32): 2464 rows x 12 heads on 2000 keys, causal, 0.35 ms,
 // matrix pipes 73 % busy, 102 TFLOP/s on visible keys of the 154 that a large product reaches.
+//
+// The same walk over a cache held in 4 bits (kPacked): a tile's codes come into registers one tile ahead, and go as bf16 values into the other
+// slot of LDS between the first products of a step, which no exponentials ride on.  That is what it takes beyond the above, 32 conversions and 8 writes of LDS a
+// wave and tile where four waves share one, and half of that where eight do: 4680 rows x 12 heads on 34,320 keys 0.92-0.98 ms (1.04 with four), the prompts
+// 0.32-0.33 ms (3 % more while rows that are written together lay in the same banks).
 #include "cache_attn.h"
 #include "packed_attn_rows.h"
 #include "store.h"
@@ -30,6 +35,9 @@ template <bool kBf16, int D> struct AttnTile {
     // 16-byte chunk c of row r lies at chunk c ^ swizzle: operand reads of a wave then fall into different banks.
     __device__ static int k_swizzle(int r) { return kBf16 ? (D == 128 ? r & 15 : (r >> 1) & 7) : r & 7; }
     __device__ static int v_swizzle(int r) { return kBf16 ? (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) : ((r >> 2) & 1) << 3; }
+    // Packed: lanes that turn codes into values write a chunk of each quarter (d = 128, 16 rows a wave) or every other chunk of their rows, several rows at
+    // once.  The low bits keep those apart too, and change nothing for the reads, which take four neighbouring chunks of a row.
+    __device__ static int packed_v_swizzle(int r) { return D == 128 ? (r & 3) * 5 : ((r >> 1) & 1) * 5; }
     // What the swizzles of load j of a segment (1024 / kRowB rows each) have on top of load 0's, as address bits.
     __device__ static constexpr uint32_t k_step(int j) { return (uint32_t)j << (kBf16 || D == 64 ? 6 : 5); }
     __device__ static constexpr uint32_t v_step(int j) { return kBf16 ? 0u : (uint32_t)(D == 64 ? j : j >> 1) << 7; }
@@ -487,7 +495,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             raw.only(((raw_exists >> (row / 16)) & 1u) && raw_key + row + Raw::row(lane) < sr.len);
         next_exists = raw_exists;
     };
-    const int raw_kx = T::k_swizzle(wave * kSeg + Raw::row(lane)), raw_vx = T::v_swizzle(wave * kSeg + Raw::row(lane));
+    const int raw_kx = T::k_swizzle(wave * kSeg + Raw::row(lane)), raw_vx = T::packed_v_swizzle(wave * kSeg + Raw::row(lane));
     auto place = [&](int slot) __attribute__((always_inline)) { return smem + slot * Sh::kSlot + wave * kSeg * kRowB; };
     // asks for the wave's segment of tile t, number `at` of the pages looked up
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
@@ -510,7 +518,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     if constexpr (kBf16) {
         // transposing read: lane i of 16 names channels 4 (i % 4) ..+3 of key i / 4 and gets channel i of the four keys
         const int key = 4 * hh + ((lane >> 2) & 3), c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        v_at = (uint32_t)(key * kRowB + ((c ^ T::v_swizzle(key)) << 4) + 8 * (lane & 1));
+        v_at = (uint32_t)(key * kRowB + ((c ^ (kPacked ? T::packed_v_swizzle(key) : T::v_swizzle(key))) << 4) + 8 * (lane & 1));
     } else {
         v_at = (uint32_t)(4 * hh * kRowB + 4 * l31 + (hh << 7));
     }
