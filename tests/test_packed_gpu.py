@@ -390,7 +390,7 @@ def test_bad_values_that_are_seen(dtype, d, n, past):
             page, at = t.table[0, key // 32], key % 32
             codes, scales = t.cache.codes(t.cache.k)[page, 0, at], t.cache.scales(t.cache.k)[page, 0, at]
             kept = codes.clone(), scales.clone()
-            if far:                                      # K = (-3072, 0 ..): a weight of e^-270 and less
+            if far:                                      # K = (-3 * 2^10, 0 ..): a weight of e^-270 and less
                 codes.zero_()
                 scales.fill_(137)
                 codes[0] = 13
