@@ -1054,21 +1054,26 @@ def veda_packed_attn_fwd(cache: PackedCache, batch: CacheBatch, q: torch.Tensor,
     return _attn_fwd("veda_packed_attn", cache, batch, q, softmax_scale, block, window, sinks, out, lse, want_lse, workspace)
 
 
-def _pairs(pairs, w: str) -> np.ndarray:
+_I32 = np.dtype(np.int32)
+
+
+def _pairs(pairs, w: str) -> Tuple[bytes, int]:
+    """The numbers as bytes, whose place ctypes knows (a numpy array takes 2 us to tell its own), and how many pairs they are."""
     p = np.asarray(pairs)
     if p.size and not (p.shape[1] == 2 if p.ndim == 2 else p.ndim == 1 and p.size % 2 == 0):     # sources and targets as two rows, say
         _refuse(w, "pairs must be page numbers [n, 2]")
-    if p.dtype != np.int32:
+    if p.dtype != _I32:
         _need(p.size == 0 or (p.dtype.kind in "iu" and 0 <= p.min() and p.max() < 1 << 31), w, "pairs must be page numbers [n, 2]")
-    return np.ascontiguousarray(p, np.int32).reshape(-1, 2)
+        p = p.astype(_I32)
+    return p.tobytes(), p.size // 2
 
 
 def veda_cache_copy_pages(cache: Cache, pairs):
     """Copies pages (from, to) [n, 2] inside both pools, as if one after the other."""
     w = "veda_cache_copy_pages"
     _on(cache.device, w)
-    p = _pairs(pairs, w)
-    _check(load().veda_cache_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream_of(cache.device)), w)
+    p, n = _pairs(pairs, w)
+    _check(load().veda_cache_copy_pages(cache._ref, p, n, _stream_of(cache.device)), w)
 
 
 def veda_packed_copy_pages(cache: PackedCache, pairs):
@@ -1076,8 +1081,8 @@ def veda_packed_copy_pages(cache: PackedCache, pairs):
     w = "veda_packed_copy_pages"
     _on(cache.device, w)
     _need(isinstance(cache, PackedCache), w, "the cache is not held in 4 bits")
-    p = _pairs(pairs, w)
-    _check(load().veda_packed_copy_pages(cache._ref, p.ctypes.data, p.shape[0], _stream_of(cache.device)), w)
+    p, n = _pairs(pairs, w)
+    _check(load().veda_packed_copy_pages(cache._ref, p, n, _stream_of(cache.device)), w)
 
 
 class Pages:
