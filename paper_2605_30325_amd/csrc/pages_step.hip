@@ -16,11 +16,14 @@ struct StepArgs {
     veda_device_pages book;
     veda_step step;
     veda_step_tables out;
-    int32_t log_page;    // of the tokens of a page, or -1
+    // t / page_tokens = t * magic >> shift for t < 2^31, without a branch for powers of two: 2^(shift - 31) is the least power of two from page_tokens on,
+    // magic = ceil(2^shift / page_tokens) less than 1 too much, so the quotient less than 2^31 / 2^shift <= 1 / page_tokens, which its floor does not show.
+    uint32_t magic;
+    int32_t shift;
 };
 
 // Whole pages in 0 .. 2^31 tokens, and pages of 0 .. 2^30 tokens.
-__device__ __forceinline__ int step_whole(const StepArgs& a, uint32_t tokens) { return (int)(a.log_page >= 0 ? tokens >> a.log_page : tokens / (uint32_t)a.book.page_tokens); }
+__device__ __forceinline__ int step_whole(const StepArgs& a, uint32_t tokens) { return (int)((uint64_t)tokens * a.magic >> a.shift); }
 __device__ __forceinline__ int step_pages(const StepArgs& a, int tokens) { return step_whole(a, (uint32_t)tokens + (uint32_t)a.book.page_tokens - 1u); }
 
 // What request i asks of its sequence.
@@ -405,9 +408,9 @@ extern "C" veda_status veda_pages_step(const veda_device_pages* book, const veda
     if (book->pages > 1 << 19 || book->max_seqs > 8192 || step->seqs > 8192 || step->rows > 1 << 30) return VEDA_ERR_UNSUPPORTED;
     if ((int64_t)book->max_pages * book->page_tokens > (int64_t)1 << 30) return VEDA_ERR_UNSUPPORTED;
     const hipStream_t s = (hipStream_t)stream;
-    int log_page = 0;
-    while (log_page < 30 && 1 << log_page < book->page_tokens) ++log_page;
-    const veda::StepArgs a{*book, *step, *out, 1 << log_page == book->page_tokens ? log_page : -1};
+    int shift = 31;
+    while ((uint64_t)1 << (shift - 31) < (uint64_t)book->page_tokens) ++shift;
+    const veda::StepArgs a{*book, *step, *out, (uint32_t)((((uint64_t)1 << shift) + book->page_tokens - 1) / book->page_tokens), shift};
     const int64_t n = step->seqs, words = (book->pages + 31) / 32, grows = std::min(step->max_new, step->rows);
     veda_status st = VEDA_OK;
     // One kernel as long as one compute unit writes it all as fast as the launches of three take.
