@@ -32,12 +32,12 @@ template <bool kBf16, int D> struct KeysTile {
 };
 
 // bf16: operand of V for channels 16 c.. of 32 keys, by transposing reads: elements 0-3 are keys 4 g + e, 4-7 keys 16 + 4 g + e.
-template <int D> __device__ __forceinline__ bf16x8 keys_v(uint32_t v, int c) {
-    const uint32_t at = v ^ (uint32_t)(c << 5);
+template <int D> __device__ __forceinline__ bf16x8 keys_v_at(uint32_t at) {
     const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
     const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 16 * (D * 2)));
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
+template <int D> __device__ __forceinline__ bf16x8 keys_v(uint32_t v, int c) { return keys_v_at<D>(v ^ (uint32_t)(c << 5)); }
 // bf16: a weight goes into its product in two parts, 2^-15 of it off at most (one part: 2^-8, which is as much as the results' own rounding).  The
 // matrix cores have the time: us with one / two parts, d = 128: ragged single tokens of 64 streams 193.7 / 193.4, one of a cache of 131,101 105.6 /
 // 105.8, 64 of 501 keys 23.9 / 24.2, 512 of 101 51.0 / 51.9; 32 rows of 16 caches of 4100 keys, the dearest, 57.2 / 60.8.

@@ -21,7 +21,7 @@
 // The same walk over a cache held in 4 bits (kPacked): a tile's codes come into registers one tile ahead, and go as bf16 values into the other
 // slot of LDS between the first products of a step, which no exponentials ride on.  That is what it takes beyond the above, 32 conversions and 8 writes of LDS a
 // wave and tile where four waves share one, and half of that where eight do: 4680 rows x 12 heads on 34,320 keys 0.92-0.98 ms (1.04 with four), the prompts
-// 0.32-0.33 ms (3 % more while rows that are written together lay in the same banks).
+// 0.31-0.33 ms.
 #include "cache_attn.h"
 #include "packed_attn_rows.h"
 #include "store.h"
@@ -35,9 +35,9 @@ template <bool kBf16, int D> struct AttnTile {
     // 16-byte chunk c of row r lies at chunk c ^ swizzle: operand reads of a wave then fall into different banks.
     __device__ static int k_swizzle(int r) { return kBf16 ? (D == 128 ? r & 15 : (r >> 1) & 7) : r & 7; }
     __device__ static int v_swizzle(int r) { return kBf16 ? (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) : ((r >> 2) & 1) << 3; }
-    // Packed: lanes that turn codes into values write a chunk of each quarter (d = 128, 16 rows a wave) or every other chunk of their rows, several rows at
-    // once.  The low bits keep those apart too, and change nothing for the reads, which take four neighbouring chunks of a row.
-    __device__ static int packed_v_swizzle(int r) { return D == 128 ? (r & 3) * 5 : ((r >> 1) & 1) * 5; }
+    // Packed (see packed_chunk): rows that are written together lie apart in the low bits too, which changes nothing for reads.
+    __device__ static int packed_k_swizzle(int r) { return D == 128 ? r & 15 : ((r >> 1) & 7) ^ (r & 1); }
+    __device__ static int packed_v_swizzle(int r) { return D == 128 ? (r & 3) * 5 : ((r >> 1) & 1) * 5 ^ (r & 1); }
     // What the swizzles of load j of a segment (1024 / kRowB rows each) have on top of load 0's, as address bits.
     __device__ static constexpr uint32_t k_step(int j) { return (uint32_t)j << (kBf16 || D == 64 ? 6 : 5); }
     __device__ static constexpr uint32_t v_step(int j) { return kBf16 ? 0u : (uint32_t)(D == 64 ? j : j >> 1) << 7; }
@@ -52,14 +52,14 @@ template <bool kBf16, int D> struct AttnRow {
 };
 
 // Scores of 32 keys whose K rows lie at LDS address `k` (+ the lane's part).
-template <bool kBf16, int D> __device__ __forceinline__ f32x16 attn_scores(const AttnRow<kBf16, D>& st, uint32_t k) {
+template <bool kBf16, int D, bool kPacked> __device__ __forceinline__ f32x16 attn_scores(const AttnRow<kBf16, D>& st, uint32_t k) {
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
     if constexpr (kBf16) {
 #pragma unroll
         for (int t = 0; t < D / 16; ++t)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8_p)(uintptr_t)(k ^ (uint32_t)(t << 5)), st.qb[t], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8_p)(uintptr_t)(k ^ (uint32_t)((kPacked ? packed_chunk<D>(2 * t) : 2 * t) << 4)), st.qb[t], s, 0, 0, 0);
     } else {
         // reads one group of products ahead, and no further: there are no registers for more
         f32x4v x = *(lds_f32x4_ptr)(uintptr_t)k;
@@ -90,15 +90,15 @@ template <bool kBf16, int D> __device__ __forceinline__ void attn_move_ref(AttnR
 }
 
 // bf16: operand of V for channels 32 nb.. and key step kk (16 keys; the lane half's are 8 (e / 4) + 4 hh + e % 4), by transposing reads.
-template <int D> __device__ __forceinline__ bf16x8 attn_v(uint32_t v, int kk, int nb) {
-    const uint32_t at = (v ^ (uint32_t)(nb << 6)) + kk * 16 * (D * 2);
+template <int D, bool kPacked> __device__ __forceinline__ bf16x8 attn_v(uint32_t v, int kk, int nb) {
+    const uint32_t at = (v ^ (uint32_t)((kPacked ? packed_chunk<D>(4 * nb) : 4 * nb) << 4)) + kk * 16 * (D * 2);
     const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)at);
     const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_p)(uintptr_t)(at + 8 * (D * 2)));
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // Whether all values of 32 keys are finite: their product with zeros is zero exactly then.
-template <int D> __device__ __forceinline__ bool attn_finite(uint32_t v) {
+template <int D, bool kPacked> __device__ __forceinline__ bool attn_finite(uint32_t v) {
     bf16x8 zero;
     f32x16 z;
 #pragma unroll
@@ -109,7 +109,7 @@ template <int D> __device__ __forceinline__ bool attn_finite(uint32_t v) {
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int nb = 0; nb < D / 32; ++nb) {
-            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D>(v, kk, nb), zero, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D, kPacked>(v, kk, nb), zero, z, 0, 0, 0);
             if (nb & 1) __builtin_amdgcn_sched_barrier(0);
         }
     float t = 0.0f;
@@ -119,7 +119,7 @@ template <int D> __device__ __forceinline__ bool attn_finite(uint32_t v) {
 }
 
 // O^T += V^T P^T of 32 keys some of whose values are not finite: those reach the rows that see their keys (bit i: register i's).
-template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& st, uint32_t v, const bf16x8 (&p)[2], uint32_t seen) {
+template <int D, bool kPacked> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& st, uint32_t v, const bf16x8 (&p)[2], uint32_t seen) {
     constexpr int NB = D / 32;
     f32x16 o[NB];   // indexed as the loop goes, so it lies in memory: this path must not cost the others registers
 #pragma unroll
@@ -131,7 +131,7 @@ template <int D> __device__ __forceinline__ void attn_careful(AttnRow<true, D>& 
         for (int i = 0; i < 16; ++i) code[i] = 0.0f;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 x = attn_v<D>(v, kk, nb), y, on;
+            bf16x8 x = attn_v<D, kPacked>(v, kk, nb), y, on;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 y[e] = (__bf16)attn_code((float)x[e]);
@@ -185,11 +185,11 @@ template <bool kBf16, int D> __device__ __forceinline__ uint32_t attn_seen(const
 
 // 32 keys from key0 on for one wave.  full: every row sees all of them.  exists: bit g = keys 16g..16g+15 exist.  check: values may be not
 // finite at keys that some row does not see (a product with a p of zero would be NaN).
-template <bool kBf16, int D>
+template <bool kBf16, int D, bool kPacked>
 __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16, D>& st, uint32_t k, uint32_t v, int key0, uint32_t exists,
                                            bool full, bool check, int hh) {
     constexpr int NB = D / 32, kRowB = AttnTile<kBf16, D>::kRowB;
-    f32x16 s = attn_scores<kBf16, D>(st, k);
+    f32x16 s = attn_scores<kBf16, D, kPacked>(st, k);
     if (!full) attn_mask<kBf16, D>(st, s, key0, exists, a.sinks, hh);
     float mx = s[0];
 #pragma unroll
@@ -209,16 +209,16 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[kk][e] = (__bf16)s[8 * kk + e];
-        if (!check || attn_finite<D>(v)) {
+        if (!check || attn_finite<D, kPacked>(v)) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D>(v, kk, nb), p[kk], st.o[nb], 0, 0, 0);
+                    st.o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attn_v<D, kPacked>(v, kk, nb), p[kk], st.o[nb], 0, 0, 0);
                     if (nb & 1) __builtin_amdgcn_sched_barrier(0);   // or every operand is read at once, into registers that are not there
                 }
         } else {
-            attn_careful<D>(st, v, p, attn_seen<kBf16, D>(st, key0, exists, a.sinks, hh));
+            attn_careful<D, kPacked>(st, v, p, attn_seen<kBf16, D>(st, key0, exists, a.sinks, hh));
         }
     } else {
         // step i takes keys 8 (i / 4) + i % 4 of either lane half: register i is the operand
@@ -290,7 +290,7 @@ __device__ __forceinline__ void attn_block(const CacheAttnArgs& a, AttnRow<kBf16
 // block's products; the exponentials assume that the reference stays, and are formed again in the rare other case.  The other
 // exponentials ride on the second product, 16 keys behind it.  (The same division of a step as the tile-sparse kernel's, attn_step.h; here
 // V lies token by token, so its operand takes two transposing reads.)
-template <int D> struct AttnStep {
+template <int D, bool kPacked> struct AttnStep {
     static constexpr int G = D / 16, NB = D / 32, kAhead = 6, kRowB = D * 2, NF = 2 * G + 4 * NB;
     static constexpr int kPieces = 4, kSeg = G / kPieces;   // block 0 comes in pieces, between which the caller asks for the next tile
     bf16x8 fr[NF], p[4];
@@ -300,10 +300,10 @@ template <int D> struct AttnStep {
 
     template <int F> __device__ __forceinline__ void read() {
         if constexpr (F < 2 * G) {
-            fr[F] = *(lds_bf16x8_p)(uintptr_t)((k ^ (uint32_t)((F % G) << 5)) + (uint32_t)((F / G) * 32 * kRowB));
+            fr[F] = *(lds_bf16x8_p)(uintptr_t)((k ^ (uint32_t)((kPacked ? packed_chunk<D>(2 * (F % G)) : 2 * (F % G)) << 4)) + (uint32_t)((F / G) * 32 * kRowB));
         } else if constexpr (F < NF) {
             constexpr int kk = (F - 2 * G) / NB, nb = (F - 2 * G) % NB;
-            fr[F] = attn_v<D>(v, kk, nb);
+            fr[F] = attn_v<D, kPacked>(v, kk, nb);
         }
     }
     template <int F, int E> __device__ __forceinline__ void read_to() {
@@ -495,7 +495,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             raw.only(((raw_exists >> (row / 16)) & 1u) && raw_key + row + Raw::row(lane) < sr.len);
         next_exists = raw_exists;
     };
-    const int raw_kx = T::k_swizzle(wave * kSeg + Raw::row(lane)), raw_vx = T::packed_v_swizzle(wave * kSeg + Raw::row(lane));
+    const int raw_kx = T::packed_k_swizzle(wave * kSeg + Raw::row(lane)), raw_vx = T::packed_v_swizzle(wave * kSeg + Raw::row(lane));
     auto place = [&](int slot) __attribute__((always_inline)) { return smem + slot * Sh::kSlot + wave * kSeg * kRowB; };
     // asks for the wave's segment of tile t, number `at` of the pages looked up
     auto load_tile = [&](int t, int at, int slot) __attribute__((always_inline)) {
@@ -513,7 +513,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
     };
 
     // the lane's part of operand addresses
-    const uint32_t k_at = (uint32_t)(l31 * kRowB + ((hh ^ T::k_swizzle(l31)) << 4));
+    const uint32_t k_at = (uint32_t)(l31 * kRowB + ((hh ^ (kPacked ? T::packed_k_swizzle(l31) : T::k_swizzle(l31))) << 4));
     uint32_t v_at;
     if constexpr (kBf16) {
         // transposing read: lane i of 16 names channels 4 (i % 4) ..+3 of key i / 4 and gets channel i of the four keys
@@ -583,7 +583,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             bool left = true;
             while (started && all(key0, 64, exists)) {
                 const uint32_t base = lds + slot * Sh::kSlot;
-                AttnStep<D> step;
+                AttnStep<D, kPacked> step;
                 step.begin(base + k_at, base + v_at + kKeyTile * kRowB);
                 step.template piece<0>(st);
                 if constexpr (kPacked) {
@@ -636,7 +636,7 @@ __device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, char* smem, i
             const uint32_t ex = (exists >> (2 * c)) & 3u;
             if (some(key, 32, ex)) {
                 const bool full = all(key, 32, ex);
-                attn_block<kBf16, D>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, full,
+                attn_block<kBf16, D, kPacked>(a, st, base + k_at + c * 32 * kRowB, base + v_at + (kKeyTile + c * 32) * kRowB, key, ex, full,
                                      !full && (careful || (!kPacked && (ex != 3u || key + 32 > sr.len))), hh);
             }
         }

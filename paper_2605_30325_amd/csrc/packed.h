@@ -59,11 +59,15 @@ template <int W> __device__ __forceinline__ void packed_words(const char* p, uin
     }
 }
 
-// bf16 V in LDS, rows of D channels, for products of 16 channels: 16-byte chunk c of row r lies at chunk c ^ swizzle.  Four rows that 16 lanes write a chunk of
-// each quarter of, and eight rows that 32 lanes read two neighbouring chunks of, then fall into different banks.
+// bf16 rows of D channels in LDS: 16-byte chunk c of row r lies at chunk packed_chunk(c) ^ swizzle(r).  Eight neighbouring lanes write at once, in 32 banks: two
+// quarters each of two rows of 128 channels, or eighths of one, or quarters of two rows of 64 (which share no banks otherwise).  Chunks half a row apart, and
+// rows that are neighbours, so have to lie apart too, beside what reads want (prompts of up to 4096 tokens, window 1024: 312 us
+// without a conflict; 318 with two quarters of a row in the same banks, 326 with rows as well).
+template <int D> __host__ __device__ constexpr int packed_chunk(int c) { return D == 128 ? c ^ (c >> 3) * 3 : c; }
+// V, for products of 16 channels: eight rows that 32 lanes read two neighbouring chunks of fall into different banks.
 template <int D> __device__ __forceinline__ int packed_v_swizzle(int r) {
     const int k0 = r & 1, k1 = (r >> 1) & 1, k2 = (r >> 2) & 1;
-    return D == 128 ? k2 << 3 | k0 << 2 | k1 << 1 | k0 : k2 << 2 | k1 << 1 | k1;
+    return D == 128 ? k2 << 3 | k0 << 2 | k1 << 1 | k0 : k2 << 2 | k1 << 1 | (k1 ^ k0);
 }
 
 #endif

@@ -63,7 +63,7 @@ template <int D, int G> struct PackedLane {
         k_scale = (uint32_t)(l15 * P::kScaleB + g * (D / 4) / 32);
         v_code = (uint32_t)(lane * (D / 8));
         v_scale = (uint32_t)((lane >> 2) * P::kScaleB + (lane & 3) * (D / 4) / 32);
-        v_to = (uint32_t)((lane >> 2) * D * 2 + ((((lane & 3) * (D / 32)) ^ packed_v_swizzle<D>(lane >> 2)) << 4));
+        v_to = (uint32_t)((lane >> 2) * D * 2 + ((packed_chunk<D>((lane & 3) * (D / 32)) ^ packed_v_swizzle<D>(lane >> 2)) << 4));
         const int key = 4 * g + (l15 >> 2);
         v_at = (uint32_t)(key * D * 2 + ((((l15 & 3) >> 1) ^ packed_v_swizzle<D>(key)) << 4) + 8 * (l15 & 1));
     }
@@ -271,7 +271,8 @@ __device__ __forceinline__ void packed_values(const CacheAttnArgs& a, PackedRow<
     for (int h = 0; h < G / 2; ++h)
 #pragma unroll
         for (int c = 0; c < C; c += 2) {   // two at a time, so that a sum's next product is not the one right behind it
-            const bf16x8 x[2] = {keys_v<D>(v + h * 32 * D * 2, c), keys_v<D>(v + h * 32 * D * 2, c + 1)};
+            const uint32_t at = v + h * 32 * D * 2;
+            const bf16x8 x[2] = {keys_v_at<D>(at ^ (uint32_t)(packed_chunk<D>(2 * c) << 4)), keys_v_at<D>(at ^ (uint32_t)(packed_chunk<D>(2 * c + 2) << 4))};
 #pragma unroll
             for (int j = 0; j < 2 * kP * RB; ++j) {
                 const int i = c + j % 2, rb = j / 2 % RB, u = kP - 1 - j / 2 / RB;

@@ -34,7 +34,7 @@ template <int D, int kRows> struct PackedTile {
     }
     // Part I of W: a word of K and of V.  k_to, v_to: the segment's first row of either in LDS; kx, vx: the swizzles of the lane's row.
     template <int I> __device__ __forceinline__ void store(char* k_to, char* v_to, int kx, int vx, int lane) const {
-        const int at = row(lane) * D * 2, c = channel(lane) / 8 + I;
+        const int at = row(lane) * D * 2, c = packed_chunk<D>(channel(lane) / 8) ^ I;
         *reinterpret_cast<uint4*>(k_to + at + ((c ^ kx) << 4)) = packed_bf16(k[I], packed_power_of(ks));
         *reinterpret_cast<uint4*>(v_to + at + ((c ^ vx) << 4)) = packed_bf16(v[I], packed_power_of(vs));
     }
@@ -187,7 +187,7 @@ __device__ __forceinline__ void split_piece(const CacheAttnArgs& a, char* smem, 
             for (int i = 0; i < D / 32; ++i) {
                 bf16x8 x[2];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) x[b] = *(lds_bf16x8_p)(uintptr_t)(((base + k_at) ^ (uint32_t)(i << 6)) + (32 * h + 16 * b) * kRowB);
+                for (int b = 0; b < 2; ++b) x[b] = *(lds_bf16x8_p)(uintptr_t)(((base + k_at) ^ (uint32_t)(packed_chunk<D>(4 * i) << 4)) + (32 * h + 16 * b) * kRowB);
 #pragma unroll
                 for (int u = 2; u >= 0; --u)
 #pragma unroll
@@ -228,7 +228,7 @@ __device__ __forceinline__ void split_piece(const CacheAttnArgs& a, char* smem, 
 #pragma unroll
             for (int c = 0; c < C; c += 2) {
                 const uint32_t v = base + v_at + 32 * h * kRowB;
-                const bf16x8 x[2] = {keys_v<D>(v, c), keys_v<D>(v, c + 1)};
+                const bf16x8 x[2] = {keys_v_at<D>(v ^ (uint32_t)(packed_chunk<D>(2 * c) << 4)), keys_v_at<D>(v ^ (uint32_t)(packed_chunk<D>(2 * c + 2) << 4))};
 #pragma unroll
                 for (int j = 0; j < 6; ++j) o[c + j % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[j % 2], p[2 - j / 2], o[c + j % 2], 0, 0, 0);
             }
