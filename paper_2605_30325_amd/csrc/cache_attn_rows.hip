@@ -20,7 +20,7 @@
 //
 // The same walk over a cache held in 4 bits (kPacked): a tile's codes come into registers one tile ahead, and go as bf16 values into the other
 // slot of LDS between the first products of a step, which no exponentials ride on.  That is what it takes beyond the above, 32 conversions and 8 writes of LDS a
-// wave and tile where four waves share one, and half of that where eight do: 4680 rows x 12 heads on 34,320 keys 0.92-0.98 ms (1.04 with four), the prompts
+// wave and tile where four waves share one, and half of that where eight do: 4680 rows x 12 heads on 34,320 keys 0.91-0.94 ms (1.04 with four), the prompts
 // 0.31-0.33 ms.
 #include "cache_attn.h"
 #include "packed_attn_rows.h"
