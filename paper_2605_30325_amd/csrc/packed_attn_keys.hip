@@ -10,8 +10,7 @@
 // barrier, no tile of raw codes in LDS, and as many waves to a compute unit as registers allow.
 //
 // What bounds it: 64 single tokens of 32 heads on 8, up to 8192 ragged keys, d = 128, bf16, read 285 MB in 62 us of walk (4.6 TB/s; the loads alone
-// take about 57, the instructions alone 51) and 6 of joining; one of 40 heads on 131,101 keys 142 MB in 33 and 11.  Tiles of 32 keys instead of 64 with two in flight: 67 us
-// as before (fp32 47 instead of 48); of 64 with two: 72, the registers do not suffice.
+// take about 57, the instructions alone 51) and 6 of joining; one of 40 heads on 131,101 keys 142 MB in 33 and 11.
 #include "cache_attn_keys.h"
 #include "packed.h"
 
@@ -45,8 +44,12 @@ template <bool kBf16, int D, int RB> struct PackedRow {
 // Waves to a SIMD that the registers are to leave room for.
 template <bool kBf16, int D, int RB> constexpr int packed_waves() { return RB == 2 ? (kBf16 || D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
 
-// Groups of 16 keys of a tile in the sharing kernel.
-template <bool kBf16, int D, int RB> constexpr int packed_groups() { return RB == 1 ? 4 : 2; }
+// The sharing kernel: tiles of a wave in flight, and groups of 16 keys of each.  Two of 32 keys are as many bytes as one of 64, asked for half a tile earlier; with bf16 and d = 64
+// instructions bound the walk, and a larger tile has fewer, and for 32 rows there are no registers (us with two of 32 / one of 64, d = 128: ragged single
+// tokens of 64 streams of 32 heads on 8 from memory 71.0 / 72.3, one of 40 heads on 131,101 keys 44.3 / 45.5; fp32, 64 streams up to 4000 keys 46.9 / 48.4, d = 64 34.1 / 37.2; bf16,
+// d = 64, up to 8192 keys 44.2 / 42.1; 4 rows of 32 heads on 4 61 / 45).
+template <bool kBf16, int D, int RB> constexpr int packed_ring() { return RB == 2 || (kBf16 && D == 64) ? 1 : 2; }
+template <bool kBf16, int D, int RB> constexpr int packed_groups() { return RB == 2 || packed_ring<kBf16, D, RB>() == 2 ? 2 : 4; }
 
 // A lane's part of a tile: of its K row (l15), and of V, where lane / 4 is the key.
 template <int D, int G> struct PackedRaw {
@@ -448,32 +451,49 @@ template <bool kBf16, int D, int RB, int G> __global__ __launch_bounds__(64, (pa
             enter(ahead, ahead.seq + 1, last);
         }
     };
+    constexpr int kRing = packed_ring<kBf16, D, RB>();
     int asked = now, at = 64;
-    PackedRaw<D, G> raw;
-    uint32_t exists = 0;
-    auto ask = [&]() __attribute__((always_inline)) {
+    PackedRaw<D, G> raw[kRing];
+    uint32_t exists[kRing] = {};
+    auto ask = [&](int i) __attribute__((always_inline)) {
         if (asked >= end) return;
         if (at == 64) {
             look_up(asked);
             at = 0;
         }
-        exists = places.ask(a.c, ln, raw, at);
+        exists[i] = places.ask(a.c, ln, raw[i], at);
         ++at;
         ++asked;
     };
-    ask();
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) ask(i);
     while (now < end && here.each) {
         const SeqRows sr = here.sr;
         const int n = min(sr.n, a.c.max_new), rows = n * a.group;
         const int t_beg = now - here.first, stop = min(end, here.first + here.each);
         PackedRow<kBf16, D, RB> st;
         const KeysSeen see = packed_rows_of<kBf16, D, RB>(a, st, sr, n, head, 0, rows, ln.l15, ln.g);
-        for (; now < stop; ++now) {
-            PackedStep<G> step{here.tiles.at(now - here.first), exists};
+        auto go = [&](int i) __attribute__((always_inline)) {      // the next tile, which is in raw[i]; false behind the last
+            PackedStep<G> step{here.tiles.at(now - here.first), exists[i]};
             f32x4v sc[RB][G];
-            packed_scores<kBf16, D, RB, G>(a, st, see, ln, raw, smem, sr.len, step, sc);
-            ask();
+            packed_scores<kBf16, D, RB, G>(a, st, see, ln, raw[i], smem, sr.len, step, sc);
+            ask(i);
             packed_values<kBf16, D, RB, G>(a, st, ln, v, step, sc);
+            return ++now < stop;
+        };
+        while (go(0)) {
+            if constexpr (kRing == 2)
+                if (!go(1)) break;
+        }
+        if constexpr (kRing == 2) {
+            if ((now - here.first - t_beg) & 1) {     // the next tile is in the other one
+                const PackedRaw<D, G> x = raw[0];
+                raw[0] = raw[1];
+                raw[1] = x;
+                const uint32_t e = exists[0];
+                exists[0] = exists[1];
+                exists[1] = e;
+            }
         }
         // The sums: finished, or to the workspace, [part][row][D] and then [part][row] reference and l.
         const bool whole = t_beg == 0 && stop == here.first + here.each;
