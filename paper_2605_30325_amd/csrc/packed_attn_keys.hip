@@ -44,45 +44,62 @@ template <bool kBf16, int D, int RB> struct PackedRow {
 // Waves to a SIMD that the registers are to leave room for.
 template <bool kBf16, int D, int RB> constexpr int packed_waves() { return RB == 2 ? (kBf16 || D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
 
-// The sharing kernel: tiles of a wave in flight, and groups of 16 keys of each.  Two of 32 keys are as many bytes as one of 64, asked for half a tile earlier; with bf16 and d = 64
-// instructions bound the walk, and a larger tile has fewer, and for 32 rows there are no registers (us with two of 32 / one of 64, d = 128: ragged single
-// tokens of 64 streams of 32 heads on 8 from memory 71.0 / 72.3, one of 40 heads on 131,101 keys 44.3 / 45.5; fp32, 64 streams up to 4000 keys 46.9 / 48.4, d = 64 34.1 / 37.2; bf16,
-// d = 64, up to 8192 keys 44.2 / 42.1; 4 rows of 32 heads on 4 61 / 45).
+// The sharing kernel: tiles of a wave in flight, and groups of 16 keys of each.  Two of 32 keys are as many bytes as one of 64, asked for a whole tile earlier; with
+// bf16 and d = 64 instructions bound the walk, and a larger tile has fewer, and for 32 rows there are no registers (us with two of 32 / one of 64, ragged single
+// tokens of 64 streams of 32 heads on 8, d = 128, 65.5 / 67.5, one of 40 heads on 131,101 keys 40.9 / 42.0; fp32, 64 streams up to 4000 keys 46.3 / 48.4, d = 64 34.4 / 37.2;
+// bf16, d = 64, up to 8192 keys 43.8 / 42.4).  From memory, not the 256 MB beside it, the first two take 71 and 44 either way.
 template <bool kBf16, int D, int RB> constexpr int packed_ring() { return RB == 2 || (kBf16 && D == 64) ? 1 : 2; }
 template <bool kBf16, int D, int RB> constexpr int packed_groups() { return RB == 2 || packed_ring<kBf16, D, RB>() == 2 ? 2 : 4; }
 
 // A lane's part of a tile: of its K row (l15), and of V, where lane / 4 is the key.
 template <int D, int G> struct PackedRaw {
     uint32_t k[G][D / 32], v[G][D / 32];
-    uint32_t ks[G], vs[G];
+    uint32_t ks[G], vs[G];                               // four bytes s, the lane's among them
 };
 template <int D, int G> struct PackedLane {
     typedef PackedKeys<D, G> P;
     uint32_t k_code, k_scale, v_code, v_scale;           // what the lane adds to addresses in a pool
     uint32_t v_to, v_at;                                 // its places in LDS: where its part of V goes, and its operand's
+    uint32_t k_shift, v_shift;                           // of the lane's byte in its four
     int lane, l15, g;
     __device__ __forceinline__ explicit PackedLane(int lane_) : lane(lane_), l15(lane_ & 15), g(lane_ >> 4) {
         k_code = (uint32_t)(l15 * P::kRowB + g * (D / 8));
         k_scale = (uint32_t)(l15 * P::kScaleB + g * (D / 4) / 32);
+        k_shift = 8 * (k_scale & 3);
+        k_scale &= ~3u;
         v_code = (uint32_t)(lane * (D / 8));
         v_scale = (uint32_t)((lane >> 2) * P::kScaleB + (lane & 3) * (D / 4) / 32);
+        v_shift = 8 * (v_scale & 3);
+        v_scale &= ~3u;
         v_to = (uint32_t)((lane >> 2) * D * 2 + ((packed_chunk<D>((lane & 3) * (D / 32)) ^ packed_v_swizzle<D>(lane >> 2)) << 4));
         const int key = 4 * g + (l15 >> 2);
         v_at = (uint32_t)(key * D * 2 + ((((l15 & 3) >> 1) ^ packed_v_swizzle<D>(key)) << 4) + 8 * (l15 & 1));
     }
-    // The same place for all lanes, in scalar registers, and what a lane adds to it.
-    __device__ static __forceinline__ const char* at(const char* all, uint32_t lane_part) {
+    // The same place for all lanes, in scalar registers, and what a lane adds to it.  (An address in global memory, or the loads would be flat ones, which are
+    // waited for all together.)
+    typedef const __attribute__((address_space(1))) char* Global;
+    __device__ static __forceinline__ Global at(const char* all, uint32_t lane_part) {
         uint64_t x = (uint64_t)(uintptr_t)all;
         asm("" : "+s"(x));
-        return (const char*)(uintptr_t)x + lane_part;
+        return (Global)(uintptr_t)x + lane_part;
+    }
+    template <int W> __device__ static __forceinline__ void words(Global p, uint32_t (&w)[W]) {
+        typedef __attribute__((ext_vector_type(W == 1 ? 2 : W))) uint32_t Words;
+        if constexpr (W == 1) {
+            w[0] = *(const __attribute__((address_space(1))) uint32_t*)p;
+        } else {
+            const Words x = *(const __attribute__((address_space(1))) Words*)p;
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = x[i];
+        }
     }
     // base: the head's place in the pools, tok: the first of 16 keys in the page.
     __device__ __forceinline__ void load(const CacheArgs& c, PackedRaw<D, G>& r, int b, int64_t base, int tok) const {
         const int64_t code = base + tok * P::kRowB, scale = base + ((int64_t)P::kRowB << c.log_page) + tok * P::kScaleB;
-        packed_words<P::W>(at(c.k + code, k_code), r.k[b]);
-        packed_words<P::W>(at(c.v + code, v_code), r.v[b]);
-        r.ks[b] = *reinterpret_cast<const uint8_t*>(at(c.k + scale, k_scale));
-        r.vs[b] = *reinterpret_cast<const uint8_t*>(at(c.v + scale, v_scale));
+        words(at(c.k + code, k_code), r.k[b]);
+        words(at(c.v + code, v_code), r.v[b]);
+        r.ks[b] = *(const __attribute__((address_space(1))) uint32_t*)at(c.k + scale, k_scale);
+        r.vs[b] = *(const __attribute__((address_space(1))) uint32_t*)at(c.v + scale, v_scale);
     }
 };
 
@@ -162,28 +179,30 @@ __device__ __forceinline__ void packed_scores(const CacheAttnArgs& a, const Pack
     step.full = end <= see.hi_all && (key0 >= see.lo_all || end <= a.sinks) && exists == (1u << G) - 1u;
 
     // V to its places; zeros for keys that do not exist, whatever lies there, and for blocks that stand for NaN (odd, nans: the lanes that have some)
-    uint32_t most = 0;
+    uint32_t most = 0, ks[G], vs[G];
 #pragma unroll
     for (int b = 0; b < G; ++b) {
-        most = max(most, raw.vs[b]);
+        ks[b] = raw.ks[b] >> ln.k_shift & 255u;
+        vs[b] = raw.vs[b] >> ln.v_shift & 255u;
+        most = max(most, vs[b]);
         step.nans[b] = 0;
     }
     step.odd = __any(most >= kPackedNan);
     if (exists != (1u << G) - 1u || end > len || step.odd) {
 #pragma unroll
         for (int b = 0; b < G; ++b) {
-            const bool there = ((exists >> b) & 1u) && key0 + 16 * b + (ln.lane >> 2) < len, nan = there && raw.vs[b] >= kPackedNan;
+            const bool there = ((exists >> b) & 1u) && key0 + 16 * b + (ln.lane >> 2) < len, nan = there && vs[b] >= kPackedNan;
             step.nans[b] = __ballot(nan);
 #pragma unroll
             for (int i = 0; i < W; ++i) raw.v[b][i] = there && !nan ? raw.v[b][i] : 0u;
-            raw.vs[b] = there && !nan ? raw.vs[b] : 127u;
+            vs[b] = there && !nan ? vs[b] : 127u;
         }
     }
 #pragma unroll
     for (int b = 0; b < G; ++b)
 #pragma unroll
         for (int i = 0; i < W; ++i)
-            *reinterpret_cast<uint4*>(smem + ((ln.v_to ^ (uint32_t)(i << 4)) + b * 16 * D * 2)) = packed_bf16(raw.v[b][i], packed_power(raw.vs[b]));
+            *reinterpret_cast<uint4*>(smem + ((ln.v_to ^ (uint32_t)(i << 4)) + b * 16 * D * 2)) = packed_bf16(raw.v[b][i], packed_power(vs[b]));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 
@@ -195,7 +214,7 @@ __device__ __forceinline__ void packed_scores(const CacheAttnArgs& a, const Pack
     for (int t = 0; t < W; ++t)
 #pragma unroll
         for (int b = 0; b < G; ++b) {
-            const bf16x8 x = __builtin_bit_cast(bf16x8, packed_bf16(raw.k[b][t], packed_power_of(raw.ks[b])));
+            const bf16x8 x = __builtin_bit_cast(bf16x8, packed_bf16(raw.k[b][t], packed_power_of(ks[b])));
 #pragma unroll
             for (int u = kQ - 1; u >= 0; --u)
 #pragma unroll
@@ -410,6 +429,7 @@ template <bool kBf16, int D, int RB, int G> __global__ __launch_bounds__(64, (pa
     if (mine >= share.parts || share.total == 0) return;
     int now = share.begin(mine);
     const int end = share.begin(mine + 1);
+    if (now >= end) return;
     const int64_t head_b = (int64_t)head * (P::kRowB + P::kScaleB) << a.c.log_page;
 
     struct Place {          // a sequence, and the numbers of its tiles
@@ -455,13 +475,13 @@ template <bool kBf16, int D, int RB, int G> __global__ __launch_bounds__(64, (pa
     int asked = now, at = 64;
     PackedRaw<D, G> raw[kRing];
     uint32_t exists[kRing] = {};
+    // Behind the last tile too, some place again: were loads left out on any path, the wait for one tile could not leave the next one's in flight.
     auto ask = [&](int i) __attribute__((always_inline)) {
-        if (asked >= end) return;
-        if (at == 64) {
+        if (at == 64 && asked < end) {
             look_up(asked);
             at = 0;
         }
-        exists[i] = places.ask(a.c, ln, raw[i], at);
+        exists[i] = places.ask(a.c, ln, raw[i], min(at, 63));
         ++at;
         ++asked;
     };
@@ -473,21 +493,23 @@ template <bool kBf16, int D, int RB, int G> __global__ __launch_bounds__(64, (pa
         const int t_beg = now - here.first, stop = min(end, here.first + here.each);
         PackedRow<kBf16, D, RB> st;
         const KeysSeen see = packed_rows_of<kBf16, D, RB>(a, st, sr, n, head, 0, rows, ln.l15, ln.g);
-        auto go = [&](int i) __attribute__((always_inline)) {      // the next tile, which is in raw[i]; false behind the last
+        auto go = [&](int i) __attribute__((always_inline)) {      // the next tile, which is in raw[i]
             PackedStep<G> step{here.tiles.at(now - here.first), exists[i]};
             f32x4v sc[RB][G];
             packed_scores<kBf16, D, RB, G>(a, st, see, ln, raw[i], smem, sr.len, step, sc);
             ask(i);
             packed_values<kBf16, D, RB, G>(a, st, ln, v, step, sc);
-            return ++now < stop;
+            ++now;
         };
-        while (go(0)) {
-            if constexpr (kRing == 2)
-                if (!go(1)) break;
+        // (A loop that can be left in its middle would wait for all loads at its top: the compiler lets every way out end in one place with the way back.)
+        for (int rounds = (stop - now) / kRing; rounds > 0; --rounds) {
+#pragma unroll
+            for (int i = 0; i < kRing; ++i) go(i);
         }
         if constexpr (kRing == 2) {
-            if ((now - here.first - t_beg) & 1) {     // the next tile is in the other one
-                const PackedRaw<D, G> x = raw[0];
+            if (now < stop) {
+                go(0);
+                const PackedRaw<D, G> x = raw[0];     // the next tile is in the other one
                 raw[0] = raw[1];
                 raw[1] = x;
                 const uint32_t e = exists[0];
