@@ -9,8 +9,8 @@
 // A byte read is worth four times as many products as in a bf16 cache, so here latency and instructions stand closer to memory than there: no
 // barrier, no tile of raw codes in LDS, and as many waves to a compute unit as registers allow.
 //
-// What bounds it: 64 single tokens of 32 heads on 8, up to 8192 ragged keys, d = 128, bf16, read 285 MB in 62 us of walk (4.6 TB/s; the loads alone
-// take about 57, the instructions alone 51) and 6 of joining; one of 40 heads on 131,101 keys 142 MB in 33 and 11.
+// What bounds it: 64 single tokens of 32 heads on 8, up to 8192 ragged keys, d = 128, bf16, read 285 MB in 61 us of walk (4.7 TB/s; 5 us before the first tile; the
+// instructions alone take 51) and 6 of joining; one of 40 heads on 131,101 keys 142 MB in 33 and 11.
 #include "cache_attn_keys.h"
 #include "packed.h"
 
