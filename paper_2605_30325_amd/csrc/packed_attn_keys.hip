@@ -571,9 +571,14 @@ template <bool kBf16, int D, int RB> static veda_status launch_keys(const CacheA
     hipLaunchKernelGGL((packed_attn_share_kernel<kBf16, D, RB, G>), dim3((unsigned)a.workers), dim3(64), (PackedKeys<D, G>::kSlot), s, a);
     veda_status st = launch_status("veda_packed_attn_fwd");
     if (st != VEDA_OK) return st;
-    const int64_t joins = (int64_t)a.c.rows * a.q_heads;
-    if (a.workers / a.c.kv_heads > 8 * a.c.seqs && joins < 1 << 22) hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 16, PackedKeys<D, G>::kKeys, 8, PackedKeys<D, G>::kLeast>), dim3((unsigned)joins), dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((cache_attn_join_parts_kernel<kBf16, D, RB, 1, PackedKeys<D, G>::kKeys, 8, PackedKeys<D, G>::kLeast>), dim3((unsigned)((joins + 7) / 8)), dim3(512), 0, s, a);
+    // Rows are joined by a wave each, by 8 or by 16: as many as leave a few parts to each (16 caches of up to 16,000 keys, 4 rows of 32 heads on 4, 32 parts, by 8 / 16:
+    // 40 / 45 us; 8 of up to 12,000, 2 rows of 12 heads, 21 parts, 26 / 27).
+    typedef PackedKeys<D, G> P;
+    const int64_t joins = (int64_t)a.c.rows * a.q_heads, parts = a.workers / a.c.kv_heads / a.c.seqs;      // of a row, about
+    auto join = [&](auto kern, int64_t blocks, int threads) { hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3((unsigned)threads), 0, s, a); };
+    if (parts <= 8 || joins >= 1 << 22) join(cache_attn_join_parts_kernel<kBf16, D, RB, 1, P::kKeys, 8, P::kLeast>, (joins + 7) / 8, 512);
+    else if (parts <= 64) join(cache_attn_join_parts_kernel<kBf16, D, RB, 8, P::kKeys, 4, P::kLeast>, joins, 512);
+    else join(cache_attn_join_parts_kernel<kBf16, D, RB, 16, P::kKeys, 8, P::kLeast>, joins, 1024);
     return launch_status("veda_packed_attn_fwd");
 }
 

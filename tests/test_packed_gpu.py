@@ -463,6 +463,15 @@ def test_logits_that_are_all_minus_infinity(dtype, d, n, past):
     assert bool((out[n + 1:n + 3] == 0).all()) and bool((lse[:, n + 1:n + 3] == -math.inf).all())
 
 
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("seqs,n", [(12, 1), (12, 4), (40, 1), (3, 1)])
+def test_shared_walks_of_many_streams(dtype, d, seqs, n):
+    """Caches cut into few and many parts, which 1, 8 or 16 waves a row join."""
+    past = [(i * 577) % 1500 for i in range(seqs)]
+    past[0] = 2900
+    check(Packed([n if i % 7 != 5 else 0 for i in range(seqs)], past, 16, 8, d, dtype, page=64, seed=90, extra_width=80), window=0)
+
+
 def tall(shared, seed=0):
     """bf16 rows that are cut into blocks of 256: shared out by walks that span workgroups, or many sequences under a wide table."""
     if shared:
