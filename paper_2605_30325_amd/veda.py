@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+import operator
 from pathlib import Path
 from typing import Optional, Sequence, Tuple
 
@@ -899,6 +900,7 @@ def _row_strides(h: int, n: int) -> veda_strides:
 
 @functools.lru_cache(maxsize=1024)
 def _visible(block: int, window: int, sinks: int) -> veda_visible:
+    """For ints alone: 7.0 equals 7, and a tensor stays itself when its number changes."""
     return veda_visible(block, window, sinks)
 
 
@@ -957,9 +959,11 @@ def veda_packed_attn_workspace_bytes(cache: PackedCache, batch: CacheBatch, q_he
     return int(load().veda_packed_attn_workspace_bytes(cache._ref, C.byref(bs), q_heads))
 
 
-def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int, window: int, sinks: int, w: str) -> veda_strides:
-    """Refuses what the library would refuse, of everything but the buffers; q's strides."""
+def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int, window: int, sinks: int,
+               w: str) -> Tuple[veda_strides, veda_visible]:
+    """Refuses what the library would refuse, of everything but the buffers; q's strides and the masks."""
     _on(cache.device, w)
+    block, window, sinks = operator.index(block), operator.index(window), operator.index(sinks)
     if not (0 <= block <= 1 << 30 and 0 <= window <= 1 << 30 and 0 <= sinks <= 1 << 30):
         _refuse(w, "block, window and sinks must be 0 .. 2^30")
     if not 0.0 < softmax_scale < math.inf:
@@ -971,13 +975,13 @@ def _attn_fits(cache: Cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: 
         raise VedaError(VEDA_ERR_UNSUPPORTED, w, "more than 32 query heads to a key head")
     if batch.page_table.device != cache.device:
         _refuse(w, "the batch must be where the cache is")
-    return sq
+    return sq, _visible(block, window, sinks)
 
 
 def _attn_fwd(kind: str, cache, batch: CacheBatch, q: torch.Tensor, softmax_scale: float, block: int, window: int, sinks: int,
               out: Optional[torch.Tensor], lse: Optional[torch.Tensor], want_lse: bool, workspace: Optional[torch.Tensor]):
     w = kind + "_fwd"
-    sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)
+    sq, visible = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)
     rows, heads = q.shape[0], q.shape[1]
     if out is None:
         out = torch.empty((rows, heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
@@ -996,7 +1000,7 @@ def _attn_fwd(kind: str, cache, batch: CacheBatch, q: torch.Tensor, softmax_scal
     elif workspace.device != cache.device or not workspace.is_contiguous():
         _refuse(w, "the workspace must be contiguous and where the cache is")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(getattr(lib, w)(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, _visible(block, window, sinks), out.data_ptr(), so,
+    _check(getattr(lib, w)(cache._ref, ref, heads, q.data_ptr(), sq, softmax_scale, visible, out.data_ptr(), so,
                            _ptr(lse), _ptr(workspace) or None, nbytes, _stream_of(cache.device)), w)
     return out, lse
 
@@ -1229,7 +1233,7 @@ def veda_cache_attention(cache: Cache, batch: CacheBatch, q, k, v, softmax_scale
     of the same rows, heads and table (a captured call writes to them whenever it is replayed, so they are never exchanged for others).
     A call that is refused appends nothing and leaves the buffers as they were."""
     w, b = "veda_cache_attention", {} if buffers is None else buffers
-    sq = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)     # before K and V are written
+    sq, _ = _attn_fits(cache, batch, q, softmax_scale, block, window, sinks, w)     # before K and V are written
     es = q.element_size()
     if rope is None and (q.data_ptr() % 16 or any(n > 1 and s * es % 16 for n, s in ((q.shape[0], sq.n), (q.shape[1], sq.h)))):
         raise VedaError(VEDA_ERR_UNSUPPORTED, w, "rows of q must begin at multiples of 16 bytes")

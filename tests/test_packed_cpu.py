@@ -220,3 +220,47 @@ def test_calls_of_the_other_cache_refuse_this_one(lib, monkeypatch):
                  lambda: veda.veda_packed_copy_pages(plain, [(0, 1)])):
         with pytest.raises(veda.VedaError, match="4 bits"):
             call()
+
+
+class Taken:
+    """Stands for the library: takes every call, and keeps its name and the masks that it was told."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            seen = [(a.block, a.window, a.sinks) for a in args if isinstance(a, veda.veda_visible)]
+            self.calls.append((name, *seen))
+            return OK
+        return call
+
+
+@pytest.mark.parametrize("kind", ["packed", "plain"])
+def test_masks_are_the_numbers_that_are_given(monkeypatch, kind):
+    """Whatever was asked before: numbers that are not whole are refused, with nothing appended, and a tensor's number is read at every call."""
+    cpu, i32 = dict(device="cpu"), torch.int32
+    cache = (veda.PackedCache if kind == "packed" else veda.Cache)(4, 16, 2, 64, torch.bfloat16, **cpu)
+    attend = veda.veda_packed_attn_fwd if kind == "packed" else veda.veda_cache_attn_fwd
+    batch = veda.CacheBatch(torch.zeros(1, 2, dtype=i32), torch.zeros(1, dtype=i32), torch.zeros(2, dtype=i32), 1)
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    lib = Taken()
+    monkeypatch.setattr(veda, "load", lambda: lib)
+    monkeypatch.setattr(veda, "_on", lambda *a: None)
+    monkeypatch.setattr(veda, "_stream_of", lambda *a: 0)
+    masks = lambda: [c[1] for c in lib.calls if len(c) > 1]
+    attend(cache, batch, x, 0.1, 7, 3, 2)
+    veda.veda_cache_attention(cache, batch, x, x, x, 0.1, block=7, window=3, sinks=2)
+    assert masks() == [(7, 3, 2)] * 2
+    lib.calls.clear()
+    for bad in (dict(block=7.0, window=3, sinks=2), dict(block=7, window=3.0, sinks=2), dict(block=7, window=3, sinks=2.0)):
+        with pytest.raises(TypeError):
+            attend(cache, batch, x, 0.1, **bad)
+        with pytest.raises(TypeError):
+            veda.veda_cache_attention(cache, batch, x, x, x, 0.1, **bad)
+    assert not [c for c in lib.calls if "append" in c[0] or c[0].endswith("_fwd")]
+    t = torch.tensor(5)
+    attend(cache, batch, x, 0.1, t, t, t)
+    t.fill_(9)
+    attend(cache, batch, x, 0.1, t, t, t)
+    assert masks() == [(5, 5, 5), (9, 9, 9)]
