@@ -472,6 +472,69 @@ def test_shared_walks_of_many_streams(dtype, d, seqs, n):
     check(Packed([n if i % 7 != 5 else 0 for i in range(seqs)], past, 16, 8, d, dtype, page=64, seed=90, extra_width=80), window=0)
 
 
+# Blocks of 17 to 32 rows to a key head: a workgroup for each, and shared walks whose parts 16, 8 or 1 waves a row join.
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("block,window,sinks", [(1, 0, 0), (0, 0, 0), (16, 48, 0), (1, 100, 70), (3, 5000, 30)])
+def test_shared_walks_of_blocks_of_32_rows(dtype, d, block, window, sinks):
+    check(Packed([8, 3], [6000, 50], 8, 2, d, dtype, page=64, seed=91), block=block, window=window, sinks=sinks)
+    check(Packed([5, 1, 0], [9000, 40, 0], 8, 2, d, dtype, page=64, seed=92, holes=[(0, 3, -1), (0, 90, 10 ** 6), (1, 0, -1)]), block=block, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("seqs,hk,extra", [(12, 4, 40), (40, 8, 80)])
+def test_shared_walks_of_many_streams_of_32_rows(dtype, d, seqs, hk, extra):
+    past = [(i * 277) % 400 for i in range(seqs)]
+    past[0] = 2900
+    check(Packed([(8, 5, 1, 0, 7)[i % 5] for i in range(seqs)], past, 4 * hk, hk, d, dtype, page=64, seed=93, extra_width=extra))
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,past", [(12, 60), (12, 6000)])
+@pytest.mark.parametrize("way", [test_bad_values_that_are_seen, test_bad_keys_that_are_seen, test_bad_queries, test_logits_that_are_all_minus_infinity],
+                         ids=lambda f: f.__name__[5:])
+def test_bad_numbers_in_blocks_of_32_rows(way, dtype, d, n, past):
+    way(dtype, d, n, past)
+
+
+class Bytes(Packed):
+    """Pools of any codes, with powers from 2^-5 to 2^0: caches of many heads, whose rows would take long to round on the host."""
+
+    def __init__(self, new, past, hq, hk, d, dtype, page=16, **more):
+        Setup.__init__(self, new, past, hq, hk, d, dtype, page, **more)
+        g = torch.Generator().manual_seed(more.get("seed", 0))
+        run = page * (d // 2 + d // 32)
+        k, v = (torch.randint(0, 256, (self.k.shape[0], hk, run), generator=g, dtype=torch.uint8) for _ in range(2))
+        live = torch.zeros(self.k.shape[0], page, dtype=torch.bool)
+        for s, n in enumerate(self.len):
+            for i in range(-(-n // page)):
+                live[self.table[s, i], :n - i * page] = True
+        for pool in (k, v):
+            s = pool[:, :, page * (d // 2):].view(-1, hk, page, d // 32)
+            s.copy_(torch.where(live[:, None, :, None], 122 + s % 6, torch.full_like(s, 255)))
+        self.cache = veda.PackedCache(self.k.shape[0], page, hk, d, dtype, k=k.to(dev()), v=v.to(dev()))
+        self.look()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+@pytest.mark.parametrize("seqs", [70, 130])
+@pytest.mark.parametrize("n,group", [(1, 1), (8, 4)])
+def test_short_caches_of_many_workgroups(dtype, d, seqs, n, group):
+    """More than 256 workgroups, of four waves, and more than 768, of two; 1 and 32 rows to a key head."""
+    past = [(i * 37) % 150 for i in range(seqs)]
+    past[5], past[seqs - 1] = 640, 900
+    new = [n if i % 3 == 0 else i % (n + 1) for i in range(seqs)]
+    check(Bytes(new, past, 8 * group, 8, d, dtype, page=32, seed=94))
+    check(Bytes(new, past, 8 * group, 8, d, dtype, page=16, seed=95), block=4, window=100, sinks=40)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_more_tiles_than_are_looked_up_at_once(dtype):
+    # 130 tiles of 32 keys for two waves, which look up 64 each at a time: 4600 workgroups, or the walk would be shared out
+    past = [i % 3 for i in range(46)]
+    past[3] = 4149
+    check(Bytes([1] * 46, past, 100, 100, 64, dtype, page=64, seed=96))
+
+
 def tall(shared, seed=0):
     """bf16 rows that are cut into blocks of 256: shared out by walks that span workgroups, or many sequences under a wide table."""
     if shared:
@@ -502,6 +565,13 @@ def test_a_window_asks_for_no_more_workspace(key_heads):
     for window in (0, 300, 1000, 2500, 5000, 2 ** 30):
         out, _ = veda.veda_packed_attn_fwd(t.cache, t.batch, t.q, 0.1, 1, window, 0, workspace=torch.empty(need, dtype=torch.uint8, device=dev()))
         assert bool(torch.isfinite(out[:257]).all())
+
+
+@pytest.mark.parametrize("key_heads", [1, 5, 12])
+@pytest.mark.parametrize("window", [300, 2500, 2 ** 30])
+def test_windows_in_the_workspace_of_a_call_without_one(key_heads, window):
+    # the same calls, against the formula: with blocks of 128 or 256 rows, shared out or not, as the window leaves keys
+    check(Packed([256, 1], [20000 // key_heads, 3], key_heads, key_heads, 128, BF16, page=256, seed=72), window=window)
 
 
 @pytest.mark.parametrize("shared", [True, False])
@@ -664,6 +734,13 @@ def test_captured_and_on_another_stream(dtype, n, past):
         t.cache.k.copy_(pools[0]), t.cache.v.copy_(pools[1])
         want, _ = veda.veda_cache_attention(t.cache, t.batch, q, x[:, :2], x[:, 2:], 0.125, rope)
         assert torch.equal(got[:n + 2], want[:n + 2]) and torch.equal(t.cache.k, after[0]) and torch.equal(t.cache.v, after[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,past", [(12, 60), (12, 6000)])
+@pytest.mark.parametrize("way", [test_strided_queries_and_results, test_captured_and_on_another_stream], ids=lambda f: f.__name__[5:])
+def test_blocks_of_32_rows_strided_and_captured(way, dtype, n, past):
+    way(dtype, n, past)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
