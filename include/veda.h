@@ -506,8 +506,8 @@ veda_status veda_packed_append(const veda_packed_cache*, const veda_cache_batch*
                                veda_strides sv_out, void* stream);
 /* veda_cache_attn_fwd over what the cache stands for: the same masks, results and errors.  A page's bytes may be anything where no row
  * sees them.  A block of K that stands for NaN makes the rows that see its key NaN, one of V its 32 channels of those rows, and neither touches
- * others.  The cache's values are exact in bf16.  f32: Q and the weights enter the products in three bf16 parts that hold all their bits, sums are
- * in fp32.  bf16: weights enter as bf16, of few rows (32 of a key head at most) in two parts. */
+ * others.  The cache's values are exact in bf16.  f32: Q and the weights enter the products in three bf16 parts that hold all their bits from
+ * 2^-110 on (numbers below are off by 2^-134 at most, where bf16 ends), sums are in fp32.  bf16: weights enter as bf16, of few rows (32 of a key head at most) in two parts. */
 size_t veda_packed_attn_workspace_bytes(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads);
 veda_status veda_packed_attn_fwd(const veda_packed_cache*, const veda_cache_batch*, int32_t q_heads, const void* q, veda_strides sq,
                                  float softmax_scale, veda_visible visible, void* out, veda_strides so, float* lse,

@@ -6,10 +6,15 @@
 namespace veda {
 
 // Keys up to which few rows of a packed cache are left to a workgroup for each block and key head: eight waves up to 256 of them, four up to 768, two
-// beyond, as many as run at once.  Sharing has 10 us of its own (what every wave looks up before it starts) and 5 of joining; the waves of a workgroup
-// go through their tiles one after the other.  Single tokens of 4 query heads a key head, us apart / shared: bf16, d = 128, one cache of 6 heads, 2000
-// keys 17 / 19, 3000 22 / 19; 32 of 8, 3000 23 / 28, 7000 44 / 39; 64 of 8, 2000 26 / 32, 4500 52 / 45; 128 of 8, 1200 32 / 40, 3000 65 / 58; d = 64, 32 of 8, 4500 24 /
-// 35, 64 of 8, 3000 28 / 30, 4500 39 / 34; fp32, d = 128, one of 6, 2000 20 / 21, 3000 26 / 21, 64 of 8, 2000 32 / 36, 3000 47 / 45.
+// beyond, as many as run at once.  The waves of a workgroup go through their tiles one after the other, and the longest cache of a batch decides; sharing levels
+// lengths out, but takes 17 to 21 us however short the walk, most of it looking up and joining.  Single tokens of 4 query heads a key head, lengths of any size up to
+// the one given, us apart / shared: bf16, d = 128, one cache of 6 heads, 2000 keys 17 / 19, 3000 22 / 19; 32 of 8, 3000 24 / 28, 5000 34 / 32, 7000 44 / 36; 64 of 8, 2000 28 /
+// 30, 3000 37 / 35, 4500 52 / 41; 128 of 8, 1200 29 / 36, 2000 47 / 44, 3000 67 / 56; 512 of 8, 3800 237 / 270; d = 64, one of 6, 2500 16 / 17, 3000 17 / 17; 32 of 8,
+// 5000 26 / 29, 7000 32 / 31; 64 of 8, 3000 28 / 28, 4500 39 / 32; 128 of 8, 2000 36 / 34; fp32, d = 128, one of 6, 2000 20 / 21, 3000 27 / 21; 32 of 8, 3000 29 / 31, 4500 38 /
+// 34; 64 of 8, 2000 33 / 33, 4500 63 / 47; 512 of 8, 3000 240 / 243, 3800 309 / 302; d = 64, 32 of 8, 7000 38 / 33; 64 of 8, 3000 32 / 30.
+// Caches of one length have nothing to level out, and are up to a fifth faster apart beyond the threshold too (bf16, d = 128, 64 of 8, 3000 40 / 45, 96 of 8, 2800 57 / 68;
+// fp32, 64 of 8, 2000 36 / 40), but lengths are on the device.  Blocks of 17 to 32 rows go by the same thresholds, which are those of single tokens (8 tokens of 4 query heads,
+// d = 128: bf16, 64 of 8, 2000 39 / 52, 3000 51 / 59, 128 of 8, 2000 70 / 85; fp32, whose short walk spills registers, 16 of 8, 2000 56 / 44, 3000 76 / 40, 64 of 8, 2000 99 / 66).
 static int64_t packed_short(bool bf16, int d, int64_t groups) {
     if (groups <= 256) return d == 64 ? 2700 + 20 * groups : bf16 ? 2400 + 10 * groups : 2200 + 8 * groups;
     if (groups <= 768) return d == 64 ? 3600 : bf16 ? 2800 : 2000;

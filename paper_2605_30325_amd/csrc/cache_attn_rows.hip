@@ -749,7 +749,8 @@ template <bool kBf16, int D, bool kPacked, int kWaves> __global__ __launch_bound
 // 0.90 with a workgroup for each.)  What is left of the lists is laid end to end and shared by the other workgroups, where every piece counts
 // for kPiece tiles more: what its set-up and its sums' way to the workspace take (fp32, 1057 rows x 12 heads in 28 blocks on 2000 keys, with 0 / 2 / 5:
 // 142 / 117 / 116 us, 449 rows 64 / 64 / 71; bf16, 2560 rows x 12 heads on 34,000 keys with 0 / 1 / 3: 531 / 491 / 492, 3840 rows 729 / 734 /
-// 752).  Every workgroup counts the blocks' tiles itself.
+// 752).  Every workgroup counts the blocks' tiles itself.  Over a packed cache, bf16, d = 128, that and the codes in flight leave too few registers: 69 are spilled
+// with four waves and 16 with eight (9 over the unpacked one): once a piece, none of them in the loops over tiles.
 template <int kTile, int kRows> __device__ __forceinline__ int rows_tiles_of(const CacheAttnArgs& a, int item) {
     if (item >= a.items) return 0;
     const SeqRows sr = seq_rows(a.c, item / a.per_seq);

@@ -112,7 +112,7 @@ __device__ __forceinline__ uint32_t packed_scale(uint32_t top) {
 // A workgroup takes up to 16 new rows of one sequence and some heads: of Q, which goes to q_out, or (from q_groups on) of K and V.  There
 // d / 8 lanes take a row, eight channels each, four lanes a block of 32: its largest magnitude by two exchanges within the four, the
 // codes by four conversions.  Everything is read and written once and the bytes bound it: 4680 rows of 12 heads of 128 are 94 MB with
-// q_out, k_out and v_out, in 22.3 us (25 in the order of the caller's rows and with k_out and v_out by way of L2).
+// q_out, k_out and v_out, in 22.3 us (25 in the order of the caller's rows and with k_out and v_out by way of L2), and as fp32 180 MB in 35.9 (5.0 TB/s).
 template <typename E, bool kChunks> __global__ __launch_bounds__(kRopeThreads) void packed_append_kernel(PackedAppendArgs a) {
     extern __shared__ __align__(16) char smem[];
     __shared__ int page_s[16];

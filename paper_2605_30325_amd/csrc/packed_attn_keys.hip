@@ -10,7 +10,9 @@
 // barrier, no tile of raw codes in LDS, and as many waves to a compute unit as registers allow.
 //
 // What bounds it: 64 single tokens of 32 heads on 8, up to 8192 ragged keys, d = 128, bf16, read 285 MB in 61 us of walk (4.7 TB/s; 5 us before the first tile; the
-// instructions alone take 51) and 6 of joining; one of 40 heads on 131,101 keys 142 MB in 33 and 11.
+// instructions alone take 51) and 6 of joining; one of 40 heads on 131,101 keys 142 MB in 33 and 11.  fp32, where six products stand for two and a weight is cut in
+// three: 64 up to 4000 ragged keys read 130 MB in 42 us of walk (3.1 TB/s; bf16 35) and 5 of joining, vector instructions 34 % and matrix pipes 21 % busy, waves waiting
+// for memory 28 % and for their turn 25 % of their time: two to a SIMD do not overlap these.
 #include "cache_attn_keys.h"
 #include "packed.h"
 
@@ -337,8 +339,9 @@ template <int D, int G> struct PackedPlaces {
     }
 };
 
-// Short caches: a workgroup for each (block of rows, key head), whose waves take its tiles in turn: eight of them, or two where workgroups are more
-// than compute units.
+// Short caches: a workgroup for each (block of rows, key head), whose waves take its tiles in turn: eight of them, four where workgroups are more than compute
+// units, two where they are more than three times as many.  32 fp32 rows of 128 channels want more registers than two waves to a SIMD leave (packed_waves), and spill 82 or 83
+// (8 tokens of 4 query heads a key head, us: one cache of 2 heads, 500 keys 22, 2000 48; 64 of 8, 500 48, 1000 72; bf16 rows, which spill none, 12, 24, 19 and 27).
 template <bool kBf16, int D, int RB, int G, int kWaves> __global__ __launch_bounds__(64 * kWaves, 2) void packed_attn_keys_kernel(CacheAttnArgs a) {
     typedef PackedKeys<D, G> P;
     constexpr int kRows = 16 * RB, kEs = kBf16 ? 2 : 4;

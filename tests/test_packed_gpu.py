@@ -628,6 +628,19 @@ def test_small_and_large_values(n, past, size):
     check(t, q=t.q * 2.0 ** size)
 
 
+@pytest.mark.parametrize("n,past", [(1, 60), (12, 60), (12, 6000), (70, 1500)])
+def test_queries_that_end_below_normal_numbers(n, past):
+    """fp32 rows around 2^-108 against keys around 2^108.  The least of three bf16 parts ends at 2^-133, so channels below 2^-110 are off by up to 2^-134: with
+    |k| below 2^111 that is 128 * 2^-23 * 128^-1/2, under 2^-19, of a logit.  The bound's own term, (128 + 8) * 2^-24 * sum |q k| * 128^-1/2, is that much for sums
+    of 2 and some 40 times as much for those of 128 such products, so it needs no more."""
+    t = Packed([n, 2], [past, 9], 2, 1, 128, F32, page=32, seed=41)
+    s = t.cache.scales(t.cache.k)
+    s.copy_(torch.where(s == 255, s, (s.int() + 108).clamp(2, 252).to(torch.uint8)))
+    t.look()
+    assert float(np.nanmax(np.abs(t.k.numpy()))) < 2.0 ** 111
+    check(t, q=t.q * 2.0 ** -108)
+
+
 @pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
 def test_offsets_beyond_32_bits(dtype, d):
     # the sequence's pages lie behind 4.5 GB of each pool, and between pages there is room
