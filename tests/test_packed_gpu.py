@@ -527,6 +527,14 @@ def test_short_caches_of_many_workgroups(dtype, d, seqs, n, group):
     check(Bytes(new, past, 8 * group, 8, d, dtype, page=16, seed=95), block=4, window=100, sinks=40)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES, ids=IDS)
+def test_shared_walks_joined_by_single_waves(dtype, d):
+    # 60 streams of 8 key heads, whose caches come in six parts and less each: a wave a row joins them at d = 64 too
+    past = [(i * 77) % 300 for i in range(60)]
+    past[7] = 2900
+    check(Bytes([1 if i % 7 != 5 else 0 for i in range(60)], past, 16, 8, d, dtype, page=32, seed=97, extra_width=160))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_more_tiles_than_are_looked_up_at_once(dtype):
     # 130 tiles of 32 keys for two waves, which look up 64 each at a time: 4600 workgroups, or the walk would be shared out
